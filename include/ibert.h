@@ -428,6 +428,153 @@ int ibert_attention_masked_i(const int8_t* qkv, int8_t* ctx, int32_t batch, int3
                              void* stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Decoder attention over an INT8 key/value cache kept in pages.  The paper quantizes an encoder; the three calls below are
+ * what a decoder quantized the same way (INT8 tensors, INT32 accumulation, dyadic requantization, the i-exp of Alg. 3) needs
+ * between its QKV projection and its output projection, in the order in which a step runs them:
+ *   ibert_page_tables_i     lengths before and after the step -> pages, and where every new token's key and value go
+ *   ibert_rotary_append_i   QKV rows -> rotated queries; rotated keys and values into the cache
+ *   ibert_paged_attention_i queries x cache -> context rows
+ * All lengths, positions and tables stay on the device, so a step can be captured in a HIP graph and replayed.
+ *
+ * The cache of one layer: num_pages pages of page_size tokens, K and V device int8, each ibert_kv_cache_bytes() bytes.  Inside
+ * a page and head the bytes stand in the order in which the matrix unit takes its operands (1 KB a wavefront, contiguous):
+ *   K[page][head][t/16][d/16][t%16][d%16]
+ *   V[page][head][t/64][d/16][(t%16)/4][d%16][(t%64)/16][t%4]            t = token in the page, d = channel of the head
+ * page_size = 64 * 2^i; head_dim 64 or 128 (else IBERT_ERR_NOT_IMPLEMENTED); k and v 16-byte aligned;
+ * 1 <= num_pages, num_pages * page_size < 2^31, 1 <= heads_kv <= 1024.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int8_t* k;                   /* device */
+    int8_t* v;                   /* device */
+    int32_t heads_kv, head_dim, page_size, num_pages;
+} ibert_kv_cache;
+
+/* Bytes of k, and of v (0 for a geometry that is refused). */
+size_t ibert_kv_cache_bytes(const ibert_kv_cache* cache);
+
+/* ------------------------------------------------------------------------------------------------
+ * ibert_page_tables_i -- block tables and slot maps from request lengths.  Sequence b of the batch holds
+ * len_before[b] tokens (in ceil(len_before[b] / page_size) pages named by its row of block_table) and is to hold
+ * len_after[b].  More: pages are taken from the ring of free pages and the new tokens get their places.  Fewer (0: the
+ * sequence has ended): the pages it no longer needs are put back.  With P = page_size, negative lengths taken as 0:
+ *   had = ceil(before / P), wants = ceil(after / P), need = max(0, wants - had), new = max(0, after - before)
+ *   granted_b = wants <= max_pages  and  (need = 0 or sum_{i<=b} need_i <= count)  and  (new = 0 or sum_{i<=b} new_i <= rows)
+ * (the sums run over all that is asked for).  A sequence that is not granted stays at len_before and gets no rows.
+ *   kv_len[b]     granted ? max(0, len_after[b]) : max(0, len_before[b])
+ *   q_start[b]    first row of sequence b's new tokens, which stand in order; q_start[batch] = their number
+ *   positions[t]  position of row t's token in its sequence, slots[t] = page * P + position mod P
+ *                 (rows behind the last token: position 0, slot -1)
+ *   block_table   the new pages are entered, in order of sequence and position; all other entries stay as they are
+ * ring_in = {head, count}: the free pages are free_ring[(head + i) mod num_pages], i < count; they are taken from the
+ * head on, and pages that come back stand behind the count.  ring_out = {head, count, sequences not granted} afterwards (pages that come
+ * back are taken by a later call).
+ * Pointers: device int32; len_before, len_after, kv_len [batch], q_start [batch + 1], block_table [batch, max_pages],
+ * free_ring [num_pages], ring_in [2], ring_out [3], slots, positions [rows].  What is written must not be one of the
+ * other arrays (ring_out is not ring_in, kv_len neither of the two lengths): programs keep two of each and swap them.
+ * Values of ring_in outside [0, num_pages) / [0, num_pages] are clamped into it.
+ * Errors: IBERT_ERR_SHAPE (batch outside [0, 8192], page_size no 64 * 2^i, num_pages or max_pages < 1, rows < 0,
+ * num_pages * page_size or max_pages * page_size or batch * max_pages >= 2^31, an output that is its input), IBERT_ERR_NULL.
+ * ---------------------------------------------------------------------------------------------- */
+int ibert_page_tables_i(const int32_t* len_before, const int32_t* len_after, int32_t batch, int32_t page_size,
+                        int32_t num_pages, const int32_t* ring_in, int32_t* free_ring, int32_t* ring_out,
+                        int32_t* block_table, int32_t max_pages, int32_t rows, int32_t* q_start, int32_t* kv_len,
+                        int32_t* slots, int32_t* positions, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * ibert_rotary_append_i -- rotary positions of queries and keys, optionally behind a norm of each head, and the append of
+ * keys and values to the cache.  Row t of qkv: heads_q queries, heads_kv keys, heads_kv values, head_dim channels each.
+ * For one head x of Q or K (D = head_dim, R = rot_dim):
+ *   with gamma:  sigma = max(1, floor(sqrt(floor(sum_i x_i^2 * 2^16 / D))))      (root mean square, 8 fractional bits; Alg. 4)
+ *                n_i   = (x_i * floor(2^30 / sigma)) >> 12                        (10 fractional bits)
+ *                u_i   = clamp((n_i * gamma[i] + 2^(shift-1)) >> shift, -32767, 32767)
+ *   without:     u_i   = x_i
+ *   (a, b) = (u_i, u_{i+R/2}), i < R/2 (IBERT_ROTARY_HALF), or (u_{2i}, u_{2i+1}) (IBERT_ROTARY_INTERLEAVED); with
+ *   (c, s) = table[position][i], cosine and sine with 14 fractional bits:  (a, b) <- (a c - b s, a s + b c)
+ *   channels from R on: u_i * 2^14
+ *   y_i = clamp(DY(.; q_dy or k_dy), -127, 127);   values: y_i = clamp(DY(x_i; v_dy), -127, 127)
+ * Queries go to q [rows, ld_q]; keys and values to the cache at slots[t] (page slots[t] / page_size).  A row whose slot is
+ * outside [0, num_pages * page_size) is left out: neither q nor the cache is written (rows behind the last token of a
+ * padded batch).  Two rows must not have the same slot.
+ * qkv: device int8 [rows, ld_qkv], ld_qkv >= (heads_q + 2 heads_kv) D; table: device int16 [max_pos, R/2, 2] (may be NULL if R = 0;
+ * see ibert_rotary_table_from_freqs); positions: device int32 [rows], clamped into [0, max_pos); slots: device int32
+ * [rows]; q_gamma, k_gamma: device int32 [D] with |gamma| < 2^14, or NULL (no norm; see ibert_head_norm_from_float).
+ * Preconditions: heads_q a multiple of heads_kv (IBERT_ERR_SHAPE); 0 <= R <= D, R a multiple of 16; shifts of the norms that
+ * are used in [1, 30], all dyadic shifts in [0, 62] (IBERT_ERR_PARAM_RANGE); qkv, q, table and both leading dimensions
+ * 16-byte aligned (IBERT_ERR_ALIGN).  q must not overlap qkv.
+ * ---------------------------------------------------------------------------------------------- */
+enum { IBERT_ROTARY_HALF = 0, IBERT_ROTARY_INTERLEAVED = 1 };
+
+typedef struct {
+    int32_t heads_q, rot_dim, layout, max_pos;
+    ibert_dyadic q_dy, k_dy, v_dy;
+    int32_t q_norm_shift, k_norm_shift;          /* used iff the gamma is given */
+} ibert_rotary_desc;
+
+int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* cache, const int8_t* qkv, int64_t ld_qkv,
+                          const int16_t* table, const int32_t* positions, const int32_t* slots, const int32_t* q_gamma,
+                          const int32_t* k_gamma, int64_t rows, int8_t* q, int64_t ld_q, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * ibert_paged_attention_i -- causal attention of query rows over the paged cache, for single new tokens and for prompts.
+ * Sequence b has the query rows q_start[b] .. q_start[b+1] (NULL: the one row b), n of them, and kv_len[b] tokens in the cache,
+ * the rows' own included.  Its i-th row has position p = kv_len[b] - n + i and sees the positions j <= p, of which with
+ * window > 0 only j > p - window and j < sinks (the first tokens stay visible).  Query head h reads key head
+ * h / (heads_q / heads_kv).  Per row and head:
+ *   s_j = q . k_j,  m = max over visible j,  d_j = DY(m - s_j; scores_dy)          (distance in steps of ln2/64)
+ *   z = d_j >> 6, f = d_j & 63:  w_j = floor(((124 - f)^2 + 8180) / 2^z + 1/2), and 0 from z = 16 on
+ *        (I-Exp of Alg. 3 with the constants of Eq. 13 at S = ln2/64, where the division by ln2 is a shift; 15 bits)
+ *   N = sum_j w_j v_j,  W = sum_j w_j  (exact),  t = (N * floor(2^48 / W)) >> 32   (mean of v with 16 fractional bits)
+ *   out = clamp(DY(t; out_dy), -127, 127);  0 if the row sees nothing (kv_len[b] < n: its first rows)
+ * The maximum is that of the whole row and every sum is exact: a row's result does not depend on how the work is split, nor on
+ * what else is in the batch.  (ibert_attention_i rounds probabilities to 7 bits, which in a row of some hundred keys leaves
+ * nothing of an even distribution; the weights here are rounded relative to the largest.)
+ * q: device int8 [rows, ld_q]; out: device int8 [rows, ld_out]; block_table: device int32 [batch, max_pages]; q_start: device int32
+ * [batch + 1], ascending; kv_len: device int32 [batch].  Lengths are clamped into [0, min(max_kv_len, max_pages *
+ * page_size)], page numbers into the cache, q_start into [0, rows]; rows of no sequence, and rows of a sequence beyond its
+ * first max_q_len, are left as they were.  max_q_len, max_kv_len: bounds of the batch that the host knows; they size the launch and the workspace.
+ * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes (may be NULL where that is 0); calls that may
+ * overlap in time need one each.
+ * Preconditions: max_kv_len <= 131072 and scores_dy.m >= 0, its shift in [24, 62], out_dy's in [0, 62], window, sinks >= 0
+ * (IBERT_ERR_PARAM_RANGE); heads_q a multiple of heads_kv, leading dimensions >= heads_q * head_dim, max_q_len >= 1
+ * (IBERT_ERR_SHAPE); q and ld_q 16-byte, out and ld_out 4-byte aligned (IBERT_ERR_ALIGN).  The cache's V holds values in
+ * [-127, 127] (what ibert_rotary_append_i writes), so that a sum over 131072 keys fits 32 bits.  out must not overlap q.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t heads_q, window, sinks;
+    ibert_dyadic scores_dy, out_dy;
+} ibert_paged_attention_desc;
+
+size_t ibert_paged_attention_workspace_bytes(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, int32_t batch,
+                                             int32_t rows, int32_t max_q_len, int32_t max_kv_len);
+int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, const int8_t* q, int64_t ld_q,
+                            const int32_t* block_table, int32_t max_pages, const int32_t* q_start, const int32_t* kv_len,
+                            int32_t batch, int32_t rows, int32_t max_q_len, int32_t max_kv_len, int8_t* out, int64_t ld_out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Host-only helpers of the three (binary64, as the helpers above).
+ * ibert_rotary_freqs: radians a position of the R/2 pairs, freqs[i] = base^(-2i/R), and for a context stretched by `factor` >= 1:
+ *   IBERT_ROPE_LINEAR  freqs / factor;   IBERT_ROPE_BASE  base * factor^(R/(R-2)) in place of base (R > 2);
+ *   IBERT_ROPE_RAMP    turns = freqs * first_len / 2 pi;  keep = clamp((turns - slow) / (fast - slow), 0, 1);
+ *                      freqs * (keep + (1 - keep) / factor)                            (first_len >= 1, 0 <= slow < fast)
+ * ibert_rotary_table_from_freqs: table[p][i] = {rint(2^14 cos(p freqs[i])), rint(2^14 sin(p freqs[i]))}, p < max_pos, to a host array.
+ * ibert_head_norm_from_float: gamma_q[i] = rint(gamma[i] / S_out * 2^(shift-10)) with the largest shift in [1, 30] such that
+ *   max |gamma_q| < 2^14; u then has the scale S_out.
+ * ibert_paged_attention_from_scales: scores_dy = dyadic(S_q S_k / sqrt(head_dim) * 64 / ln2), out_dy = dyadic(S_v / S_out / 2^16);
+ *   leaves the other fields. */
+enum { IBERT_ROPE_NONE = 0, IBERT_ROPE_LINEAR = 1, IBERT_ROPE_BASE = 2, IBERT_ROPE_RAMP = 3 };
+
+typedef struct {
+    double base, factor, first_len, slow, fast;
+    int32_t kind;
+} ibert_rotary_scaling;
+
+int ibert_rotary_freqs(const ibert_rotary_scaling* scaling, int32_t rot_dim, double* freqs);
+int ibert_rotary_table_from_freqs(const double* freqs, int32_t rot_dim, int32_t max_pos, int16_t* table);
+int ibert_head_norm_from_float(const double* gamma, int32_t head_dim, double S_out, int32_t* gamma_q, int32_t* shift);
+int ibert_paged_attention_from_scales(double S_q, double S_k, double S_v, double S_out, int32_t head_dim,
+                                      ibert_paged_attention_desc* out);
+
+/* ------------------------------------------------------------------------------------------------
  * Optional instrumentation for benchmarks (not part of the method): while a profile is open,
  * ibert_encoder_layer_i / ibert_encoder_i bracket each of the ten steps with HIP events on the caller's
  * stream.  ibert_profile_begin creates the events (host objects; no device memory) for up to `capacity`

@@ -78,6 +78,16 @@ class LayerQuantT(C.Structure):
                 ("res2_m", C.c_int32), ("res2_s", C.c_int32), ("ln2_shift", C.c_int32)]
 
 
+class RotaryT(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads_q", "heads_kv", "D", "P", "R", "interleaved", "max_pos", "pages",
+                                         "q_m", "q_s", "k_m", "k_s", "v_m", "v_s", "q_shift", "k_shift")]
+
+
+class PagedT(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads_q", "heads_kv", "D", "P", "pages", "width", "window", "sinks",
+                                         "s_m", "s_s", "o_m", "o_s")]
+
+
 class LayerDumpT(C.Structure):
     _fields_ = [(n, _P) for n in ("qkv", "scores", "probs", "ctx", "r1", "h1", "f1", "g", "r2")]
 
@@ -134,6 +144,14 @@ def lib():
         L.orc_embedding.restype = C.c_int
         L.orc_embedding.argtypes = [_P, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, _P, _P, C.c_int32, C.c_int32,
                                     C.c_int32, C.c_int32, _P, _P, C.c_int, _P, _P]
+        L.orc_page_tables.restype = C.c_int
+        L.orc_page_tables.argtypes = [_P, _P, C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int64, _P, _P, C.c_int, C.c_int64] + 5 * [_P]
+        L.orc_rotary_append.restype = C.c_int
+        L.orc_rotary_append.argtypes = [C.POINTER(RotaryT), _P, C.c_int64] + 5 * [_P] + [C.c_int64, _P, C.c_int64, _P, _P]
+        L.orc_weight.restype = C.c_int64
+        L.orc_weight.argtypes = [C.c_int64]
+        L.orc_paged_attention.restype = C.c_int
+        L.orc_paged_attention.argtypes = [C.POINTER(PagedT), _P, C.c_int64] + 5 * [_P] + [C.c_int, _P, C.c_int64]
         L.orc_num_threads.restype = C.c_int
         _lib = L
     return _lib
@@ -364,6 +382,47 @@ def embedding(ids, seq: int, tok, pos, tok_dy, pos_dy, gamma_q, beta_q, ln_shift
                              pos_dy[0], pos_dy[1], _ptr(gq), _ptr(bq), ln_shift, _ptr(r), _ptr(y))
     _chk(rc, "embedding")
     return (y, r) if return_sum else y
+
+
+def page_tables(before, after, page: int, ring_in, ring, table, rows: int):
+    """Lengths before / after a step -> dict of everything ibert_page_tables_i writes (ring and table are copied)."""
+    before, after = _arr(before, np.int32), _arr(after, np.int32)
+    out = {"ring": _arr(ring, np.int32).copy(), "table": _arr(table, np.int32).copy(), "q_start": np.zeros(before.size + 1, np.int32),
+           "kv_len": np.zeros(before.size, np.int32), "slots": np.zeros(rows, np.int32), "positions": np.zeros(rows, np.int32)}
+    num = np.zeros(3, np.int64)
+    rc = lib().orc_page_tables(_ptr(before), _ptr(after), before.size, page, out["ring"].size, int(ring_in[0]), int(ring_in[1]),
+                               _ptr(out["ring"]), _ptr(out["table"]), out["table"].shape[1], rows, _ptr(out["q_start"]),
+                               _ptr(out["kv_len"]), _ptr(out["slots"]), _ptr(out["positions"]), _ptr(num))
+    _chk(rc, "page_tables")
+    out["ring_out"] = num.astype(np.int32)
+    return out
+
+
+def rotary_append(d: RotaryT, qkv, table, positions, slots, q_gamma, k_gamma, q, k, v):
+    """qkv int8 [rows, ld]; q [rows, ld_q], k, v: what is there before the call.  Returns copies of the three after it."""
+    qkv, q, k, v = _arr(qkv, np.int8), _arr(q, np.int8).copy(), _arr(k, np.int8).copy(), _arr(v, np.int8).copy()
+    table = None if table is None else _arr(table, np.int16)
+    positions, slots = _arr(positions, np.int32), _arr(slots, np.int32)
+    gq, gk = (None if g is None else _arr(g, np.int32) for g in (q_gamma, k_gamma))
+    p = lambda a: None if a is None else _ptr(a)                     # noqa: E731
+    rc = lib().orc_rotary_append(C.byref(d), _ptr(qkv), qkv.shape[1], p(table), _ptr(positions), _ptr(slots), p(gq), p(gk), slots.size,
+                                 _ptr(q), q.shape[1], _ptr(k), _ptr(v))
+    _chk(rc, "rotary_append")
+    return q, k, v
+
+
+def weight(d: int) -> int:
+    return int(lib().orc_weight(int(d)))
+
+
+def paged_attention(d: PagedT, q, k, v, table, q_start, kv_len, out):
+    """q int8 [rows, ld]; out [rows, ld_out]: what is there before the call.  Returns its copy afterwards."""
+    q, k, v, out = _arr(q, np.int8), _arr(k, np.int8), _arr(v, np.int8), _arr(out, np.int8).copy()
+    table, q_start, kv_len = _arr(table, np.int32), _arr(q_start, np.int32), _arr(kv_len, np.int32)
+    rc = lib().orc_paged_attention(C.byref(d), _ptr(q), q.shape[1], _ptr(k), _ptr(v), _ptr(table), _ptr(q_start), _ptr(kv_len), kv_len.size,
+                                   _ptr(out), out.shape[1])
+    _chk(rc, "paged_attention")
+    return out
 
 
 def num_threads() -> int:

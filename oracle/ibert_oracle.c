@@ -43,7 +43,11 @@
  *                        looked-up rows are added and normalized is not
  *                        spelled out; reading below).
  *
- * Parity pins live in tests/test_oracle_*.py.
+ *   orc_page_tables / orc_rotary_append / orc_weight / orc_paged_attention
+ *                        decoder attention over a paged INT8 cache (not in the
+ *                        paper; readings in its arithmetic).
+ *
+ * Parity pins live in tests/test_oracle_*.py and tests/test_decoder_*.py.
  */
 #include <stdint.h>
 #include <stdlib.h>
@@ -669,6 +673,186 @@ int orc_embedding(const int32_t* ids, int64_t tokens, int seq, int hidden, int v
     if (r_out) memcpy(r_out, r, sizeof(int32_t) * (size_t)(tokens * hidden));
     const int rc = orc_layernorm(r, y, tokens, hidden, hidden, hidden, gamma_q, beta_q, ln_shift);
     free(r);
+    return rc;
+}
+
+/* ------------------------------------------------------------------------- */
+/* Decoder attention over a paged INT8 cache.  The paper quantizes an        */
+/* encoder only; everything here is a reading in its arithmetic.             */
+/* ------------------------------------------------------------------------- */
+
+/* Where channel d of token t of a page and head stands, of P tokens x D channels. */
+static int64_t cell_k(int64_t page, int head, int heads, int P, int D, int t, int d)
+{
+    return (((((page * heads + head) * (P / 16) + t / 16) * (D / 16) + d / 16) * 16) + t % 16) * 16 + d % 16;
+}
+static int64_t cell_v(int64_t page, int head, int heads, int P, int D, int t, int d)
+{
+    const int in = t % 64;
+    return ((((((page * heads + head) * (P / 64) + t / 64) * (D / 16) + d / 16) * 4 + (in % 16) / 4) * 16 + d % 16) * 4 + in / 16) * 4 + in % 4;
+}
+
+/* Lengths before and after -> pages, table, rows.  The sequences one after the other; what is asked for is added up whether it is
+ * granted or not.  num[3]: {head, count, refused} after the call. */
+int orc_page_tables(const int32_t* before, const int32_t* after, int batch, int P, int64_t pages, int64_t head, int64_t count, int32_t* ring,
+                    int32_t* table, int width, int64_t rows, int32_t* q_start, int32_t* kv_len, int32_t* slots, int32_t* positions, int64_t* num)
+{
+    if (batch < 0 || P < 1 || pages < 1 || width < 1 || rows < 0) return ORC_E_ARG;
+    if (head < 0 || head >= pages || count < 0 || count > pages) return ORC_E_ARG;
+    int32_t* freed = (int32_t*)malloc(sizeof(int32_t) * ((size_t)batch * (size_t)width + 1));
+    if (!freed) return ORC_E_NOMEM;
+    int64_t asked_pages = 0, asked_rows = 0, taken = 0, back = 0, row = 0, refused = 0;
+    q_start[0] = 0;
+    for (int b = 0; b < batch; ++b) {
+        const int64_t lb = before[b] < 0 ? 0 : before[b], la = after[b] < 0 ? 0 : after[b];
+        const int64_t had = (lb + P - 1) / P, wants = (la + P - 1) / P;
+        const int64_t need = wants > had ? wants - had : 0, fresh = la > lb ? la - lb : 0;
+        asked_pages += need;
+        asked_rows += fresh;
+        const int granted = wants <= width && (need == 0 || asked_pages <= count) && (fresh == 0 || asked_rows <= rows);
+        if (granted) {
+            for (int64_t p = had; p < wants; ++p) table[(int64_t)b * width + p] = ring[(head + taken++) % pages];
+            for (int64_t p = wants; p < had && p < width; ++p) freed[back++] = table[(int64_t)b * width + p];
+            for (int64_t p = lb; p < la; ++p) {
+                positions[row] = (int32_t)p;
+                slots[row++] = (int32_t)(table[(int64_t)b * width + p / P] * (int64_t)P + p % P);
+            }
+        } else refused++;
+        kv_len[b] = (int32_t)(granted ? la : lb);
+        q_start[b + 1] = (int32_t)row;
+    }
+    for (int64_t i = 0; i < back; ++i) ring[(head + count + i) % pages] = freed[i];
+    for (; row < rows; ++row) { slots[row] = -1; positions[row] = 0; }
+    num[0] = (head + taken) % pages;
+    num[1] = count - taken + back;
+    num[2] = refused;
+    free(freed);
+    return ORC_OK;
+}
+
+/* One head of Q or K: optional norm, rotation, requantization.  table: the position's row, pairs of (cosine, sine). */
+static int head_turned(const int8_t* x, int D, int R, int interleaved, const int16_t* table, const int32_t* gamma, int shift, int32_t m, int32_t s, int8_t* y)
+{
+    int64_t u[256];
+    if (gamma) {
+        int64_t sum = 0;
+        for (int i = 0; i < D; ++i) sum += (int64_t)x[i] * x[i];
+        int passes;
+        int64_t sigma = (int64_t)orc_isqrt((uint64_t)((sum << 16) / D), &passes);
+        if (sigma < 1) sigma = 1;
+        const int64_t f = ((int64_t)1 << 30) / sigma;
+        for (int i = 0; i < D; ++i) {
+            if ((int64_t)x[i] * f > I32_MAX || (int64_t)x[i] * f < I32_MIN) return ORC_E_RANGE;
+            const int64_t v = (int64_t)floor_shr((int64_t)x[i] * f, 12) * gamma[i] + ((int64_t)1 << (shift - 1));
+            if (v > I32_MAX || v < I32_MIN) return ORC_E_RANGE;
+            u[i] = clamp64((int64_t)floor_shr(v, shift), -32767, 32767);
+        }
+    } else {
+        for (int i = 0; i < D; ++i) u[i] = x[i];
+    }
+    for (int i = 0; i < D; ++i) {
+        int64_t v = u[i] * 16384;
+        if (i < R) {
+            const int pair = interleaved ? i / 2 : i % (R / 2), second = interleaved ? i % 2 : i >= R / 2;
+            const int64_t c = table[2 * pair], sn = table[2 * pair + 1];
+            const int64_t a = u[interleaved ? 2 * pair : pair], b = u[interleaved ? 2 * pair + 1 : pair + R / 2];
+            v = second ? a * sn + b * c : a * c - b * sn;
+        }
+        if (v > I32_MAX || v < I32_MIN) return ORC_E_RANGE;
+        y[i] = (int8_t)clamp64(orc_dyadic(v, m, s), -127, 127);
+    }
+    return ORC_OK;
+}
+
+typedef struct {
+    int32_t heads_q, heads_kv, D, P, R, interleaved, max_pos, pages;
+    int32_t q_m, q_s, k_m, k_s, v_m, v_s, q_shift, k_shift;
+} orc_rotary_t;
+
+int orc_rotary_append(const orc_rotary_t* d, const int8_t* qkv, int64_t ld, const int16_t* table, const int32_t* positions, const int32_t* slots,
+                      const int32_t* q_gamma, const int32_t* k_gamma, int64_t rows, int8_t* q, int64_t ld_q, int8_t* k, int8_t* v)
+{
+    if (!d || d->D > 256 || d->D % 16 || d->R > d->D || d->R % 2) return ORC_E_ARG;
+    for (int64_t t = 0; t < rows; ++t) {
+        const int64_t slot = slots[t];
+        if (slot < 0 || slot >= (int64_t)d->pages * d->P) continue;
+        const int64_t pos = d->R ? clamp64(positions[t], 0, d->max_pos - 1) : 0;
+        const int16_t* cs = d->R ? table + pos * d->R : 0;
+        const int8_t* x = qkv + t * ld;
+        for (int h = 0; h < d->heads_q; ++h) {
+            const int rc = head_turned(x + (int64_t)h * d->D, d->D, d->R, d->interleaved, cs, q_gamma, d->q_shift, d->q_m, d->q_s, q + t * ld_q + (int64_t)h * d->D);
+            if (rc) return rc;
+        }
+        x += (int64_t)d->heads_q * d->D;
+        for (int h = 0; h < d->heads_kv; ++h) {
+            int8_t y[256];
+            const int rc = head_turned(x + (int64_t)h * d->D, d->D, d->R, d->interleaved, cs, k_gamma, d->k_shift, d->k_m, d->k_s, y);
+            if (rc) return rc;
+            for (int i = 0; i < d->D; ++i) k[cell_k(slot / d->P, h, d->heads_kv, d->P, d->D, (int)(slot % d->P), i)] = y[i];
+        }
+        x += (int64_t)d->heads_kv * d->D;
+        for (int h = 0; h < d->heads_kv; ++h)
+            for (int i = 0; i < d->D; ++i)
+                v[cell_v(slot / d->P, h, d->heads_kv, d->P, d->D, (int)(slot % d->P), i)] = (int8_t)clamp64(orc_dyadic(x[h * d->D + i], d->v_m, d->v_s), -127, 127);
+    }
+    return ORC_OK;
+}
+
+/* I-Exp of Alg. 3 at S = ln2/64 (q_ln2 = 64, q_b = 124, q_c = 8180 by Eq. 13), of a distance d >= 0, rounded half up instead of down. */
+int64_t orc_weight(int64_t d)
+{
+    const int64_t z = d / 64, p = -(d % 64);
+    if (z >= 16) return 0;
+    const int64_t e = orc_ipoly(p, 124, 8180);
+    return z == 0 ? e : (int64_t)floor_shr(e + ((int64_t)1 << (z - 1)), (int)z);
+}
+
+typedef struct {
+    int32_t heads_q, heads_kv, D, P, pages, width, window, sinks;
+    int32_t s_m, s_s, o_m, o_s;
+} orc_paged_t;
+
+int orc_paged_attention(const orc_paged_t* d, const int8_t* q, int64_t ld_q, const int8_t* k, const int8_t* v, const int32_t* table, const int32_t* q_start,
+                        const int32_t* kv_len, int batch, int8_t* out, int64_t ld_out)
+{
+    if (!d || d->D > 256 || d->heads_q % d->heads_kv) return ORC_E_ARG;
+    if (!dyadic_ok(d->s_s) || !dyadic_ok(d->o_s)) return ORC_E_PARAM;
+    int rc = ORC_OK;
+    for (int b = 0; b < batch; ++b) {
+        const int64_t n = q_start[b + 1] - q_start[b], kv = kv_len[b];
+        if (kv < 0 || kv > (int64_t)d->width * d->P) return ORC_E_ARG;
+#pragma omp parallel for schedule(dynamic)
+        for (int64_t w = 0; w < n * d->heads_q; ++w) {
+            const int64_t i = w / d->heads_q, pos = kv - n + i;
+            const int h = (int)(w % d->heads_q), hk = h / (d->heads_q / d->heads_kv);
+            const int8_t* x = q + (q_start[b] + i) * ld_q + (int64_t)h * d->D;
+            int8_t* y = out + (q_start[b] + i) * ld_out + (int64_t)h * d->D;
+            int64_t* s = (int64_t*)malloc(sizeof(int64_t) * (size_t)(kv + 1));
+            int64_t top = 0, W = 0, N[256] = {0};
+            int any = 0;
+            if (!s) { rc = ORC_E_NOMEM; continue; }
+            for (int64_t j = 0; j <= pos; ++j) {
+                if (d->window && j <= pos - d->window && j >= d->sinks) continue;
+                const int64_t page = table[(int64_t)b * d->width + j / d->P];
+                s[j] = 0;
+                for (int c = 0; c < d->D; ++c) s[j] += (int64_t)x[c] * k[cell_k(page, hk, d->heads_kv, d->P, d->D, (int)(j % d->P), c)];
+                if (!any || s[j] > top) top = s[j];
+                any = 1;
+            }
+            for (int64_t j = 0; j <= pos; ++j) {
+                if (d->window && j <= pos - d->window && j >= d->sinks) continue;
+                const int64_t page = table[(int64_t)b * d->width + j / d->P];
+                const int64_t e = orc_weight(orc_dyadic(top - s[j], d->s_m, d->s_s));
+                W += e;
+                for (int c = 0; c < d->D; ++c) N[c] += e * v[cell_v(page, hk, d->heads_kv, d->P, d->D, (int)(j % d->P), c)];
+            }
+            for (int c = 0; c < d->D; ++c) {
+                const int64_t t = any ? (int64_t)floor_shr((i128)N[c] * (((int64_t)1 << 48) / W), 32) : 0;
+                y[c] = (int8_t)clamp64(orc_dyadic(t, d->o_m, d->o_s), -127, 127);
+            }
+            free(s);
+        }
+    }
     return rc;
 }
 

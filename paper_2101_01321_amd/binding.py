@@ -88,6 +88,30 @@ class LayerScales(C.Structure):
                                           "S_g_in", "S_g_out", "S_r2", "S_y")] + [("softmax_k", C.c_int32)]
 
 
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
+
+
+class KvCache(C.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("heads_kv", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("num_pages", C.c_int32)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("heads_q", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("max_pos", C.c_int32),
+                ("q_dy", Dyadic), ("k_dy", Dyadic), ("v_dy", Dyadic), ("q_norm_shift", C.c_int32),
+                ("k_norm_shift", C.c_int32)]
+
+
+class RotaryScaling(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("base", "factor", "first_len", "slow", "fast")] + [("kind", C.c_int32)]
+
+
+class PagedAttentionDesc(C.Structure):
+    _fields_ = [("heads_q", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("scores_dy", Dyadic),
+                ("out_dy", Dyadic)]
+
+
 class ProfileRecord(C.Structure):
     _fields_ = [("step", C.c_int32), ("ms", C.c_float), ("ops", C.c_double), ("bytes", C.c_double),
                 ("kernel", C.c_char * 96)]
@@ -146,6 +170,17 @@ SIGNATURES = {
     "ibert_gelu_params_from_scale": (C.c_int, [C.c_double, C.c_double, C.POINTER(GeluParams)]),
     "ibert_layernorm_params_from_float": (C.c_int, [_P, _P, C.c_int32, C.c_double, _P, _P, C.POINTER(C.c_int32)]),
     "ibert_layer_quant_from_scales": (C.c_int, [C.POINTER(LayerScales), C.c_int32, C.c_int32, C.POINTER(LayerQuant)]),
+    "ibert_kv_cache_bytes": (C.c_size_t, [C.POINTER(KvCache)]),
+    "ibert_page_tables_i": (C.c_int, [_P, _P] + [C.c_int32] * 3 + [_P] * 4 + [C.c_int32] * 2 + [_P] * 5),
+    "ibert_rotary_append_i": (C.c_int, [C.POINTER(RotaryDesc), C.POINTER(KvCache), _P, C.c_int64] + [_P] * 5 +
+                              [C.c_int64, _P, C.c_int64, _P]),
+    "ibert_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PagedAttentionDesc), C.POINTER(KvCache)] + [C.c_int32] * 4),
+    "ibert_paged_attention_i": (C.c_int, [C.POINTER(PagedAttentionDesc), C.POINTER(KvCache), _P, C.c_int64, _P, C.c_int32, _P, _P] +
+                                [C.c_int32] * 4 + [_P, C.c_int64, _P, C.c_size_t, _P]),
+    "ibert_rotary_freqs": (C.c_int, [C.POINTER(RotaryScaling), C.c_int32, _P]),
+    "ibert_rotary_table_from_freqs": (C.c_int, [_P, C.c_int32, C.c_int32, _P]),
+    "ibert_head_norm_from_float": (C.c_int, [_P, C.c_int32, C.c_double, _P, C.POINTER(C.c_int32)]),
+    "ibert_paged_attention_from_scales": (C.c_int, [C.c_double] * 4 + [C.c_int32, C.POINTER(PagedAttentionDesc)]),
     "ibert_profile_begin": (C.c_int, [C.c_int32]),
     "ibert_profile_end": (C.c_int, [C.POINTER(ProfileRecord), C.c_int32, C.POINTER(C.c_int32)]),
     "ibert_status_string": (C.c_char_p, [C.c_int]),
@@ -250,6 +285,38 @@ def ibert_layer_quant_from_scales(sc: dict, seq: int, head_dim: int) -> LayerQua
     q = LayerQuant()
     _chk(lib().ibert_layer_quant_from_scales(C.byref(s), seq, head_dim, C.byref(q)), "ibert_layer_quant_from_scales")
     return q
+
+
+def ibert_rotary_freqs(scaling: RotaryScaling, rot_dim: int) -> np.ndarray:
+    freqs = np.empty(max(rot_dim, 0) // 2, np.float64)
+    _chk(lib().ibert_rotary_freqs(C.byref(scaling), rot_dim, freqs.ctypes.data), "ibert_rotary_freqs")
+    return freqs
+
+
+def ibert_rotary_table_from_freqs(freqs: np.ndarray, max_pos: int) -> np.ndarray:
+    """int16 [max_pos, pairs, 2], on the host."""
+    freqs = np.ascontiguousarray(freqs, dtype=np.float64)
+    table = np.empty((max(max_pos, 0), freqs.size, 2), np.int16)
+    _chk(lib().ibert_rotary_table_from_freqs(freqs.ctypes.data, 2 * freqs.size, max_pos, table.ctypes.data),
+         "ibert_rotary_table_from_freqs")
+    return table
+
+
+def ibert_head_norm_from_float(gamma: np.ndarray, S_out: float):
+    gamma = np.ascontiguousarray(gamma, dtype=np.float64)
+    gq = np.empty(gamma.shape, np.int32)
+    s = C.c_int32(0)
+    _chk(lib().ibert_head_norm_from_float(gamma.ctypes.data, gamma.size, float(S_out), gq.ctypes.data, C.byref(s)),
+         "ibert_head_norm_from_float")
+    return gq, int(s.value)
+
+
+def ibert_paged_attention_from_scales(S_q: float, S_k: float, S_v: float, S_out: float, head_dim: int, heads_q: int,
+                                      window: int = 0, sinks: int = 0) -> PagedAttentionDesc:
+    d = PagedAttentionDesc(heads_q, window, sinks)
+    _chk(lib().ibert_paged_attention_from_scales(float(S_q), float(S_k), float(S_v), float(S_out), head_dim, C.byref(d)),
+         "ibert_paged_attention_from_scales")
+    return d
 
 
 # ------------------------------------------------------------------------- compute entry points
@@ -392,6 +459,38 @@ def ibert_encoder_i(weights, quant, n_layers: int, x, y, batch, seq, hidden, hea
     _chk(lib().ibert_encoder_i(weights, quant, n_layers, _dp(x), _dp(y), batch, seq, hidden, heads, ffn,
                                _dp(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
          "ibert_encoder_i")
+
+
+def ibert_kv_cache_bytes(cache: KvCache) -> int:
+    return int(lib().ibert_kv_cache_bytes(C.byref(cache)))
+
+
+def ibert_page_tables_i(len_before, len_after, batch: int, page_size: int, num_pages: int, ring_in, free_ring, ring_out,
+                        block_table, max_pages: int, rows: int, q_start, kv_len, slots, positions, stream=None):
+    _chk(lib().ibert_page_tables_i(_dp(len_before), _dp(len_after), batch, page_size, num_pages, _dp(ring_in), _dp(free_ring),
+                                   _dp(ring_out), _dp(block_table), max_pages, rows, _dp(q_start), _dp(kv_len), _dp(slots),
+                                   _dp(positions), _stream(stream)), "ibert_page_tables_i")
+
+
+def ibert_rotary_append_i(desc: RotaryDesc, cache: KvCache, qkv, ld_qkv: int, table, positions, slots, q_gamma, k_gamma,
+                          rows: int, q, ld_q: int, stream=None):
+    _chk(lib().ibert_rotary_append_i(C.byref(desc), C.byref(cache), _dp(qkv), ld_qkv, _dp(table), _dp(positions), _dp(slots),
+                                     _dp(q_gamma), _dp(k_gamma), rows, _dp(q), ld_q, _stream(stream)),
+         "ibert_rotary_append_i")
+
+
+def ibert_paged_attention_workspace_bytes(desc: PagedAttentionDesc, cache: KvCache, batch: int, rows: int, max_q_len: int,
+                                          max_kv_len: int) -> int:
+    return int(lib().ibert_paged_attention_workspace_bytes(C.byref(desc), C.byref(cache), batch, rows, max_q_len, max_kv_len))
+
+
+def ibert_paged_attention_i(desc: PagedAttentionDesc, cache: KvCache, q, ld_q: int, block_table, max_pages: int, q_start,
+                            kv_len, batch: int, rows: int, max_q_len: int, max_kv_len: int, out, ld_out: int,
+                            workspace=None, stream=None):
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _chk(lib().ibert_paged_attention_i(C.byref(desc), C.byref(cache), _dp(q), ld_q, _dp(block_table), max_pages, _dp(q_start),
+                                       _dp(kv_len), batch, rows, max_q_len, max_kv_len, _dp(out), ld_out, _dp(workspace),
+                                       nbytes, _stream(stream)), "ibert_paged_attention_i")
 
 
 def ibert_profile_begin(capacity: int):

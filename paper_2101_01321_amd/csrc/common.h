@@ -246,5 +246,6 @@ int check_softmax(const ibert_softmax_params& p, int32_t cols);
 int check_gelu(const ibert_gelu_params& p);
 int check_hgelu(const ibert_hgelu_params& p);
 int check_layernorm(int32_t C, int32_t shift);
+int check_cache(const ibert_kv_cache* c);
 
 }  // namespace ibert

@@ -21,6 +21,15 @@ const char* g_last_kernel = "";
 
 static const double kLn2 = 0.6931471805599453;   // ln 2 rounded to binary64
 
+int check_cache(const ibert_kv_cache* c)
+{
+    if (!c) return IBERT_ERR_NULL;
+    if (c->heads_kv < 1 || c->page_size < 64 || (c->page_size & (c->page_size - 1)) || c->num_pages < 1 ||
+        (int64_t)c->num_pages * c->page_size > 0x7fffffffLL || c->heads_kv > 1024) return IBERT_ERR_SHAPE;
+    if (c->head_dim != 64 && c->head_dim != 128) return IBERT_ERR_NOT_IMPLEMENTED;
+    return IBERT_OK;
+}
+
 }  // namespace ibert
 
 extern "C" {
@@ -186,6 +195,83 @@ int ibert_layer_quant_from_scales(const ibert_layer_scales* sc, int32_t seq, int
     out->ln1_shift = 0;
     out->ln2_shift = 0;
     return IBERT_OK;
+}
+
+size_t ibert_kv_cache_bytes(const ibert_kv_cache* cache)
+{
+    if (ibert::check_cache(cache)) return 0;
+    return (size_t)cache->num_pages * cache->page_size * cache->heads_kv * cache->head_dim;
+}
+
+int ibert_rotary_freqs(const ibert_rotary_scaling* sc, int32_t rot_dim, double* freqs)
+{
+    if (!sc || (!freqs && rot_dim > 0)) return IBERT_ERR_NULL;
+    if (rot_dim < 0 || rot_dim % 2) return IBERT_ERR_SHAPE;
+    if (!(sc->base > 0.0) || !std::isfinite(sc->base) || sc->kind < IBERT_ROPE_NONE || sc->kind > IBERT_ROPE_RAMP) return IBERT_ERR_PARAM_RANGE;
+    if (sc->kind != IBERT_ROPE_NONE && (!(sc->factor >= 1.0) || !std::isfinite(sc->factor))) return IBERT_ERR_PARAM_RANGE;
+    if (sc->kind == IBERT_ROPE_BASE && rot_dim == 2) return IBERT_ERR_PARAM_RANGE;
+    if (sc->kind == IBERT_ROPE_RAMP && (!(sc->first_len >= 1.0) || !(sc->slow >= 0.0) || !(sc->fast > sc->slow) ||
+                                        !std::isfinite(sc->first_len) || !std::isfinite(sc->fast))) return IBERT_ERR_PARAM_RANGE;
+    const double two_pi = 6.283185307179586;
+    const double base = sc->kind == IBERT_ROPE_BASE ? sc->base * std::pow(sc->factor, (double)rot_dim / (rot_dim - 2)) : sc->base;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot_dim);
+        if (sc->kind == IBERT_ROPE_LINEAR) f /= sc->factor;
+        if (sc->kind == IBERT_ROPE_RAMP) {
+            double keep = (f * sc->first_len / two_pi - sc->slow) / (sc->fast - sc->slow);
+            keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+            f *= keep + (1.0 - keep) / sc->factor;
+        }
+        freqs[i] = f;
+    }
+    return IBERT_OK;
+}
+
+int ibert_rotary_table_from_freqs(const double* freqs, int32_t rot_dim, int32_t max_pos, int16_t* table)
+{
+    if (rot_dim < 0 || rot_dim % 2 || max_pos < 0) return IBERT_ERR_SHAPE;
+    if (rot_dim == 0 || max_pos == 0) return IBERT_OK;
+    if (!freqs || !table) return IBERT_ERR_NULL;
+    const int n = rot_dim / 2;
+    for (int i = 0; i < n; ++i)
+        if (!std::isfinite(freqs[i])) return IBERT_ERR_PARAM_RANGE;
+    for (int64_t p = 0; p < max_pos; ++p)
+        for (int i = 0; i < n; ++i) {
+            const double angle = (double)p * freqs[i];
+            table[(p * n + i) * 2] = (int16_t)std::nearbyint(16384.0 * std::cos(angle));
+            table[(p * n + i) * 2 + 1] = (int16_t)std::nearbyint(16384.0 * std::sin(angle));
+        }
+    return IBERT_OK;
+}
+
+int ibert_head_norm_from_float(const double* gamma, int32_t head_dim, double S_out, int32_t* gamma_q, int32_t* shift)
+{
+    if (!gamma || !gamma_q || !shift) return IBERT_ERR_NULL;
+    if (head_dim < 1) return IBERT_ERR_SHAPE;
+    if (!(S_out > 0.0) || !std::isfinite(S_out)) return IBERT_ERR_PARAM_RANGE;
+    for (int s = 30; s >= 1; --s) {
+        const double p = std::ldexp(1.0, s - 10);
+        bool ok = true;
+        for (int i = 0; i < head_dim && ok; ++i) ok = std::fabs(std::nearbyint(gamma[i] / S_out * p)) < 16384.0;
+        if (!ok) continue;
+        for (int i = 0; i < head_dim; ++i) gamma_q[i] = (int32_t)std::nearbyint(gamma[i] / S_out * p);
+        *shift = s;
+        return IBERT_OK;
+    }
+    return IBERT_ERR_PARAM_RANGE;
+}
+
+int ibert_paged_attention_from_scales(double S_q, double S_k, double S_v, double S_out, int32_t head_dim,
+                                      ibert_paged_attention_desc* out)
+{
+    if (!out) return IBERT_ERR_NULL;
+    if (head_dim < 1) return IBERT_ERR_SHAPE;
+    if (!(S_q > 0.0) || !(S_k > 0.0) || !(S_v > 0.0) || !(S_out > 0.0)) return IBERT_ERR_PARAM_RANGE;
+    int rc = ibert_dyadic_from_double(S_q * S_k / std::sqrt((double)head_dim) * 64.0 / ibert::kLn2, &out->scores_dy);
+    if (rc) return rc;
+    if (out->scores_dy.m == 0) out->scores_dy.s = 62;         // (a multiplier that vanishes: all keys weigh the same)
+    if (out->scores_dy.s < 24) return IBERT_ERR_PARAM_RANGE;
+    return ibert_dyadic_from_double(S_v / S_out / 65536.0, &out->out_dy);
 }
 
 }  // extern "C"

@@ -1,0 +1,266 @@
+// Causal attention of query rows over an INT8 key/value cache in pages (ibert_paged_attention_i).
+//
+// Rows: the query heads of a sequence that share a key head are rows of one problem, n queries x (heads_q / heads_kv) heads,
+// the query outermost; 16 of them are a tile.  Scores: v_mfma_i32_16x16x64_i8 with 16 keys as the first operand and the tile's
+// rows as the second; lane l then holds, for row l % 16, the keys 16 i + 4 (l / 16) + r of 64.  Their weights, 15 bits in
+// two INT8 halves (w = 256 h + l), packed four to a dword i, are the second operand of the product with the values as they
+// stand: the cache keeps 64 tokens of a channel in exactly that order, so that neither scores nor weights cross lanes.
+// The weights are relative to the row's maximum and cannot be rescaled exactly, so the maximum is made first, over the raw
+// accumulators (the distance is monotone in them), and the scores are made a second time.
+#include "common.h"
+
+namespace ibert {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+constexpr int PA_MOST_KEYS = 131072;
+
+struct PagedArgs {
+    const int8_t *q, *k, *v;
+    int8_t* out;
+    const int32_t *table, *q_start, *kv_len;
+    int64_t ld_q, ld_out;
+    int32_t heads_q, heads_kv, group, log_page, num_pages, max_pages, rows, max_q, keys;   // keys: most that a sequence can have
+    int32_t window, sinks;
+    uint32_t s_m;
+    int32_t s_l, s_r;          // DY(d) = (((uint64)(d << s_l) * s_m + s_rnd) >> 32) >> s_r
+    uint64_t s_rnd;
+    ibert_dyadic out_dy;
+};
+
+// What one workgroup works on: 16 rows of one sequence and key head.
+struct Tile {
+    int32_t row0, n;           // first query row of the sequence in q; its queries
+    int32_t pos0;              // position of its first query
+    int32_t kv;                // keys
+    int32_t first, count;      // the tile's first flat row; how many rows it has
+    int32_t low, high;         // positions of its first and last query
+    int32_t sink_blocks, from, blocks;   // 64-key blocks to look at: [0, sink_blocks) and from [from ..), blocks in all
+};
+
+__device__ __forceinline__ Tile tile_of(const PagedArgs& a, int b, int tile, int tile_rows)
+{
+    Tile t;
+    int32_t r0 = b, r1 = b + 1;
+    if (a.q_start) {
+        r0 = clamp_i32(a.q_start[b], 0, a.rows);
+        r1 = clamp_i32(a.q_start[b + 1], r0, a.rows);
+    }
+    t.row0 = r0; t.n = r1 - r0;
+    t.kv = clamp_i32(a.kv_len[b], 0, a.keys);
+    t.pos0 = t.kv - t.n;
+    t.first = tile * tile_rows;
+    const int64_t left = (int64_t)(t.n < a.max_q ? t.n : a.max_q) * a.group - t.first;
+    t.count = left < tile_rows ? (int32_t)(left < 0 ? 0 : left) : tile_rows;
+    t.low = t.pos0 + t.first / a.group;
+    t.high = t.pos0 + (t.first + (t.count > 0 ? t.count - 1 : 0)) / a.group;
+    const int32_t end = t.high < 0 ? 0 : (t.high >> 6) + 1;
+    int32_t from = 0, sb = 0;
+    if (a.window > 0 && t.low >= a.window) {
+        from = (t.low - a.window + 1) >> 6;
+        sb = (a.sinks >> 6) + ((a.sinks & 63) != 0);
+        if (sb >= from) { sb = 0; from = 0; }
+    }
+    t.sink_blocks = sb; t.from = from; t.blocks = sb + (end > from ? end - from : 0);
+    return t;
+}
+
+__device__ __forceinline__ int block_at(const Tile& t, int x) { return x < t.sink_blocks ? x : x - t.sink_blocks + t.from; }
+
+// Offset of a block of 64 tokens in k and in v.
+template <int D>
+__device__ __forceinline__ int64_t block_offset(const PagedArgs& a, int b, int h, int block)
+{
+    const int lp = a.log_page - 6;
+    int32_t page = a.table[(int64_t)b * a.max_pages + (block >> lp)];
+    page = clamp_i32(page, 0, a.num_pages - 1);
+    return ((((int64_t)page * a.heads_kv + h) << lp) + (block & ((1 << lp) - 1))) * (64 * D);
+}
+
+// May every row of the tile see every key of the block?
+__device__ __forceinline__ bool whole_block(const PagedArgs& a, const Tile& t, int block)
+{
+    return 64 * block + 63 <= t.low && (a.window == 0 || 64 * block > t.high - a.window || 64 * block + 63 < a.sinks);
+}
+__device__ __forceinline__ bool visible(const PagedArgs& a, int key, int pos)
+{
+    return key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks);
+}
+
+// Weight of a key whose raw score is d under the row's largest.
+__device__ __forceinline__ uint32_t weight_of(const PagedArgs& a, uint32_t d)
+{
+    uint32_t e = (uint32_t)(((uint64_t)(d << a.s_l) * a.s_m + a.s_rnd) >> 32) >> a.s_r;
+    e = e < 1024u ? e : 1024u;
+    const uint32_t z = e >> 6, f = 124u - (e & 63u);
+    return (umad24(f, f, 8180u) + ((1u << z) >> 1)) >> z;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
+{
+    constexpr int NJ = D / 64, ND = D / 16, NW = 4;
+    __shared__ int32_t s_max[NW][16];
+    __shared__ int32_t s_hi[D * 16], s_lo[D * 16], s_w[32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x, b = blockIdx.y;
+    const Tile t = tile_of(a, b, blockIdx.z, 16);
+    if (t.count == 0) return;
+    for (int i = tid; i < D * 16; i += 256) { s_hi[i] = 0; s_lo[i] = 0; }
+    if (tid < 32) s_w[tid] = 0;
+
+    const int flat = t.first + (c < t.count ? c : t.count - 1);
+    const int qi = flat / a.group, head = h * a.group + (flat - qi * a.group), pos = t.pos0 + qi;
+    v4i qf[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+        qf[j] = *reinterpret_cast<const v4i*>(a.q + (int64_t)(t.row0 + qi) * a.ld_q + head * D + 64 * j + 16 * g);
+
+    auto scores = [&](int block, int64_t at, v4i (&s)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[i] = v4i{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const v4i*>(a.k + at + i * 16 * D + j * 1024 + lane * 16), qf[j], s[i], 0, 0, 0);
+        }
+        if (!whole_block(a, t, block)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos)) s[i][r] = INT32_MIN;
+        }
+    };
+
+    int32_t mx = INT32_MIN;
+    for (int x = wave; x < t.blocks; x += NW) {
+        const int block = block_at(t, x);
+        v4i s[4];
+        scores(block, block_offset<D>(a, b, h, block), s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = mx > s[i][r] ? mx : s[i][r];
+    }
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+    mx = combine_rows32(combine_rows16(mx, larger), larger);
+    if (g == 0) s_max[wave][c] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mx = larger(mx, s_max[w][c]);
+
+    v4i hi[ND], lo[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
+    uint32_t sum = 0;
+    for (int x = wave; x < t.blocks; x += NW) {
+        const int block = block_at(t, x);
+        const int64_t at = block_offset<D>(a, b, h, block);
+        v4i s[4], wh, wl;
+        scores(block, at, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                w[r] = s[i][r] == INT32_MIN ? 0 : weight_of(a, (uint32_t)mx - (uint32_t)s[i][r]);
+                sum += w[r];
+            }
+            wl[i] = (int32_t)pack4_i8((int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]);
+            wh[i] = (int32_t)pack4_i8((int32_t)((w[0] + 128) >> 8), (int32_t)((w[1] + 128) >> 8), (int32_t)((w[2] + 128) >> 8), (int32_t)((w[3] + 128) >> 8));
+        }
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const v4i vf = *reinterpret_cast<const v4i*>(a.v + at + i * 1024 + lane * 16);
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wl, lo[i], 0, 0, 0);
+        }
+    }
+    // whole numbers: the order of these additions changes nothing
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            atomicAdd(&s_hi[(16 * i + 4 * g + r) * 16 + c], hi[i][r]);
+            atomicAdd(&s_lo[(16 * i + 4 * g + r) * 16 + c], lo[i][r]);
+        }
+    atomicAdd(&s_w[c], (int32_t)sum);
+    __syncthreads();
+    if (tid < 16) {
+        const uint32_t W = (uint32_t)s_w[tid];
+        const uint64_t R = W ? ((uint64_t)1 << 48) / W : 0;
+        s_w[tid] = (int32_t)(uint32_t)R;
+        s_w[16 + tid] = (int32_t)(uint32_t)(R >> 32);
+    }
+    __syncthreads();
+    for (int e = tid; e < D * 16; e += 256) {
+        const int r = e / D, d = e - r * D;
+        if (r >= t.count) break;
+        const int f = t.first + r, qr = f / a.group, hd = h * a.group + (f - qr * a.group);
+        const int64_t N = (int64_t)s_hi[d * 16 + r] * 256 + s_lo[d * 16 + r];
+        const int64_t R = (int64_t)(((uint64_t)(uint32_t)s_w[16 + r] << 32) | (uint32_t)s_w[r]);
+        const int32_t m = (int32_t)((N * R) >> 32);
+        a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = (int8_t)clamp_i64_to_i32(dyadic64(m, a.out_dy.m, a.out_dy.s), 127);
+    }
+}
+
+template <int D>
+static int launch_paged(const PagedArgs& a, int32_t batch, int32_t max_q_len, hipStream_t stream)
+{
+    const int64_t tiles = ((int64_t)max_q_len * a.group + 15) / 16;
+    if (tiles > 65535 || batch > 65535) return IBERT_ERR_SHAPE;
+    hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)tiles), dim3(256), 0, stream, a);
+    IBERT_LAUNCH_CHECK("paged_attention_kernel");
+    g_last_kernel = "paged_attention_kernel";
+    return IBERT_OK;
+}
+
+static int check_paged(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, int32_t batch, int32_t rows, int32_t max_q_len, int32_t max_kv_len)
+{
+    if (!desc || !cache) return IBERT_ERR_NULL;
+    if (const int rc = check_cache(cache)) return rc;
+    const ibert_paged_attention_desc& d = *desc;
+    if (batch < 0 || batch > 65535 || rows < 0 || max_q_len < 1 || max_kv_len < 0 || d.heads_q < 1 || d.heads_q > (1 << 20) || d.heads_q % cache->heads_kv)
+        return IBERT_ERR_SHAPE;
+    if (max_kv_len > PA_MOST_KEYS || d.scores_dy.m < 0 || d.scores_dy.s < 24 || d.scores_dy.s > 62 || !dyadic_ok(d.out_dy) || d.window < 0 || d.sinks < 0)
+        return IBERT_ERR_PARAM_RANGE;
+    return IBERT_OK;
+}
+
+}  // namespace ibert
+
+extern "C" size_t ibert_paged_attention_workspace_bytes(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, int32_t batch,
+                                                        int32_t rows, int32_t max_q_len, int32_t max_kv_len)
+{
+    (void)desc; (void)cache; (void)batch; (void)rows; (void)max_q_len; (void)max_kv_len;
+    return 0;
+}
+
+extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, const int8_t* q, int64_t ld_q,
+                                       const int32_t* block_table, int32_t max_pages, const int32_t* q_start, const int32_t* kv_len,
+                                       int32_t batch, int32_t rows, int32_t max_q_len, int32_t max_kv_len, int8_t* out, int64_t ld_out,
+                                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace ibert;
+    if (const int rc = check_paged(desc, cache, batch, rows, max_q_len, max_kv_len)) return rc;
+    const ibert_paged_attention_desc& d = *desc;
+    const int D = cache->head_dim;
+    if (max_pages < 1 || ld_q < (int64_t)d.heads_q * D || ld_out < (int64_t)d.heads_q * D || (!q_start && rows < batch)) return IBERT_ERR_SHAPE;
+    if (batch == 0 || rows == 0) return IBERT_OK;
+    if (!q || !out || !block_table || !kv_len || !cache->k || !cache->v) return IBERT_ERR_NULL;
+    if (!aligned(q, 16) || ld_q % 16 || !aligned(out, 4) || ld_out % 4 || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return IBERT_ERR_ALIGN;
+    (void)workspace; (void)workspace_bytes;
+    PagedArgs a;
+    a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.table = block_table; a.q_start = q_start; a.kv_len = kv_len;
+    a.ld_q = ld_q; a.ld_out = ld_out; a.heads_q = d.heads_q; a.heads_kv = cache->heads_kv; a.group = d.heads_q / cache->heads_kv;
+    a.log_page = __builtin_ctz((unsigned)cache->page_size); a.num_pages = cache->num_pages; a.max_pages = max_pages; a.rows = rows; a.max_q = max_q_len;
+    const int64_t held = (int64_t)max_pages << a.log_page;
+    a.keys = (int32_t)(held < max_kv_len ? held : max_kv_len);
+    a.window = d.window; a.sinks = d.sinks;
+    const int s = d.scores_dy.s;
+    a.s_m = (uint32_t)d.scores_dy.m; a.s_l = s < 32 ? 32 - s : 0; a.s_r = s > 32 ? s - 32 : 0; a.s_rnd = (uint64_t)1 << (s < 32 ? 31 : s - 1);
+    a.out_dy = d.out_dy;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return D == 64 ? launch_paged<64>(a, batch, max_q_len, st) : launch_paged<128>(a, batch, max_q_len, st);
+}

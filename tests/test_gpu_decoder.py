@@ -1,0 +1,459 @@
+"""The decoder attention on the GPU against the oracle, bit for bit: page tables, rotation with append, attention over the paged
+cache, and the three together as a decoder would run them."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+import oracle
+import decoder_util as U
+
+
+def libs():
+    import torch
+    import gpu_util as G
+    from paper_2101_01321_amd import binding as B
+    return torch, G, B
+
+
+def same(got, want, what):
+    got = got.cpu().numpy() if hasattr(got, "cpu") else got
+    bad = np.flatnonzero(got.reshape(-1) != want.reshape(-1))
+    assert bad.size == 0, "%s: %d of %d differ, first at %d: %s, not %s" % (what, bad.size, want.size, bad[0], got.reshape(-1)[bad[0]], want.reshape(-1)[bad[0]])
+
+
+# ------------------------------------------------------------------------------------------- page tables
+class DevicePages:
+    def __init__(self, p):
+        torch, G, B = libs()
+        self.p = p
+        self.t = {k: G.to_dev(getattr(p, k)) for k in ("before", "after", "ring_in", "ring", "table")}
+        guard = lambda n: torch.full((n + 8,), 77, dtype=torch.int32, device=G.DEV)      # noqa: E731
+        self.o = {"ring_out": guard(3), "q_start": guard(len(p.before) + 1), "kv_len": guard(len(p.before)), "slots": guard(p.rows), "positions": guard(p.rows)}
+        self.n = {"ring_out": 3, "q_start": len(p.before) + 1, "kv_len": len(p.before), "slots": p.rows, "positions": p.rows}
+
+    def call(self, stream=None):
+        _, _, B = libs()
+        p, t, o = self.p, self.t, self.o
+        B.ibert_page_tables_i(t["before"], t["after"], len(p.before), p.page, p.num, t["ring_in"], t["ring"], o["ring_out"], t["table"], p.width, p.rows, o["q_start"],
+                              o["kv_len"], o["slots"], o["positions"], stream)
+
+    def check(self):
+        want = self.p.oracle()
+        same(self.t["table"], want["table"], "table")
+        same(self.t["ring"], want["ring"], "ring")
+        for k, n in self.n.items():
+            same(self.o[k][:n], want[k], k)
+            assert bool((self.o[k][n:] == 77).all()), "wrote past the end of " + k
+        return want
+
+
+def _pages_cases():
+    rng = np.random.default_rng(11)
+    yield "one token", U.Pages(0, [0], [1], 64)
+    yield "one more", U.Pages(1, [64], [65], 64)
+    yield "no page needed", U.Pages(2, [65], [66], 64)
+    yield "nothing to do", U.Pages(3, [65, 0], [65, 0], 64, extra_rows=4)
+    yield "no sequences", U.Pages(4, [], [], 64, rows=9)
+    yield "no rows", U.Pages(5, [100, 70], [50, 0], 64, rows=0)
+    yield "negative lengths", U.Pages(6, [-5, 70, -2 ** 31], [3, -1, 0], 64)
+    for batch in (2, 63, 64, 65, 512, 513, 1500, 8192):
+        yield "mixed %d" % batch, U.Pages(batch, *U.mixed_lengths(rng, batch, 700 if batch < 2000 else 130), 64, extra_rows=batch % 5)
+    yield "wide pages", U.Pages(7, *U.mixed_lengths(rng, 40, 5000), 1024)
+    yield "too few pages", U.Pages(8, *U.mixed_lengths(rng, 600, 700), 64, count=400)
+    yield "no pages at all", U.Pages(9, [10, 64, 0], [11, 65, 1], 64, count=0, more_pages=0)
+    yield "too few rows", U.Pages(10, *U.mixed_lengths(rng, 600, 300), 128, rows=3000)
+    yield "a row of the table too short", U.Pages(11, [60, 5, 128], [300, 6, 129], 64, width=2)
+    yield "asked for far too much", U.Pages(12, [0, 5, 10, 0], [2 ** 31 - 1, 2 ** 31 - 1, 11, 2 ** 31 - 1], 64, width=4, count=5, rows=64)
+
+
+@pytest.mark.parametrize("name,case", list(_pages_cases()), ids=lambda v: v.replace(" ", "_") if isinstance(v, str) else "")
+def test_page_tables(gpu, name, case):
+    torch, G, B = libs()
+    G.say("page tables: " + name)
+    d = DevicePages(case)
+    d.call()
+    torch.cuda.synchronize()
+    want = d.check()
+    if name.startswith(("too", "no pages", "a row", "asked")):
+        assert want["ring_out"][2] > 0
+
+
+def test_page_tables_clamp_what_the_ring_says(gpu):
+    # a head and a count outside the ring are taken as the nearest inside; nothing else is touched
+    torch, G, B = libs()
+    for head, count in ((-3, 5), (10 ** 9, 3), (2, -1), (1, 10 ** 9)):
+        case = U.Pages(13, [10, 64, 0], [11, 65, 1], 64)
+        case.ring_in = np.array([head, count], np.int32)
+        G.say("page tables: ring says %d, %d" % (head, count))
+        d = DevicePages(case)
+        d.call()
+        torch.cuda.synchronize()
+        case.ring_in = np.array([np.clip(head, 0, case.num - 1), np.clip(count, 0, case.num)], np.int32)
+        d.check()
+
+
+# ------------------------------------------------------------------------------------------- rotation and append
+def run_rotary(case, stream=None):
+    torch, G, B = libs()
+    tk, tv, tq = G.to_dev(case.k0), G.to_dev(case.v0), G.to_dev(case.q0)
+    desc, cache = case.descs(tk, tv)
+    dev = lambda a: None if a is None else G.to_dev(a)      # noqa: E731
+    B.ibert_rotary_append_i(desc, cache, G.to_dev(case.qkv), case.qkv.shape[1], dev(case.cs if case.R else None), dev(case.positions), dev(case.slots), dev(case.gq), dev(case.gk),
+                            case.rows, tq, case.q0.shape[1], stream)
+    torch.cuda.synchronize()
+    return tq, tk, tv
+
+
+ROTARY = [  # rows, hq, hk, D, R, interleaved, page, q_norm, k_norm, ld, skip
+    (1, 1, 1, 64, 64, False, 64, False, False, 0, ()), (1, 1, 1, 128, 128, True, 64, True, True, 0, ()),
+    (7, 12, 12, 64, 64, False, 64, False, False, 0, (2, 3)), (130, 12, 12, 64, 32, True, 128, False, False, 48, (0, 7, 129)),
+    (65, 32, 8, 128, 128, False, 64, True, True, 16, (64,)), (33, 7, 1, 128, 48, True, 256, True, False, 0, ()),
+    (64, 5, 5, 64, 16, False, 64, False, True, 32, (1,)), (200, 2, 2, 128, 16, False, 512, False, False, 0, ()),
+    (31, 3, 3, 64, 0, False, 64, True, False, 0, ()), (300, 4, 2, 128, 112, False, 64, True, True, 0, range(100, 140)), (1, 64, 8, 128, 64, True, 64, False, False, 0, ())]
+
+
+@pytest.mark.parametrize("args", ROTARY, ids=lambda a: "t%d_q%d_k%d_d%d_r%d_%s_n%d%d" % (a[0], a[1], a[2], a[3], a[4], "il" if a[5] else "half", a[7], a[8]))
+def test_rotary_append(gpu, args):
+    torch, G, B = libs()
+    rows, hq, hk, D, R, inter, page, qn, kn, ld, skip = args
+    case = U.Rotary(rows + R, rows, hq, hk, D, R, inter, page, qn, kn, ld, skip)
+    G.say("rotary %s" % (args,))
+    for got, want, what in zip(run_rotary(case), case.oracle(), "qkv"):
+        same(got, want, what)
+
+
+@pytest.mark.parametrize("dy", [(0, 0), (1, 0), (-(2 ** 31 - 1), 62), (2 ** 31 - 1, 31), (2 ** 30, 32), (2 ** 31 - 1, 33), (12345, 7)])
+def test_rotary_append_of_any_dyadic(gpu, dy):
+    torch, G, B = libs()
+    case = U.Rotary(3, 10, 3, 1, 64, 32, False, 64, False, True)
+    case.q_dy = case.k_dy = case.v_dy = dy
+    G.say("rotary dyadic %s" % (dy,))
+    for got, want, what in zip(run_rotary(case), case.oracle(), "qkv"):
+        same(got, want, what)
+
+
+def test_rotary_append_of_many_rows(gpu):
+    torch, G, B = libs()
+    for D, rows in ((64, 3001), (128, 1403)):
+        case = U.Rotary(D, rows, 8, 2, D, D, D == 64, 64, D == 128, D == 128)
+        # prompts stand in a row: the slots of a sequence follow each other
+        case.slots = (np.arange(rows) + 17).astype(np.int32)
+        G.say("rotary %d rows of D %d" % (rows, D))
+        for got, want, what in zip(run_rotary(case), case.oracle(), "qkv"):
+            same(got, want, what)
+
+
+# ------------------------------------------------------------------------------------------- attention
+class DeviceAttention:
+    def __init__(self, case, max_q=None, max_kv=None, plain_rows=False):
+        torch, G, B = libs()
+        self.case = case
+        self.tq, self.tk, self.tv, self.table, self.kv = (G.to_dev(a) for a in (case.q, case.k, case.v, case.table, case.kv_len))
+        self.start = None if plain_rows else G.to_dev(case.q_start)
+        self.out = torch.cat([G.to_dev(case.out).reshape(-1), torch.full((64,), 77, dtype=torch.int8, device=G.DEV)])
+        self.desc, self.cache = case.descs(self.tk, self.tv)
+        self.max_q = max(1, int(case.n.max(initial=1))) if max_q is None else max_q
+        self.max_kv = int(case.kv.max(initial=0)) if max_kv is None else max_kv
+        size = B.ibert_paged_attention_workspace_bytes(self.desc, self.cache, case.batch, case.rows, self.max_q, self.max_kv)
+        self.ws = torch.randint(-128, 128, (size + 256,), dtype=torch.int8, device=G.DEV) if size else None
+        self.size = size
+
+    def call(self, stream=None):
+        _, _, B = libs()
+        c = self.case
+        B.ibert_paged_attention_i(self.desc, self.cache, self.tq, c.q.shape[1], self.table, c.table.shape[1], self.start, self.kv, c.batch, c.rows, self.max_q, self.max_kv,
+                                  self.out, c.out.shape[1], None if self.ws is None else self.ws[:self.size], stream)
+
+    def result(self):
+        torch, _, _ = libs()
+        torch.cuda.synchronize()
+        assert bool((self.out[-64:] == 77).all()), "wrote past the end"
+        return self.out[:-64].reshape(self.case.out.shape)
+
+
+def check_attention(case, **kw):
+    torch, G, B = libs()
+    G.say("attention q%d k%d d%d page %d n %s kv %s window %d sinks %d" % (case.hq, case.hk, case.D, case.page, case.n[:8].tolist(), case.kv[:8].tolist(), case.window, case.sinks))
+    d = DeviceAttention(case, **kw)
+    d.call()
+    want = case.oracle()
+    same(d.result(), want, "out")
+    return d, want
+
+
+@pytest.mark.parametrize("hq,hk,D,page", [(1, 1, 64, 64), (12, 12, 64, 64), (8, 2, 128, 64), (7, 1, 128, 128), (16, 1, 64, 256), (40, 2, 64, 64), (17, 1, 128, 64)])
+def test_attention_of_single_rows(gpu, hq, hk, D, page):
+    kv = [1, 2, 63, 64, 65, 127, 128, 129, 0, 300, 700]
+    check_attention(U.Attention(hq + D, hq, hk, D, page, [1] * len(kv), kv))
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (64, 0), (63, 4), (200, 64), (100, 65), (65, 1000), (5000, 4), (128, 130)])
+def test_attention_window_and_sinks(gpu, window, sinks):
+    kv = [1, 64, 65, 200, 201, 333, 512, 1000]
+    check_attention(U.Attention(window + sinks, 4, 2, 64, 64, [1] * len(kv), kv, window, sinks))
+    check_attention(U.Attention(window + sinks, 3, 1, 128, 128, [50, 1, 70, 200], [50, 90, 400, 333], window, sinks))
+
+
+@pytest.mark.parametrize("hq,hk,D,page", [(1, 1, 64, 64), (12, 12, 64, 64), (8, 2, 128, 64), (7, 1, 128, 256), (32, 2, 64, 128), (5, 1, 64, 64)])
+def test_attention_of_prompts(gpu, hq, hk, D, page):
+    check_attention(U.Attention(hq, hq, hk, D, page, [1, 2, 0, 65, 130, 16], [1, 2, 30, 65, 140, 300]))
+
+
+def test_attention_of_a_long_prompt(gpu):
+    check_attention(U.Attention(21, 4, 1, 128, 64, [517], [517]))
+    check_attention(U.Attention(22, 2, 2, 64, 64, [1030, 3], [1111, 1000]))
+
+
+def test_attention_of_a_long_context(gpu):
+    # one and a few rows on long caches: the work of a row is split and joined
+    check_attention(U.Attention(23, 4, 1, 64, 64, [1], [70001], std=20.0))
+    check_attention(U.Attention(24, 2, 2, 128, 256, [1, 1, 1], [20000, 0, 9]))
+    check_attention(U.Attention(25, 4, 2, 64, 64, [3, 1, 2], [9000, 5, 4097], 0, 0))
+    check_attention(U.Attention(26, 2, 1, 64, 64, [1, 1], [40000, 30000], 20000, 100))
+
+
+def test_attention_at_the_longest_context(gpu):
+    # 131072 keys that all weigh the same, values at the ends of their range: the largest sums there are
+    case = U.Attention(27, 1, 1, 64, 1024, [1], [131072])
+    case.q[:] = 0
+    case.v[:] = np.where(np.arange(case.v.size) % 64 < 32, 127, -127)
+    d, want = check_attention(case)
+    assert np.all(np.abs(want[0, :64]) >= 126)
+    # one key 380 steps above all others, whose weight there is 256 h - 128: the low halves are all at the end of their range
+    assert oracle.weight(380) % 256 == 128
+    case.s_dy = (1 << 30, 30)                    # a raw score is a step
+    case.k[:] = 0
+    case.q[0, 0] = 4
+    t = 5
+    case.k[int(case.table[0, 0]) * 1024 * 64 + t * 16] = 95
+    check_attention(case)
+
+
+def test_attention_rows_that_see_nothing(gpu):
+    # more rows than the cache has tokens: the first ones come before every key
+    d, want = check_attention(U.Attention(28, 6, 3, 64, 64, [5, 40, 1, 3], [2, 30, 0, 0]))
+    assert np.all(want[:3, :6 * 64] == 0) and want[3].any()
+
+
+def test_attention_of_padded_batches_and_strides(gpu):
+    # rows behind the last sequence, columns behind those of a row: left as they were
+    for n, kv in (([1, 1, 1], [100, 5, 64]), ([30, 1, 9], [100, 5, 64])):
+        case = U.Attention(29, 4, 2, 64, 64, n, kv, pad=11, ld=32)
+        d, want = check_attention(case, max_q=50, max_kv=5000)
+        same(want[int(sum(n)):], case.out[int(sum(n)):], "padding")
+
+
+def test_attention_of_one_row_a_sequence_needs_no_starts(gpu):
+    check_attention(U.Attention(30, 8, 2, 128, 64, [1] * 5, [1, 700, 64, 0, 129], pad=2), plain_rows=True)
+
+
+def test_attention_leaves_rows_beyond_max_q_len(gpu):
+    torch, G, B = libs()
+    case = U.Attention(31, 3, 1, 64, 64, [40, 10, 21], [60, 10, 90])
+    for most in (1, 7, 20, 30):
+        G.say("attention: at most %d rows of each sequence" % most)
+        d = DeviceAttention(case, max_q=most)
+        d.call()
+        want, seen = case.oracle(), np.concatenate([np.arange(k) < most for k in case.n])
+        same(d.result(), np.where(seen[:, None], want, case.out), "out")
+
+
+def test_attention_clamps_lengths_and_pages(gpu):
+    torch, G, B = libs()
+    case = U.Attention(32, 4, 2, 64, 64, [1, 1, 1], [100, 128, 70])
+    d = DeviceAttention(case, max_kv=100)
+    d.kv.copy_(torch.tensor([100, 10 ** 9, -7], dtype=torch.int32))
+    G.say("attention: lengths beyond their bounds")
+    d.call()
+    case.kv_len[:] = (100, 100, 0)
+    same(d.result(), case.oracle(), "lengths")
+    case = U.Attention(33, 4, 2, 64, 64, [1, 2], [100, 128])
+    d = DeviceAttention(case)
+    wild = case.table.copy()
+    wild[0, 0], wild[1, 1] = -1, 2 ** 31 - 1
+    d.table.copy_(torch.from_numpy(wild))
+    G.say("attention: pages that the cache does not have")
+    d.call()
+    case.table = np.clip(wild, 0, case.pages - 1)
+    same(d.result(), case.oracle(), "pages")
+    case = U.Attention(34, 4, 2, 64, 64, [3, 4], [100, 128])
+    d = DeviceAttention(case)
+    d.start.copy_(torch.tensor([-9, 3, 10 ** 9], dtype=torch.int32))
+    G.say("attention: starts beyond the rows")
+    d.call()
+    same(d.result(), case.oracle(), "starts")
+
+
+@pytest.mark.parametrize("s_dy,o_dy", [((0, 62), (1 << 30, 46)), ((2 ** 31 - 1, 24), (1 << 30, 46)), ((2 ** 31 - 1, 31), (2 ** 31 - 1, 45)), ((2 ** 31 - 1, 32), (1, 0)),
+                                       ((2 ** 31 - 1, 33), (-(1 << 30), 45)), ((2 ** 31 - 1, 38), (1 << 30, 47)), ((3, 27), (0, 0)), ((2 ** 31 - 1, 62), (1 << 30, 45))])
+def test_attention_of_any_dyadic(gpu, s_dy, o_dy):
+    for n, kv in (([1, 1], [90, 700]), ([70, 1], [90, 200])):
+        case = U.Attention(35, 3, 1, 64, 64, n, kv)
+        case.s_dy, case.o_dy = s_dy, o_dy
+        check_attention(case)
+
+
+def test_attention_of_extreme_values(gpu):
+    # -128 in queries and keys, scores at both ends, one key that outweighs all others and ties for the maximum
+    for D in (64, 128):
+        for n, kv in (([1, 1], [400, 64]), ([100], [300])):
+            case = U.Attention(36, 2, 1, D, 64, n, kv)
+            case.q[:] = np.where(np.random.default_rng(1).random(case.q.shape) < 0.5, -128, 127)
+            case.k[:] = np.where(np.random.default_rng(2).random(case.k.shape) < 0.5, -128, 127)
+            check_attention(case)
+            case.k[:], case.q[:] = -128, -128
+            check_attention(case)
+
+
+def test_attention_does_not_depend_on_the_batch(gpu):
+    # a row alone, among others, and as the last of a prompt's rows
+    torch, G, B = libs()
+    case = U.Attention(37, 8, 2, 128, 64, [6, 1, 33], [3000, 500, 700])
+    d, want = check_attention(case)
+    for b in range(3):
+        last = int(case.q_start[b + 1]) - 1
+        one = U.Attention(37, 8, 2, 128, 64, [6, 1, 33], [3000, 500, 700])
+        one.q, one.out = case.q[last:last + 1].copy(), case.out[last:last + 1].copy()
+        one.n, one.kv, one.batch, one.rows = np.array([1]), case.kv[b:b + 1], 1, 1
+        one.q_start, one.kv_len, one.table = np.array([0, 1], np.int32), case.kv_len[b:b + 1], case.table[b:b + 1]
+        e = DeviceAttention(one)
+        e.call()
+        same(e.result(), want[last:last + 1], "row alone")
+
+
+def test_attention_of_many_sequences(gpu):
+    rng = np.random.default_rng(38)
+    kv = rng.integers(0, 150, 700)
+    check_attention(U.Attention(38, 2, 1, 64, 64, [1] * 700, kv))
+    n = rng.integers(0, 4, 300)
+    check_attention(U.Attention(39, 2, 1, 64, 64, n, rng.integers(0, 150, 300)))
+
+
+# ------------------------------------------------------------------------------------------- graphs and streams
+def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
+    torch, G, B = libs()
+    cases = [U.Attention(40, 8, 2, 128, 64, [1, 1], [5000, 77]), U.Attention(41, 4, 4, 64, 64, [70, 5], [90, 300]), U.Attention(42, 12, 12, 64, 64, [1] * 3, [10, 64, 200])]
+    devs = [DeviceAttention(c) for c in cases]
+    pages = DevicePages(U.Pages(43, *U.mixed_lengths(np.random.default_rng(43), 70, 300), 64))
+    rot = U.Rotary(44, 40, 4, 2, 64, 64, False, 64, True, True)
+    tk, tv, tq, tx, tc, tp, ts, gq, gk = (G.to_dev(a) for a in (rot.k0, rot.v0, rot.q0, rot.qkv, rot.cs, rot.positions, rot.slots, rot.gq, rot.gk))
+    desc, cache = rot.descs(tk, tv)
+    want, rot_want = [c.oracle() for c in cases], rot.oracle()
+
+    def everything(stream=None):
+        for d in devs:
+            d.call(stream)
+        pages.call(stream)
+        B.ibert_rotary_append_i(desc, cache, tx, rot.qkv.shape[1], tc, tp, ts, gq, gk, rot.rows, tq, rot.q0.shape[1], stream)
+
+    def check():
+        torch.cuda.synchronize()
+        for d, w in zip(devs, want):
+            same(d.result(), w, "out")
+            d.out[:-64].fill_(5)
+            d.out[:-64].view(w.shape).copy_(torch.from_numpy(d.case.out))
+        pages.check()
+        for got, w, what in zip((tq, tk, tv), rot_want, "qkv"):
+            same(got, w, what)
+        tq.copy_(torch.from_numpy(rot.q0))
+        tk.copy_(torch.from_numpy(rot.k0))
+        tv.copy_(torch.from_numpy(rot.v0))
+        for t in pages.o.values():
+            t.fill_(77)
+    G.say("decoder calls: eager")
+    everything()
+    check()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    G.say("decoder calls: another stream, named")
+    everything(side)
+    side.synchronize()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        everything()
+    for k in range(4):
+        G.say("decoder calls: replay %d" % k)
+        graph.replay()
+        check()
+        everything()
+        check()
+    # a replay takes the lengths that stand there now
+    devs[0].kv.copy_(torch.tensor([3000, 64], dtype=torch.int32))
+    graph.replay()
+    torch.cuda.synchronize()
+    cases[0].kv_len[:] = (3000, 64)
+    same(devs[0].result(), cases[0].oracle(), "after other lengths")
+
+
+# ------------------------------------------------------------------------------------------- as a decoder runs them
+@pytest.mark.parametrize("hq,hk,D,R,inter,norm,window,sinks", [(12, 12, 64, 64, False, False, 0, 0), (8, 2, 128, 64, True, True, 100, 4)])
+def test_a_decoder_layer_step_by_step(gpu, hq, hk, D, R, inter, norm, window, sinks):
+    """QKV projection, page tables, rotation + append and attention of prompts and of the tokens after them, with sequences that
+    come, go and wait for pages, against the oracle's chain of the same steps."""
+    torch, G, B = libs()
+    rng = np.random.default_rng(50)
+    H, page, width, num, rows, batch, max_pos = 256, 64, 6, 14, 260, 4, 400
+    heads = hq + 2 * hk
+    w = rng.integers(-127, 128, (heads * D, H)).astype(np.int8)
+    bias = rng.integers(-1000, 1000, heads * D).astype(np.int32)
+    mult, shift = B.ibert_channel_dyadics_from_scales(1.0, np.full(heads * D, 32 / (30 * 73 * 16.0)), 1.0)
+    freqs = B.ibert_rotary_freqs(B.RotaryScaling(10000.0, 1.0, 1.0, 0.0, 1.0, B.ROPE_NONE), R)
+    cs = B.ibert_rotary_table_from_freqs(freqs, max_pos)
+    g, gs = B.ibert_head_norm_from_float(rng.normal(1, 0.1, D), 2.0 ** -12)
+    dy = U.dyadic(127 / 4 / 4096 / 16384) if norm else U.dyadic(0.9 / 16384)
+    s_qk = 4.0 / 127
+    att = B.ibert_paged_attention_from_scales(s_qk, s_qk, 1.0, 0.5, D, hq, window, sinks)
+    rot = B.RotaryDesc(hq, R, B.ROTARY_INTERLEAVED if inter else B.ROTARY_HALF, max_pos, B.Dyadic(*dy), B.Dyadic(*dy), B.Dyadic(*U.dyadic(0.8)), gs, gs)
+    o_rot = oracle.RotaryT(hq, hk, D, page, R, int(inter), max_pos, num, *dy, *dy, *U.dyadic(0.8), gs, gs)
+    o_att = oracle.PagedT(hq, hk, D, page, num, width, window, sinks, *att.scores_dy.tuple(), *att.out_dy.tuple())
+    cells = num * page * hk * D
+    k, v = np.zeros(cells, np.int8), np.zeros(cells, np.int8)
+    ring, state, lens, table = rng.permutation(num).astype(np.int32), np.array([0, num], np.int32), np.zeros(batch, np.int32), np.zeros((batch, width), np.int32)
+    tk, tv = G.to_dev(k), G.to_dev(v)
+    cache = B.KvCache(tk.data_ptr(), tv.data_ptr(), hk, D, page, num)
+    t_w, t_b, t_m, t_s, t_cs, t_g, t_ring, t_table = (G.to_dev(a) for a in (w, bias, mult, shift, cs, g, ring, table))
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device=G.DEV)       # noqa: E731
+    t_state, t_lens = [G.to_dev(np.append(state, 0).astype(np.int32)), i32(3)], [i32(batch), i32(batch)]
+    t_start, t_slots, t_pos = i32(batch + 1), i32(rows), i32(rows)
+    t_qkv, t_q, t_out = (torch.zeros(rows, n, dtype=torch.int8, device=G.DEV) for n in (heads * D, hq * D, hq * D))
+    ws = torch.empty(max(256, B.ibert_paged_attention_workspace_bytes(att, cache, batch, rows, rows, width * page)), dtype=torch.uint8, device=G.DEV)
+    d = B.GemmDesc()
+    d.M, d.N, d.K, d.batch_outer, d.batch_inner, d.lda, d.ldw, d.ldc = rows, heads * D, H, 1, 1, H, H, heads * D
+    d.per_channel, d.out_dtype, d.out_clamp = 1, B.I8, 127
+    q, out = np.zeros((rows, hq * D), np.int8), np.zeros((rows, hq * D), np.int8)
+    refused = 0
+    for step, more in enumerate([(100, 130, 20, 0), (1, 1, 1, 0), (1, 1, 1, 230), (1, -131, 1, 230), (1, 0, 1, 1), (140, 3, 2, 1), (-50, 64, 300, 1)]):
+        after = np.maximum(0, lens + np.array(more)).astype(np.int32)
+        x = U.normal8(rng, 30, rows, H)
+        # the oracle's step
+        o = oracle.page_tables(lens, after, page, state, ring, table, rows)
+        ring, state, table = o["ring"], o["ring_out"], o["table"]
+        refused += int(state[2])
+        og = oracle.GemmT(**dict(M=rows, N=heads * D, K=H, batch_outer=1, batch_inner=1, lda=H, ldw=H, ldc=heads * D, per_channel=1, out_dtype=oracle.I8, out_clamp=127))
+        qkv = oracle_gemm(og, x, w, bias, mult, shift).reshape(rows, heads * D)
+        q, k, v = oracle.rotary_append(o_rot, qkv, cs, o["positions"], o["slots"], g if norm else None, g if norm else None, q, k, v)
+        out = oracle.paged_attention(o_att, q, k, v, table, o["q_start"], o["kv_len"], out)
+        # the library's
+        G.say("decoder step %d" % step)
+        B.ibert_page_tables_i(t_lens[step % 2], G.to_dev(after), batch, page, num, t_state[step % 2], t_ring, t_state[1 - step % 2], t_table, width, rows, t_start,
+                              t_lens[1 - step % 2], t_slots, t_pos)
+        B.ibert_gemm_i8_requant(d, G.to_dev(x), t_w, t_b, t_m, t_s, None, t_qkv)
+        B.ibert_rotary_append_i(rot, cache, t_qkv, heads * D, t_cs, t_pos, t_slots, t_g if norm else None, t_g if norm else None, rows, t_q, hq * D)
+        B.ibert_paged_attention_i(att, cache, t_q, hq * D, t_table, width, t_start, t_lens[1 - step % 2], batch, rows, rows, width * page, t_out, hq * D, ws)
+        torch.cuda.synchronize()
+        same(t_qkv, qkv, "qkv of step %d" % step)
+        for got, want, what in ((t_q, q, "q"), (tk, k, "k"), (tv, v, "v"), (t_out, out, "out"), (t_table, table, "table"), (t_ring, ring, "ring")):
+            same(got, want, "%s of step %d" % (what, step))
+        lens = o["kv_len"]
+    assert refused > 0 and out.any()
+
+
+def oracle_gemm(desc, x, w, bias, mult, shift):
+    out = np.zeros(desc.M * desc.N, np.int8)
+    rc = oracle.lib().orc_gemm_requant(oracle.C.byref(desc), x.ctypes.data, w.ctypes.data, bias.ctypes.data, mult.ctypes.data, shift.ctypes.data, None, out.ctypes.data)
+    assert rc == 0
+    return out
