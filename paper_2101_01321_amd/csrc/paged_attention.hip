@@ -96,52 +96,107 @@ __device__ __forceinline__ uint32_t weight_of(const PagedArgs& a, uint32_t d)
     return (umad24(f, f, 8180u) + ((1u << z) >> 1)) >> z;
 }
 
+// Operands of a block of 64 keys: K as four tiles of 16 keys, V as D / 16 tiles of 16 channels.
+template <int D>
+__device__ __forceinline__ void load_k(const PagedArgs& a, int64_t at, int lane, v4i (&kf)[D / 16])
+{
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) kf[i] = *reinterpret_cast<const v4i*>(a.k + at + i * 1024 + lane * 16);
+}
+template <int D>
+__device__ __forceinline__ void load_v(const PagedArgs& a, int64_t at, int lane, v4i (&vf)[D / 16])
+{
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) vf[i] = *reinterpret_cast<const v4i*>(a.v + at + i * 1024 + lane * 16);
+}
+
+// Raw scores of the lane's row; keys that it may not see: INT32_MIN.
+template <int D>
+__device__ __forceinline__ void block_scores(const PagedArgs& a, const Tile& t, int block, int pos, int g, const v4i (&kf)[D / 16], const v4i (&qf)[D / 64], v4i (&s)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s[i] = v4i{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[i * (D / 64) + j], qf[j], s[i], 0, 0, 0);
+    }
+    if (!whole_block(a, t, block)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos)) s[i][r] = INT32_MIN;
+    }
+}
+
+__device__ __forceinline__ int32_t largest(const v4i (&s)[4], int32_t mx)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = mx > s[i][r] ? mx : s[i][r];
+    return mx;
+}
+
+// Weights of a block as MFMA operands, in two halves; sum: of the weights.
+__device__ __forceinline__ void block_weights(const PagedArgs& a, const v4i (&s)[4], int32_t mx, v4i& wh, v4i& wl, uint32_t& sum)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            w[r] = weight_of(a, (uint32_t)mx - (uint32_t)s[i][r]);
+            w[r] = s[i][r] == INT32_MIN ? 0 : w[r];
+            sum += w[r];
+        }
+        wl[i] = (int32_t)pack4_perm((int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]);
+        wh[i] = (int32_t)pack4_perm((int32_t)((w[0] + 128) >> 8), (int32_t)((w[1] + 128) >> 8), (int32_t)((w[2] + 128) >> 8), (int32_t)((w[3] + 128) >> 8));
+    }
+}
+
+// floor(2^48 / W), and 0 for a row that sees nothing.
+__device__ __forceinline__ uint64_t reciprocal(uint32_t W) { return W ? ((uint64_t)1 << 48) / W : 0; }
+__device__ __forceinline__ int8_t finished(const PagedArgs& a, int64_t N, uint64_t R)
+{
+    return (int8_t)clamp_i64_to_i32(dyadic64((int32_t)((N * (int64_t)R) >> 32), a.out_dy.m, a.out_dy.s), 127);
+}
+
+// The row of a tile that a lane's column stands for (columns behind the last row repeat it), and its queries as operand.
+template <int D>
+__device__ __forceinline__ void tile_row(const PagedArgs& a, const Tile& t, int h, int c, int g, int& pos, v4i (&qf)[D / 64])
+{
+    const int flat = t.first + (c < t.count ? c : t.count - 1), qi = flat / a.group;
+    const int8_t* src = a.q + (int64_t)(t.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) qf[j] = *reinterpret_cast<const v4i*>(src + 64 * j);
+    pos = t.pos0 + qi;
+}
+
+// ---- any number of rows, no workspace: the scores are made twice -----------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
 {
     constexpr int NJ = D / 64, ND = D / 16, NW = 4;
     __shared__ int32_t s_max[NW][16];
     __shared__ int32_t s_hi[D * 16], s_lo[D * 16], s_w[32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int h = blockIdx.x, b = blockIdx.y;
     const Tile t = tile_of(a, b, blockIdx.z, 16);
     if (t.count == 0) return;
     for (int i = tid; i < D * 16; i += 256) { s_hi[i] = 0; s_lo[i] = 0; }
     if (tid < 32) s_w[tid] = 0;
-
-    const int flat = t.first + (c < t.count ? c : t.count - 1);
-    const int qi = flat / a.group, head = h * a.group + (flat - qi * a.group), pos = t.pos0 + qi;
+    int pos;
     v4i qf[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-        qf[j] = *reinterpret_cast<const v4i*>(a.q + (int64_t)(t.row0 + qi) * a.ld_q + head * D + 64 * j + 16 * g);
-
-    auto scores = [&](int block, int64_t at, v4i (&s)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[i] = v4i{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const v4i*>(a.k + at + i * 16 * D + j * 1024 + lane * 16), qf[j], s[i], 0, 0, 0);
-        }
-        if (!whole_block(a, t, block)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos)) s[i][r] = INT32_MIN;
-        }
-    };
+    tile_row<D>(a, t, h, c, g, pos, qf);
 
     int32_t mx = INT32_MIN;
     for (int x = wave; x < t.blocks; x += NW) {
         const int block = block_at(t, x);
-        v4i s[4];
-        scores(block, block_offset<D>(a, b, h, block), s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) mx = mx > s[i][r] ? mx : s[i][r];
+        v4i kf[ND], s[4];
+        load_k<D>(a, block_offset<D>(a, b, h, block), lane, kf);
+        block_scores<D>(a, t, block, pos, g, kf, qf, s);
+        mx = largest(s, mx);
     }
     const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
     mx = combine_rows32(combine_rows16(mx, larger), larger);
@@ -157,24 +212,15 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
     for (int x = wave; x < t.blocks; x += NW) {
         const int block = block_at(t, x);
         const int64_t at = block_offset<D>(a, b, h, block);
-        v4i s[4], wh, wl;
-        scores(block, at, s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                w[r] = s[i][r] == INT32_MIN ? 0 : weight_of(a, (uint32_t)mx - (uint32_t)s[i][r]);
-                sum += w[r];
-            }
-            wl[i] = (int32_t)pack4_i8((int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]);
-            wh[i] = (int32_t)pack4_i8((int32_t)((w[0] + 128) >> 8), (int32_t)((w[1] + 128) >> 8), (int32_t)((w[2] + 128) >> 8), (int32_t)((w[3] + 128) >> 8));
-        }
+        v4i kf[ND], vf[ND], s[4], wh, wl;
+        load_k<D>(a, at, lane, kf);
+        load_v<D>(a, at, lane, vf);
+        block_scores<D>(a, t, block, pos, g, kf, qf, s);
+        block_weights(a, s, mx, wh, wl, sum);
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-            const v4i vf = *reinterpret_cast<const v4i*>(a.v + at + i * 1024 + lane * 16);
-            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wh, hi[i], 0, 0, 0);
-            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wl, lo[i], 0, 0, 0);
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], wl, lo[i], 0, 0, 0);
         }
     }
     // whole numbers: the order of these additions changes nothing
@@ -188,8 +234,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
     atomicAdd(&s_w[c], (int32_t)sum);
     __syncthreads();
     if (tid < 16) {
-        const uint32_t W = (uint32_t)s_w[tid];
-        const uint64_t R = W ? ((uint64_t)1 << 48) / W : 0;
+        const uint64_t R = reciprocal((uint32_t)s_w[tid]);
         s_w[tid] = (int32_t)(uint32_t)R;
         s_w[16 + tid] = (int32_t)(uint32_t)(R >> 32);
     }
@@ -199,20 +244,247 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
         if (r >= t.count) break;
         const int f = t.first + r, qr = f / a.group, hd = h * a.group + (f - qr * a.group);
         const int64_t N = (int64_t)s_hi[d * 16 + r] * 256 + s_lo[d * 16 + r];
-        const int64_t R = (int64_t)(((uint64_t)(uint32_t)s_w[16 + r] << 32) | (uint32_t)s_w[r]);
-        const int32_t m = (int32_t)((N * R) >> 32);
-        a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = (int8_t)clamp_i64_to_i32(dyadic64(m, a.out_dy.m, a.out_dy.s), 127);
+        a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = finished(a, N, ((uint64_t)(uint32_t)s_w[16 + r] << 32) | (uint32_t)s_w[r]);
     }
 }
 
-template <int D>
-static int launch_paged(const PagedArgs& a, int32_t batch, int32_t max_q_len, hipStream_t stream)
+// ---- few rows on many keys: three launches, the keys of a tile of rows split into chunks ---------------------------------
+// Scores and each chunk's maximum; weights, sums over the chunk, with the maximum of all chunks; the chunks' sums joined.
+struct SplitArgs {
+    PagedArgs p;
+    int32_t tiles, splits, chunk;      // row tiles of a key head; chunks of at most `chunk` blocks
+    int32_t blocks, held;              // room in `scores`: blocks, and rows of a tile (min(16, rows there are))
+    int32_t* maxima;                   // [batch][key head][tile][split][16]
+    uint32_t* sums;                    // the same
+    int64_t* parts;                    // [..][split][held][D]
+    int32_t* scores;                   // [..][blocks][held][64], of a row the four lanes' 16 values one after the other
+};
+
+struct SplitAt {
+    int b, h, split, x0, x1;
+    int64_t index;                     // of (sequence, key head, tile)
+    Tile t;
+};
+__device__ __forceinline__ SplitAt split_at(const SplitArgs& a, int split, int ht, int b)
 {
-    const int64_t tiles = ((int64_t)max_q_len * a.group + 15) / 16;
-    if (tiles > 65535 || batch > 65535) return IBERT_ERR_SHAPE;
-    hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)tiles), dim3(256), 0, stream, a);
-    IBERT_LAUNCH_CHECK("paged_attention_kernel");
-    g_last_kernel = "paged_attention_kernel";
+    SplitAt s;
+    s.b = b; s.split = split;
+    s.h = ht / a.tiles;
+    s.index = (int64_t)b * a.p.heads_kv * a.tiles + ht;
+    s.t = tile_of(a.p, b, ht - s.h * a.tiles, 16);
+    s.x0 = split * a.chunk;
+    s.x1 = s.x0 + a.chunk < s.t.blocks ? s.x0 + a.chunk : s.t.blocks;
+    return s;
+}
+__device__ __forceinline__ int splits_used(const SplitArgs& a, const Tile& t) { return (t.blocks + a.chunk - 1) / a.chunk; }
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_scores_kernel(SplitArgs a)
+{
+    constexpr int ND = D / 16, NW = 4;
+    __shared__ int32_t s_max[NW][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const SplitAt w = split_at(a, blockIdx.x, blockIdx.y, blockIdx.z);
+    if (w.t.count == 0 || w.x0 >= w.x1) return;
+    int pos;
+    v4i qf[D / 64];
+    tile_row<D>(a.p, w.t, w.h, c, g, pos, qf);
+    int32_t mx = INT32_MIN;
+    v4i kf[2][ND];
+    auto ask = [&](int x, v4i (&k)[ND]) { load_k<D>(a.p, block_offset<D>(a.p, w.b, w.h, block_at(w.t, x)), lane, k); };
+    auto take = [&](int x, const v4i (&k)[ND]) {
+        v4i s[4];
+        block_scores<D>(a.p, w.t, block_at(w.t, x), pos, g, k, qf, s);
+        mx = largest(s, mx);
+        if (c < a.held) {
+            v4i* dst = reinterpret_cast<v4i*>(a.scores + ((w.index * a.blocks + x) * a.held + c) * 64 + g * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = s[i];
+        }
+    };
+    int x = w.x0 + wave;
+    if (x < w.x1) ask(x, kf[0]);
+    while (x < w.x1) {
+        if (x + NW < w.x1) ask(x + NW, kf[1]);
+        take(x, kf[0]);
+        x += NW;
+        if (x >= w.x1) break;
+        if (x + NW < w.x1) ask(x + NW, kf[0]);
+        take(x, kf[1]);
+        x += NW;
+    }
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+    mx = combine_rows32(combine_rows16(mx, larger), larger);
+    if (g == 0) s_max[wave][c] = mx;
+    __syncthreads();
+    if (tid < 16) a.maxima[(w.index * a.splits + w.split) * 16 + tid] = larger(larger(s_max[0][tid], s_max[1][tid]), larger(s_max[2][tid], s_max[3][tid]));
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_values_kernel(SplitArgs a)
+{
+    constexpr int ND = D / 16, NW = 4;
+    __shared__ int32_t s_max[16][17];
+    __shared__ int32_t s_hi[D * 16], s_lo[D * 16], s_w[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const SplitAt w = split_at(a, blockIdx.x, blockIdx.y, blockIdx.z);
+    if (w.t.count == 0 || w.x0 >= w.x1) return;
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+    auto ask = [&](int x, v4i (&v)[ND], v4i (&s)[4]) {
+        const v4i* src = reinterpret_cast<const v4i*>(a.scores + ((w.index * a.blocks + x) * a.held + (c < a.held ? c : a.held - 1)) * 64 + g * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = src[i];
+        load_v<D>(a.p, block_offset<D>(a.p, w.b, w.h, block_at(w.t, x)), lane, v);
+    };
+    v4i vf[2][ND], sc[2][4];
+    int x = w.x0 + wave;
+    if (x < w.x1) ask(x, vf[0], sc[0]);
+    // the row's maximum: of all chunks
+    {
+        const int used = splits_used(a, w.t);
+        int32_t m = INT32_MIN;
+        for (int i = tid >> 4; i < used; i += 16) m = larger(m, a.maxima[(w.index * a.splits + i) * 16 + (tid & 15)]);
+        s_max[tid >> 4][tid & 15] = m;
+        for (int i = tid; i < D * 16; i += 256) { s_hi[i] = 0; s_lo[i] = 0; }
+        if (tid < 16) s_w[tid] = 0;
+    }
+    __syncthreads();
+    int32_t mx = s_max[0][c];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = larger(mx, s_max[i][c]);
+
+    v4i hi[ND], lo[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
+    uint32_t sum = 0;
+    auto take = [&](const v4i (&v)[ND], const v4i (&s)[4]) {
+        v4i wh, wl;
+        block_weights(a.p, s, mx, wh, wl, sum);
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[i], wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[i], wl, lo[i], 0, 0, 0);
+        }
+    };
+    while (x < w.x1) {
+        if (x + NW < w.x1) ask(x + NW, vf[1], sc[1]);
+        take(vf[0], sc[0]);
+        x += NW;
+        if (x >= w.x1) break;
+        if (x + NW < w.x1) ask(x + NW, vf[0], sc[0]);
+        take(vf[1], sc[1]);
+        x += NW;
+    }
+    // whole numbers: the order of these additions changes nothing
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            atomicAdd(&s_hi[(16 * i + 4 * g + r) * 16 + c], hi[i][r]);
+            atomicAdd(&s_lo[(16 * i + 4 * g + r) * 16 + c], lo[i][r]);
+        }
+    atomicAdd(&s_w[c], (int32_t)sum);
+    __syncthreads();
+    const int64_t at = w.index * a.splits + w.split;
+    if (tid < 16) a.sums[at * 16 + tid] = (uint32_t)s_w[tid];
+    for (int e = tid; e < a.held * D; e += 256) {
+        const int r = e / D, d = e - r * D;
+        a.parts[at * a.held * D + e] = (int64_t)s_hi[d * 16 + r] * 256 + s_lo[d * 16 + r];
+    }
+}
+
+// A workgroup for each row of a tile.
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(SplitArgs a)
+{
+    constexpr int GROUPS = 256 / D;
+    __shared__ int64_t s_n[256];
+    __shared__ uint32_t s_w[GROUPS];
+    const int tid = threadIdx.x, d = tid % D, part = tid / D, r = blockIdx.x;
+    const SplitAt w = split_at(a, 0, blockIdx.y, blockIdx.z);
+    if (r >= w.t.count) return;
+    const int used = splits_used(a, w.t);
+    int64_t N = 0;
+    uint32_t W = 0;
+#pragma unroll 8
+    for (int i = part; i < used; i += GROUPS) {
+        const int64_t at = w.index * a.splits + i;
+        N += a.parts[(at * a.held + r) * D + d];
+        W += a.sums[at * 16 + r];
+    }
+    s_n[tid] = N;
+    if (d == 0) s_w[part] = W;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) {
+        N += s_n[i * D + d];
+        W += s_w[i];
+    }
+    const int f = w.t.first + r, qr = f / a.p.group, hd = w.h * a.p.group + (f - qr * a.p.group);
+    a.p.out[(int64_t)(w.t.row0 + qr) * a.p.ld_out + hd * D + d] = finished(a.p, N, reciprocal(W));
+}
+
+// Which kernels run, and their workspace.
+struct Plan {
+    int32_t tiles, splits, chunk, blocks, held;
+    size_t maxima, sums, parts, scores, total;      // bytes from the workspace's start
+};
+static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache& c, int32_t batch, int32_t max_q_len, int32_t max_kv_len)
+{
+    Plan p = {};
+    const int64_t rows = (int64_t)max_q_len * (d.heads_q / c.heads_kv);
+    int64_t blocks = ((int64_t)max_kv_len + 63) / 64;
+    if (d.window > 0) {
+        const int64_t seen = ((int64_t)d.sinks + 63) / 64 + ((int64_t)d.window + max_q_len + 62) / 64 + 1;
+        blocks = blocks < seen ? blocks : seen;
+    }
+    p.tiles = (int32_t)((rows + 15) / 16);
+    p.held = rows < 16 ? (int32_t)rows : 16;
+    p.splits = 1;
+    if (rows > 16 || blocks <= 8 || batch == 0) return p;
+    const int64_t problems = (int64_t)batch * c.heads_kv * p.tiles;
+    int64_t splits = (1024 + problems - 1) / problems;
+    int64_t chunk = (blocks + splits - 1) / splits;
+    if (chunk < 4) chunk = 4;
+    splits = (blocks + chunk - 1) / chunk;
+    p.splits = (int32_t)splits; p.chunk = (int32_t)chunk; p.blocks = (int32_t)blocks;
+    const auto room = [&](int64_t n) {
+        const size_t at = p.total;
+        p.total += (size_t)((n + 255) / 256 * 256);
+        return at;
+    };
+    p.maxima = room(problems * splits * 64);
+    p.sums = room(problems * splits * 64);
+    p.parts = room(problems * splits * p.held * c.head_dim * 8);
+    p.scores = room(problems * blocks * p.held * 256);
+    if (p.total > ((size_t)2 << 30)) { p.total = 0; p.chunk = 0; }      // (not for so much room: the scores are made twice then)
+    return p;
+}
+
+template <int D>
+static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
+{
+    if (plan.chunk == 0) {
+        if (plan.tiles > 65535) return IBERT_ERR_SHAPE;
+        hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles), dim3(256), 0, stream, a);
+        IBERT_LAUNCH_CHECK("paged_attention_kernel");
+        g_last_kernel = "paged_attention_kernel";
+        return IBERT_OK;
+    }
+    SplitArgs s;
+    s.p = a; s.tiles = plan.tiles; s.splits = plan.splits; s.chunk = plan.chunk; s.blocks = plan.blocks; s.held = plan.held;
+    char* ws = static_cast<char*>(workspace);
+    s.maxima = reinterpret_cast<int32_t*>(ws + plan.maxima); s.sums = reinterpret_cast<uint32_t*>(ws + plan.sums);
+    s.parts = reinterpret_cast<int64_t*>(ws + plan.parts); s.scores = reinterpret_cast<int32_t*>(ws + plan.scores);
+    const dim3 grid((unsigned)plan.splits, (unsigned)(a.heads_kv * plan.tiles), (unsigned)batch);
+    hipLaunchKernelGGL(paged_scores_kernel<D>, grid, dim3(256), 0, stream, s);
+    IBERT_LAUNCH_CHECK("paged_scores_kernel");
+    hipLaunchKernelGGL(paged_values_kernel<D>, grid, dim3(256), 0, stream, s);
+    IBERT_LAUNCH_CHECK("paged_values_kernel");
+    hipLaunchKernelGGL(paged_join_kernel<D>, dim3((unsigned)plan.held, grid.y, grid.z), dim3(256), 0, stream, s);
+    IBERT_LAUNCH_CHECK("paged_join_kernel");
+    g_last_kernel = "paged_join_kernel";
     return IBERT_OK;
 }
 
@@ -233,8 +505,8 @@ static int check_paged(const ibert_paged_attention_desc* desc, const ibert_kv_ca
 extern "C" size_t ibert_paged_attention_workspace_bytes(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, int32_t batch,
                                                         int32_t rows, int32_t max_q_len, int32_t max_kv_len)
 {
-    (void)desc; (void)cache; (void)batch; (void)rows; (void)max_q_len; (void)max_kv_len;
-    return 0;
+    if (ibert::check_paged(desc, cache, batch, rows, max_q_len, max_kv_len)) return 0;
+    return ibert::plan_paged(*desc, *cache, batch, max_q_len, max_kv_len).total;
 }
 
 extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, const int8_t* q, int64_t ld_q,
@@ -250,7 +522,8 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     if (batch == 0 || rows == 0) return IBERT_OK;
     if (!q || !out || !block_table || !kv_len || !cache->k || !cache->v) return IBERT_ERR_NULL;
     if (!aligned(q, 16) || ld_q % 16 || !aligned(out, 4) || ld_out % 4 || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return IBERT_ERR_ALIGN;
-    (void)workspace; (void)workspace_bytes;
+    const Plan plan = plan_paged(d, *cache, batch, max_q_len, max_kv_len);
+    if (plan.total > 0 && (!workspace || workspace_bytes < plan.total || !aligned(workspace, 256))) return IBERT_ERR_WORKSPACE;
     PagedArgs a;
     a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.table = block_table; a.q_start = q_start; a.kv_len = kv_len;
     a.ld_q = ld_q; a.ld_out = ld_out; a.heads_q = d.heads_q; a.heads_kv = cache->heads_kv; a.group = d.heads_q / cache->heads_kv;
@@ -262,5 +535,5 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     a.s_m = (uint32_t)d.scores_dy.m; a.s_l = s < 32 ? 32 - s : 0; a.s_r = s > 32 ? s - 32 : 0; a.s_rnd = (uint64_t)1 << (s < 32 ? 31 : s - 1);
     a.out_dy = d.out_dy;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return D == 64 ? launch_paged<64>(a, batch, max_q_len, st) : launch_paged<128>(a, batch, max_q_len, st);
+    return D == 64 ? launch_paged<64>(a, plan, batch, workspace, st) : launch_paged<128>(a, plan, batch, workspace, st);
 }
