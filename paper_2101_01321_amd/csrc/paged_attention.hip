@@ -25,6 +25,7 @@ struct PagedArgs {
     uint32_t s_m;
     int32_t s_l, s_r;          // DY(d) = (((uint64)(d << s_l) * s_m + s_rnd) >> 32) >> s_r
     uint64_t s_rnd;
+    int32_t s_high, t_l, t_r;  // floor(2 DY's unrounded value): s_high ? mulhi(d, s_m) >> t_r : mulhi(d << t_l, s_m)
     ibert_dyadic out_dy;
 };
 
@@ -425,9 +426,188 @@ __global__ __launch_bounds__(256) void paged_join_kernel(SplitArgs a)
     a.p.out[(int64_t)(w.t.row0 + qr) * a.p.ld_out + hd * D + d] = finished(a.p, N, reciprocal(W));
 }
 
+// ---- many rows: prompts ------------------------------------------------------------------------------------------------
+// A workgroup of four wavefronts owns 128 rows, a wavefront two tiles of 16; K, and in the second pass K and V, come a block of 64
+// keys at a time straight into LDS, in operand order as the cache keeps them, one block ahead.  The first pass makes the
+// rows' maxima, the second the weights and the sums, which stay in registers.  A weight is read from a table in LDS: with
+// e = floor(2 (m - s) factor), one 32-bit product, the rounded distance is (e + 1) / 2 rounded down, and entry e is the two halves of its weight.
+constexpr int PP_THREADS = 256, PP_RT = 2, PP_ROWS = 4 * 16 * PP_RT, PP_TABLE = 2048;
+
+template <int D, bool HIGH>
+__global__ __launch_bounds__(PP_THREADS, 2) void paged_prompt_kernel(PagedArgs a)
+{
+    constexpr int NJ = D / 64, ND = D / 16, RT = PP_RT, BLOCK = 64 * D;
+    extern __shared__ __attribute__((aligned(16))) int8_t pp_lds[];          // K [2][BLOCK], V [2][BLOCK], table
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x, b = blockIdx.z;
+    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, PP_ROWS);        // (the rows with most keys first)
+    if (t.count == 0) return;
+    uint16_t* const table = reinterpret_cast<uint16_t*>(pp_lds + 4 * BLOCK);
+    for (int e = tid; e < PP_TABLE; e += PP_THREADS) {
+        const uint32_t d = (uint32_t)(e + 1) >> 1, z = d >> 6, f = 124u - (d & 63u);
+        const uint32_t w = (umad24(f, f, 8180u) + ((1u << z) >> 1)) >> z;
+        table[e] = (uint16_t)((w & 255u) | ((w + 128u) >> 8 << 8));
+    }
+
+    // the wavefront's tiles
+    int pos[RT];
+    v4i qf[RT][NJ];
+    Tile own = t;                                          // rows of this wavefront
+    own.first = t.first + wave * 16 * RT;
+    own.count = t.count - wave * 16 * RT;
+    own.count = own.count < 0 ? 0 : (own.count > 16 * RT ? 16 * RT : own.count);
+    const int last = own.count > 0 ? own.first + own.count - 1 : t.first;
+    own.low = t.pos0 + (own.count > 0 ? own.first : t.first) / a.group;
+    own.high = own.count > 0 ? t.pos0 + last / a.group : -1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        int flat = own.first + 16 * rt + c;
+        flat = flat < last ? flat : last;
+        const int qi = flat / a.group;
+        const int8_t* src = a.q + (int64_t)(t.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) qf[rt][j] = *reinterpret_cast<const v4i*>(src + 64 * j);
+        pos[rt] = t.pos0 + qi;
+    }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)pp_lds;
+    auto request = [&](const int8_t* from, int64_t at, uint32_t to) {
+#pragma unroll
+        for (int i = 0; i < ND / 4; ++i)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :: "s"(to + (uint32_t)((4 * i + wave) * 1024)), "v"((uint32_t)((4 * i + wave) * 1024 + lane * 16)), "s"(from + at) : "memory", "m0");
+    };
+    auto landed = [&]() {                                  // this wavefront's requests, then everybody's; and everybody has left the buffer before
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("s_barrier" ::: "memory");
+    };
+    auto scores = [&](const int8_t* ks, v4i (&s)[RT][4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][i] = v4i{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const v4i kf = *reinterpret_cast<const v4i*>(ks + (i * NJ + j) * 1024 + lane * 16);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qf[rt][j], s[rt][i], 0, 0, 0);
+            }
+        }
+    };
+
+    int32_t mx[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) mx[rt] = INT32_MIN;
+    const int n = t.blocks;
+    if (n > 0) request(a.k, block_offset<D>(a, b, h, block_at(t, 0)), lds0);
+    for (int x = 0; x < n; ++x) {
+        const int block = block_at(t, x);
+        const int64_t next = x + 1 < n ? block_offset<D>(a, b, h, block_at(t, x + 1)) : 0;
+        landed();
+        if (x + 1 < n) request(a.k, next, lds0 + (uint32_t)(((x + 1) & 1) * BLOCK));
+        if (64 * block > own.high) continue;
+        v4i s[RT][4];
+        scores(pp_lds + (x & 1) * BLOCK, s);
+        if (!whole_block(a, own, block)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) s[rt][i][r] = INT32_MIN;
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) mx[rt] = largest(s[rt], mx[rt]);
+    }
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) mx[rt] = combine_rows32(combine_rows16(mx[rt], larger), larger);
+
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");          // everybody has left the buffers, and the table is made
+    v4i hi[RT][ND], lo[RT][ND];
+    int32_t sum_h[RT], sum_l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        sum_h[rt] = sum_l[rt] = 0;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) { hi[rt][i] = v4i{0, 0, 0, 0}; lo[rt][i] = v4i{0, 0, 0, 0}; }
+    }
+    if (n > 0) {
+        const int64_t at = block_offset<D>(a, b, h, block_at(t, 0));
+        request(a.k, at, lds0);
+        request(a.v, at, lds0 + 2 * BLOCK);
+    }
+    for (int x = 0; x < n; ++x) {
+        const int block = block_at(t, x);
+        const int64_t next = x + 1 < n ? block_offset<D>(a, b, h, block_at(t, x + 1)) : 0;
+        landed();
+        if (x + 1 < n) {
+            request(a.k, next, lds0 + (uint32_t)(((x + 1) & 1) * BLOCK));
+            request(a.v, next, lds0 + (uint32_t)((2 + ((x + 1) & 1)) * BLOCK));
+        }
+        if (64 * block > own.high) continue;
+        v4i s[RT][4], wh[RT], wl[RT];
+        scores(pp_lds + (x & 1) * BLOCK, s);
+        const bool whole = whole_block(a, own, block);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t d = (uint32_t)mx[rt] - (uint32_t)s[rt][i][r];
+                    uint32_t e = HIGH ? __umulhi(d, a.s_m) >> (a.t_r & 31) : __umulhi(d << (a.t_l & 31), a.s_m);
+                    e = e < PP_TABLE - 1u ? e : PP_TABLE - 1u;
+                    w[r] = table[e];
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) w[r] = 0;
+                }
+                const uint32_t p = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), q = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+                wl[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x05040100u);
+                wh[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x07060302u);
+                sum_l[rt] = __builtin_amdgcn_sdot4(wl[rt][i], 0x01010101, sum_l[rt], false);
+                sum_h[rt] = __builtin_amdgcn_sdot4(wh[rt][i], 0x01010101, sum_h[rt], false);
+            }
+        const int8_t* vs = pp_lds + (2 + (x & 1)) * BLOCK;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const v4i vf = *reinterpret_cast<const v4i*>(vs + i * 1024 + lane * 16);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                hi[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wh[rt], hi[rt][i], 0, 0, 0);
+                lo[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wl[rt], lo[rt][i], 0, 0, 0);
+            }
+        }
+    }
+    const auto add = [](int32_t p, int32_t q) { return (int32_t)((uint32_t)p + (uint32_t)q); };
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        int32_t W = add((int32_t)((uint32_t)sum_h[rt] << 8), sum_l[rt]);
+        W = combine_rows32(combine_rows16(W, add), add);
+        const uint64_t R = reciprocal((uint32_t)W);
+        const int flat = own.first + 16 * rt + c;
+        if (16 * rt + c >= own.count) continue;
+        const int qi = flat / a.group;
+        int8_t* dst = a.out + (int64_t)(t.row0 + qi) * a.ld_out + (h * a.group + (flat - qi * a.group)) * D + 4 * g;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            int32_t y[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = finished(a, (int64_t)hi[rt][i][r] * 256 + lo[rt][i][r], R);
+            *reinterpret_cast<uint32_t*>(dst + 16 * i) = pack4_perm(y[0], y[1], y[2], y[3]);
+        }
+    }
+}
+
 // Which kernels run, and their workspace.
 struct Plan {
-    int32_t tiles, splits, chunk, blocks, held;
+    int32_t prompt_tiles;                           // > 0: paged_prompt_kernel
+    int32_t tiles, splits, chunk, blocks, held;     // chunk > 0: the three kernels for few rows
     size_t maxima, sums, parts, scores, total;      // bytes from the workspace's start
 };
 static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache& c, int32_t batch, int32_t max_q_len, int32_t max_kv_len)
@@ -442,6 +622,11 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     p.tiles = (int32_t)((rows + 15) / 16);
     p.held = rows < 16 ? (int32_t)rows : 16;
     p.splits = 1;
+    const int64_t prompt_tiles = (rows + PP_ROWS - 1) / PP_ROWS;
+    if (rows > 16 && prompt_tiles * batch * c.heads_kv >= 64) {
+        p.prompt_tiles = (int32_t)prompt_tiles;
+        return p;
+    }
     if (rows > 16 || blocks <= 8 || batch == 0) return p;
     const int64_t problems = (int64_t)batch * c.heads_kv * p.tiles;
     int64_t splits = (1024 + problems - 1) / problems;
@@ -465,6 +650,16 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
 template <int D>
 static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
 {
+    if (plan.prompt_tiles > 0) {
+        if (plan.prompt_tiles > 65535) return IBERT_ERR_SHAPE;
+        const size_t lds = 4 * 64 * D + 2 * PP_TABLE;
+        const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch);
+        if (a.s_high) hipLaunchKernelGGL((paged_prompt_kernel<D, true>), grid, dim3(PP_THREADS), lds, stream, a);
+        else hipLaunchKernelGGL((paged_prompt_kernel<D, false>), grid, dim3(PP_THREADS), lds, stream, a);
+        IBERT_LAUNCH_CHECK("paged_prompt_kernel");
+        g_last_kernel = "paged_prompt_kernel";
+        return IBERT_OK;
+    }
     if (plan.chunk == 0) {
         if (plan.tiles > 65535) return IBERT_ERR_SHAPE;
         hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles), dim3(256), 0, stream, a);
@@ -533,6 +728,7 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     a.window = d.window; a.sinks = d.sinks;
     const int s = d.scores_dy.s;
     a.s_m = (uint32_t)d.scores_dy.m; a.s_l = s < 32 ? 32 - s : 0; a.s_r = s > 32 ? s - 32 : 0; a.s_rnd = (uint64_t)1 << (s < 32 ? 31 : s - 1);
+    a.s_high = s >= 33; a.t_r = s >= 33 ? s - 33 : 0; a.t_l = s < 33 ? 33 - s : 0;
     a.out_dy = d.out_dy;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return D == 64 ? launch_paged<64>(a, plan, batch, workspace, st) : launch_paged<128>(a, plan, batch, workspace, st);
