@@ -25,7 +25,7 @@ struct PagedArgs {
     uint32_t s_m;
     int32_t s_l, s_r;          // DY(d) = (((uint64)(d << s_l) * s_m + s_rnd) >> 32) >> s_r
     uint64_t s_rnd;
-    int32_t s_high, t_l, t_r;  // floor(2 DY's unrounded value): s_high ? mulhi(d, s_m) >> t_r : mulhi(d << t_l, s_m)
+    int32_t s_s;               // the shift of DY; less 32 where that is not negative
     ibert_dyadic out_dy;
 };
 
@@ -73,7 +73,9 @@ template <int D>
 __device__ __forceinline__ int64_t block_offset(const PagedArgs& a, int b, int h, int block)
 {
     const int lp = a.log_page - 6;
-    int32_t page = a.table[(int64_t)b * a.max_pages + (block >> lp)];
+    // (a scalar load: no wait for it counts the requests of keys and values that are on their way)
+    const auto* entries = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.table;
+    int32_t page = entries[(int64_t)b * a.max_pages + (block >> lp)];
     page = clamp_i32(page, 0, a.num_pages - 1);
     return ((((int64_t)page * a.heads_kv + h) << lp) + (block & ((1 << lp) - 1))) * (64 * D);
 }
@@ -81,7 +83,8 @@ __device__ __forceinline__ int64_t block_offset(const PagedArgs& a, int b, int h
 // May every row of the tile see every key of the block?
 __device__ __forceinline__ bool whole_block(const PagedArgs& a, const Tile& t, int block)
 {
-    return 64 * block + 63 <= t.low && (a.window == 0 || 64 * block > t.high - a.window || 64 * block + 63 < a.sinks);
+    // (no branches: the tests stand beside matrix instructions, which a branch would part from what is to run beside them)
+    return (64 * block + 63 <= t.low) & ((a.window == 0) | (64 * block > t.high - a.window) | (64 * block + 63 < a.sinks));
 }
 __device__ __forceinline__ bool visible(const PagedArgs& a, int key, int pos)
 {
@@ -427,87 +430,202 @@ __global__ __launch_bounds__(256) void paged_join_kernel(SplitArgs a)
 }
 
 // ---- many rows: prompts ------------------------------------------------------------------------------------------------
-// A workgroup of four wavefronts owns 128 rows, a wavefront two tiles of 16; K, and in the second pass K and V, come a block of 64
-// keys at a time straight into LDS, in operand order as the cache keeps them, one block ahead.  The first pass makes the
-// rows' maxima, the second the weights and the sums, which stay in registers.  A weight is read from a table in LDS: with
-// e = floor(2 (m - s) factor), one 32-bit product, the rounded distance is (e + 1) / 2 rounded down, and entry e is the two halves of its weight.
-constexpr int PP_THREADS = 256, PP_RT = 2, PP_ROWS = 4 * 16 * PP_RT, PP_TABLE = 2048;
+// A workgroup of NW wavefronts owns 16 NW RT rows, a wavefront RT tiles of 16.  First the rows' maxima: a wavefront takes 64 of the
+// rows and every so-manieth block of keys, straight from memory into registers (operand order as the cache keeps it), so that
+// no key is read by more wavefronts than there are groups of 64 rows, and none waits for another before the end.  Then weights and sums, which stay in
+// registers: K and V come a block of 64 keys at a time into LDS, one block ahead, for all wavefronts.  A weight's two halves are read
+// from a table in LDS, entry DY(m - s): the maximum goes into the addend of the score's own 64-bit multiply-add.
+constexpr int PP_TABLE = 1025, PP_RT = 1, PP_NW = 4;
+constexpr int pp_rows(int rt, int nw) { return 16 * rt * nw; }
+constexpr int pp_lds_bytes(int d, int rt, int nw) { return 4 * 64 * d + 2064 + 4 * (nw / (pp_rows(rt, nw) / 64)) * pp_rows(rt, nw); }
 
-template <int D, bool HIGH>
-__global__ __launch_bounds__(PP_THREADS, 2) void paged_prompt_kernel(PagedArgs a)
+// Rows [first, first + n) of a tile, as a tile.
+__device__ __forceinline__ Tile part_of(const PagedArgs& a, const Tile& t, int first, int n)
 {
-    constexpr int NJ = D / 64, ND = D / 16, RT = PP_RT, BLOCK = 64 * D;
-    extern __shared__ __attribute__((aligned(16))) int8_t pp_lds[];          // K [2][BLOCK], V [2][BLOCK], table
+    Tile p = t;
+    p.first = t.first + first;
+    p.count = t.count - first;
+    p.count = p.count < 0 ? 0 : (p.count > n ? n : p.count);
+    p.low = t.pos0 + (p.count > 0 ? p.first : t.first) / a.group;
+    p.high = p.count > 0 ? t.pos0 + (p.first + p.count - 1) / a.group : -1;
+    return p;
+}
+// How many of the workgroup's blocks some row of the part may see (the others come last).
+__device__ __forceinline__ int blocks_of(const Tile& p)
+{
+    const int end = (p.high >> 6) + 1;
+    return p.high < 0 ? 0 : p.sink_blocks + (end > p.from ? end - p.from : 0);
+}
+// A lane's row of the part's tile rt: its position and its queries as operand (rows behind the last repeat it).
+template <int D>
+__device__ __forceinline__ void part_row(const PagedArgs& a, const Tile& p, int h, int rt, int c, int g, int& pos, v4i (&qf)[D / 64])
+{
+    const int last = p.first + (p.count > 0 ? p.count - 1 : 0);
+    int flat = p.first + 16 * rt + c;
+    flat = flat < last ? flat : last;
+    flat = p.count > 0 ? flat : 0;                         // (a part without rows: the sequence's first, not used)
+    const int qi = flat / a.group;
+    const int8_t* src = a.q + (int64_t)(p.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) qf[j] = *reinterpret_cast<const v4i*>(src + 64 * j);
+    pos = p.pos0 + qi;
+}
+
+// Largest raw scores of 64 rows over the blocks first, first + step, ... of the part's: K goes straight from memory into registers.
+template <int D>
+__device__ __forceinline__ void part_maxima(const PagedArgs& a, const Tile& p, int h, int b, int first, int step, int lane, int32_t (&mx)[4])
+{
+    constexpr int NJ = D / 64, ND = D / 16;
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+    const int c = lane & 15, g = lane >> 4, mine = blocks_of(p);
+    int pos[4];
+    v4i qf[4][NJ];
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+        part_row<D>(a, p, h, rt, c, g, pos[rt], qf[rt]);
+        mx[rt] = INT32_MIN;
+    }
+    v4i k0[ND / 2], k1[ND / 2];
+    auto ask = [&](int64_t at, v4i (&k)[ND / 2]) {
+#pragma unroll
+        for (int i = 0; i < ND / 2; ++i) k[i] = *reinterpret_cast<const v4i*>(a.k + at + i * 1024 + lane * 16);
+    };
+    auto take = [&](int key, bool whole, const v4i (&k)[ND / 2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v4i s[4];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) s[rt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[i * NJ + j], qf[rt][j], j == 0 ? v4i{0, 0, 0, 0} : s[rt], 0, 0, 0);
+            if (!whole) {
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!visible(a, key + 16 * i + 4 * g + r, pos[rt])) s[rt][r] = INT32_MIN;
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mx[rt] = larger(mx[rt], s[rt][r]);
+        }
+    };
+    // (of wide heads no registers are left for what is on its way)
+    constexpr bool AHEAD = D == 64;
+    if (AHEAD && first < mine) ask(block_offset<D>(a, b, h, block_at(p, first)), k0);
+    for (int x = first; x < mine; x += step) {
+        const int block = block_at(p, x);
+        const bool whole = whole_block(a, p, block);
+        const int64_t at = block_offset<D>(a, b, h, block);
+        if (!AHEAD) ask(at, k0);
+        ask(at + 32 * D, k1);
+        take(64 * block, whole, k0);
+        if (AHEAD) ask(block_offset<D>(a, b, h, block_at(p, x + step < mine ? x + step : x)), k0);
+        take(64 * block + 32, whole, k1);
+    }
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) mx[rt] = combine_rows32(combine_rows16(mx[rt], larger), larger);
+}
+
+template <int D, bool HIGH, int RT, int NW>
+__global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
+{
+    constexpr int NJ = D / 64, ND = D / 16, BLOCK = 64 * D, ROWS = pp_rows(RT, NW), GROUPS = ROWS / 64, SPLIT = NW / GROUPS;
+    extern __shared__ __attribute__((aligned(16))) int8_t pp_lds[];          // K [2][BLOCK], V [2][BLOCK], table, maxima [SPLIT][ROWS]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int h = blockIdx.x, b = blockIdx.z;
-    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, PP_ROWS);        // (the rows with most keys first)
+    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, ROWS);           // (the rows with most keys first)
     if (t.count == 0) return;
-    uint16_t* const table = reinterpret_cast<uint16_t*>(pp_lds + 4 * BLOCK);
-    for (int e = tid; e < PP_TABLE; e += PP_THREADS) {
-        const uint32_t d = (uint32_t)(e + 1) >> 1, z = d >> 6, f = 124u - (d & 63u);
+    typedef __attribute__((address_space(3))) uint16_t* lds_u16;
+    typedef __attribute__((address_space(3))) int32_t* lds_i32;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)pp_lds, table = lds0 + 4 * BLOCK;
+    const uint32_t maxima = table + 2064;
+    const int n = t.blocks;
+    auto offset = [&](int x) { return block_offset<D>(a, b, h, block_at(t, x < n ? x : (n > 0 ? n - 1 : 0))); };
+    auto request = [&](int64_t at, int buffer) {
+#pragma unroll
+        for (int i = 0; i < (2 * ND + NW - 1) / NW; ++i) {
+            const int piece = NW * i + wave;               // K's pieces of 1 KB, then V's
+            const bool of_v = piece >= ND;
+            if (2 * ND % NW == 0 || piece < 2 * ND)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(lds0 + (uint32_t)((of_v ? 2 * BLOCK - ND * 1024 : 0) + buffer * BLOCK + piece * 1024)),
+                                "v"((uint32_t)((piece - (of_v ? ND : 0)) * 1024 + lane * 16)), "s"((of_v ? a.v : a.k) + at) : "memory", "m0");
+        }
+    };
+    if (n > 0) request(offset(0), 0);
+    for (int e = tid; e < PP_TABLE; e += 64 * NW) {
+        const uint32_t z = (uint32_t)e >> 6, f = 124u - (e & 63u);
         const uint32_t w = (umad24(f, f, 8180u) + ((1u << z) >> 1)) >> z;
-        table[e] = (uint16_t)((w & 255u) | ((w + 128u) >> 8 << 8));
+        *(lds_u16)(uintptr_t)(table + 2u * (uint32_t)e) = (uint16_t)((w & 255u) | ((w + 128u) >> 8 << 8));
     }
 
-    // the wavefront's tiles
+    // ---- maxima -------------------------------------------------------------------------------------------------
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+    {
+        int32_t mx[4];
+        part_maxima<D>(a, part_of(a, t, 64 * (wave % GROUPS), 64), h, b, wave / GROUPS, SPLIT, lane, mx);
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+            if (g == 0) *(lds_i32)(uintptr_t)(maxima + 4u * (uint32_t)((wave / GROUPS) * ROWS + 64 * (wave % GROUPS) + 16 * rt + c)) = mx[rt];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");          // (and the table is made)
+
+    // ---- weights and sums ----------------------------------------------------------------------------------------
+    const Tile own = part_of(a, t, wave * 16 * RT, 16 * RT);
+    const int mine = blocks_of(own);
     int pos[RT];
     v4i qf[RT][NJ];
-    Tile own = t;                                          // rows of this wavefront
-    own.first = t.first + wave * 16 * RT;
-    own.count = t.count - wave * 16 * RT;
-    own.count = own.count < 0 ? 0 : (own.count > 16 * RT ? 16 * RT : own.count);
-    const int last = own.count > 0 ? own.first + own.count - 1 : t.first;
-    own.low = t.pos0 + (own.count > 0 ? own.first : t.first) / a.group;
-    own.high = own.count > 0 ? t.pos0 + last / a.group : -1;
+    int32_t mx[RT];
+    v4i hi[RT][ND], lo[RT][ND];
+    int32_t sum_h[RT], sum_l[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        int flat = own.first + 16 * rt + c;
-        flat = flat < last ? flat : last;
-        const int qi = flat / a.group;
-        const int8_t* src = a.q + (int64_t)(t.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
+        part_row<D>(a, own, h, rt, c, g, pos[rt], qf[rt]);
+        mx[rt] = INT32_MIN;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) qf[rt][j] = *reinterpret_cast<const v4i*>(src + 64 * j);
-        pos[rt] = t.pos0 + qi;
+        for (int i = 0; i < SPLIT; ++i) mx[rt] = larger(mx[rt], *(lds_i32)(uintptr_t)(maxima + 4u * (uint32_t)(i * ROWS + (wave * RT + rt) * 16 + c)));
+        sum_h[rt] = sum_l[rt] = 0;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) { hi[rt][i] = v4i{0, 0, 0, 0}; lo[rt][i] = v4i{0, 0, 0, 0}; }
     }
-
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)pp_lds;
-    auto request = [&](const int8_t* from, int64_t at, uint32_t to) {
-#pragma unroll
-        for (int i = 0; i < ND / 4; ++i)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                         :: "s"(to + (uint32_t)((4 * i + wave) * 1024)), "v"((uint32_t)((4 * i + wave) * 1024 + lane * 16)), "s"(from + at) : "memory", "m0");
-    };
-    auto landed = [&]() {                                  // this wavefront's requests, then everybody's; and everybody has left the buffer before
-        __builtin_amdgcn_s_waitcnt(0x0070);
-        asm volatile("s_barrier" ::: "memory");
-    };
     auto scores = [&](const int8_t* ks, v4i (&s)[RT][4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) s[rt][i] = v4i{0, 0, 0, 0};
-#pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 const v4i kf = *reinterpret_cast<const v4i*>(ks + (i * NJ + j) * 1024 + lane * 16);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qf[rt][j], s[rt][i], 0, 0, 0);
+                for (int rt = 0; rt < RT; ++rt) s[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qf[rt][j], j == 0 ? v4i{0, 0, 0, 0} : s[rt][i], 0, 0, 0);
             }
         }
     };
-
-    int32_t mx[RT];
+    // DY(m - s) = (s * -factor + (m * factor + 2^(shift-1))) >> shift
+    const int32_t minus_m = -(int32_t)a.s_m;
+    int64_t row_c[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) mx[rt] = INT32_MIN;
-    const int n = t.blocks;
-    if (n > 0) request(a.k, block_offset<D>(a, b, h, block_at(t, 0)), lds0);
+    for (int rt = 0; rt < RT; ++rt) row_c[rt] = (int64_t)mx[rt] * (int32_t)a.s_m + ((int64_t)1 << (HIGH ? a.s_s + 31 : a.s_s - 1));
     for (int x = 0; x < n; ++x) {
+        const int64_t next = offset(x + 1);
+        // block x has landed, for everybody, and everybody has left block x - 1
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("s_barrier" ::: "memory");
+        request(next, (x + 1) & 1);                        // (behind the last block: that one again)
+        if (x >= mine) continue;
         const int block = block_at(t, x);
-        const int64_t next = x + 1 < n ? block_offset<D>(a, b, h, block_at(t, x + 1)) : 0;
-        landed();
-        if (x + 1 < n) request(a.k, next, lds0 + (uint32_t)(((x + 1) & 1) * BLOCK));
-        if (64 * block > own.high) continue;
-        v4i s[RT][4];
+        v4i s[RT][4], wh[RT], wl[RT];
         scores(pp_lds + (x & 1) * BLOCK, s);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t p = (int64_t)s[rt][i][r] * minus_m + row_c[rt];
+                    const uint32_t d = HIGH ? (uint32_t)(p >> 32) >> (a.s_s & 31) : __builtin_amdgcn_alignbit((uint32_t)(p >> 32), (uint32_t)p, (uint32_t)(a.s_s & 31));
+                    s[rt][i][r] = (int32_t)(((d < PP_TABLE - 1u ? d : PP_TABLE - 1u) << 1) + table);
+                }
         if (!whole_block(a, own, block)) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -515,59 +633,20 @@ __global__ __launch_bounds__(PP_THREADS, 2) void paged_prompt_kernel(PagedArgs a
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) s[rt][i][r] = INT32_MIN;
+                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) s[rt][i][r] = (int32_t)(table + 2 * (PP_TABLE - 1));
         }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) mx[rt] = largest(s[rt], mx[rt]);
-    }
-    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) mx[rt] = combine_rows32(combine_rows16(mx[rt], larger), larger);
-
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");          // everybody has left the buffers, and the table is made
-    v4i hi[RT][ND], lo[RT][ND];
-    int32_t sum_h[RT], sum_l[RT];
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        sum_h[rt] = sum_l[rt] = 0;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) { hi[rt][i] = v4i{0, 0, 0, 0}; lo[rt][i] = v4i{0, 0, 0, 0}; }
-    }
-    if (n > 0) {
-        const int64_t at = block_offset<D>(a, b, h, block_at(t, 0));
-        request(a.k, at, lds0);
-        request(a.v, at, lds0 + 2 * BLOCK);
-    }
-    for (int x = 0; x < n; ++x) {
-        const int block = block_at(t, x);
-        const int64_t next = x + 1 < n ? block_offset<D>(a, b, h, block_at(t, x + 1)) : 0;
-        landed();
-        if (x + 1 < n) {
-            request(a.k, next, lds0 + (uint32_t)(((x + 1) & 1) * BLOCK));
-            request(a.v, next, lds0 + (uint32_t)((2 + ((x + 1) & 1)) * BLOCK));
-        }
-        if (64 * block > own.high) continue;
-        v4i s[RT][4], wh[RT], wl[RT];
-        scores(pp_lds + (x & 1) * BLOCK, s);
-        const bool whole = whole_block(a, own, block);
+                for (int r = 0; r < 4; ++r) s[rt][i][r] = *(lds_u16)(uintptr_t)(uint32_t)s[rt][i][r];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                uint32_t w[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t d = (uint32_t)mx[rt] - (uint32_t)s[rt][i][r];
-                    uint32_t e = HIGH ? __umulhi(d, a.s_m) >> (a.t_r & 31) : __umulhi(d << (a.t_l & 31), a.s_m);
-                    e = e < PP_TABLE - 1u ? e : PP_TABLE - 1u;
-                    w[r] = table[e];
-                }
-                if (!whole) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) w[r] = 0;
-                }
-                const uint32_t p = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), q = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+                const uint32_t p = __builtin_amdgcn_perm((uint32_t)s[rt][i][1], (uint32_t)s[rt][i][0], 0x05010400u);
+                const uint32_t q = __builtin_amdgcn_perm((uint32_t)s[rt][i][3], (uint32_t)s[rt][i][2], 0x05010400u);
                 wl[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x05040100u);
                 wh[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x07060302u);
                 sum_l[rt] = __builtin_amdgcn_sdot4(wl[rt][i], 0x01010101, sum_l[rt], false);
@@ -584,6 +663,7 @@ __global__ __launch_bounds__(PP_THREADS, 2) void paged_prompt_kernel(PagedArgs a
             }
         }
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);                    // (nothing is on its way into LDS any more)
     const auto add = [](int32_t p, int32_t q) { return (int32_t)((uint32_t)p + (uint32_t)q); };
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -606,7 +686,7 @@ __global__ __launch_bounds__(PP_THREADS, 2) void paged_prompt_kernel(PagedArgs a
 
 // Which kernels run, and their workspace.
 struct Plan {
-    int32_t prompt_tiles;                           // > 0: paged_prompt_kernel
+    int32_t prompt_tiles, high;                     // > 0: paged_prompt_kernel; the scores' shift is 32 or more
     int32_t tiles, splits, chunk, blocks, held;     // chunk > 0: the three kernels for few rows
     size_t maxima, sums, parts, scores, total;      // bytes from the workspace's start
 };
@@ -622,7 +702,8 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     p.tiles = (int32_t)((rows + 15) / 16);
     p.held = rows < 16 ? (int32_t)rows : 16;
     p.splits = 1;
-    const int64_t prompt_tiles = (rows + PP_ROWS - 1) / PP_ROWS;
+    p.high = d.scores_dy.s >= 32;
+    const int64_t prompt_tiles = (rows + pp_rows(PP_RT, PP_NW) - 1) / pp_rows(PP_RT, PP_NW);
     if (rows > 16 && prompt_tiles * batch * c.heads_kv >= 64) {
         p.prompt_tiles = (int32_t)prompt_tiles;
         return p;
@@ -652,10 +733,10 @@ static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, voi
 {
     if (plan.prompt_tiles > 0) {
         if (plan.prompt_tiles > 65535) return IBERT_ERR_SHAPE;
-        const size_t lds = 4 * 64 * D + 2 * PP_TABLE;
-        const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch);
-        if (a.s_high) hipLaunchKernelGGL((paged_prompt_kernel<D, true>), grid, dim3(PP_THREADS), lds, stream, a);
-        else hipLaunchKernelGGL((paged_prompt_kernel<D, false>), grid, dim3(PP_THREADS), lds, stream, a);
+        constexpr size_t lds = pp_lds_bytes(D, PP_RT, PP_NW);
+        const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch), block(64 * PP_NW);
+        if (plan.high) hipLaunchKernelGGL((paged_prompt_kernel<D, true, PP_RT, PP_NW>), grid, block, lds, stream, a);
+        else hipLaunchKernelGGL((paged_prompt_kernel<D, false, PP_RT, PP_NW>), grid, block, lds, stream, a);
         IBERT_LAUNCH_CHECK("paged_prompt_kernel");
         g_last_kernel = "paged_prompt_kernel";
         return IBERT_OK;
@@ -728,7 +809,7 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     a.window = d.window; a.sinks = d.sinks;
     const int s = d.scores_dy.s;
     a.s_m = (uint32_t)d.scores_dy.m; a.s_l = s < 32 ? 32 - s : 0; a.s_r = s > 32 ? s - 32 : 0; a.s_rnd = (uint64_t)1 << (s < 32 ? 31 : s - 1);
-    a.s_high = s >= 33; a.t_r = s >= 33 ? s - 33 : 0; a.t_l = s < 33 ? 33 - s : 0;
+    a.s_s = s >= 32 ? s - 32 : s;
     a.out_dy = d.out_dy;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return D == 64 ? launch_paged<64>(a, plan, batch, workspace, st) : launch_paged<128>(a, plan, batch, workspace, st);
