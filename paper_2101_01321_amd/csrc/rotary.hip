@@ -1,11 +1,16 @@
 // Rotary positions of queries and keys, the optional norm of each head in front of them, and the append of keys and values to
-// the paged cache (ibert_rotary_append_i): one pass over the packed QKV rows.
+// the paged cache (ibert_rotary_append_i): one launch over the packed QKV rows, in which some workgroups take queries, some keys,
+// some values.
 //
-// A head takes D / 16 lanes, 16 channels each, as two pieces of 8: the two halves of 8 pairs, so that no value crosses lanes
-// for the rotation.  (Half layout: channels 8 j .. and 8 j + R/2 ..; interleaved, and behind the rotated part: 16 j .. and
-// 16 j + 8 ..)  The norm adds up squares over the head's lanes in registers.  Cosine and sine stand in a table with 14
-// fractional bits: a rotated value is below 2^30, and its requantization is the same 64-bit step as a MatMul's.
-// Bound: HBM and the memory pipeline (16 bytes in and out of a lane).
+// Queries and keys: a head takes D / 2P lanes, each the two halves of P pairs, so that no value crosses lanes for the rotation.
+// (Half layout: channels P j .. and P j + R/2 ..; interleaved, and behind the rotated part: 2P j .. and 2P j + P ..)  P = 16 where
+// whole pieces of 16 bytes come out of it (R a multiple of 32), else 8.  The norm adds up squares over the head's lanes in
+// registers.  Cosine and sine stand in a table with 14 fractional bits: a rotated value is below 2^30, and its requantization is the
+// same 64-bit step as a MatMul's.
+// Values: the cache wants 16 tokens of a channel side by side.  A wavefront takes 16 channels of 64 rows.  Where rows L .. L + 63 fill a block
+// of the cache (a prompt), their bytes are transposed, four rows by lane swaps and the rest through LDS, and leave as 1 KB;
+// single rows are stored byte by byte.
+// Bound: HBM, and with norms the vector ALU next to it.
 #include "layernorm_math.h"
 
 namespace ibert {
@@ -13,130 +18,255 @@ namespace ibert {
 struct RotaryArgs {
     const int8_t* qkv;
     const int16_t* table;
-    const int32_t *positions, *slots, *q_gamma, *k_gamma;
+    const int32_t *positions, *slots;
+    const int32_t* gamma[2];   // queries, keys
     int8_t *q, *k, *v;
-    int64_t ld_qkv, ld_q;
-    int64_t groups;            // rows * heads of all three kinds
-    int32_t heads, heads_q, heads_kv, rot, max_pos, log_page, page_slots;
-    int32_t q_shift, k_shift;
-    ibert_dyadic q_dy, k_dy, v_dy;
+    int64_t ld_qkv, ld_q, rows;
+    int64_t wgs[2];            // workgroups of queries and of keys
+    int32_t heads_q, heads_kv, rot, max_pos, log_page, page_slots;
+    int32_t shift[2];
+    ibert_dyadic dy[2];
+    int32_t fast[2];           // the dyadic's shift is 33 or more: the high half of one multiply-add, shifted
+    int32_t v_l, v_r, v_m;     // DY(x) = ((x << v_l) * v_m + 2^(v_r + 31)) >> 32 >> v_r of a value
+    uint32_t heads_magic[2];
 };
 
 constexpr int RO_THREADS = 256;
 
-// DY(x; m, s), clamped to 8 bits.
-__device__ __forceinline__ int32_t requant8(int32_t x, ibert_dyadic dy)
-{
-    return clamp_i64_to_i32(dyadic64(x, dy.m, dy.s), 127);
-}
+__device__ __forceinline__ int32_t byte_of(uint32_t p, int i) { return (int32_t)(int8_t)(p >> (8 * i)); }
 
-__device__ __forceinline__ void unpack8(uint2 p, int32_t* x)
+template <int D, bool INTERLEAVED, int P>
+__device__ __forceinline__ void rotate_heads(const RotaryArgs& a, int64_t wg, int kind)
 {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (int32_t)(int8_t)((i < 4 ? p.x : p.y) >> (8 * (i & 3)));
-}
-__device__ __forceinline__ uint2 pack8(const int32_t* x)
-{
-    return make_uint2(pack4_perm(x[0], x[1], x[2], x[3]), pack4_perm(x[4], x[5], x[6], x[7]));
-}
-
-template <int D, bool INTERLEAVED>
-__global__ __launch_bounds__(RO_THREADS) void rotary_append_kernel(RotaryArgs a)
-{
-    constexpr int LPH = D / 16;
-    const int64_t group = (int64_t)blockIdx.x * (RO_THREADS / LPH) + threadIdx.x / LPH;
-    if (group >= a.groups) return;                         // (the lanes of a head together)
+    constexpr int LPH = D / (2 * P), W = P / 4;                // lanes of a head; dwords of a half
+    const int heads = kind ? a.heads_kv : a.heads_q;
+    const int64_t group = wg * (RO_THREADS / LPH) + threadIdx.x / LPH;
     const int j = threadIdx.x % LPH;
-    const int64_t row = group / a.heads;
-    const int head = (int)(group - row * a.heads);
+    int64_t row;
+    if (group <= 0x7fffffff) row = udiv_fix((int32_t)group, heads, a.heads_magic[kind]);
+    else row = group / heads;
+    if (row >= a.rows) return;                             // (the lanes of a head together)
+    const int head = (int)(group - row * heads);
     const int32_t slot = a.slots[row];
     if ((uint32_t)slot >= (uint32_t)a.page_slots) return;
-    const int8_t* src = a.qkv + row * a.ld_qkv + head * D;
-    const int kv = head - a.heads_q;                       // which key head, or heads_kv + which value head
-    const int64_t page = slot >> a.log_page;
-    const int t = slot & ((1 << a.log_page) - 1);
-
-    if (kv >= a.heads_kv) {
-        int32_t x[16];
-        const uint4 p = *reinterpret_cast<const uint4*>(src + 16 * j);
-        unpack8(make_uint2(p.x, p.y), x);
-        unpack8(make_uint2(p.z, p.w), x + 8);
-        int8_t* dst = a.v + (((page * a.heads_kv + (kv - a.heads_kv)) << a.log_page) + (t & ~63)) * D + j * 1024 + ((t >> 2) & 3) * 256 +
-                      ((t >> 4) & 3) * 4 + (t & 3);
+    const bool turned = 2 * P * j < a.rot;
+    const int c0 = turned && !INTERLEAVED ? P * j : 2 * P * j, c1 = turned && !INTERLEAVED ? P * j + a.rot / 2 : 2 * P * j + P;
+    const int8_t* src = a.qkv + row * a.ld_qkv + (head + (kind ? a.heads_q : 0)) * D;
+    uint32_t p0[W], p1[W], cs[P];
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
+    {
+        const words w0 = *reinterpret_cast<const words*>(src + c0), w1 = *reinterpret_cast<const words*>(src + c1);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dst[16 * i] = (int8_t)requant8(x[i], a.v_dy);
-        return;
+        for (int i = 0; i < W; ++i) { p0[i] = w0[i]; p1[i] = w1[i]; }
     }
-    const bool turned = 16 * j < a.rot;
-    const int c0 = turned && !INTERLEAVED ? 8 * j : 16 * j, c1 = turned && !INTERLEAVED ? 8 * j + a.rot / 2 : 16 * j + 8;
-    int32_t x[16];
-    unpack8(*reinterpret_cast<const uint2*>(src + c0), x);
-    unpack8(*reinterpret_cast<const uint2*>(src + c1), x + 8);
+    if (turned) {
+        const int32_t pos = clamp_i32(a.positions[row], 0, a.max_pos - 1);
+        const uint4* t = reinterpret_cast<const uint4*>(a.table + ((int64_t)pos * (a.rot / 2) + P * j) * 2);
+#pragma unroll
+        for (int i = 0; i < P / 4; ++i) {
+            const uint4 w = t[i];
+            cs[4 * i] = w.x; cs[4 * i + 1] = w.y; cs[4 * i + 2] = w.z; cs[4 * i + 3] = w.w;
+        }
+    }
+    int32_t x[2 * P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) { x[i] = byte_of(p0[i / 4], i & 3); x[P + i] = byte_of(p1[i / 4], i & 3); }
 
-    const int32_t* gamma = kv < 0 ? a.q_gamma : a.k_gamma;
+    const int32_t* gamma = a.gamma[kind];
     if (gamma) {
-        const int32_t shift = kv < 0 ? a.q_shift : a.k_shift;
+        const int32_t shift = a.shift[kind];
         int32_t ss = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ss += smul24(x[i], x[i]);
+        for (int i = 0; i < W; ++i) {
+            ss = __builtin_amdgcn_sdot4((int32_t)p0[i], (int32_t)p0[i], ss, false);
+            ss = __builtin_amdgcn_sdot4((int32_t)p1[i], (int32_t)p1[i], ss, false);
+        }
         const auto add = [](int32_t p, int32_t q) { return p + q; };
         ss = add(ss, dpp_mov<0xB1>(ss));
-        ss = add(ss, dpp_mov<0x4E>(ss));
+        if (LPH > 2) ss = add(ss, dpp_mov<0x4E>(ss));
         if (LPH > 4) ss = add(ss, dpp_mov<0x141>(ss));
-        // sum <= 2^14 D: the mean's 16 fractional bits make it less than 2^31
+        // sum <= 2^14 D: the mean's 16 fractional bits make it at most 2^30
         uint32_t sigma = isqrt_floor_lane((uint32_t)ss * (65536u / D));
         sigma = sigma < 1 ? 1 : sigma;
-        const int32_t f = (int32_t)((1u << 30) / sigma);
-        const int32_t rnd = 1 << (shift - 1);
+        const int32_t f = (int32_t)((1u << 30) / sigma), rnd = 1 << (shift - 1);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int32_t n = (x[i] * f) >> 12;
-            x[i] = clamp_i32((n * gamma[i < 8 ? c0 + i : c1 + i - 8] + rnd) >> shift, -32767, 32767);
+        for (int half = 0; half < 2; ++half) {
+            const int4* g4 = reinterpret_cast<const int4*>(gamma + (half ? c1 : c0));
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const int4 w = g4[i];
+                const int32_t gm[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    int32_t& u = x[P * half + 4 * i + r];
+                    u = clamp_i32(smad24((u * f) >> 12, gm[r], rnd) >> shift, -32767, 32767);
+                }
+            }
         }
     }
     if (turned) {
-        int32_t pos = a.positions[row];
-        pos = clamp_i32(pos, 0, a.max_pos - 1);
-        const uint4* cs4 = reinterpret_cast<const uint4*>(a.table + ((int64_t)pos * (a.rot / 2) + 8 * j) * 2);
-        const uint4 w0 = cs4[0], w1 = cs4[1];
-        const uint32_t cs[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < P; ++i) {
             const int32_t c = (int32_t)(int16_t)cs[i], s = (int32_t)cs[i] >> 16;
-            int32_t& p = INTERLEAVED ? x[2 * i] : x[i];
-            int32_t& q = INTERLEAVED ? x[2 * i + 1] : x[8 + i];
+            int32_t& p = x[INTERLEAVED ? 2 * i : i];
+            int32_t& q = x[INTERLEAVED ? 2 * i + 1 : P + i];
             const int32_t y = smul24(p, c) - smul24(q, s);
-            q = smul24(p, s) + smul24(q, c);
+            q = smad24(p, s, smul24(q, c));
             p = y;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] <<= 14;
+        for (int i = 0; i < 2 * P; ++i) x[i] <<= 14;
     }
-    const ibert_dyadic dy = kv < 0 ? a.q_dy : a.k_dy;
+    const ibert_dyadic dy = a.dy[kind];
+    if (a.fast[kind]) {
+        const int64_t rnd = (int64_t)1 << (dy.s - 1);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = requant8(x[i], dy);
-    if (kv < 0) {
-        int8_t* dst = a.q + row * a.ld_q + head * D;
-        *reinterpret_cast<uint2*>(dst + c0) = pack8(x);
-        *reinterpret_cast<uint2*>(dst + c1) = pack8(x + 8);
+        for (int i = 0; i < 2 * P; ++i) x[i] = med3_const<-127, 127>((int32_t)(((int64_t)x[i] * dy.m + rnd) >> 32) >> ((dy.s - 32) & 31));
     } else {
-        int8_t* dst = a.k + (((page * a.heads_kv + kv) << a.log_page) + (t & ~15)) * D + (t & 15) * 16;
-        *reinterpret_cast<uint2*>(dst + (c0 >> 4) * 256 + (c0 & 15)) = pack8(x);
-        *reinterpret_cast<uint2*>(dst + (c1 >> 4) * 256 + (c1 & 15)) = pack8(x + 8);
+#pragma unroll
+        for (int i = 0; i < 2 * P; ++i) x[i] = clamp_i64_to_i32(dyadic64(x[i], dy.m, dy.s), 127);
+    }
+    words o0, o1;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        o0[i] = pack4_perm(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        o1[i] = pack4_perm(x[P + 4 * i], x[P + 4 * i + 1], x[P + 4 * i + 2], x[P + 4 * i + 3]);
+    }
+    if (kind == 0) {
+        int8_t* dst = a.q + row * a.ld_q + head * D;
+        *reinterpret_cast<words*>(dst + c0) = o0;
+        *reinterpret_cast<words*>(dst + c1) = o1;
+    } else {
+        const int64_t page = slot >> a.log_page;
+        const int t = slot & ((1 << a.log_page) - 1);
+        int8_t* dst = a.k + (((page * a.heads_kv + head) << a.log_page) + (t & ~15)) * D + (t & 15) * 16;
+        *reinterpret_cast<words*>(dst + (c0 >> 4) * 256 + (c0 & 15)) = o0;
+        *reinterpret_cast<words*>(dst + (c1 >> 4) * 256 + (c1 & 15)) = o1;
     }
 }
 
-template <int D, bool INTERLEAVED>
-static int launch_rotary(const RotaryArgs& a, hipStream_t stream)
+// 16 values of a row, requantized.
+__device__ __forceinline__ void value_row(const RotaryArgs& a, const int8_t* src, uint32_t (&y)[4])
 {
-    constexpr int per = RO_THREADS / (D / 16);
-    const int64_t wgs = (a.groups + per - 1) / per;
+    const uint4 p = *reinterpret_cast<const uint4*>(src);
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    const int64_t rnd = (int64_t)1 << (a.v_r + 31);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        int32_t x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int32_t v = (int32_t)(((int64_t)(int32_t)((uint32_t)byte_of(w[i], r) << a.v_l) * a.v_m + rnd) >> 32) >> a.v_r;
+            x[r] = med3_const<-127, 127>(v);
+        }
+        y[i] = pack4_perm(x[0], x[1], x[2], x[3]);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, uint32_t* lds)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = (int)(wg % a.heads_kv);
+    const int64_t row0 = wg / a.heads_kv * 64, row = row0 + lane;
+    // slots of the 64 rows, of those before and of those behind; which continue the row before
+    const auto slot_at = [&](int64_t r) { return r >= 0 && r < a.rows ? a.slots[r] : -1; };
+    const int32_t s0 = slot_at(row - 64), s1 = slot_at(row), s2 = slot_at(row + 64);
+    const auto goes_on = [&](int32_t s, int32_t first_before) {
+        const int32_t b = __shfl_up(s, 1), before = lane ? b : first_before;
+        return __builtin_amdgcn_ballot_w64(s > 0 && (uint32_t)s < (uint32_t)a.page_slots && s == (int32_t)((uint32_t)before + 1u));
+    };
+    const uint64_t g0 = goes_on(s0, -1), g1 = goes_on(s1, __shfl(s0, 63)), g2 = goes_on(s2, __shfl(s1, 63));
+    const bool in = (uint32_t)s1 < (uint32_t)a.page_slots;
+    // row L of this row's block, seen from row0: the 63 rows behind L have to go on from it (an aligned block lies within one page)
+    const int at = lane - (s1 & 63);
+    bool filled = false;
+    if (in) {
+        const int from = at + 1;                           // in -62 .. 64
+        uint64_t run;
+        if (from < 0) run = (g0 >> (64 + from)) | (g1 << -from);
+        else if (from == 0) run = g1;
+        else if (from < 64) run = (g1 >> from) | (g2 << (64 - from));
+        else run = g2;
+        filled = (run << 1) == ~(uint64_t)1;
+    }
+    const uint64_t starts = __builtin_amdgcn_ballot_w64(filled && (s1 & 63) == 0);
+    for (int j = wave; j < D / 16; j += RO_THREADS / 64) {
+        const int8_t* src = a.qkv + (a.heads_q + a.heads_kv + head) * D + 16 * j;
+        if (in && !filled) {
+            uint32_t y[4];
+            value_row(a, src + row * a.ld_qkv, y);
+            const int64_t page = s1 >> a.log_page;
+            const int t = s1 & ((1 << a.log_page) - 1);
+            int8_t* dst = a.v + (((page * a.heads_kv + head) << a.log_page) + (t & ~63)) * D + j * 1024 + ((t >> 2) & 3) * 256 + ((t >> 4) & 3) * 4 + (t & 3);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dst[16 * i] = (int8_t)byte_of(y[i / 4], i & 3);
+        }
+        if (starts) {                                      // (one at most)
+            const int first = __builtin_ctzll(starts);
+            const int32_t slot = __builtin_amdgcn_readlane(s1, first);
+            uint32_t y[4];
+            value_row(a, src + (row0 + first + lane) * a.ld_qkv, y);
+            // four rows are four neighbouring lanes: byte r' of lane r becomes byte r of lane r'
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t o = (uint32_t)dpp_mov<0xB1>((int32_t)y[i]);
+                y[i] = __builtin_amdgcn_perm(o, y[i], lane & 1 ? 0x03070105u : 0x06020400u);
+                const uint32_t q = (uint32_t)dpp_mov<0x4E>((int32_t)y[i]);
+                y[i] = __builtin_amdgcn_perm(q, y[i], lane & 2 ? 0x03020706u : 0x05040100u);
+            }
+            // lane 16 i + 4 g + r: its dword of channel 4 n + r goes to [g][channel][i]
+            uint32_t* mine = lds + wave * 256;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) mine[((lane >> 2) & 3) * 64 + (4 * n + (lane & 3)) * 4 + (lane >> 4)] = y[n];
+            __builtin_amdgcn_wave_barrier();
+            const uint4 o = *reinterpret_cast<const uint4*>(mine + 4 * lane);
+            __builtin_amdgcn_wave_barrier();
+            const int64_t page = slot >> a.log_page;
+            const int t = slot & ((1 << a.log_page) - 1);
+            *reinterpret_cast<uint4*>(a.v + (((page * a.heads_kv + head) << a.log_page) + t) * D + j * 1024 + lane * 16) = o;
+        }
+    }
+}
+
+template <int D, bool INTERLEAVED, int P>
+__global__ __launch_bounds__(RO_THREADS) void rotary_append_kernel(RotaryArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t lds[RO_THREADS / 64 * 256];
+    const int64_t wg = blockIdx.x;
+    if (wg < a.wgs[0]) rotate_heads<D, INTERLEAVED, P>(a, wg, 0);
+    else if (wg < a.wgs[0] + a.wgs[1]) rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[0], 1);
+    else append_values<D>(a, wg - a.wgs[0] - a.wgs[1], lds);
+}
+
+// The same multiplier with a shift of at least `least`, where 31 bits hold it: DY(x; 2m, s + 1) = DY(x; m, s).
+static ibert_dyadic shifted(ibert_dyadic d, int least)
+{
+    while (d.s < least && d.m < (1 << 30) && d.m > -(1 << 30)) { d.m *= 2; ++d.s; }
+    return d;
+}
+
+template <int D, bool INTERLEAVED, int P>
+static int launch_rotary(RotaryArgs& a, hipStream_t stream)
+{
+    constexpr int per = RO_THREADS / (D / (2 * P));
+    a.wgs[0] = (a.rows * a.heads_q + per - 1) / per;
+    a.wgs[1] = (a.rows * a.heads_kv + per - 1) / per;
+    const int64_t wgs = a.wgs[0] + a.wgs[1] + (a.rows + 63) / 64 * a.heads_kv;
     if (wgs > 0x7fffffffLL) return IBERT_ERR_SHAPE;
-    hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED>), dim3((unsigned)wgs), dim3(RO_THREADS), 0, stream, a);
+    hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED, P>), dim3((unsigned)wgs), dim3(RO_THREADS), 0, stream, a);
     IBERT_LAUNCH_CHECK("rotary_append_kernel");
     g_last_kernel = "rotary_append_kernel";
     return IBERT_OK;
+}
+
+template <int D>
+static int launch_rotary(RotaryArgs& a, bool interleaved, hipStream_t stream)
+{
+    const bool wide = a.rot % 32 == 0;
+    if (interleaved) return wide ? launch_rotary<D, true, 16>(a, stream) : launch_rotary<D, true, 8>(a, stream);
+    return wide ? launch_rotary<D, false, 16>(a, stream) : launch_rotary<D, false, 8>(a, stream);
 }
 
 }  // namespace ibert
@@ -157,18 +287,23 @@ extern "C" int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_
         !dyadic_ok(d.q_dy) || !dyadic_ok(d.k_dy) || !dyadic_ok(d.v_dy) || (d.rot_dim > 0 && d.max_pos < 1) ||
         (q_gamma && (d.q_norm_shift < 1 || d.q_norm_shift > 30)) || (k_gamma && (d.k_norm_shift < 1 || d.k_norm_shift > 30))) return IBERT_ERR_PARAM_RANGE;
     if (rows == 0) return IBERT_OK;
-    if (rows > INT64_MAX / heads) return IBERT_ERR_SHAPE;
+    if (rows > INT32_MAX) return IBERT_ERR_SHAPE;
     if (!qkv || !slots || !q || !cache->k || !cache->v || (d.rot_dim > 0 && (!table || !positions))) return IBERT_ERR_NULL;
-    if (!aligned(qkv, 16) || !aligned(q, 16) || !aligned(cache->k, 16) || !aligned(cache->v, 16) || !aligned(table, 16) || ld_qkv % 16 || ld_q % 16)
-        return IBERT_ERR_ALIGN;
+    if (!aligned(qkv, 16) || !aligned(q, 16) || !aligned(cache->k, 16) || !aligned(cache->v, 16) || !aligned(table, 16) || ld_qkv % 16 || ld_q % 16 ||
+        !aligned(q_gamma, 16) || !aligned(k_gamma, 16)) return IBERT_ERR_ALIGN;
     RotaryArgs a;
-    a.qkv = qkv; a.table = table; a.positions = positions; a.slots = slots; a.q_gamma = q_gamma; a.k_gamma = k_gamma;
-    a.q = q; a.k = cache->k; a.v = cache->v; a.ld_qkv = ld_qkv; a.ld_q = ld_q;
-    a.groups = rows * heads; a.heads = heads; a.heads_q = d.heads_q; a.heads_kv = cache->heads_kv;
-    a.rot = d.rot_dim; a.max_pos = d.max_pos;
+    a.qkv = qkv; a.table = table; a.positions = positions; a.slots = slots; a.gamma[0] = q_gamma; a.gamma[1] = k_gamma;
+    a.q = q; a.k = cache->k; a.v = cache->v; a.ld_qkv = ld_qkv; a.ld_q = ld_q; a.rows = rows;
+    a.heads_q = d.heads_q; a.heads_kv = cache->heads_kv; a.rot = d.rot_dim; a.max_pos = d.max_pos;
     a.log_page = __builtin_ctz((unsigned)cache->page_size); a.page_slots = cache->num_pages * cache->page_size;
-    a.q_shift = d.q_norm_shift; a.k_shift = d.k_norm_shift; a.q_dy = d.q_dy; a.k_dy = d.k_dy; a.v_dy = d.v_dy;
+    a.shift[0] = d.q_norm_shift; a.shift[1] = d.k_norm_shift; 
+    a.dy[0] = shifted(d.q_dy, 33); a.dy[1] = shifted(d.k_dy, 33);
+    a.fast[0] = a.dy[0].s >= 33; a.fast[1] = a.dy[1].s >= 33;
+    // (a shift that stays below 9 stands for a multiplier of 2^21 and more: any value but 0 comes out at the end of the range)
+    ibert_dyadic v = shifted(d.v_dy, 33);
+    if (v.s < 9) v.s = 9;
+    a.v_m = v.m; a.v_l = v.s < 33 ? 33 - v.s : 0; a.v_r = v.s < 33 ? 1 : v.s - 32;
+    a.heads_magic[0] = udiv_magic(d.heads_q); a.heads_magic[1] = udiv_magic(cache->heads_kv);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (d.layout == IBERT_ROTARY_INTERLEAVED) return D == 64 ? launch_rotary<64, true>(a, st) : launch_rotary<128, true>(a, st);
-    return D == 64 ? launch_rotary<64, false>(a, st) : launch_rotary<128, false>(a, st);
+    return D == 64 ? launch_rotary<64>(a, d.layout == IBERT_ROTARY_INTERLEAVED, st) : launch_rotary<128>(a, d.layout == IBERT_ROTARY_INTERLEAVED, st);
 }

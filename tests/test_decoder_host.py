@@ -230,7 +230,7 @@ def test_rotary_refuses():
         return B.lib().ibert_rotary_append_i(C.byref(d), C.byref(c or cache()), p["qkv"], ld, p["table"], p["positions"], p["slots"], p["gq"], p["gk"], rows, p["q"], ld_q, None)
     for kw, rc in BAD_CACHES:
         assert call(c=cache(**kw)) == rc, kw
-    for kw in (dict(rows=-1), dict(ld=8 * 64 - 16), dict(ld_q=4 * 64 - 16), dict(desc=dict(heads_q=0)), dict(desc=dict(heads_q=5)), dict(rows=1 << 62)):
+    for kw in (dict(rows=-1), dict(ld=8 * 64 - 16), dict(ld_q=4 * 64 - 16), dict(desc=dict(heads_q=0)), dict(desc=dict(heads_q=5)), dict(rows=1 << 62), dict(rows=1 << 31)):
         assert call(**kw) == -2, kw
     for kw in (dict(desc=dict(rot_dim=-16)), dict(desc=dict(rot_dim=8)), dict(desc=dict(rot_dim=80)), dict(desc=dict(layout=2)), dict(desc=dict(max_pos=0)),
                dict(desc=dict(q_dy=B.Dyadic(1, 63))), dict(desc=dict(k_dy=B.Dyadic(1, -1))), dict(desc=dict(v_dy=B.Dyadic(1, 63))),
@@ -239,7 +239,7 @@ def test_rotary_refuses():
     for name in ("qkv", "table", "positions", "slots", "q"):
         assert call(**{name: None}) == -1, name
     assert call(c=cache(k=None)) == -1 and call(c=cache(v=None)) == -1
-    for kw in (dict(qkv=DUMMY + 8), dict(q=DUMMY + 8), dict(table=DUMMY + 4), dict(ld=8 * 64 + 8), dict(ld_q=4 * 64 + 8), dict(c=cache(k=DUMMY + 8)), dict(c=cache(v=DUMMY + 1))):
+    for kw in (dict(qkv=DUMMY + 8), dict(q=DUMMY + 8), dict(table=DUMMY + 4), dict(gq=DUMMY + 8), dict(gk=DUMMY + 4), dict(ld=8 * 64 + 8), dict(ld_q=4 * 64 + 8), dict(c=cache(k=DUMMY + 8)), dict(c=cache(v=DUMMY + 1))):
         assert call(**kw) == -4, kw
     assert call(rows=0, qkv=None, q=None, slots=None) == 0
 

@@ -135,6 +135,36 @@ def test_rotary_append_of_any_dyadic(gpu, dy):
         same(got, want, what)
 
 
+@pytest.mark.parametrize("D,page", [(64, 64), (128, 256)])
+def test_values_of_rows_that_fill_blocks(gpu, D, page):
+    # runs of rows on runs of slots that start and end anywhere, with gaps, rows without a slot and runs that meet in one block
+    torch, G, B = libs()
+    runs = [(0, 64), (70, 64), (200, 300), (640, 1), (641, 63), (704, 128), (900, 59), (960, 63), (1024, 64), (1090, 190), (1280, 130)]
+    rows = sum(n for _, n in runs) + 5
+    case = U.Rotary(D, rows, 2, 2, D, 32, False, page)
+    order = np.random.default_rng(D).permutation(len(runs))
+    slots = np.concatenate([np.arange(s, s + n) for s, n in (runs[i] for i in order)] + [np.full(5, -1)])
+    case.slots = slots.astype(np.int32)
+    for skip in ((), (3, 64, 300), range(0, rows, 65)):
+        for i in skip:
+            case.slots[i] = -1
+        G.say("values in blocks, D %d, %d rows without a slot" % (D, len(skip)))
+        for got, want, what in zip(run_rotary(case), case.oracle(), "qkv"):
+            same(got, want, what)
+
+
+@pytest.mark.parametrize("dy", [(0, 0), (1, 0), (-1, 0), (3, 1), (127, 8), (2 ** 31 - 1, 0), (-(2 ** 31 - 1), 8), (2 ** 30, 9), (2 ** 30, 30), (2 ** 31 - 1, 32), (-(2 ** 30), 33), (2 ** 31 - 1, 40), (5, 62)])
+def test_values_of_any_dyadic(gpu, dy):
+    torch, G, B = libs()
+    case = U.Rotary(9, 200, 1, 1, 64, 0, False, 64)
+    case.slots = (np.arange(200) + 10).astype(np.int32)
+    case.qkv[:, 128:192] = np.arange(200 * 64).reshape(200, 64) % 256 - 128          # every value there is
+    case.v_dy = dy
+    G.say("values, dyadic %s" % (dy,))
+    for got, want, what in zip(run_rotary(case), case.oracle(), "qkv"):
+        same(got, want, what)
+
+
 def test_rotary_append_of_many_rows(gpu):
     torch, G, B = libs()
     for D, rows in ((64, 3001), (128, 1403)):
