@@ -7,9 +7,9 @@
 // whole pieces of 16 bytes come out of it (R a multiple of 32), else 8.  The norm adds up squares over the head's lanes in
 // registers.  Cosine and sine stand in a table with 14 fractional bits: a rotated value is below 2^30, and its requantization is the
 // same 64-bit step as a MatMul's.
-// Values: the cache wants 16 tokens of a channel side by side.  A wavefront takes 16 channels of 64 rows.  Where rows L .. L + 63 fill a block
-// of the cache (a prompt), their bytes are transposed, four rows by lane swaps and the rest through LDS, and leave as 1 KB;
-// single rows are stored byte by byte.
+// Values: the cache wants 16 tokens of a channel side by side.  A wavefront takes 16 channels of 64 rows.  Where rows follow each other into
+// a block of 64 tokens (a prompt), their bytes are transposed, four rows by lane swaps and the rest through LDS, and leave as 1 KB, or
+// as the dwords and bytes of it that they fill; single rows are stored byte by byte.
 // Bound: HBM, and with norms the vector ALU next to it.
 #include "layernorm_math.h"
 
@@ -22,7 +22,7 @@ struct RotaryArgs {
     const int32_t* gamma[2];   // queries, keys
     int8_t *q, *k, *v;
     int64_t ld_qkv, ld_q, rows;
-    int64_t wgs[2];            // workgroups of queries and of keys
+    int64_t wgs[3];            // workgroups of queries, of keys, of values
     int32_t heads_q, heads_kv, rot, max_pos, log_page, page_slots;
     int32_t shift[2];
     ibert_dyadic dy[2];
@@ -179,22 +179,23 @@ __device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, u
     };
     const uint64_t g0 = goes_on(s0, -1), g1 = goes_on(s1, __shfl(s0, 63)), g2 = goes_on(s2, __shfl(s1, 63));
     const bool in = (uint32_t)s1 < (uint32_t)a.page_slots;
-    // row L of this row's block, seen from row0: the 63 rows behind L have to go on from it (an aligned block lies within one page)
-    const int at = lane - (s1 & 63);
-    bool filled = false;
+    // The rows on the slots around this one that are in the same block of the cache: how many behind this row, how many before it.
+    int after = 0, before = 0;
     if (in) {
-        const int from = at + 1;                           // in -62 .. 64
-        uint64_t run;
-        if (from < 0) run = (g0 >> (64 + from)) | (g1 << -from);
-        else if (from == 0) run = g1;
-        else if (from < 64) run = (g1 >> from) | (g2 << (64 - from));
-        else run = g2;
-        filled = (run << 1) == ~(uint64_t)1;
+        uint64_t run = g2;                                 // bit k: row lane + 1 + k goes on from the one before it
+        if (lane < 63) run = (g1 >> (lane + 1)) | (g2 << (63 - lane));
+        after = __builtin_ctzll(~run | (uint64_t)1 << 63);
+        run = lane < 63 ? (g1 << (63 - lane)) | (g0 >> (lane + 1)) : g1;        // from bit 63 down: row lane and those before it
+        before = __builtin_clzll(~run | 1);
+        after = after < 63 - (s1 & 63) ? after : 63 - (s1 & 63);
+        before = before < (s1 & 63) ? before : s1 & 63;
     }
-    const uint64_t starts = __builtin_amdgcn_ballot_w64(filled && (s1 & 63) == 0);
+    const bool alone = in && after + before < 3;           // (fewer than four rows: each by itself)
+    uint64_t starts = __builtin_amdgcn_ballot_w64(in && !alone && before == 0);
+    uint32_t* const mine = lds + wave * 256;
     for (int j = wave; j < D / 16; j += RO_THREADS / 64) {
         const int8_t* src = a.qkv + (a.heads_q + a.heads_kv + head) * D + 16 * j;
-        if (in && !filled) {
+        if (alone) {
             uint32_t y[4];
             value_row(a, src + row * a.ld_qkv, y);
             const int64_t page = s1 >> a.log_page;
@@ -203,11 +204,12 @@ __device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, u
 #pragma unroll
             for (int i = 0; i < 16; ++i) dst[16 * i] = (int8_t)byte_of(y[i / 4], i & 3);
         }
-        if (starts) {                                      // (one at most)
-            const int first = __builtin_ctzll(starts);
-            const int32_t slot = __builtin_amdgcn_readlane(s1, first);
-            uint32_t y[4];
-            value_row(a, src + (row0 + first + lane) * a.ld_qkv, y);
+        for (uint64_t left = starts; left; left &= left - 1) {
+            // lane = token of the block; rows `first` .. on tokens from .. to - 1
+            const int first = __builtin_ctzll(left);
+            const int32_t slot = __builtin_amdgcn_readlane(s1, first), from = slot & 63, to = from + 1 + __builtin_amdgcn_readlane(after, first);
+            uint32_t y[4] = {0, 0, 0, 0};
+            if (lane >= from && lane < to) value_row(a, src + (row0 + first + lane - from) * a.ld_qkv, y);
             // four rows are four neighbouring lanes: byte r' of lane r becomes byte r of lane r'
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -217,15 +219,30 @@ __device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, u
                 y[i] = __builtin_amdgcn_perm(q, y[i], lane & 2 ? 0x03020706u : 0x05040100u);
             }
             // lane 16 i + 4 g + r: its dword of channel 4 n + r goes to [g][channel][i]
-            uint32_t* mine = lds + wave * 256;
 #pragma unroll
             for (int n = 0; n < 4; ++n) mine[((lane >> 2) & 3) * 64 + (4 * n + (lane & 3)) * 4 + (lane >> 4)] = y[n];
             __builtin_amdgcn_wave_barrier();
             const uint4 o = *reinterpret_cast<const uint4*>(mine + 4 * lane);
             __builtin_amdgcn_wave_barrier();
             const int64_t page = slot >> a.log_page;
-            const int t = slot & ((1 << a.log_page) - 1);
-            *reinterpret_cast<uint4*>(a.v + (((page * a.heads_kv + head) << a.log_page) + t) * D + j * 1024 + lane * 16) = o;
+            const int t = slot & ((1 << a.log_page) - 1) & ~63;
+            int8_t* dst = a.v + (((page * a.heads_kv + head) << a.log_page) + t) * D + j * 1024 + lane * 16;
+            if (to - from == 64) {
+                *reinterpret_cast<uint4*>(dst) = o;
+            } else {
+                const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = 16 * i + 4 * (lane >> 4);
+                    if (token >= from && token + 4 <= to) {
+                        *reinterpret_cast<uint32_t*>(dst + 4 * i) = w[i];
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (token + r >= from && token + r < to) dst[4 * i + r] = (int8_t)byte_of(w[i], r);
+                    }
+                }
+            }
         }
     }
 }
@@ -235,9 +252,10 @@ __global__ __launch_bounds__(RO_THREADS) void rotary_append_kernel(RotaryArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint32_t lds[RO_THREADS / 64 * 256];
     const int64_t wg = blockIdx.x;
-    if (wg < a.wgs[0]) rotate_heads<D, INTERLEAVED, P>(a, wg, 0);
-    else if (wg < a.wgs[0] + a.wgs[1]) rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[0], 1);
-    else append_values<D>(a, wg - a.wgs[0] - a.wgs[1], lds);
+    // (values first: theirs is the longest chain of loads)
+    if (wg < a.wgs[2]) append_values<D>(a, wg, lds);
+    else if (wg < a.wgs[2] + a.wgs[1]) rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[2], 1);
+    else rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[2] - a.wgs[1], 0);
 }
 
 // The same multiplier with a shift of at least `least`, where 31 bits hold it: DY(x; 2m, s + 1) = DY(x; m, s).
@@ -253,7 +271,8 @@ static int launch_rotary(RotaryArgs& a, hipStream_t stream)
     constexpr int per = RO_THREADS / (D / (2 * P));
     a.wgs[0] = (a.rows * a.heads_q + per - 1) / per;
     a.wgs[1] = (a.rows * a.heads_kv + per - 1) / per;
-    const int64_t wgs = a.wgs[0] + a.wgs[1] + (a.rows + 63) / 64 * a.heads_kv;
+    a.wgs[2] = (a.rows + 63) / 64 * a.heads_kv;
+    const int64_t wgs = a.wgs[0] + a.wgs[1] + a.wgs[2];
     if (wgs > 0x7fffffffLL) return IBERT_ERR_SHAPE;
     hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED, P>), dim3((unsigned)wgs), dim3(RO_THREADS), 0, stream, a);
     IBERT_LAUNCH_CHECK("rotary_append_kernel");

@@ -139,7 +139,7 @@ def test_rotary_append_of_any_dyadic(gpu, dy):
 def test_values_of_rows_that_fill_blocks(gpu, D, page):
     # runs of rows on runs of slots that start and end anywhere, with gaps, rows without a slot and runs that meet in one block
     torch, G, B = libs()
-    runs = [(0, 64), (70, 64), (200, 300), (640, 1), (641, 63), (704, 128), (900, 59), (960, 63), (1024, 64), (1090, 190), (1280, 130)]
+    runs = [(0, 64), (70, 64), (200, 300), (640, 1), (641, 63), (704, 128), (900, 59), (960, 63), (1024, 64), (1090, 190), (1281, 3), (1290, 4), (1299, 5), (1310, 2), (1312, 1), (1344, 130)]
     rows = sum(n for _, n in runs) + 5
     case = U.Rotary(D, rows, 2, 2, D, 32, False, page)
     order = np.random.default_rng(D).permutation(len(runs))
