@@ -252,6 +252,108 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
     }
 }
 
+// ---- few rows, one launch: a workgroup for each sequence, key head and tile, scores in LDS --------------------------------
+// K once, the scores into LDS, the maximum over the workgroup, then V once.  LDS: scores [held][64 blocks], then the sums [held][D], high
+// and low halves.
+constexpr int PW_NW = 8;
+template <int D>
+__global__ __launch_bounds__(64 * PW_NW, 2) void paged_row_kernel(PagedArgs a, int32_t held, int32_t room)
+{
+    constexpr int ND = D / 16, NW = PW_NW;
+    extern __shared__ __attribute__((aligned(16))) int32_t pw_lds[];
+    __shared__ int32_t s_max[NW][16];
+    __shared__ uint32_t s_w[16];
+    __shared__ uint64_t s_r[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x, b = blockIdx.y;
+    const Tile t = tile_of(a, b, blockIdx.z, 16);
+    if (t.count == 0) return;
+    int32_t* const s_hi = pw_lds + held * 64 * room;
+    int32_t* const s_lo = s_hi + held * D;
+    int pos;
+    v4i qf[D / 64];
+    tile_row<D>(a, t, h, c, g, pos, qf);
+    const int n = t.blocks < room ? t.blocks : room;       // (room is made for all there can be)
+    auto offset = [&](int x) { return block_offset<D>(a, b, h, block_at(t, x)); };
+    const int mine = (c < held ? c : held - 1) * 64 * room + g * 16;
+    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+
+    v4i f0[ND], f1[ND];
+    int32_t mx = INT32_MIN;
+    auto score = [&](int x, const v4i (&k)[ND]) {
+        v4i s[4];
+        block_scores<D>(a, t, block_at(t, x), pos, g, k, qf, s);
+        mx = largest(s, mx);
+        if (c < held) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<v4i*>(pw_lds + mine + x * 64 + 4 * i) = s[i];
+        }
+    };
+    int x = wave;
+    if (x < n) load_k<D>(a, offset(x), lane, f0);
+    while (x < n) {
+        if (x + NW < n) load_k<D>(a, offset(x + NW), lane, f1);
+        score(x, f0);
+        x += NW;
+        if (x >= n) break;
+        if (x + NW < n) load_k<D>(a, offset(x + NW), lane, f0);
+        score(x, f1);
+        x += NW;
+    }
+    x = wave;
+    if (x < n) load_v<D>(a, offset(x), lane, f0);
+    mx = combine_rows32(combine_rows16(mx, larger), larger);
+    if (g == 0) s_max[wave][c] = mx;
+    for (int i = tid; i < 2 * held * D; i += 64 * NW) s_hi[i] = 0;
+    if (tid < 16) s_w[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mx = larger(mx, s_max[w][c]);
+
+    v4i hi[ND], lo[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
+    uint32_t sum = 0;
+    auto value = [&](int x, const v4i (&v)[ND]) {
+        v4i s[4], wh, wl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const v4i*>(pw_lds + mine + x * 64 + 4 * i);
+        block_weights(a, s, mx, wh, wl, sum);
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[i], wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[i], wl, lo[i], 0, 0, 0);
+        }
+    };
+    while (x < n) {
+        if (x + NW < n) load_v<D>(a, offset(x + NW), lane, f1);
+        value(x, f0);
+        x += NW;
+        if (x >= n) break;
+        if (x + NW < n) load_v<D>(a, offset(x + NW), lane, f0);
+        value(x, f1);
+        x += NW;
+    }
+    // whole numbers: the order of these additions changes nothing
+    if (c < held) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                atomicAdd(&s_hi[c * D + 16 * i + 4 * g + r], hi[i][r]);
+                atomicAdd(&s_lo[c * D + 16 * i + 4 * g + r], lo[i][r]);
+            }
+        atomicAdd(&s_w[c], sum);
+    }
+    __syncthreads();
+    if (tid < held) s_r[tid] = reciprocal(s_w[tid]);
+    __syncthreads();
+    for (int e = tid; e < t.count * D; e += 64 * NW) {
+        const int r = e / D, d = e - r * D, f = t.first + r, qr = f / a.group, hd = h * a.group + (f - qr * a.group);
+        a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = finished(a, (int64_t)s_hi[e] * 256 + s_lo[e], s_r[r]);
+    }
+}
+
 // ---- few rows on many keys: three launches, the keys of a tile of rows split into chunks ---------------------------------
 // Scores and each chunk's maximum; weights, sums over the chunk, with the maximum of all chunks; the chunks' sums joined.
 struct SplitArgs {
@@ -380,20 +482,21 @@ __global__ __launch_bounds__(256) void paged_values_kernel(SplitArgs a)
         x += NW;
     }
     // whole numbers: the order of these additions changes nothing
+    if (c < a.held) {
 #pragma unroll
-    for (int i = 0; i < ND; ++i)
+        for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            atomicAdd(&s_hi[(16 * i + 4 * g + r) * 16 + c], hi[i][r]);
-            atomicAdd(&s_lo[(16 * i + 4 * g + r) * 16 + c], lo[i][r]);
-        }
-    atomicAdd(&s_w[c], (int32_t)sum);
+            for (int r = 0; r < 4; ++r) {
+                atomicAdd(&s_hi[c * D + 16 * i + 4 * g + r], hi[i][r]);
+                atomicAdd(&s_lo[c * D + 16 * i + 4 * g + r], lo[i][r]);
+            }
+        atomicAdd(&s_w[c], (int32_t)sum);
+    }
     __syncthreads();
     const int64_t at = w.index * a.splits + w.split;
     if (tid < 16) a.sums[at * 16 + tid] = (uint32_t)s_w[tid];
     for (int e = tid; e < a.held * D; e += 256) {
-        const int r = e / D, d = e - r * D;
-        a.parts[at * a.held * D + e] = (int64_t)s_hi[d * 16 + r] * 256 + s_lo[d * 16 + r];
+        a.parts[at * a.held * D + e] = (int64_t)s_hi[e] * 256 + s_lo[e];
     }
 }
 
@@ -687,6 +790,7 @@ __global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
 // Which kernels run, and their workspace.
 struct Plan {
     int32_t prompt_tiles, high;                     // > 0: paged_prompt_kernel; the scores' shift is 32 or more
+    int32_t room;                                   // > 0: paged_row_kernel, with so many blocks of scores
     int32_t tiles, splits, chunk, blocks, held;     // chunk > 0: the three kernels for few rows
     size_t maxima, sums, parts, scores, total;      // bytes from the workspace's start
 };
@@ -708,9 +812,18 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
         p.prompt_tiles = (int32_t)prompt_tiles;
         return p;
     }
-    if (rows > 16 || blocks <= 8 || batch == 0) return p;
+    if (batch == 0) return p;
     const int64_t problems = (int64_t)batch * c.heads_kv * p.tiles;
-    int64_t splits = (1024 + problems - 1) / problems;
+    // One launch where the scores of all keys fit LDS, unless that leaves few workgroups with long ways: a workgroup takes some 0.2 us a block and the three
+    // launches 12 and more.  us, three launches / one, of 8 key heads of width 128, 4 rows: 1 x 1000 keys 11.9 / 9.9, 1 x 2000 12.4 / 13.4, 1 x 4000 12.9 / 20.1,
+    // 8 x 4000 22.3 / 22.3, 16 x 1500 18.6 / 13.4, 24 x 4000 44.0 / 32.1, 64 x 4096 94.6 / 71.6; 12 of width 64, 1 row: 4 x 2000 12.8 / 11.2, 2 x 4000 13.5 / 18.2.
+    const int64_t lds = (int64_t)p.held * (256 * blocks + 8 * c.head_dim);
+    if (rows <= 16 && lds <= 128 * 1024 && (blocks <= 24 || problems >= 64)) {
+        p.room = (int32_t)(blocks > 0 ? blocks : 1);
+        return p;
+    }
+    if (rows > 16) return p;
+    int64_t splits = (512 + problems - 1) / problems;
     int64_t chunk = (blocks + splits - 1) / splits;
     if (chunk < 4) chunk = 4;
     splits = (blocks + chunk - 1) / chunk;
@@ -739,6 +852,16 @@ static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, voi
         else hipLaunchKernelGGL((paged_prompt_kernel<D, false, PP_RT, PP_NW>), grid, block, lds, stream, a);
         IBERT_LAUNCH_CHECK("paged_prompt_kernel");
         g_last_kernel = "paged_prompt_kernel";
+        return IBERT_OK;
+    }
+    if (plan.room > 0) {
+        const size_t lds = (size_t)plan.held * (256 * plan.room + 8 * D);
+        auto kern = paged_row_kernel<D>;
+        if (lds > 60000)
+            IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 132 * 1024));
+        hipLaunchKernelGGL(kern, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles), dim3(64 * PW_NW), lds, stream, a, plan.held, plan.room);
+        IBERT_LAUNCH_CHECK("paged_row_kernel");
+        g_last_kernel = "paged_row_kernel";
         return IBERT_OK;
     }
     if (plan.chunk == 0) {
