@@ -535,8 +535,8 @@ int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* c
  * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes (may be NULL where that is 0); calls that may
  * overlap in time need one each.
  * Preconditions: max_kv_len <= 131072 and scores_dy.m >= 0, its shift in [24, 62], out_dy's in [0, 62], window, sinks >= 0
- * (IBERT_ERR_PARAM_RANGE); heads_q a multiple of heads_kv, leading dimensions >= heads_q * head_dim, max_q_len >= 1
- * (IBERT_ERR_SHAPE); q and ld_q 16-byte, out and ld_out 4-byte aligned (IBERT_ERR_ALIGN).  The cache's V holds values in
+ * (IBERT_ERR_PARAM_RANGE); heads_q a multiple of heads_kv, leading dimensions >= heads_q * head_dim, batch <= 65535, max_q_len >= 1,
+ * max_q_len * heads_q / heads_kv <= 64 * 65535, rows >= batch where q_start is NULL (IBERT_ERR_SHAPE); q and ld_q 16-byte, out and ld_out 4-byte aligned (IBERT_ERR_ALIGN).  The cache's V holds values in
  * [-127, 127] (what ibert_rotary_append_i writes), so that a sum over 131072 keys fits 32 bits.  out must not overlap q.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {

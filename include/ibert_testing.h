@@ -56,6 +56,12 @@ int ibert_attention_buffers(int32_t seq, int32_t form, int64_t workgroups, int32
  * layernorm_rows_kernel.  (The name that ibert_last_kernel() gives is the same for 1 and 4.)  Host only. */
 int ibert_layernorm_i16_plan(int64_t rows, int32_t C, int32_t shift, int32_t* rows_of_wavefront);
 
+/* Which kernels ibert_paged_attention_i runs, and what its workspace query asks for: the scores made twice by workgroups of 16 rows; the same rows
+ * in one launch with the scores in LDS (where they do not fit, the former); three launches with the keys split; the kernel for prompts.
+ * Negative: where each is the faster one (the default).  The result never depends on it.  Process-wide, not thread-safe. */
+enum { IBERT_PAGED_TWICE = 0, IBERT_PAGED_ONE = 1, IBERT_PAGED_SPLIT = 2, IBERT_PAGED_PROMPT = 3 };
+void ibert_paged_attention_override(int32_t form);
+
 /* Steps 1 to 4 of a layer as one kernel: 0 never; a tile (1000 wavefronts + 100 MFMA rows of one + 10 sequences + stages, one of those ibert_qkv_attention_plan names)
  * wherever its rows hold a sequence and the parameters allow it; negative where it is the faster way (the default).  Process-wide, not thread-safe. */
 void ibert_qkv_attention_override(int32_t tile);

@@ -8,6 +8,7 @@
 // The weights are relative to the row's maximum and cannot be rescaled exactly, so the maximum is made first, over the raw
 // accumulators (the distance is monotone in them), and the scores are made a second time.
 #include "common.h"
+#include "ibert_testing.h"
 
 namespace ibert {
 
@@ -787,6 +788,8 @@ __global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
     }
 }
 
+static int g_paged_form = -1;          // see ibert_paged_attention_override
+
 // Which kernels run, and their workspace.
 struct Plan {
     int32_t prompt_tiles, high;                     // > 0: paged_prompt_kernel; the scores' shift is 32 or more
@@ -807,8 +810,13 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     p.held = rows < 16 ? (int32_t)rows : 16;
     p.splits = 1;
     p.high = d.scores_dy.s >= 32;
+    const int form = g_paged_form;
     const int64_t prompt_tiles = (rows + pp_rows(PP_RT, PP_NW) - 1) / pp_rows(PP_RT, PP_NW);
-    if (rows > 16 && prompt_tiles * batch * c.heads_kv >= 64) {
+    // Prompts: a workgroup of the prompt kernel takes four times the rows, so it wants more of them before the chip is full.  us, the scores made twice / this,
+    // 8 key heads of width 128 with 4 queries each: 1 x 300 rows on 8000 keys (152 workgroups) 99 / 135, 1 x 512 (256) 20.7 / 18.5, on 8000 keys 136 / 140,
+    // 1 x 1024 (512) 39.6 / 29.4, on 8000 keys 245 / 168; 16 heads of width 64: 2 x 512 (256) 12.5 / 14.7, 1 x 2048 (512) 38.4 / 36.4, 4 x 512 (512) 19.7 / 16.4;
+    // 12: 2 x 700 on 4000 keys (264) 61 / 64, 8 x 200 (384) 11.3 / 11.9, 32 x 200 (1536) 30.4 / 23.3.
+    if (p.tiles > 65535 || (form < 0 ? rows > 16 && prompt_tiles * batch * c.heads_kv >= 320 : form == IBERT_PAGED_PROMPT)) {
         p.prompt_tiles = (int32_t)prompt_tiles;
         return p;
     }
@@ -818,11 +826,13 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     // launches 12 and more.  us, three launches / one, of 8 key heads of width 128, 4 rows: 1 x 1000 keys 11.9 / 9.9, 1 x 2000 12.4 / 13.4, 1 x 4000 12.9 / 20.1,
     // 8 x 4000 22.3 / 22.3, 16 x 1500 18.6 / 13.4, 24 x 4000 44.0 / 32.1, 64 x 4096 94.6 / 71.6; 12 of width 64, 1 row: 4 x 2000 12.8 / 11.2, 2 x 4000 13.5 / 18.2.
     const int64_t lds = (int64_t)p.held * (256 * blocks + 8 * c.head_dim);
-    if (rows <= 16 && lds <= 128 * 1024 && (blocks <= 24 || problems >= 64)) {
+    if (lds <= 128 * 1024 && (form < 0 ? rows <= 16 && (blocks <= 24 || problems >= 64) : form == IBERT_PAGED_ONE)) {
         p.room = (int32_t)(blocks > 0 ? blocks : 1);
         return p;
     }
-    if (rows > 16) return p;
+    // More rows than a tile: their tiles fill the chip by themselves unless they are very few and the keys many.  us, the scores made twice / split, 8 key heads of
+    // width 128: 8 rows of 4 queries on 8000 keys (16 workgroups) 54 / 28, 16 rows (32) 52 / 31, 64 rows (128) 52 / 60; 32 rows on 1000 keys (64) 13.3 / 19.8.
+    if (form < 0 ? rows > 16 && (problems > 48 || blocks < 48) : form != IBERT_PAGED_SPLIT) return p;
     int64_t splits = (512 + problems - 1) / problems;
     int64_t chunk = (blocks + splits - 1) / splits;
     if (chunk < 4) chunk = 4;
@@ -845,7 +855,6 @@ template <int D>
 static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
 {
     if (plan.prompt_tiles > 0) {
-        if (plan.prompt_tiles > 65535) return IBERT_ERR_SHAPE;
         constexpr size_t lds = pp_lds_bytes(D, PP_RT, PP_NW);
         const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch), block(64 * PP_NW);
         if (plan.high) hipLaunchKernelGGL((paged_prompt_kernel<D, true, PP_RT, PP_NW>), grid, block, lds, stream, a);
@@ -865,7 +874,6 @@ static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, voi
         return IBERT_OK;
     }
     if (plan.chunk == 0) {
-        if (plan.tiles > 65535) return IBERT_ERR_SHAPE;
         hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles), dim3(256), 0, stream, a);
         IBERT_LAUNCH_CHECK("paged_attention_kernel");
         g_last_kernel = "paged_attention_kernel";
@@ -892,14 +900,16 @@ static int check_paged(const ibert_paged_attention_desc* desc, const ibert_kv_ca
     if (!desc || !cache) return IBERT_ERR_NULL;
     if (const int rc = check_cache(cache)) return rc;
     const ibert_paged_attention_desc& d = *desc;
-    if (batch < 0 || batch > 65535 || rows < 0 || max_q_len < 1 || max_kv_len < 0 || d.heads_q < 1 || d.heads_q > (1 << 20) || d.heads_q % cache->heads_kv)
-        return IBERT_ERR_SHAPE;
+    if (batch < 0 || batch > 65535 || rows < 0 || max_q_len < 1 || max_kv_len < 0 || d.heads_q < 1 || d.heads_q > (1 << 20) || d.heads_q % cache->heads_kv ||
+        (int64_t)max_q_len * (d.heads_q / cache->heads_kv) > 65535 * 64) return IBERT_ERR_SHAPE;
     if (max_kv_len > PA_MOST_KEYS || d.scores_dy.m < 0 || d.scores_dy.s < 24 || d.scores_dy.s > 62 || !dyadic_ok(d.out_dy) || d.window < 0 || d.sinks < 0)
         return IBERT_ERR_PARAM_RANGE;
     return IBERT_OK;
 }
 
 }  // namespace ibert
+
+extern "C" void ibert_paged_attention_override(int32_t form) { ibert::g_paged_form = form; }
 
 extern "C" size_t ibert_paged_attention_workspace_bytes(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, int32_t batch,
                                                         int32_t rows, int32_t max_q_len, int32_t max_kv_len)

@@ -257,7 +257,7 @@ def test_paged_attention_refuses():
                                          p["workspace"], ws, None)
     for kw, rc in BAD_CACHES:
         assert call(c=cache(**kw)) == rc, kw
-    for kw in (dict(batch=-1), dict(batch=65536), dict(rows=-1), dict(max_q=0), dict(max_kv=-1), dict(ld_q=240), dict(ld_out=255), dict(width=0), dict(desc=dict(heads_q=3)),
+    for kw in (dict(batch=-1), dict(batch=65536), dict(rows=-1), dict(max_q=0), dict(max_q=64 * 65535 // 2 + 1), dict(max_kv=-1), dict(ld_q=240), dict(ld_out=255), dict(width=0), dict(desc=dict(heads_q=3)),
                dict(desc=dict(heads_q=0)), dict(start=None, rows=1)):
         assert call(**kw) == -2, kw
     for kw in (dict(max_kv=131073), dict(desc=dict(window=-1)), dict(desc=dict(sinks=-1)), dict(desc=dict(scores_dy=B.Dyadic(-1, 30))), dict(desc=dict(scores_dy=B.Dyadic(1, 23))),

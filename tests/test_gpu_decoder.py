@@ -205,13 +205,34 @@ class DeviceAttention:
 
 
 def check_attention(case, **kw):
+    """The call as it is, and in each of its four forms."""
     torch, G, B = libs()
-    G.say("attention q%d k%d d%d page %d n %s kv %s window %d sinks %d" % (case.hq, case.hk, case.D, case.page, case.n[:8].tolist(), case.kv[:8].tolist(), case.window, case.sinks))
-    d = DeviceAttention(case, **kw)
-    d.call()
     want = case.oracle()
-    same(d.result(), want, "out")
+    for form in (B.PAGED_TWICE, B.PAGED_ONE, B.PAGED_SPLIT, B.PAGED_PROMPT, -1):
+        G.say("attention form %d q%d k%d d%d page %d n %s kv %s window %d sinks %d" % (form, case.hq, case.hk, case.D, case.page, case.n[:8].tolist(), case.kv[:8].tolist(), case.window,
+                                                                                       case.sinks))
+        B.ibert_paged_attention_override(form)
+        try:
+            d = DeviceAttention(case, **kw)
+            d.call()
+            same(d.result(), want, "out, form %d" % form)
+        finally:
+            B.ibert_paged_attention_override(-1)
     return d, want
+
+
+@pytest.mark.parametrize("n,kv,hq,hk,D,window,kernel", [
+    ([1], [77], 12, 12, 64, 0, "paged_row_kernel"), ([1] * 64, [3000] * 64, 8, 2, 128, 0, "paged_row_kernel"), ([1], [3000], 8, 2, 128, 0, "paged_join_kernel"),
+    ([1], [9000], 8, 2, 128, 500, "paged_row_kernel"), ([8], [5000], 8, 2, 128, 0, "paged_join_kernel"), ([64], [200], 8, 2, 128, 0, "paged_attention_kernel"),
+    ([200] * 3, [200] * 3, 8, 2, 128, 0, "paged_attention_kernel"), ([200] * 14, [200] * 14, 8, 2, 128, 0, "paged_prompt_kernel")])
+def test_attention_takes_the_kernel_that_the_rule_names(gpu, n, kv, hq, hk, D, window, kernel):
+    torch, G, B = libs()
+    case = U.Attention(60, hq, hk, D, 64, n, kv, window)
+    G.say("attention by rule: %s" % kernel)
+    d = DeviceAttention(case)
+    d.call()
+    d.result()
+    assert B.lib().ibert_last_kernel().decode().startswith(kernel)
 
 
 @pytest.mark.parametrize("hq,hk,D,page", [(1, 1, 64, 64), (12, 12, 64, 64), (8, 2, 128, 64), (7, 1, 128, 128), (16, 1, 64, 256), (40, 2, 64, 64), (17, 1, 128, 64)])
