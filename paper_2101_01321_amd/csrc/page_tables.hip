@@ -25,6 +25,13 @@ __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b)
     return s > 0x7fffffffu ? 0x7fffffffu : s;
 }
 
+// The value some lanes before this one in its row of 16 (or the last of the rows before it), 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_before(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int32_t)v, CTRL, ROWS, 0xF, false);
+}
+
 // Inclusive sums of N values over the workgroup; total[] = those of all threads.  tmp: PT_WAVES * N words.
 template <int N, bool SAT>
 __device__ __forceinline__ void block_scan(uint32_t (&v)[N], uint32_t (&total)[N], uint32_t* tmp)
@@ -32,12 +39,14 @@ __device__ __forceinline__ void block_scan(uint32_t (&v)[N], uint32_t (&total)[N
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const auto add = [](uint32_t a, uint32_t b) { return SAT ? add_sat(a, b) : a + b; };
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const uint32_t o = __shfl_up(v[n], d);
-            v[n] = lane >= d ? add(v[n], o) : v[n];
-        }
+    for (int n = 0; n < N; ++n) {
+        v[n] = add(v[n], dpp_before<0x111, 0xF>(v[n]));    // row_shr 1, 2, 4, 8
+        v[n] = add(v[n], dpp_before<0x112, 0xF>(v[n]));
+        v[n] = add(v[n], dpp_before<0x114, 0xF>(v[n]));
+        v[n] = add(v[n], dpp_before<0x118, 0xF>(v[n]));
+        v[n] = add(v[n], dpp_before<0x142, 0xA>(v[n]));    // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+        v[n] = add(v[n], dpp_before<0x143, 0xC>(v[n]));
+    }
     __syncthreads();                                       // (tmp may still be read from an earlier call)
     if (lane == 63)
 #pragma unroll
@@ -76,6 +85,7 @@ __global__ __launch_bounds__(PT_THREADS) void page_tables_kernel(PageArgs a)
     uint32_t* const row_end = pt_lds;                      // running sums of what is granted: rows, pages taken, pages put back
     uint32_t* const take_end = row_end + a.batch;
     uint32_t* const back_end = take_end + a.batch;
+    int32_t* const before_of = reinterpret_cast<int32_t*>(back_end + a.batch);
     const int tid = threadIdx.x, lp = a.log_page;
     const uint32_t R = (uint32_t)a.num_pages;
     int32_t head = a.ring_in[0], count = a.ring_in[1];
@@ -103,6 +113,7 @@ __global__ __launch_bounds__(PT_THREADS) void page_tables_kernel(PageArgs a)
         uint32_t g[4] = {granted ? rows : 0, granted ? need : 0, granted && held > wants ? held - wants : 0, in && !granted}, sum[4];
         block_scan<4, false>(g, sum, tmp);
         if (in) {
+            before_of[b] = before;
             row_end[b] = given[0] + g[0];
             take_end[b] = given[1] + g[1];
             back_end[b] = given[2] + g[2];
@@ -125,12 +136,12 @@ __global__ __launch_bounds__(PT_THREADS) void page_tables_kernel(PageArgs a)
     __syncthreads();
 
     const uint32_t first = blockIdx.x * PT_THREADS + tid, step = gridDim.x * PT_THREADS;
-    const auto length = [&](int b) {
-        const int32_t n = a.before[b];
-        return n < 0 ? 0 : n;
-    };
+    const auto length = [&](int b) { return before_of[b]; };
     // the i-th page that is taken
-    const auto page_of = [&](uint32_t i) { return a.ring[((uint32_t)head + i) % R]; };
+    const auto page_of = [&](uint32_t i) {                 // (i < count <= R)
+        const uint32_t k = (uint32_t)head + i;
+        return a.ring[k < R ? k : k - R];
+    };
     for (uint32_t i = first; i < taken; i += step) {
         const int b = above(take_end, a.batch, i);
         const uint32_t p = pages(length(b)) + i - (b ? take_end[b - 1] : 0);
@@ -160,10 +171,10 @@ static int launch_page_tables(const PageArgs& a, hipStream_t stream)
 {
     // a thread for every row, as long as a workgroup has 512 to do
     const int64_t wgs = ((int64_t)a.rows + PT_THREADS - 1) / PT_THREADS;
-    const size_t lds = 12 * (size_t)a.batch;
+    const size_t lds = 16 * (size_t)a.batch;
     auto kern = page_tables_kernel;
     if (lds > 60000)
-        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 12 * PT_MOST));
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * PT_MOST));
     hipLaunchKernelGGL(kern, dim3((unsigned)(wgs < 1 ? 1 : (wgs > 256 ? 256 : wgs))), dim3(PT_THREADS), lds, stream, a);
     IBERT_LAUNCH_CHECK("page_tables_kernel");
     g_last_kernel = "page_tables_kernel";

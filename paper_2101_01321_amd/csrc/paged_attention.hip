@@ -23,12 +23,15 @@ struct PagedArgs {
     int64_t ld_q, ld_out;
     int32_t heads_q, heads_kv, group, log_page, num_pages, max_pages, rows, max_q, keys;   // keys: most that a sequence can have
     int32_t window, sinks;
-    uint32_t s_m;
+    uint32_t group_magic, s_m;
     int32_t s_l, s_r;          // DY(d) = (((uint64)(d << s_l) * s_m + s_rnd) >> 32) >> s_r
     uint64_t s_rnd;
     int32_t s_s;               // the shift of DY; less 32 where that is not negative
     ibert_dyadic out_dy;
 };
+
+// Query of the flat row n.
+__device__ __forceinline__ int32_t group_of(const PagedArgs& a, int32_t n) { return udiv_fix(n, a.group, a.group_magic); }
 
 // What one workgroup works on: 16 rows of one sequence and key head.
 struct Tile {
@@ -54,8 +57,8 @@ __device__ __forceinline__ Tile tile_of(const PagedArgs& a, int b, int tile, int
     t.first = tile * tile_rows;
     const int64_t left = (int64_t)(t.n < a.max_q ? t.n : a.max_q) * a.group - t.first;
     t.count = left < tile_rows ? (int32_t)(left < 0 ? 0 : left) : tile_rows;
-    t.low = t.pos0 + t.first / a.group;
-    t.high = t.pos0 + (t.first + (t.count > 0 ? t.count - 1 : 0)) / a.group;
+    t.low = t.pos0 + group_of(a, t.first);
+    t.high = t.pos0 + group_of(a, t.first + (t.count > 0 ? t.count - 1 : 0));
     const int32_t end = t.high < 0 ? 0 : (t.high >> 6) + 1;
     int32_t from = 0, sb = 0;
     if (a.window > 0 && t.low >= a.window) {
@@ -171,7 +174,7 @@ __device__ __forceinline__ int8_t finished(const PagedArgs& a, int64_t N, uint64
 template <int D>
 __device__ __forceinline__ void tile_row(const PagedArgs& a, const Tile& t, int h, int c, int g, int& pos, v4i (&qf)[D / 64])
 {
-    const int flat = t.first + (c < t.count ? c : t.count - 1), qi = flat / a.group;
+    const int flat = t.first + (c < t.count ? c : t.count - 1), qi = group_of(a, flat);
     const int8_t* src = a.q + (int64_t)(t.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) qf[j] = *reinterpret_cast<const v4i*>(src + 64 * j);
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
     for (int e = tid; e < D * 16; e += 256) {
         const int r = e / D, d = e - r * D;
         if (r >= t.count) break;
-        const int f = t.first + r, qr = f / a.group, hd = h * a.group + (f - qr * a.group);
+        const int f = t.first + r, qr = group_of(a, f), hd = h * a.group + (f - qr * a.group);
         const int64_t N = (int64_t)s_hi[d * 16 + r] * 256 + s_lo[d * 16 + r];
         a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = finished(a, N, ((uint64_t)(uint32_t)s_w[16 + r] << 32) | (uint32_t)s_w[r]);
     }
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(64 * PW_NW, 2) void paged_row_kernel(PagedArgs a, i
     if (tid < held) s_r[tid] = reciprocal(s_w[tid]);
     __syncthreads();
     for (int e = tid; e < t.count * D; e += 64 * NW) {
-        const int r = e / D, d = e - r * D, f = t.first + r, qr = f / a.group, hd = h * a.group + (f - qr * a.group);
+        const int r = e / D, d = e - r * D, f = t.first + r, qr = group_of(a, f), hd = h * a.group + (f - qr * a.group);
         a.out[(int64_t)(t.row0 + qr) * a.ld_out + hd * D + d] = finished(a, (int64_t)s_hi[e] * 256 + s_lo[e], s_r[r]);
     }
 }
@@ -529,7 +532,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(SplitArgs a)
         N += s_n[i * D + d];
         W += s_w[i];
     }
-    const int f = w.t.first + r, qr = f / a.p.group, hd = w.h * a.p.group + (f - qr * a.p.group);
+    const int f = w.t.first + r, qr = group_of(a.p, f), hd = w.h * a.p.group + (f - qr * a.p.group);
     a.p.out[(int64_t)(w.t.row0 + qr) * a.p.ld_out + hd * D + d] = finished(a.p, N, reciprocal(W));
 }
 
@@ -550,8 +553,8 @@ __device__ __forceinline__ Tile part_of(const PagedArgs& a, const Tile& t, int f
     p.first = t.first + first;
     p.count = t.count - first;
     p.count = p.count < 0 ? 0 : (p.count > n ? n : p.count);
-    p.low = t.pos0 + (p.count > 0 ? p.first : t.first) / a.group;
-    p.high = p.count > 0 ? t.pos0 + (p.first + p.count - 1) / a.group : -1;
+    p.low = t.pos0 + group_of(a, p.count > 0 ? p.first : t.first);
+    p.high = p.count > 0 ? t.pos0 + group_of(a, p.first + p.count - 1) : -1;
     return p;
 }
 // How many of the workgroup's blocks some row of the part may see (the others come last).
@@ -568,7 +571,7 @@ __device__ __forceinline__ void part_row(const PagedArgs& a, const Tile& p, int 
     int flat = p.first + 16 * rt + c;
     flat = flat < last ? flat : last;
     flat = p.count > 0 ? flat : 0;                         // (a part without rows: the sequence's first, not used)
-    const int qi = flat / a.group;
+    const int qi = group_of(a, flat);
     const int8_t* src = a.q + (int64_t)(p.row0 + qi) * a.ld_q + (h * a.group + (flat - qi * a.group)) * D + 16 * g;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) qf[j] = *reinterpret_cast<const v4i*>(src + 64 * j);
@@ -776,7 +779,7 @@ __global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
         const uint64_t R = reciprocal((uint32_t)W);
         const int flat = own.first + 16 * rt + c;
         if (16 * rt + c >= own.count) continue;
-        const int qi = flat / a.group;
+        const int qi = group_of(a, flat);
         int8_t* dst = a.out + (int64_t)(t.row0 + qi) * a.ld_out + (h * a.group + (flat - qi * a.group)) * D + 4 * g;
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
@@ -936,6 +939,7 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     PagedArgs a;
     a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.table = block_table; a.q_start = q_start; a.kv_len = kv_len;
     a.ld_q = ld_q; a.ld_out = ld_out; a.heads_q = d.heads_q; a.heads_kv = cache->heads_kv; a.group = d.heads_q / cache->heads_kv;
+    a.group_magic = udiv_magic(a.group);
     a.log_page = __builtin_ctz((unsigned)cache->page_size); a.num_pages = cache->num_pages; a.max_pages = max_pages; a.rows = rows; a.max_q = max_q_len;
     const int64_t held = (int64_t)max_pages << a.log_page;
     a.keys = (int32_t)(held < max_kv_len ? held : max_kv_len);
