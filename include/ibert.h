@@ -499,7 +499,8 @@ int ibert_page_tables_i(const int32_t* len_before, const int32_t* len_after, int
  * see ibert_rotary_table_from_freqs); positions: device int32 [rows], clamped into [0, max_pos); slots: device int32
  * [rows]; q_gamma, k_gamma: device int32 [D] with |gamma| < 2^14, or NULL (no norm; see ibert_head_norm_from_float).
  * Preconditions: heads_q a multiple of heads_kv (IBERT_ERR_SHAPE); 0 <= R <= D, R a multiple of 16; shifts of the norms that
- * are used in [1, 30], all dyadic shifts in [0, 62] (IBERT_ERR_PARAM_RANGE); rows < 2^31; qkv, q, table, both gammas and both leading
+ * are used in [1, 30], all dyadic shifts in [0, 62] (IBERT_ERR_PARAM_RANGE); rows * (heads_q + 2 heads_kv + 1) <
+ * 2^31 (IBERT_ERR_SHAPE); qkv, q, table, both gammas and both leading
  * dimensions 16-byte aligned (IBERT_ERR_ALIGN).  q must not overlap qkv.
  * ---------------------------------------------------------------------------------------------- */
 enum { IBERT_ROTARY_HALF = 0, IBERT_ROTARY_INTERLEAVED = 1 };

@@ -22,43 +22,48 @@ struct RotaryArgs {
     const int32_t* gamma[2];   // queries, keys
     int8_t *q, *k, *v;
     int64_t ld_qkv, ld_q, rows;
-    int64_t wgs[3];            // workgroups of queries, of keys, of values
+    int32_t wgs[3];            // workgroups of queries, of keys, of values
+    int32_t teams[2];          // of a row's queries, and of its keys
+    uint32_t teams_magic[2];
     int32_t heads_q, heads_kv, rot, max_pos, log_page, page_slots;
     int32_t shift[2];
     ibert_dyadic dy[2];
     int32_t fast[2];           // the dyadic's shift is 33 or more: the high half of one multiply-add, shifted
     int32_t v_l, v_r, v_m;     // DY(x) = ((x << v_l) * v_m + 2^(v_r + 31)) >> 32 >> v_r of a value
-    uint32_t heads_magic[2];
 };
 
-constexpr int RO_THREADS = 256;
+constexpr int RO_THREADS = 256, RO_TEAM_HEADS = 262144;
 
 __device__ __forceinline__ int32_t byte_of(uint32_t p, int i) { return (int32_t)(int8_t)(p >> (8 * i)); }
 
-template <int D, bool INTERLEAVED, int P>
-__device__ __forceinline__ void rotate_heads(const RotaryArgs& a, int64_t wg, int kind)
+// NH: heads of a row that a team of lanes takes one after the other.  With two the table's row, the row's slot and what else is the same for both is
+// fetched once, and each lane finds the root and the reciprocal of one head for all; it halves the wavefronts, so it is for many rows.  us, one head /
+// two, 32 query heads of width 128: 1024 rows with norms 7.4 / 8.4, 2048 12.9 / 13.0, 4096 without 14.0 / 14.5, 16384 without 55.5 / 48.9, with 74.6 / 66.9.
+// (Four heads: 132 registers, 69.7.  Width 64, 2 lanes a head: no change at 16384 rows.)
+template <int D, bool INTERLEAVED, int P, int NH>
+__device__ __forceinline__ void rotate_heads(const RotaryArgs& a, int32_t wg, int kind)
 {
-    constexpr int LPH = D / (2 * P), W = P / 4;                // lanes of a head; dwords of a half
+    constexpr int LPH = D / (2 * P), W = P / 4;            // lanes of a head; dwords of a half
+    static_assert(NH == 1 || (NH == 2 && LPH == 4), "heads of a team");
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
     const int heads = kind ? a.heads_kv : a.heads_q;
-    const int64_t group = wg * (RO_THREADS / LPH) + threadIdx.x / LPH;
+    const int32_t team = wg * (RO_THREADS / LPH) + threadIdx.x / LPH, row = udiv_fix(team, a.teams[kind], a.teams_magic[kind]);
     const int j = threadIdx.x % LPH;
-    int64_t row;
-    if (group <= 0x7fffffff) row = udiv_fix((int32_t)group, heads, a.heads_magic[kind]);
-    else row = group / heads;
-    if (row >= a.rows) return;                             // (the lanes of a head together)
-    const int head = (int)(group - row * heads);
+    if (row >= (int32_t)a.rows) return;                    // (the lanes of a team together)
+    const int head = (team - row * a.teams[kind]) * NH;
     const int32_t slot = a.slots[row];
     if ((uint32_t)slot >= (uint32_t)a.page_slots) return;
     const bool turned = 2 * P * j < a.rot;
     const int c0 = turned && !INTERLEAVED ? P * j : 2 * P * j, c1 = turned && !INTERLEAVED ? P * j + a.rot / 2 : 2 * P * j + P;
-    const int8_t* src = a.qkv + row * a.ld_qkv + (head + (kind ? a.heads_q : 0)) * D;
-    uint32_t p0[W], p1[W], cs[P];
-    typedef uint32_t words __attribute__((ext_vector_type(W)));
-    {
-        const words w0 = *reinterpret_cast<const words*>(src + c0), w1 = *reinterpret_cast<const words*>(src + c1);
+    const int8_t* src = a.qkv + row * a.ld_qkv + (kind ? a.heads_q : 0) * D;
+    words w0[NH], w1[NH];
 #pragma unroll
-        for (int i = 0; i < W; ++i) { p0[i] = w0[i]; p1[i] = w1[i]; }
+    for (int n = 0; n < NH; ++n) {
+        const int8_t* from = src + (head + n < heads ? head + n : heads - 1) * D;
+        w0[n] = *reinterpret_cast<const words*>(from + c0);
+        w1[n] = *reinterpret_cast<const words*>(from + c1);
     }
+    uint32_t cs[P];
     if (turned) {
         const int32_t pos = clamp_i32(a.positions[row], 0, a.max_pos - 1);
         const uint4* t = reinterpret_cast<const uint4*>(a.table + ((int64_t)pos * (a.rot / 2) + P * j) * 2);
@@ -68,81 +73,97 @@ __device__ __forceinline__ void rotate_heads(const RotaryArgs& a, int64_t wg, in
             cs[4 * i] = w.x; cs[4 * i + 1] = w.y; cs[4 * i + 2] = w.z; cs[4 * i + 3] = w.w;
         }
     }
-    int32_t x[2 * P];
-#pragma unroll
-    for (int i = 0; i < P; ++i) { x[i] = byte_of(p0[i / 4], i & 3); x[P + i] = byte_of(p1[i / 4], i & 3); }
-
     const int32_t* gamma = a.gamma[kind];
+    int32_t f[NH];
     if (gamma) {
-        const int32_t shift = a.shift[kind];
-        int32_t ss = 0;
+        int32_t mine = 0;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            ss = __builtin_amdgcn_sdot4((int32_t)p0[i], (int32_t)p0[i], ss, false);
-            ss = __builtin_amdgcn_sdot4((int32_t)p1[i], (int32_t)p1[i], ss, false);
-        }
-        const auto add = [](int32_t p, int32_t q) { return p + q; };
-        ss = add(ss, dpp_mov<0xB1>(ss));
-        if (LPH > 2) ss = add(ss, dpp_mov<0x4E>(ss));
-        if (LPH > 4) ss = add(ss, dpp_mov<0x141>(ss));
-        // sum <= 2^14 D: the mean's 16 fractional bits make it at most 2^30
-        uint32_t sigma = isqrt_floor_lane((uint32_t)ss * (65536u / D));
-        sigma = sigma < 1 ? 1 : sigma;
-        const int32_t f = (int32_t)((1u << 30) / sigma), rnd = 1 << (shift - 1);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int4* g4 = reinterpret_cast<const int4*>(gamma + (half ? c1 : c0));
+        for (int n = 0; n < NH; ++n) {
+            int32_t ss = 0;
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                const int4 w = g4[i];
-                const int32_t gm[4] = {w.x, w.y, w.z, w.w};
+                ss = __builtin_amdgcn_sdot4((int32_t)w0[n][i], (int32_t)w0[n][i], ss, false);
+                ss = __builtin_amdgcn_sdot4((int32_t)w1[n][i], (int32_t)w1[n][i], ss, false);
+            }
+            const auto add = [](int32_t p, int32_t q) { return p + q; };
+            ss = add(ss, dpp_mov<0xB1>(ss));
+            if (LPH > 2) ss = add(ss, dpp_mov<0x4E>(ss));
+            if (LPH > 4) ss = add(ss, dpp_mov<0x141>(ss));
+            mine = NH == 1 || n == (j & 1) ? ss : mine;
+        }
+        // sum <= 2^14 D: the mean's 16 fractional bits make it at most 2^30
+        uint32_t sigma = isqrt_floor_lane((uint32_t)mine * (65536u / D));
+        sigma = sigma < 1 ? 1 : sigma;
+        const int32_t r = (int32_t)((1u << 30) / sigma);
+        f[0] = r;
+        if constexpr (NH == 2) {
+            f[0] = dpp_mov<0x00>(r);                       // lane 0 of the team's, and lane 1's
+            f[1] = dpp_mov<0x55>(r);
+        }
+    }
+    const int32_t shift = a.shift[kind], norm_rnd = 1 << ((shift - 1) & 31);
+    const ibert_dyadic dy = a.dy[kind];
+    const int64_t rnd = (int64_t)1 << ((dy.s - 1) & 63);
+    const int64_t page = slot >> a.log_page;
+    const int t = slot & ((1 << a.log_page) - 1);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    int32_t& u = x[P * half + 4 * i + r];
-                    u = clamp_i32(smad24((u * f) >> 12, gm[r], rnd) >> shift, -32767, 32767);
+    for (int n = 0; n < NH; ++n) {
+        if (NH > 1 && head + n >= heads) return;
+        int32_t x[2 * P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) { x[i] = byte_of(w0[n][i / 4], i & 3); x[P + i] = byte_of(w1[n][i / 4], i & 3); }
+        if (gamma) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int4* g4 = reinterpret_cast<const int4*>(gamma + (half ? c1 : c0));
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const int4 w = g4[i];
+                    const int32_t gm[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        int32_t& u = x[P * half + 4 * i + r];
+                        u = clamp_i32(smad24((u * f[n]) >> 12, gm[r], norm_rnd) >> shift, -32767, 32767);
+                    }
                 }
             }
         }
-    }
-    if (turned) {
+        if (turned) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int32_t c = (int32_t)(int16_t)cs[i], s = (int32_t)cs[i] >> 16;
-            int32_t& p = x[INTERLEAVED ? 2 * i : i];
-            int32_t& q = x[INTERLEAVED ? 2 * i + 1 : P + i];
-            const int32_t y = smul24(p, c) - smul24(q, s);
-            q = smad24(p, s, smul24(q, c));
-            p = y;
+            for (int i = 0; i < P; ++i) {
+                const int32_t c = (int32_t)(int16_t)cs[i], s = (int32_t)cs[i] >> 16;
+                int32_t& p = x[INTERLEAVED ? 2 * i : i];
+                int32_t& q = x[INTERLEAVED ? 2 * i + 1 : P + i];
+                const int32_t y = smul24(p, c) - smul24(q, s);
+                q = smad24(p, s, smul24(q, c));
+                p = y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * P; ++i) x[i] <<= 14;
         }
-    } else {
+        if (a.fast[kind]) {
 #pragma unroll
-        for (int i = 0; i < 2 * P; ++i) x[i] <<= 14;
-    }
-    const ibert_dyadic dy = a.dy[kind];
-    if (a.fast[kind]) {
-        const int64_t rnd = (int64_t)1 << (dy.s - 1);
+            for (int i = 0; i < 2 * P; ++i) x[i] = med3_const<-127, 127>((int32_t)(((int64_t)x[i] * dy.m + rnd) >> 32) >> ((dy.s - 32) & 31));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2 * P; ++i) x[i] = med3_const<-127, 127>((int32_t)(((int64_t)x[i] * dy.m + rnd) >> 32) >> ((dy.s - 32) & 31));
-    } else {
+            for (int i = 0; i < 2 * P; ++i) x[i] = clamp_i64_to_i32(dyadic64(x[i], dy.m, dy.s), 127);
+        }
+        words o0, o1;
 #pragma unroll
-        for (int i = 0; i < 2 * P; ++i) x[i] = clamp_i64_to_i32(dyadic64(x[i], dy.m, dy.s), 127);
-    }
-    words o0, o1;
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        o0[i] = pack4_perm(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-        o1[i] = pack4_perm(x[P + 4 * i], x[P + 4 * i + 1], x[P + 4 * i + 2], x[P + 4 * i + 3]);
-    }
-    if (kind == 0) {
-        int8_t* dst = a.q + row * a.ld_q + head * D;
-        *reinterpret_cast<words*>(dst + c0) = o0;
-        *reinterpret_cast<words*>(dst + c1) = o1;
-    } else {
-        const int64_t page = slot >> a.log_page;
-        const int t = slot & ((1 << a.log_page) - 1);
-        int8_t* dst = a.k + (((page * a.heads_kv + head) << a.log_page) + (t & ~15)) * D + (t & 15) * 16;
-        *reinterpret_cast<words*>(dst + (c0 >> 4) * 256 + (c0 & 15)) = o0;
-        *reinterpret_cast<words*>(dst + (c1 >> 4) * 256 + (c1 & 15)) = o1;
+        for (int i = 0; i < W; ++i) {
+            o0[i] = pack4_perm(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            o1[i] = pack4_perm(x[P + 4 * i], x[P + 4 * i + 1], x[P + 4 * i + 2], x[P + 4 * i + 3]);
+        }
+        if (kind == 0) {
+            int8_t* dst = a.q + row * a.ld_q + (head + n) * D;
+            *reinterpret_cast<words*>(dst + c0) = o0;
+            *reinterpret_cast<words*>(dst + c1) = o1;
+        } else {
+            int8_t* dst = a.k + (((page * a.heads_kv + head + n) << a.log_page) + (t & ~15)) * D + (t & 15) * 16;
+            *reinterpret_cast<words*>(dst + (c0 >> 4) * 256 + (c0 & 15)) = o0;
+            *reinterpret_cast<words*>(dst + (c1 >> 4) * 256 + (c1 & 15)) = o1;
+        }
     }
 }
 
@@ -165,11 +186,11 @@ __device__ __forceinline__ void value_row(const RotaryArgs& a, const int8_t* src
 }
 
 template <int D>
-__device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, uint32_t* lds)
+__device__ __forceinline__ void append_values(const RotaryArgs& a, int32_t wg, uint32_t* lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = (int)(wg % a.heads_kv);
-    const int64_t row0 = wg / a.heads_kv * 64, row = row0 + lane;
+    const int window = wg / a.heads_kv, head = wg - window * a.heads_kv;
+    const int64_t row0 = (int64_t)window * 64, row = row0 + lane;
     // slots of the 64 rows, of those before and of those behind; which continue the row before
     const auto slot_at = [&](int64_t r) { return r >= 0 && r < a.rows ? a.slots[r] : -1; };
     const int32_t s0 = slot_at(row - 64), s1 = slot_at(row), s2 = slot_at(row + 64);
@@ -247,15 +268,15 @@ __device__ __forceinline__ void append_values(const RotaryArgs& a, int64_t wg, u
     }
 }
 
-template <int D, bool INTERLEAVED, int P>
+template <int D, bool INTERLEAVED, int P, int NH>
 __global__ __launch_bounds__(RO_THREADS) void rotary_append_kernel(RotaryArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint32_t lds[RO_THREADS / 64 * 256];
-    const int64_t wg = blockIdx.x;
+    const int32_t wg = (int32_t)blockIdx.x;
     // (values first: theirs is the longest chain of loads)
     if (wg < a.wgs[2]) append_values<D>(a, wg, lds);
-    else if (wg < a.wgs[2] + a.wgs[1]) rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[2], 1);
-    else rotate_heads<D, INTERLEAVED, P>(a, wg - a.wgs[2] - a.wgs[1], 0);
+    else if (wg < a.wgs[2] + a.wgs[1]) rotate_heads<D, INTERLEAVED, P, NH>(a, wg - a.wgs[2], 1);
+    else rotate_heads<D, INTERLEAVED, P, NH>(a, wg - a.wgs[2] - a.wgs[1], 0);
 }
 
 // The same multiplier with a shift of at least `least`, where 31 bits hold it: DY(x; 2m, s + 1) = DY(x; m, s).
@@ -265,16 +286,18 @@ static ibert_dyadic shifted(ibert_dyadic d, int least)
     return d;
 }
 
-template <int D, bool INTERLEAVED, int P>
+template <int D, bool INTERLEAVED, int P, int NH>
 static int launch_rotary(RotaryArgs& a, hipStream_t stream)
 {
     constexpr int per = RO_THREADS / (D / (2 * P));
-    a.wgs[0] = (a.rows * a.heads_q + per - 1) / per;
-    a.wgs[1] = (a.rows * a.heads_kv + per - 1) / per;
-    a.wgs[2] = (a.rows + 63) / 64 * a.heads_kv;
-    const int64_t wgs = a.wgs[0] + a.wgs[1] + a.wgs[2];
-    if (wgs > 0x7fffffffLL) return IBERT_ERR_SHAPE;
-    hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED, P>), dim3((unsigned)wgs), dim3(RO_THREADS), 0, stream, a);
+    const int32_t heads[2] = {a.heads_q, a.heads_kv};
+    for (int k = 0; k < 2; ++k) {
+        a.teams[k] = (heads[k] + NH - 1) / NH;
+        a.teams_magic[k] = udiv_magic(a.teams[k]);
+        a.wgs[k] = (int32_t)((a.rows * a.teams[k] + per - 1) / per);
+    }
+    a.wgs[2] = (int32_t)((a.rows + 63) / 64 * a.heads_kv);
+    hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED, P, NH>), dim3((unsigned)(a.wgs[0] + a.wgs[1] + a.wgs[2])), dim3(RO_THREADS), 0, stream, a);
     IBERT_LAUNCH_CHECK("rotary_append_kernel");
     g_last_kernel = "rotary_append_kernel";
     return IBERT_OK;
@@ -283,9 +306,11 @@ static int launch_rotary(RotaryArgs& a, hipStream_t stream)
 template <int D>
 static int launch_rotary(RotaryArgs& a, bool interleaved, hipStream_t stream)
 {
-    const bool wide = a.rot % 32 == 0;
-    if (interleaved) return wide ? launch_rotary<D, true, 16>(a, stream) : launch_rotary<D, true, 8>(a, stream);
-    return wide ? launch_rotary<D, false, 16>(a, stream) : launch_rotary<D, false, 8>(a, stream);
+    if (a.rot % 32) return interleaved ? launch_rotary<D, true, 8, 1>(a, stream) : launch_rotary<D, false, 8, 1>(a, stream);
+    if constexpr (D == 128) {
+        if (a.rows * a.heads_q >= RO_TEAM_HEADS) return interleaved ? launch_rotary<D, true, 16, 2>(a, stream) : launch_rotary<D, false, 16, 2>(a, stream);
+    }
+    return interleaved ? launch_rotary<D, true, 16, 1>(a, stream) : launch_rotary<D, false, 16, 1>(a, stream);
 }
 
 }  // namespace ibert
@@ -306,7 +331,7 @@ extern "C" int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_
         !dyadic_ok(d.q_dy) || !dyadic_ok(d.k_dy) || !dyadic_ok(d.v_dy) || (d.rot_dim > 0 && d.max_pos < 1) ||
         (q_gamma && (d.q_norm_shift < 1 || d.q_norm_shift > 30)) || (k_gamma && (d.k_norm_shift < 1 || d.k_norm_shift > 30))) return IBERT_ERR_PARAM_RANGE;
     if (rows == 0) return IBERT_OK;
-    if (rows > INT32_MAX) return IBERT_ERR_SHAPE;
+    if (rows > INT32_MAX / heads - 256) return IBERT_ERR_SHAPE;          // (teams of lanes are counted in 32 bits)
     if (!qkv || !slots || !q || !cache->k || !cache->v || (d.rot_dim > 0 && (!table || !positions))) return IBERT_ERR_NULL;
     if (!aligned(qkv, 16) || !aligned(q, 16) || !aligned(cache->k, 16) || !aligned(cache->v, 16) || !aligned(table, 16) || ld_qkv % 16 || ld_q % 16 ||
         !aligned(q_gamma, 16) || !aligned(k_gamma, 16)) return IBERT_ERR_ALIGN;
@@ -322,7 +347,6 @@ extern "C" int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_
     ibert_dyadic v = shifted(d.v_dy, 33);
     if (v.s < 9) v.s = 9;
     a.v_m = v.m; a.v_l = v.s < 33 ? 33 - v.s : 0; a.v_r = v.s < 33 ? 1 : v.s - 32;
-    a.heads_magic[0] = udiv_magic(d.heads_q); a.heads_magic[1] = udiv_magic(cache->heads_kv);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return D == 64 ? launch_rotary<64>(a, d.layout == IBERT_ROTARY_INTERLEAVED, st) : launch_rotary<128>(a, d.layout == IBERT_ROTARY_INTERLEAVED, st);
 }
