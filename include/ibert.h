@@ -13,9 +13,9 @@
  *   - Only integers reach the device: real scales appear solely in the host helpers at the end,
  *     which pre-compute the integer constants (static quantization, Sec. 3.1 and App. A; footnote
  *     of Alg. 1).  The device sources contain no floating-point type or operation (the integer square root of
- *     Alg. 4 included); the only place the compiler may use its reciprocal unit is its own expansion of the two
- *     per-row integer divisions with data-dependent divisors (2^31 / sum in Softmax, 2^24 / sigma in LayerNorm),
- *     each of which returns the exact integer quotient.
+ *     Alg. 4 included); the only place the compiler may use its reciprocal unit is its own expansion of integer
+ *     divisions (by a sum or a root: 2^31 / sum in Softmax, 2^24 / sigma in LayerNorm, 2^30 / sigma and 2^48 / W in the
+ *     decoder calls; by an argument: workgroups to rows), each of which returns the exact integer quotient.
  *   - Out-of-range data never faults: it is clamped as documented (the functions are total on int32
  *     inputs); out-of-range *constants* are refused with IBERT_ERR_PARAM_RANGE.
  *   - floor(.) is the mathematical floor; ">>" on signed values is an arithmetic shift.
@@ -499,8 +499,8 @@ int ibert_page_tables_i(const int32_t* len_before, const int32_t* len_after, int
  * see ibert_rotary_table_from_freqs); positions: device int32 [rows], clamped into [0, max_pos); slots: device int32
  * [rows]; q_gamma, k_gamma: device int32 [D] with |gamma| < 2^14, or NULL (no norm; see ibert_head_norm_from_float).
  * Preconditions: heads_q a multiple of heads_kv (IBERT_ERR_SHAPE); 0 <= R <= D, R a multiple of 16; shifts of the norms that
- * are used in [1, 30], all dyadic shifts in [0, 62] (IBERT_ERR_PARAM_RANGE); rows * (heads_q + 2 heads_kv + 1) <
- * 2^31 (IBERT_ERR_SHAPE); qkv, q, table, both gammas and both leading
+ * are used in [1, 30], all dyadic shifts in [0, 62] (IBERT_ERR_PARAM_RANGE); rows + 256 <=
+ * (2^31 - 1) / (heads_q + 2 heads_kv) (IBERT_ERR_SHAPE); qkv, q, table, both gammas and both leading
  * dimensions 16-byte aligned (IBERT_ERR_ALIGN).  q must not overlap qkv.
  * ---------------------------------------------------------------------------------------------- */
 enum { IBERT_ROTARY_HALF = 0, IBERT_ROTARY_INTERLEAVED = 1 };
@@ -533,8 +533,8 @@ int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* c
  * [batch + 1], ascending; kv_len: device int32 [batch].  Lengths are clamped into [0, min(max_kv_len, max_pages *
  * page_size)], page numbers into the cache, q_start into [0, rows]; rows of no sequence, and rows of a sequence beyond its
  * first max_q_len, are left as they were.  max_q_len, max_kv_len: bounds of the batch that the host knows; they size the launch and the workspace.
- * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes (may be NULL where that is 0); calls that may
- * overlap in time need one each.
+ * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes for the same arguments (smaller bounds may ask for
+ * more; else IBERT_ERR_WORKSPACE; may be NULL where that is 0); calls that may overlap in time need one each.
  * Preconditions: max_kv_len <= 131072 and scores_dy.m >= 0, its shift in [24, 62], out_dy's in [0, 62], window, sinks >= 0
  * (IBERT_ERR_PARAM_RANGE); heads_q a multiple of heads_kv, leading dimensions >= heads_q * head_dim, batch <= 65535, max_q_len >= 1,
  * max_q_len * heads_q / heads_kv <= 64 * 65535, rows >= batch where q_start is NULL (IBERT_ERR_SHAPE); q and ld_q 16-byte, out and ld_out 4-byte aligned (IBERT_ERR_ALIGN).  The cache's V holds values in

@@ -301,6 +301,19 @@ def test_attention_of_one_row_a_sequence_needs_no_starts(gpu):
     check_attention(U.Attention(30, 8, 2, 128, 64, [1] * 5, [1, 700, 64, 0, 129], pad=2), plain_rows=True)
 
 
+def test_attention_without_keys(gpu):
+    for n in ([1, 1], [70, 3]):
+        d, want = check_attention(U.Attention(46, 4, 2, 64, 64, n, [0, 0], pad=2))
+        assert not want[:int(sum(n))].any()
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (131071, 2 ** 31 - 1), (1, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_attention_of_the_largest_windows(gpu, window, sinks):
+    # (rows before the first key among them)
+    check_attention(U.Attention(47, 4, 2, 64, 64, [1, 1, 1], [100, 300, 0], window, sinks))
+    check_attention(U.Attention(48, 4, 2, 64, 64, [100, 70, 5], [50, 200, 2], window, sinks))
+
+
 def test_attention_leaves_rows_beyond_max_q_len(gpu):
     torch, G, B = libs()
     case = U.Attention(31, 3, 1, 64, 64, [40, 10, 21], [60, 10, 90])
@@ -386,7 +399,8 @@ def test_attention_of_many_sequences(gpu):
 # ------------------------------------------------------------------------------------------- graphs and streams
 def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
     torch, G, B = libs()
-    cases = [U.Attention(40, 8, 2, 128, 64, [1, 1], [5000, 77]), U.Attention(41, 4, 4, 64, 64, [70, 5], [90, 300]), U.Attention(42, 12, 12, 64, 64, [1] * 3, [10, 64, 200])]
+    cases = [U.Attention(40, 8, 2, 128, 64, [1, 1], [5000, 77]), U.Attention(41, 4, 4, 64, 64, [70, 5], [90, 300]), U.Attention(42, 12, 12, 64, 64, [1] * 3, [10, 64, 200]),
+             U.Attention(45, 4, 1, 64, 64, [1] * 64, [4500] * 64)]          # (the last: more LDS than a launch has by itself)
     devs = [DeviceAttention(c) for c in cases]
     pages = DevicePages(U.Pages(43, *U.mixed_lengths(np.random.default_rng(43), 70, 300), 64))
     rot = U.Rotary(44, 40, 4, 2, 64, 64, False, 64, True, True)
