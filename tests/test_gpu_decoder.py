@@ -314,6 +314,66 @@ def test_attention_of_the_largest_windows(gpu, window, sinks):
     check_attention(U.Attention(48, 4, 2, 64, 64, [100, 70, 5], [50, 200, 2], window, sinks))
 
 
+def test_offsets_beyond_32_bits(gpu):
+    # a cache of over 4 GB for each of K and V, whose last pages are the ones in use
+    torch, G, B = libs()
+    D, hk, page = 128, 8, 256
+    high = (4 << 30) // (page * hk * D) + 50
+    case = U.Attention(49, 16, hk, D, page, [1, 40], [600, 700])
+    rot = U.Rotary(50, 70, 16, hk, D, D, False, page)
+    cells = (high + max(case.pages, rot.pages)) * page * hk * D
+    tk, tv = (torch.zeros(cells, dtype=torch.int8, device=G.DEV) for _ in range(2))
+    base = high * page * hk * D
+    assert base > 1 << 32
+    tk[base:base + case.k.size], tv[base:base + case.v.size] = G.to_dev(case.k), G.to_dev(case.v)
+    want = case.oracle()
+    for form in (B.PAGED_TWICE, B.PAGED_ONE, B.PAGED_SPLIT, B.PAGED_PROMPT):
+        G.say("attention in a cache of %d MB, form %d" % (cells >> 20, form))
+        B.ibert_paged_attention_override(form)
+        try:
+            d = DeviceAttention(case)
+            d.table += high
+            d.cache = B.KvCache(tk.data_ptr(), tv.data_ptr(), hk, D, page, high + case.pages)
+            d.call()
+            same(d.result(), want, "out, form %d" % form)
+        finally:
+            B.ibert_paged_attention_override(-1)
+    want = rot.oracle()
+    tk[base:base + rot.k0.size], tv[base:base + rot.v0.size] = G.to_dev(rot.k0), G.to_dev(rot.v0)
+    tq = G.to_dev(rot.q0)
+    desc, cache = rot.descs(tk, tv)
+    cache.num_pages = high + rot.pages
+    G.say("rotary into a cache of %d MB" % (cells >> 20))
+    B.ibert_rotary_append_i(desc, cache, G.to_dev(rot.qkv), rot.qkv.shape[1], G.to_dev(rot.cs), G.to_dev(rot.positions), G.to_dev(rot.slots + high * page), None, None, rot.rows, tq,
+                            rot.q0.shape[1])
+    torch.cuda.synchronize()
+    same(tq, want[0], "q")
+    same(tk[base:base + rot.k0.size], want[1], "k")
+    same(tv[base:base + rot.v0.size], want[2], "v")
+
+
+def test_attention_of_rows_that_start_anywhere_allowed(gpu):
+    # q 16 bytes into its buffer, out 4 bytes into its own
+    torch, G, B = libs()
+    for n, kv in (([1, 1], [90, 3000]), ([70, 5], [90, 200])):
+        case = U.Attention(51, 4, 2, 64, 64, n, kv, ld=16)
+        want = case.oracle()
+        for form in (B.PAGED_TWICE, B.PAGED_ONE, B.PAGED_SPLIT, B.PAGED_PROMPT):
+            G.say("attention of shifted rows, form %d" % form)
+            B.ibert_paged_attention_override(form)
+            try:
+                d = DeviceAttention(case)
+                tq, to = torch.zeros(case.q.size + 16, dtype=torch.int8, device=G.DEV), torch.full((case.out.size + 4,), 77, dtype=torch.int8, device=G.DEV)
+                tq[16:], to[4:] = G.to_dev(case.q).reshape(-1), G.to_dev(case.out).reshape(-1)
+                d.tq, d.out = tq[16:], to[4:]
+                d.call()
+                torch.cuda.synchronize()
+                same(to[4:], want.reshape(-1), "out, form %d" % form)
+                assert bool((to[:4] == 77).all())
+            finally:
+                B.ibert_paged_attention_override(-1)
+
+
 def test_attention_leaves_rows_beyond_max_q_len(gpu):
     torch, G, B = libs()
     case = U.Attention(31, 3, 1, 64, 64, [40, 10, 21], [60, 10, 90])
