@@ -539,14 +539,16 @@ __global__ __launch_bounds__(PJ_THREADS) void paged_join_kernel(SplitArgs a)
 }
 
 // ---- many rows: prompts ------------------------------------------------------------------------------------------------
-// A workgroup of NW wavefronts owns 16 NW RT rows, a wavefront RT tiles of 16.  First the rows' maxima: a wavefront takes 64 of the
-// rows and every so-manieth block of keys, straight from memory into registers (operand order as the cache keeps it), so that
-// no key is read by more wavefronts than there are groups of 64 rows, and none waits for another before the end.  Then weights and sums, which stay in
-// registers: K and V come a block of 64 keys at a time into LDS, one block ahead, for all wavefronts.  A weight's two halves are read
-// from a table in LDS, entry DY(m - s): the maximum goes into the addend of the score's own 64-bit multiply-add.
-constexpr int PP_TABLE = 1025, PP_RT = 1, PP_NW = 4;
-constexpr int pp_rows(int rt, int nw) { return 16 * rt * nw; }
-constexpr int pp_lds_bytes(int d, int rt, int nw) { return 4 * 64 * d + 2064 + 4 * (nw / (pp_rows(rt, nw) / 64)) * pp_rows(rt, nw); }
+// A workgroup of four wavefronts owns 64 rows, a wavefront 16.  First the rows' maxima: a wavefront takes all 64 rows and every fourth
+// block of keys, straight from memory into registers (operand order as the cache keeps it), so that no key is read twice and no wavefront
+// waits for another before the end.  Then weights and sums, which stay in registers: K and V come a block of 64 keys at a time into
+// LDS, one block ahead, for all four.  A weight's two halves are read from a table in LDS, entry DY(m - s): the maximum goes into the
+// addend of the score's own 64-bit multiply-add.
+// Bound: issue.  A score costs a multiply-add, a shift, a cap, an address, a read of 16 bits, a permute and half an addition, and an MFMA takes the
+// place of two and a half vector instructions, so that four wavefronts a SIMD, which is what 16 rows each allow, beat two of 32 rows: those
+// read every key from LDS half as often, but two wavefronts issue only every 5.8 cycles.  us, 4096 rows of 32 heads of width 128, 16 rows a wavefront / 32:
+// 176 / 194; 32 x 200 rows of 12 heads of width 64 23.0 / 22.6, 4096 of 16 75.8 / 101.
+constexpr int PP_TABLE = 1025, PP_NW = 4, PP_ROWS = 64;
 
 // Rows [first, first + n) of a tile, as a tile.
 __device__ __forceinline__ Tile part_of(const PagedArgs& a, const Tile& t, int first, int n)
@@ -580,7 +582,8 @@ __device__ __forceinline__ void part_row(const PagedArgs& a, const Tile& p, int 
     pos = p.pos0 + qi;
 }
 
-// Largest raw scores of 64 rows over the blocks first, first + step, ... of the part's: K goes straight from memory into registers.
+// Largest raw scores of 64 rows over the blocks first, first + step, ... of the part's: K goes straight from memory into registers, 32 keys while
+// the 32 before them are multiplied.
 template <int D>
 __device__ __forceinline__ void part_maxima(const PagedArgs& a, const Tile& p, int h, int b, int first, int step, int lane, int32_t (&mx)[4])
 {
@@ -599,122 +602,108 @@ __device__ __forceinline__ void part_maxima(const PagedArgs& a, const Tile& p, i
 #pragma unroll
         for (int i = 0; i < ND / 2; ++i) k[i] = *reinterpret_cast<const v4i*>(a.k + at + i * 1024 + lane * 16);
     };
+    // (a block that all rows see whole in one run of code, without tests between its matrix instructions)
+    auto scores = [&](int i, const v4i (&k)[ND / 2], v4i (&s)[4]) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) s[rt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[i * NJ + j], qf[rt][j], j == 0 ? v4i{0, 0, 0, 0} : s[rt], 0, 0, 0);
+    };
+    auto compare = [&](const v4i (&s)[4]) {
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx[rt] = larger(mx[rt], s[rt][r]);
+    };
     auto take = [&](int key, bool whole, const v4i (&k)[ND / 2]) {
+        if (whole) {
+            v4i s[2][4];
+            scores(0, k, s[0]);
+            scores(1, k, s[1]);
+            compare(s[0]);
+            compare(s[1]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            v4i s[4];
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) s[rt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[i * NJ + j], qf[rt][j], j == 0 ? v4i{0, 0, 0, 0} : s[rt], 0, 0, 0);
-            if (!whole) {
+            for (int i = 0; i < 2; ++i) {
+                v4i s[4];
+                scores(i, k, s);
 #pragma unroll
                 for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!visible(a, key + 16 * i + 4 * g + r, pos[rt])) s[rt][r] = INT32_MIN;
+                compare(s);
             }
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) mx[rt] = larger(mx[rt], s[rt][r]);
         }
     };
-    // (of wide heads no registers are left for what is on its way)
-    constexpr bool AHEAD = D == 64;
-    if (AHEAD && first < mine) ask(block_offset<D>(a, b, h, block_at(p, first)), k0);
+    if (first < mine) ask(block_offset<D>(a, b, h, block_at(p, first)), k0);
     for (int x = first; x < mine; x += step) {
         const int block = block_at(p, x);
         const bool whole = whole_block(a, p, block);
-        const int64_t at = block_offset<D>(a, b, h, block);
-        if (!AHEAD) ask(at, k0);
-        ask(at + 32 * D, k1);
+        ask(block_offset<D>(a, b, h, block) + 32 * D, k1);
         take(64 * block, whole, k0);
-        if (AHEAD) ask(block_offset<D>(a, b, h, block_at(p, x + step < mine ? x + step : x)), k0);
+        ask(block_offset<D>(a, b, h, block_at(p, x + step < mine ? x + step : x)), k0);
         take(64 * block + 32, whole, k1);
     }
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) mx[rt] = combine_rows32(combine_rows16(mx[rt], larger), larger);
 }
 
-template <int D, bool HIGH, int RT, int NW>
-__global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
+template <int D, bool HIGH>
+__global__ __launch_bounds__(64 * PP_NW, 4) void paged_prompt_kernel(PagedArgs a)
 {
-    constexpr int NJ = D / 64, ND = D / 16, BLOCK = 64 * D, ROWS = pp_rows(RT, NW), GROUPS = ROWS / 64, SPLIT = NW / GROUPS;
-    extern __shared__ __attribute__((aligned(16))) int8_t pp_lds[];          // K [2][BLOCK], V [2][BLOCK], table, maxima [SPLIT][ROWS]
+    constexpr int NJ = D / 64, ND = D / 16, BLOCK = 64 * D, NW = PP_NW;
+    __shared__ __attribute__((aligned(16))) int8_t blocks[4][BLOCK];          // K twice, V twice
+    __shared__ uint16_t table[PP_TABLE];
+    __shared__ int32_t maxima[NW][PP_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int h = blockIdx.x, b = blockIdx.z;
-    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, ROWS);           // (the rows with most keys first)
+    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, PP_ROWS);        // (the rows with most keys first)
     if (t.count == 0) return;
-    typedef __attribute__((address_space(3))) uint16_t* lds_u16;
-    typedef __attribute__((address_space(3))) int32_t* lds_i32;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)pp_lds, table = lds0 + 4 * BLOCK;
-    const uint32_t maxima = table + 2064;
     const int n = t.blocks;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)&blocks[0][0];
     auto offset = [&](int x) { return block_offset<D>(a, b, h, block_at(t, x < n ? x : (n > 0 ? n - 1 : 0))); };
     auto request = [&](int64_t at, int buffer) {
 #pragma unroll
-        for (int i = 0; i < (2 * ND + NW - 1) / NW; ++i) {
+        for (int i = 0; i < 2 * ND / NW; ++i) {
             const int piece = NW * i + wave;               // K's pieces of 1 KB, then V's
             const bool of_v = piece >= ND;
-            if (2 * ND % NW == 0 || piece < 2 * ND)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             :: "s"(lds0 + (uint32_t)((of_v ? 2 * BLOCK - ND * 1024 : 0) + buffer * BLOCK + piece * 1024)),
-                                "v"((uint32_t)((piece - (of_v ? ND : 0)) * 1024 + lane * 16)), "s"((of_v ? a.v : a.k) + at) : "memory", "m0");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :: "s"(lds0 + (uint32_t)((of_v ? 2 * BLOCK - ND * 1024 : 0) + buffer * BLOCK + piece * 1024)),
+                            "v"((uint32_t)((piece - (of_v ? ND : 0)) * 1024 + lane * 16)), "s"((of_v ? a.v : a.k) + at) : "memory", "m0");
         }
     };
     if (n > 0) request(offset(0), 0);
     for (int e = tid; e < PP_TABLE; e += 64 * NW) {
         const uint32_t z = (uint32_t)e >> 6, f = 124u - (e & 63u);
         const uint32_t w = (umad24(f, f, 8180u) + ((1u << z) >> 1)) >> z;
-        *(lds_u16)(uintptr_t)(table + 2u * (uint32_t)e) = (uint16_t)((w & 255u) | ((w + 128u) >> 8 << 8));
+        table[e] = (uint16_t)((w & 255u) | ((w + 128u) >> 8 << 8));
     }
 
     // ---- maxima -------------------------------------------------------------------------------------------------
-    const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
     {
         int32_t mx[4];
-        part_maxima<D>(a, part_of(a, t, 64 * (wave % GROUPS), 64), h, b, wave / GROUPS, SPLIT, lane, mx);
+        part_maxima<D>(a, t, h, b, wave, NW, lane, mx);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
-            if (g == 0) *(lds_i32)(uintptr_t)(maxima + 4u * (uint32_t)((wave / GROUPS) * ROWS + 64 * (wave % GROUPS) + 16 * rt + c)) = mx[rt];
+            if (g == 0) maxima[wave][16 * rt + c] = mx[rt];
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");          // (and the table is made)
 
     // ---- weights and sums ----------------------------------------------------------------------------------------
-    const Tile own = part_of(a, t, wave * 16 * RT, 16 * RT);
+    const Tile own = part_of(a, t, wave * 16, 16);
     const int mine = blocks_of(own);
-    int pos[RT];
-    v4i qf[RT][NJ];
-    int32_t mx[RT];
-    v4i hi[RT][ND], lo[RT][ND];
-    int32_t sum_h[RT], sum_l[RT];
+    int pos;
+    v4i qf[NJ], hi[ND], lo[ND];
+    part_row<D>(a, own, h, 0, c, g, pos, qf);
+    int32_t mx = INT32_MIN, sum_h = 0, sum_l = 0;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        part_row<D>(a, own, h, rt, c, g, pos[rt], qf[rt]);
-        mx[rt] = INT32_MIN;
+    for (int i = 0; i < NW; ++i) mx = mx > maxima[i][wave * 16 + c] ? mx : maxima[i][wave * 16 + c];
 #pragma unroll
-        for (int i = 0; i < SPLIT; ++i) mx[rt] = larger(mx[rt], *(lds_i32)(uintptr_t)(maxima + 4u * (uint32_t)(i * ROWS + (wave * RT + rt) * 16 + c)));
-        sum_h[rt] = sum_l[rt] = 0;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) { hi[rt][i] = v4i{0, 0, 0, 0}; lo[rt][i] = v4i{0, 0, 0, 0}; }
-    }
-    auto scores = [&](const int8_t* ks, v4i (&s)[RT][4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const v4i kf = *reinterpret_cast<const v4i*>(ks + (i * NJ + j) * 1024 + lane * 16);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qf[rt][j], j == 0 ? v4i{0, 0, 0, 0} : s[rt][i], 0, 0, 0);
-            }
-        }
-    };
+    for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
     // DY(m - s) = (s * -factor + (m * factor + 2^(shift-1))) >> shift
     const int32_t minus_m = -(int32_t)a.s_m;
-    int64_t row_c[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) row_c[rt] = (int64_t)mx[rt] * (int32_t)a.s_m + ((int64_t)1 << (HIGH ? a.s_s + 31 : a.s_s - 1));
+    const int64_t row_c = (int64_t)mx * (int32_t)a.s_m + ((int64_t)1 << (HIGH ? a.s_s + 31 : a.s_s - 1));
     for (int x = 0; x < n; ++x) {
         const int64_t next = offset(x + 1);
         // block x has landed, for everybody, and everybody has left block x - 1
@@ -723,73 +712,63 @@ __global__ __launch_bounds__(64 * NW, 4) void paged_prompt_kernel(PagedArgs a)
         request(next, (x + 1) & 1);                        // (behind the last block: that one again)
         if (x >= mine) continue;
         const int block = block_at(t, x);
-        v4i s[RT][4], wh[RT], wl[RT];
-        scores(pp_lds + (x & 1) * BLOCK, s);
+        v4i s[4], wh, wl;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < NJ; ++j) {
+                const v4i kf = *reinterpret_cast<const v4i*>(&blocks[x & 1][(i * NJ + j) * 1024 + lane * 16]);
+                s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qf[j], j == 0 ? v4i{0, 0, 0, 0} : s[i], 0, 0, 0);
+            }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t p = (int64_t)s[rt][i][r] * minus_m + row_c[rt];
-                    const uint32_t d = HIGH ? (uint32_t)(p >> 32) >> (a.s_s & 31) : __builtin_amdgcn_alignbit((uint32_t)(p >> 32), (uint32_t)p, (uint32_t)(a.s_s & 31));
-                    s[rt][i][r] = (int32_t)(((d < PP_TABLE - 1u ? d : PP_TABLE - 1u) << 1) + table);
-                }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t p = (int64_t)s[i][r] * minus_m + row_c;
+                const uint32_t d = HIGH ? (uint32_t)(p >> 32) >> (a.s_s & 31) : __builtin_amdgcn_alignbit((uint32_t)(p >> 32), (uint32_t)p, (uint32_t)(a.s_s & 31));
+                s[i][r] = (int32_t)(d < PP_TABLE - 1u ? d : PP_TABLE - 1u);
+            }
         if (!whole_block(a, own, block)) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos[rt])) s[rt][i][r] = (int32_t)(table + 2 * (PP_TABLE - 1));
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[rt][i][r] = *(lds_u16)(uintptr_t)(uint32_t)s[rt][i][r];
+                for (int r = 0; r < 4; ++r)
+                    if (!visible(a, 64 * block + 16 * i + 4 * g + r, pos)) s[i][r] = PP_TABLE - 1;
+        }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t p = __builtin_amdgcn_perm((uint32_t)s[rt][i][1], (uint32_t)s[rt][i][0], 0x05010400u);
-                const uint32_t q = __builtin_amdgcn_perm((uint32_t)s[rt][i][3], (uint32_t)s[rt][i][2], 0x05010400u);
-                wl[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x05040100u);
-                wh[rt][i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x07060302u);
-                sum_l[rt] = __builtin_amdgcn_sdot4(wl[rt][i], 0x01010101, sum_l[rt], false);
-                sum_h[rt] = __builtin_amdgcn_sdot4(wh[rt][i], 0x01010101, sum_h[rt], false);
-            }
-        const int8_t* vs = pp_lds + (2 + (x & 1)) * BLOCK;
+            for (int r = 0; r < 4; ++r) s[i][r] = table[s[i][r]];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = __builtin_amdgcn_perm((uint32_t)s[i][1], (uint32_t)s[i][0], 0x05010400u);
+            const uint32_t q = __builtin_amdgcn_perm((uint32_t)s[i][3], (uint32_t)s[i][2], 0x05010400u);
+            wl[i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x05040100u);
+            wh[i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x07060302u);
+            sum_l = __builtin_amdgcn_sdot4(wl[i], 0x01010101, sum_l, false);
+            sum_h = __builtin_amdgcn_sdot4(wh[i], 0x01010101, sum_h, false);
+        }
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-            const v4i vf = *reinterpret_cast<const v4i*>(vs + i * 1024 + lane * 16);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                hi[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wh[rt], hi[rt][i], 0, 0, 0);
-                lo[rt][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wl[rt], lo[rt][i], 0, 0, 0);
-            }
+            const v4i vf = *reinterpret_cast<const v4i*>(&blocks[2 + (x & 1)][i * 1024 + lane * 16]);
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf, wl, lo[i], 0, 0, 0);
         }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                    // (nothing is on its way into LDS any more)
     const auto add = [](int32_t p, int32_t q) { return (int32_t)((uint32_t)p + (uint32_t)q); };
+    int32_t W = add((int32_t)((uint32_t)sum_h << 8), sum_l);
+    W = combine_rows32(combine_rows16(W, add), add);
+    if (c >= own.count) return;
+    const uint64_t R = reciprocal((uint32_t)W);
+    const int flat = own.first + c, qi = group_of(a, flat);
+    int8_t* dst = a.out + (int64_t)(t.row0 + qi) * a.ld_out + (h * a.group + (flat - qi * a.group)) * D + 4 * g;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        int32_t W = add((int32_t)((uint32_t)sum_h[rt] << 8), sum_l[rt]);
-        W = combine_rows32(combine_rows16(W, add), add);
-        const uint64_t R = reciprocal((uint32_t)W);
-        const int flat = own.first + 16 * rt + c;
-        if (16 * rt + c >= own.count) continue;
-        const int qi = group_of(a, flat);
-        int8_t* dst = a.out + (int64_t)(t.row0 + qi) * a.ld_out + (h * a.group + (flat - qi * a.group)) * D + 4 * g;
+    for (int i = 0; i < ND; ++i) {
+        int32_t y[4];
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            int32_t y[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = finished(a, (int64_t)hi[rt][i][r] * 256 + lo[rt][i][r], R);
-            *reinterpret_cast<uint32_t*>(dst + 16 * i) = pack4_perm(y[0], y[1], y[2], y[3]);
-        }
+        for (int r = 0; r < 4; ++r) y[r] = finished(a, (int64_t)hi[i][r] * 256 + lo[i][r], R);
+        *reinterpret_cast<uint32_t*>(dst + 16 * i) = pack4_perm(y[0], y[1], y[2], y[3]);
     }
 }
 
@@ -816,7 +795,7 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     p.splits = 1;
     p.high = d.scores_dy.s >= 32;
     const int form = g_paged_form;
-    const int64_t prompt_tiles = (rows + pp_rows(PP_RT, PP_NW) - 1) / pp_rows(PP_RT, PP_NW);
+    const int64_t prompt_tiles = (rows + PP_ROWS - 1) / PP_ROWS;
     // Prompts: a workgroup of the prompt kernel takes four times the rows, so it wants more of them before the chip is full.  us, the scores made twice / this,
     // 8 key heads of width 128 with 4 queries each: 1 x 300 rows on 8000 keys (152 workgroups) 99 / 135, 1 x 512 (256) 20.7 / 18.5, on 8000 keys 136 / 140,
     // 1 x 1024 (512) 39.6 / 29.4, on 8000 keys 245 / 168; 16 heads of width 64: 2 x 512 (256) 12.5 / 14.7, 1 x 2048 (512) 38.4 / 36.4, 4 x 512 (512) 19.7 / 16.4;
@@ -860,10 +839,9 @@ template <int D>
 static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
 {
     if (plan.prompt_tiles > 0) {
-        constexpr size_t lds = pp_lds_bytes(D, PP_RT, PP_NW);
         const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch), block(64 * PP_NW);
-        if (plan.high) hipLaunchKernelGGL((paged_prompt_kernel<D, true, PP_RT, PP_NW>), grid, block, lds, stream, a);
-        else hipLaunchKernelGGL((paged_prompt_kernel<D, false, PP_RT, PP_NW>), grid, block, lds, stream, a);
+        if (plan.high) hipLaunchKernelGGL((paged_prompt_kernel<D, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((paged_prompt_kernel<D, false>), grid, block, 0, stream, a);
         IBERT_LAUNCH_CHECK("paged_prompt_kernel");
         g_last_kernel = "paged_prompt_kernel";
         return IBERT_OK;
