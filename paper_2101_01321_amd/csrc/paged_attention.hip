@@ -182,31 +182,55 @@ __device__ __forceinline__ void tile_row(const PagedArgs& a, const Tile& t, int 
 }
 
 // ---- any number of rows, no workspace: the scores are made twice -----------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
+// NW wavefronts take every NW-th block of keys.  Eight, which ask for a block ahead (177 registers at width 128: one workgroup on a unit), where each workgroup has a
+// unit to itself; else four, which leave it to the other workgroups on the unit.  us, four / eight, 8 key heads of width 128 on 4000 keys: 32 workgroups 25.9 / 21.9, 128
+// 33.1 / 25.1, 256 44.1 / 38.9, 384 68.7 / 72.0, 512 73.9 / 90.7; 16 heads of width 64, 192 31.2 / 26.5.  Bound: latency up to there, then HBM or L2.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void paged_attention_kernel(PagedArgs a)
 {
-    constexpr int NJ = D / 64, ND = D / 16, NW = 4;
+    constexpr int NJ = D / 64, ND = D / 16;
+    constexpr bool AHEAD = NW == 8;
     __shared__ int32_t s_max[NW][16];
     __shared__ int32_t s_hi[D * 16], s_lo[D * 16], s_w[32];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int h = blockIdx.x, b = blockIdx.y;
     const Tile t = tile_of(a, b, blockIdx.z, 16);
     if (t.count == 0) return;
-    for (int i = tid; i < D * 16; i += 256) { s_hi[i] = 0; s_lo[i] = 0; }
+    for (int i = tid; i < D * 16; i += 64 * NW) { s_hi[i] = 0; s_lo[i] = 0; }
     if (tid < 32) s_w[tid] = 0;
     int pos;
     v4i qf[NJ];
     tile_row<D>(a, t, h, c, g, pos, qf);
-
-    int32_t mx = INT32_MIN;
-    for (int x = wave; x < t.blocks; x += NW) {
-        const int block = block_at(t, x);
-        v4i kf[ND], s[4];
-        load_k<D>(a, block_offset<D>(a, b, h, block), lane, kf);
-        block_scores<D>(a, t, block, pos, g, kf, qf, s);
-        mx = largest(s, mx);
-    }
+    const int n = t.blocks;
+    auto offset = [&](int x) { return block_offset<D>(a, b, h, block_at(t, x)); };
     const auto larger = [](int32_t p, int32_t q) { return p > q ? p : q; };
+
+    v4i f0[ND], f1[ND];
+    int32_t mx = INT32_MIN;
+    auto compare = [&](int x, const v4i (&k)[ND]) {
+        v4i s[4];
+        block_scores<D>(a, t, block_at(t, x), pos, g, k, qf, s);
+        mx = largest(s, mx);
+    };
+    if constexpr (AHEAD) {
+        int x = wave;
+        if (x < n) load_k<D>(a, offset(x), lane, f0);
+        while (x < n) {
+            if (x + NW < n) load_k<D>(a, offset(x + NW), lane, f1);
+            compare(x, f0);
+            x += NW;
+            if (x >= n) break;
+            if (x + NW < n) load_k<D>(a, offset(x + NW), lane, f0);
+            compare(x, f1);
+            x += NW;
+        }
+        if (wave < n) load_k<D>(a, offset(wave), lane, f0);
+    } else {
+        for (int x = wave; x < n; x += NW) {
+            load_k<D>(a, offset(x), lane, f0);
+            compare(x, f0);
+        }
+    }
     mx = combine_rows32(combine_rows16(mx, larger), larger);
     if (g == 0) s_max[wave][c] = mx;
     __syncthreads();
@@ -217,18 +241,17 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
 #pragma unroll
     for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
     uint32_t sum = 0;
-    for (int x = wave; x < t.blocks; x += NW) {
-        const int block = block_at(t, x);
-        const int64_t at = block_offset<D>(a, b, h, block);
-        v4i kf[ND], vf[ND], s[4], wh, wl;
-        load_k<D>(a, at, lane, kf);
-        load_v<D>(a, at, lane, vf);
-        block_scores<D>(a, t, block, pos, g, kf, qf, s);
+    for (int x = wave; x < n; x += NW) {
+        v4i s[4], wh, wl;
+        if (!AHEAD) load_k<D>(a, offset(x), lane, f0);
+        load_v<D>(a, offset(x), lane, f1);
+        block_scores<D>(a, t, block_at(t, x), pos, g, f0, qf, s);
+        if (AHEAD && x + NW < n) load_k<D>(a, offset(x + NW), lane, f0);
         block_weights(a, s, mx, wh, wl, sum);
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], wh, hi[i], 0, 0, 0);
-            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], wl, lo[i], 0, 0, 0);
+            hi[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f1[i], wh, hi[i], 0, 0, 0);
+            lo[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f1[i], wl, lo[i], 0, 0, 0);
         }
     }
     // whole numbers: the order of these additions changes nothing
@@ -247,7 +270,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedArgs a)
         s_w[16 + tid] = (int32_t)(uint32_t)(R >> 32);
     }
     __syncthreads();
-    for (int e = tid; e < D * 16; e += 256) {
+    for (int e = tid; e < D * 16; e += 64 * NW) {
         const int r = e / D, d = e - r * D;
         if (r >= t.count) break;
         const int f = t.first + r, qr = group_of(a, f), hd = h * a.group + (f - qr * a.group);
@@ -796,16 +819,18 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     p.high = d.scores_dy.s >= 32;
     const int form = g_paged_form;
     const int64_t prompt_tiles = (rows + PP_ROWS - 1) / PP_ROWS;
-    // Prompts: a workgroup of the prompt kernel takes four times the rows, so it wants more of them before the chip is full.  us, the scores made twice / this,
-    // 8 key heads of width 128 with 4 queries each: 1 x 300 rows on 8000 keys (152 workgroups) 99 / 135, 1 x 512 (256) 20.7 / 18.5, on 8000 keys 136 / 140,
-    // 1 x 1024 (512) 39.6 / 29.4, on 8000 keys 245 / 168; 16 heads of width 64: 2 x 512 (256) 12.5 / 14.7, 1 x 2048 (512) 38.4 / 36.4, 4 x 512 (512) 19.7 / 16.4;
-    // 12: 2 x 700 on 4000 keys (264) 61 / 64, 8 x 200 (384) 11.3 / 11.9, 32 x 200 (1536) 30.4 / 23.3.
-    if (p.tiles > 65535 || (form < 0 ? rows > 16 && prompt_tiles * batch * c.heads_kv >= 320 : form == IBERT_PAGED_PROMPT)) {
+    const int64_t seqs = (int64_t)batch * c.heads_kv, problems = seqs * p.tiles;
+    // Prompts: a workgroup of the prompt kernel takes four times the rows, so it wants more of them before the chip is full, and most of their rows filled.  us,
+    // the scores made twice / this, 8 key heads of width 128 with 4 queries each: 1 x 300 rows on 8000 keys (152 workgroups) 99 / 135, 1 x 512 (256) 20.7 / 18.5, on
+    // 8000 keys 136 / 140, 1 x 1024 (512) 39.6 / 29.4, on 8000 keys 245 / 168; 16 heads of width 64: 2 x 512 (256) 12.5 / 14.7, 1 x 2048 (512) 38.4 / 36.4; 12:
+    // 8 x 200 (384) 11.3 / 11.9, 32 x 200 (1536) 30.4 / 23.3.  Few rows each, by 16-row tiles: width 128, 40 x 5 (640) on 600 keys 18.8 / 21.3, on 1500 42.1 / 40.5, on
+    // 4000 111 / 98, 40 x 12 (960) on 600 27.1 / 22.4; width 64, 30 x 20 (720) on 1000 17.5 / 21.7, on 4000 60 / 66, 30 x 40 (1080) on 1000 23.5 / 22.4, on 4000 87 / 69.
+    const bool many = prompt_tiles * seqs >= 320 && problems >= (c.head_dim == 128 && blocks >= 24 ? 640 : 960);
+    if (p.tiles > 65535 || (form < 0 ? rows > 16 && many : form == IBERT_PAGED_PROMPT)) {
         p.prompt_tiles = (int32_t)prompt_tiles;
         return p;
     }
     if (batch == 0) return p;
-    const int64_t problems = (int64_t)batch * c.heads_kv * p.tiles;
     // One launch where the scores of all keys fit LDS, unless that leaves few workgroups with long ways: a workgroup takes some 0.2 us a block and the three
     // launches 12 and more.  us, three launches / one, of 8 key heads of width 128, 4 rows: 1 x 1000 keys 11.9 / 9.9, 1 x 2000 12.4 / 13.4, 1 x 4000 12.9 / 20.1,
     // 8 x 4000 22.3 / 22.3, 16 x 1500 18.6 / 13.4, 24 x 4000 44.0 / 32.1, 64 x 4096 94.6 / 71.6; 12 of width 64, 1 row: 4 x 2000 12.8 / 11.2, 2 x 4000 13.5 / 18.2.
@@ -814,13 +839,18 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
         p.room = (int32_t)blocks;
         return p;
     }
-    // More rows than a tile: their tiles fill the chip by themselves unless they are very few and the keys many.  us, the scores made twice / split, 8 key heads of
-    // width 128: 8 rows of 4 queries on 8000 keys (16 workgroups) 54 / 28, 16 rows (32) 52 / 31, 64 rows (128) 52 / 60; 32 rows on 1000 keys (64) 13.3 / 19.8.
-    if (form < 0 ? rows > 16 && (problems > 48 || blocks < 48) : form != IBERT_PAGED_SPLIT) return p;
     int64_t splits = (512 + problems - 1) / problems;
     int64_t chunk = (blocks + splits - 1) / splits;
     if (chunk < 4) chunk = 4;
     splits = (blocks + chunk - 1) / chunk;
+    // Keys split where a workgroup's way along them takes longer than two more launches and what they hand on.  Both are estimated, in ns, with the bounds that the host
+    // knows: 0.27 us a block (width 64 0.23) or the bytes of K twice and V; 11 us, the bytes of K and V, and those of the scores and partial sums.  us, twice / split,
+    // blocks of keys x tiles, width 128: 4 rows a tile 47 x 8 17.0 / 12.3, 47 x 128 20.8 / 24.4, 188 x 128 88 / 70, 188 x 320 208 / 190; 8 rows 188 x 32 69 / 35, 47 x 128
+    // 27 / 38; 16 rows 63 x 16 21.9 / 19.2, 63 x 32 22 / 27, 188 x 32 69 / 46, 188 x 128 110 / 135, 938 x 16 310 / 67; width 64, 1 row 125 x 48 31.8 / 20.0, 12 rows
+    // 125 x 12 32 / 18, 125 x 48 33 / 33, 125 x 144 41 / 75.
+    const int64_t block_bytes = seqs * blocks * 64 * c.head_dim, along = blocks * (c.head_dim == 128 ? 270 : 230), thrice = block_bytes * 3 / 4600;
+    const int64_t handed_on = problems * p.held * (blocks * 512 + splits * c.head_dim * 16);
+    if (form < 0 ? 6000 + (along > thrice ? along : thrice) <= 11000 + block_bytes * 2 / 5000 + handed_on / 3000 : form != IBERT_PAGED_SPLIT) return p;
     p.splits = (int32_t)splits; p.chunk = (int32_t)chunk; p.blocks = (int32_t)blocks;
     const auto room = [&](int64_t n) {
         const size_t at = p.total;
@@ -857,7 +887,9 @@ static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, voi
         return IBERT_OK;
     }
     if (plan.chunk == 0) {
-        hipLaunchKernelGGL(paged_attention_kernel<D>, dim3((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles), dim3(256), 0, stream, a);
+        const dim3 grid((unsigned)a.heads_kv, (unsigned)batch, (unsigned)plan.tiles);
+        if ((int64_t)a.heads_kv * batch * plan.tiles <= 256) hipLaunchKernelGGL((paged_attention_kernel<D, 8>), grid, dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((paged_attention_kernel<D, 4>), grid, dim3(256), 0, stream, a);
         IBERT_LAUNCH_CHECK("paged_attention_kernel");
         g_last_kernel = "paged_attention_kernel";
         return IBERT_OK;
