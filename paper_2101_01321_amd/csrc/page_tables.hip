@@ -4,7 +4,8 @@
 // are a few thousand integers, so every workgroup makes all of them for itself in LDS (two passes: what is asked for decides
 // what is granted) and then writes its share of the rows and of the pages, each of which finds its sequence by bisection of
 // those sums.  One launch, no workspace, nothing passed between workgroups; the order of the pages is that of the sequences.
-// Bound: latency (a launch, two dependent trips to memory, the sums).
+// Bound: latency (a launch, two dependent trips to memory, the sums): a batch of one 2.9 us, 512 sequences of up to 8192 tokens with prompts among them 5.3
+// (kernel trace), where an empty kernel takes 2.2.  Passing the sums from one workgroup to the others would be a second launch or a wait.
 #include "common.h"
 
 namespace ibert {

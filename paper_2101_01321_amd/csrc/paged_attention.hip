@@ -281,7 +281,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void paged_attention_kern
 
 // ---- few rows, one launch: a workgroup for each sequence, key head and tile, scores in LDS --------------------------------
 // K once, the scores into LDS, the maximum over the workgroup, then V once.  LDS: scores [held][64 blocks], then the sums [held][D], high
-// and low halves.
+// and low halves.  Bound: HBM.  64 sequences of up to 4096 keys, 8 key heads of width 128 with 4 queries each: 342 MB in 67.7 us (5.05 TB/s; a copy reaches 5.17);
+// 32 x 1025 visible keys in 16 heads of width 64: 67 MB in 16.4 us (4.1 TB/s); few keys: the launch and four dependent trips to memory, 5.2 us for 77.
 constexpr int PW_NW = 8;
 template <int D>
 __global__ __launch_bounds__(64 * PW_NW, 2) void paged_row_kernel(PagedArgs a, int32_t held, int32_t room)
@@ -382,7 +383,9 @@ __global__ __launch_bounds__(64 * PW_NW, 2) void paged_row_kernel(PagedArgs a, i
 }
 
 // ---- few rows on many keys: three launches, the keys of a tile of rows split into chunks ---------------------------------
-// Scores and each chunk's maximum; weights, sums over the chunk, with the maximum of all chunks; the chunks' sums joined.
+// Scores and each chunk's maximum; weights, sums over the chunk, with the maximum of all chunks; the chunks' sums joined.  (The weights need the whole row's
+// maximum, so there is a launch between the scores and them.)  Bound: HBM.  One sequence of 131071 keys, 8 key heads of width 128 with 4 queries each: 30.1, 32.4 and
+// 4.6 us, K's and V's 134 MB each at 4.5 and 4.1 TB/s with 17 MB of scores between them.
 struct SplitArgs {
     PagedArgs p;
     int32_t tiles, splits, chunk;      // row tiles of a key head; chunks of at most `chunk` blocks
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(PJ_THREADS) void paged_join_kernel(SplitArgs a)
 // waits for another before the end.  Then weights and sums, which stay in registers: K and V come a block of 64 keys at a time into
 // LDS, one block ahead, for all four.  A weight's two halves are read from a table in LDS, entry DY(m - s): the maximum goes into the
 // addend of the score's own 64-bit multiply-add.
-// Bound: issue.  A score costs a multiply-add, a shift, a cap, an address, a read of 16 bits, a permute and half an addition, and an MFMA takes the
+// Bound: issue.  A score costs a multiply-add, a shift, a cap, an address, a read of 16 bits and a permute, and an MFMA takes the
 // place of two and a half vector instructions, so that four wavefronts a SIMD, which is what 16 rows each allow, beat two of 32 rows: those
 // read every key from LDS half as often, but two wavefronts issue only every 5.8 cycles.  us, 4096 rows of 32 heads of width 128, 16 rows a wavefront / 32:
 // 176 / 194; 32 x 200 rows of 12 heads of width 64 23.0 / 22.6, 4096 of 16 75.8 / 101.
@@ -719,13 +722,15 @@ __global__ __launch_bounds__(64 * PP_NW, 4) void paged_prompt_kernel(PagedArgs a
     int pos;
     v4i qf[NJ], hi[ND], lo[ND];
     part_row<D>(a, own, h, 0, c, g, pos, qf);
-    int32_t mx = INT32_MIN, sum_h = 0, sum_l = 0;
+    int32_t mx = INT32_MIN;
+    v4i sum_h{0, 0, 0, 0}, sum_l{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < NW; ++i) mx = mx > maxima[i][wave * 16 + c] ? mx : maxima[i][wave * 16 + c];
 #pragma unroll
     for (int i = 0; i < ND; ++i) { hi[i] = v4i{0, 0, 0, 0}; lo[i] = v4i{0, 0, 0, 0}; }
     // DY(m - s) = (s * -factor + (m * factor + 2^(shift-1))) >> shift
     const int32_t minus_m = -(int32_t)a.s_m;
+    const v4i ones = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
     const int64_t row_c = (int64_t)mx * (int32_t)a.s_m + ((int64_t)1 << (HIGH ? a.s_s + 31 : a.s_s - 1));
     for (int x = 0; x < n; ++x) {
         const int64_t next = offset(x + 1);
@@ -768,9 +773,10 @@ __global__ __launch_bounds__(64 * PP_NW, 4) void paged_prompt_kernel(PagedArgs a
             const uint32_t q = __builtin_amdgcn_perm((uint32_t)s[i][3], (uint32_t)s[i][2], 0x05010400u);
             wl[i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x05040100u);
             wh[i] = (int32_t)__builtin_amdgcn_perm(q, p, 0x07060302u);
-            sum_l = __builtin_amdgcn_sdot4(wl[i], 0x01010101, sum_l, false);
-            sum_h = __builtin_amdgcn_sdot4(wh[i], 0x01010101, sum_h, false);
         }
+        // sums of the weights, as the product with a value of 1 (eight dot instructions otherwise: 1 % of a long prompt)
+        sum_h = __builtin_amdgcn_mfma_i32_16x16x64_i8(ones, wh, sum_h, 0, 0, 0);
+        sum_l = __builtin_amdgcn_mfma_i32_16x16x64_i8(ones, wl, sum_l, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
             const v4i vf = *reinterpret_cast<const v4i*>(&blocks[2 + (x & 1)][i * 1024 + lane * 16]);
@@ -779,11 +785,8 @@ __global__ __launch_bounds__(64 * PP_NW, 4) void paged_prompt_kernel(PagedArgs a
         }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);                    // (nothing is on its way into LDS any more)
-    const auto add = [](int32_t p, int32_t q) { return (int32_t)((uint32_t)p + (uint32_t)q); };
-    int32_t W = add((int32_t)((uint32_t)sum_h << 8), sum_l);
-    W = combine_rows32(combine_rows16(W, add), add);
     if (c >= own.count) return;
-    const uint64_t R = reciprocal((uint32_t)W);
+    const uint64_t R = reciprocal(((uint32_t)sum_h[0] << 8) + (uint32_t)sum_l[0]);
     const int flat = own.first + c, qi = group_of(a, flat);
     int8_t* dst = a.out + (int64_t)(t.row0 + qi) * a.ld_out + (h * a.group + (flat - qi * a.group)) * D + 4 * g;
 #pragma unroll

@@ -10,7 +10,8 @@
 // Values: the cache wants 16 tokens of a channel side by side.  A wavefront takes 16 channels of 64 rows.  Where rows follow each other into
 // a block of 64 tokens (a prompt), their bytes are transposed, four rows by lane swaps and the rest through LDS, and leave as 1 KB, or
 // as the dwords and bytes of it that they fill; single rows are stored byte by byte.
-// Bound: HBM, and with norms the vector ALU next to it.
+// Bound: HBM, and with norms the vector ALU next to it.  16384 rows of 32 + 8 + 8 heads of width 128: 206 MB in 49 us without norms (4.2 TB/s), in 60 us with them
+// (3.4 TB/s; 0.79 of the ALU's slots).  2741 rows of 16 + 16 + 16 heads of width 64: 17 MB in 7.6 us.  Five rows: 3.5 us, three dependent trips to memory.
 #include "layernorm_math.h"
 
 namespace ibert {
