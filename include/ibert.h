@@ -532,7 +532,8 @@ int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* c
  * q: device int8 [rows, ld_q]; out: device int8 [rows, ld_out]; block_table: device int32 [batch, max_pages]; q_start: device int32
  * [batch + 1], ascending; kv_len: device int32 [batch].  Lengths are clamped into [0, min(max_kv_len, max_pages *
  * page_size)], page numbers into the cache, q_start into [0, rows]; rows of no sequence, and rows of a sequence beyond its
- * first max_q_len, are left as they were.  max_q_len, max_kv_len: bounds of the batch that the host knows; they size the launch and the workspace.
+ * first max_q_len, are left as they were.  max_q_len, max_kv_len: bounds of the batch that the host knows; they size the launch and the workspace, and say with
+ * rows whether single rows stand among prompts, which are then worked on apart.
  * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes for the same arguments (smaller bounds may ask for
  * more; else IBERT_ERR_WORKSPACE; may be NULL where that is 0); calls that may overlap in time need one each.
  * Preconditions: max_kv_len <= 131072 and scores_dy.m >= 0, its shift in [24, 62], out_dy's in [0, 62], window, sinks >= 0

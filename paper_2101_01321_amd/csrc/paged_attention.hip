@@ -23,6 +23,8 @@ struct PagedArgs {
     int64_t ld_q, ld_out;
     int32_t heads_q, heads_kv, group, log_page, num_pages, max_pages, rows, max_q, keys;   // keys: most that a sequence can have
     int32_t window, sinks;
+    int32_t only;              // 1: the sequences of one row, 2: the others, 0: all
+    int32_t packed;            // sequences, where the prompt kernel's workgroups find theirs by counting; else 0
     uint32_t group_magic, s_m;
     int32_t s_l, s_r;          // DY(d) = (((uint64)(d << s_l) * s_m + s_rnd) >> 32) >> s_r
     uint64_t s_rnd;
@@ -52,11 +54,13 @@ __device__ __forceinline__ Tile tile_of(const PagedArgs& a, int b, int tile, int
         r1 = clamp_i32(a.q_start[b + 1], r0, a.rows);
     }
     t.row0 = r0; t.n = r1 - r0;
+    const bool skip = a.only && (a.only == 1) != (t.n == 1);
     t.kv = clamp_i32(a.kv_len[b], 0, a.keys);
     t.pos0 = t.kv - t.n;
     t.first = tile * tile_rows;
     const int64_t left = (int64_t)(t.n < a.max_q ? t.n : a.max_q) * a.group - t.first;
     t.count = left < tile_rows ? (int32_t)(left < 0 ? 0 : left) : tile_rows;
+    if (skip) t.count = 0;
     t.low = t.pos0 + group_of(a, t.first);
     t.high = t.pos0 + group_of(a, t.first + (t.count > 0 ? t.count - 1 : 0));
     const int32_t end = t.high < 0 ? 0 : (t.high >> 6) + 1;
@@ -587,6 +591,33 @@ __device__ __forceinline__ Tile part_of(const PagedArgs& a, const Tile& t, int f
     p.high = p.count > 0 ? t.pos0 + group_of(a, p.first + p.count - 1) : -1;
     return p;
 }
+// The sequence and the tile of PP_ROWS rows that are the index-th of all there are; false: not so many.  A wavefront takes 64 sequences at a time.
+__device__ __forceinline__ bool packed_tile(const PagedArgs& a, int32_t index, int& b, int& tile)
+{
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.packed; b0 += 64) {
+        int32_t mine = 0;
+        if (b0 + lane < a.packed) {
+            const int32_t r0 = clamp_i32(a.q_start[b0 + lane], 0, a.rows), n = clamp_i32(a.q_start[b0 + lane + 1], r0, a.rows) - r0;
+            if (!a.only || n != 1) mine = ((n < a.max_q ? n : a.max_q) * a.group + PP_ROWS - 1) / PP_ROWS;
+        }
+        int32_t sum = mine;
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) {
+            const int32_t before = __shfl_up(sum, i);
+            sum += lane >= i ? before : 0;
+        }
+        const uint64_t beyond = __builtin_amdgcn_ballot_w64(sum > index);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond);
+            b = b0 + at;
+            tile = __builtin_amdgcn_readlane(sum, at) - 1 - index;           // (a sequence's last tile, which has most keys, first)
+            return true;
+        }
+        index -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
 // How many of the workgroup's blocks some row of the part may see (the others come last).
 __device__ __forceinline__ int blocks_of(const Tile& p)
 {
@@ -683,8 +714,10 @@ __global__ __launch_bounds__(64 * PP_NW, 4) void paged_prompt_kernel(PagedArgs a
     __shared__ uint16_t table[PP_TABLE];
     __shared__ int32_t maxima[NW][PP_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    const int h = blockIdx.x, b = blockIdx.z;
-    const Tile t = tile_of(a, b, gridDim.y - 1 - blockIdx.y, PP_ROWS);        // (the rows with most keys first)
+    const int h = blockIdx.x;
+    int b = blockIdx.z, tile = gridDim.y - 1 - blockIdx.y;                   // (the rows with most keys first)
+    if (a.packed && !packed_tile(a, blockIdx.y, b, tile)) return;
+    const Tile t = tile_of(a, b, tile, PP_ROWS);
     if (t.count == 0) return;
     const int n = t.blocks;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)&blocks[0][0];
@@ -868,11 +901,25 @@ static Plan plan_paged(const ibert_paged_attention_desc& d, const ibert_kv_cache
     return p;
 }
 
+// Single rows among prompts (a step of a server): the prompt kernel walks a single row's keys with one workgroup a key head.  Where the others have a sixteenth of the
+// longest's rows on average, sequences of one row go by a plan of their own, and the prompt kernel leaves them out.  us, together / apart, 8 key heads of width 128 with 4
+// queries each, single rows on 2000 keys and a prompt: 63 and 512 rows 110 / 62, 15 and 512 50 / 34, 63 (4000 keys) and 2048 272 / 157, 1 (60000 keys) and 1024 755 / 59.  Not
+// where prompts are short or many: 15 rows on 500 keys and 40 rows 18 / 23, 180 on 800 and 20 prompts of 100 115 / 138, 8 of 8 to 500 rows 19 / 21.
+static bool is_mixed(const ibert_paged_attention_desc& d, const ibert_kv_cache& c, const Plan& plan, int32_t batch, int32_t rows, int32_t max_q_len)
+{
+    return g_paged_form < 0 && plan.prompt_tiles > 0 && batch > 1 && (int64_t)max_q_len * (d.heads_q / c.heads_kv) >= 512 &&
+           (int64_t)rows - max_q_len <= (int64_t)(batch - 1) * max_q_len / 16;
+}
+
 template <int D>
-static int launch_paged(const PagedArgs& a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
+static int launch_paged(PagedArgs a, const Plan& plan, int32_t batch, void* workspace, hipStream_t stream)
 {
     if (plan.prompt_tiles > 0) {
-        const dim3 grid((unsigned)a.heads_kv, (unsigned)plan.prompt_tiles, (unsigned)batch), block(64 * PP_NW);
+        // At most so many tiles have rows.  Where the grid would be four times that, tiles are counted instead: a workgroup without rows costs some 0.5 ns, and 64 x 2048 rows
+        // of which 2111 are there, 190 us with them, 157 without.
+        const int64_t filled = (int64_t)a.rows * a.group / PP_ROWS + (batch < a.rows ? batch : a.rows);
+        a.packed = a.q_start && filled <= 65535 && 4 * filled <= (int64_t)batch * plan.prompt_tiles ? batch : 0;
+        const dim3 grid((unsigned)a.heads_kv, (unsigned)(a.packed ? filled : plan.prompt_tiles), (unsigned)(a.packed ? 1 : batch)), block(64 * PP_NW);
         if (plan.high) hipLaunchKernelGGL((paged_prompt_kernel<D, true>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((paged_prompt_kernel<D, false>), grid, block, 0, stream, a);
         IBERT_LAUNCH_CHECK("paged_prompt_kernel");
@@ -933,7 +980,9 @@ extern "C" size_t ibert_paged_attention_workspace_bytes(const ibert_paged_attent
                                                         int32_t rows, int32_t max_q_len, int32_t max_kv_len)
 {
     if (ibert::check_paged(desc, cache, batch, rows, max_q_len, max_kv_len)) return 0;
-    return ibert::plan_paged(*desc, *cache, batch, max_q_len, max_kv_len).total;
+    const ibert::Plan plan = ibert::plan_paged(*desc, *cache, batch, max_q_len, max_kv_len);
+    if (ibert::is_mixed(*desc, *cache, plan, batch, rows, max_q_len)) return ibert::plan_paged(*desc, *cache, batch, 1, max_kv_len).total;
+    return plan.total;
 }
 
 extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, const ibert_kv_cache* cache, const int8_t* q, int64_t ld_q,
@@ -949,7 +998,9 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     if (batch == 0 || rows == 0) return IBERT_OK;
     if (!q || !out || !block_table || !kv_len || !cache->k || !cache->v) return IBERT_ERR_NULL;
     if (!aligned(q, 16) || ld_q % 16 || !aligned(out, 4) || ld_out % 4 || !aligned(cache->k, 16) || !aligned(cache->v, 16)) return IBERT_ERR_ALIGN;
-    const Plan plan = plan_paged(d, *cache, batch, max_q_len, max_kv_len);
+    const Plan prompts = plan_paged(d, *cache, batch, max_q_len, max_kv_len);
+    const bool mixed = is_mixed(d, *cache, prompts, batch, rows, max_q_len);
+    const Plan plan = mixed ? plan_paged(d, *cache, batch, 1, max_kv_len) : prompts;
     if (plan.total > 0 && (!workspace || workspace_bytes < plan.total || !aligned(workspace, 256))) return IBERT_ERR_WORKSPACE;
     PagedArgs a;
     a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.table = block_table; a.q_start = q_start; a.kv_len = kv_len;
@@ -963,7 +1014,11 @@ extern "C" int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, c
     const int s = d.scores_dy.s;
     a.s_m = (uint32_t)d.scores_dy.m; a.s_l = s < 32 ? 32 - s : 0; a.s_r = s > 32 ? s - 32 : 0; a.s_rnd = (uint64_t)1 << (s < 32 ? 31 : s - 1);
     a.s_s = s >= 32 ? s - 32 : s;
-    a.out_dy = d.out_dy;
+    a.out_dy = d.out_dy; a.only = mixed;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return D == 64 ? launch_paged<64>(a, plan, batch, workspace, st) : launch_paged<128>(a, plan, batch, workspace, st);
+    const auto launch = [&](const Plan& p) { return D == 64 ? launch_paged<64>(a, p, batch, workspace, st) : launch_paged<128>(a, p, batch, workspace, st); };
+    const int rc = launch(plan);
+    if (rc || !mixed) return rc;
+    a.only = 2;
+    return launch(prompts);
 }

@@ -456,6 +456,47 @@ def test_attention_of_many_sequences(gpu):
     check_attention(U.Attention(39, 2, 1, 64, 64, n, rng.integers(0, 150, 300)))
 
 
+@pytest.mark.parametrize("batch,heads,D,window,sinks", [(64, 2, 64, 0, 0), (65, 2, 64, 0, 0), (32, 4, 128, 0, 0), (33, 4, 128, 0, 0), (33, 4, 128, 130, 70), (16, 4, 128, 130, 70)])
+def test_attention_on_both_sides_of_a_workgroup_a_unit(gpu, batch, heads, D, window, sinks):
+    # two tiles of rows each: 256 workgroups and a few more, ways of no block up to more than twice eight
+    rng = np.random.default_rng(batch + D)
+    n = rng.integers(0, 18, batch)
+    n[0] = 17
+    check_attention(U.Attention(40 + batch, heads, heads, D, 64, n, rng.integers(0, 1300, batch), window, sinks))
+
+
+@pytest.mark.parametrize("n,kv,hq,hk,D,kernel", [
+    ([16], [4000], 32, 8, 128, "paged_attention_kernel"), ([4], [4000], 32, 8, 128, "paged_join_kernel"), ([16] * 12, [4000] * 12, 16, 16, 64, "paged_attention_kernel"),
+    ([20] * 30, [1000] * 30, 12, 12, 64, "paged_attention_kernel"), ([40] * 30, [1000] * 30, 12, 12, 64, "paged_prompt_kernel"),
+    ([5] * 40, [2000] * 40, 32, 8, 128, "paged_prompt_kernel"), ([5] * 40, [600] * 40, 32, 8, 128, "paged_attention_kernel")])
+def test_attention_rules_for_few_rows(gpu, n, kv, hq, hk, D, kernel):
+    torch, G, B = libs()
+    case = U.Attention(61, hq, hk, D, 64, n, kv)
+    G.say("attention by rule: %s" % kernel)
+    d = DeviceAttention(case)
+    d.call()
+    d.result()
+    assert B.lib().ibert_last_kernel().decode().startswith(kernel)
+
+
+@pytest.mark.parametrize("n,kv,hq,hk,D,window,sinks,kernel", [
+    # one prompt among single rows that take one launch, three, or the scores twice; sequences of no and of two rows among them; a window
+    ([1] * 20 + [600] + [1] * 10, [700] * 20 + [600] + [0, 1, 64, 65, 300, 5, 128, 129, 1000, 900], 8, 2, 128, 0, 0, "paged_prompt_kernel"),
+    ([1, 0, 2, 1500, 1, 1, 3, 1] + [0] * 12, [9000, 70, 80, 1600, 1, 0, 2, 5000] + [10] * 12, 8, 2, 128, 0, 0, "paged_prompt_kernel"),
+    ([1] * 30 + [700] + [1] * 34, [3000] * 30 + [900] + [2500] * 34, 16, 1, 128, 0, 0, "paged_prompt_kernel"),
+    ([700] + [1] * 20, [900] + [2100] * 20, 12, 12, 64, 333, 5, "paged_prompt_kernel"),
+    ([1] * 24 + [520], [100] * 24 + [520], 24, 4, 64, 0, 0, "paged_prompt_kernel")])
+def test_attention_of_single_rows_among_prompts(gpu, n, kv, hq, hk, D, window, sinks, kernel):
+    torch, G, B = libs()
+    case = U.Attention(70 + hq, hq, hk, D, 64, n, kv, window, sinks, pad=5)
+    G.say("single rows among prompts: %d sequences, %d rows" % (case.batch, case.rows))
+    d, want = check_attention(case)
+    for _ in range(2):
+        d.call()
+        same(d.result(), want, "out")
+    assert B.lib().ibert_last_kernel().decode().startswith(kernel)
+
+
 # ------------------------------------------------------------------------------------------- graphs and streams
 def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
     torch, G, B = libs()
