@@ -35,6 +35,9 @@ struct PagedArgs {
 // Query of the flat row n.
 __device__ __forceinline__ int32_t group_of(const PagedArgs& a, int32_t n) { return udiv_fix(n, a.group, a.group_magic); }
 
+// Is a sequence of n rows one that this launch leaves to another?
+__device__ __forceinline__ bool left_out(const PagedArgs& a, int32_t n) { return a.only && (a.only == 1) != (n == 1); }
+
 // What one workgroup works on: 16 rows of one sequence and key head.
 struct Tile {
     int32_t row0, n;           // first query row of the sequence in q; its queries
@@ -54,13 +57,12 @@ __device__ __forceinline__ Tile tile_of(const PagedArgs& a, int b, int tile, int
         r1 = clamp_i32(a.q_start[b + 1], r0, a.rows);
     }
     t.row0 = r0; t.n = r1 - r0;
-    const bool skip = a.only && (a.only == 1) != (t.n == 1);
     t.kv = clamp_i32(a.kv_len[b], 0, a.keys);
     t.pos0 = t.kv - t.n;
     t.first = tile * tile_rows;
     const int64_t left = (int64_t)(t.n < a.max_q ? t.n : a.max_q) * a.group - t.first;
     t.count = left < tile_rows ? (int32_t)(left < 0 ? 0 : left) : tile_rows;
-    if (skip) t.count = 0;
+    if (left_out(a, t.n)) t.count = 0;
     t.low = t.pos0 + group_of(a, t.first);
     t.high = t.pos0 + group_of(a, t.first + (t.count > 0 ? t.count - 1 : 0));
     const int32_t end = t.high < 0 ? 0 : (t.high >> 6) + 1;
@@ -599,7 +601,7 @@ __device__ __forceinline__ bool packed_tile(const PagedArgs& a, int32_t index, i
         int32_t mine = 0;
         if (b0 + lane < a.packed) {
             const int32_t r0 = clamp_i32(a.q_start[b0 + lane], 0, a.rows), n = clamp_i32(a.q_start[b0 + lane + 1], r0, a.rows) - r0;
-            if (!a.only || n != 1) mine = ((n < a.max_q ? n : a.max_q) * a.group + PP_ROWS - 1) / PP_ROWS;
+            if (!left_out(a, n)) mine = ((n < a.max_q ? n : a.max_q) * a.group + PP_ROWS - 1) / PP_ROWS;
         }
         int32_t sum = mine;
 #pragma unroll

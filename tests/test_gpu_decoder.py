@@ -497,6 +497,16 @@ def test_attention_of_single_rows_among_prompts(gpu, n, kv, hq, hk, D, window, s
     assert B.lib().ibert_last_kernel().decode().startswith(kernel)
 
 
+def test_attention_of_single_rows_in_a_batch_that_is_mostly_empty(gpu):
+    # the single rows' heads are tiles of prompts themselves, and counted; with and without a longer sequence among them
+    rng = np.random.default_rng(80)
+    for longest in (20, 2):
+        n = np.zeros(400, np.int64)
+        n[rng.permutation(400)[:30]] = 1
+        n[137] = longest
+        check_attention(U.Attention(80 + longest, 40, 1, 64, 64, n, rng.integers(0, 200, 400)), max_q=20)
+
+
 # ------------------------------------------------------------------------------------------- graphs and streams
 def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
     torch, G, B = libs()
