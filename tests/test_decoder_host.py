@@ -276,3 +276,17 @@ def test_paged_attention_refuses():
         for kw in (dict(), dict(workspace=DUMMY, ws=need - 1), dict(workspace=DUMMY + 16, ws=need)):
             assert call(c=big, batch=1, rows=1, width=4096, max_kv=131072, ld_q=512, ld_out=512, **kw) == -5, kw
     assert B.ibert_paged_attention_workspace_bytes(d, cache(), 1, 1, 0, 100) == 0
+
+
+def test_single_rows_among_prompts_ask_for_the_room_of_single_rows():
+    d = B.PagedAttentionDesc(32, 0, 0, B.Dyadic(1, 30), B.Dyadic(1, 16))
+    c = cache(heads_kv=8, num_pages=100000, head_dim=128)
+
+    def need(batch, rows, max_q, max_kv):
+        return B.ibert_paged_attention_workspace_bytes(d, c, batch, rows, max_q, max_kv)
+    singles = need(3, 3, 1, 60000)
+    assert singles > 0
+    assert need(3, 1026, 1024, 60000) == singles                       # one prompt, two single rows
+    assert need(3, 3 * 1024, 1024, 60000) == 0                         # three prompts
+    assert need(2, 41, 40, 500) == need(2, 80, 40, 500) == 0           # short ones
+    assert B.lib().ibert_paged_attention_i(C.byref(d), C.byref(c), DUMMY, 4096, DUMMY, 1000, DUMMY, DUMMY, 3, 1026, 1024, 60000, DUMMY, 4096, None, 0, None) == -5
