@@ -62,6 +62,10 @@ int ibert_layernorm_i16_plan(int64_t rows, int32_t C, int32_t shift, int32_t* ro
 enum { IBERT_PAGED_TWICE = 0, IBERT_PAGED_ONE = 1, IBERT_PAGED_SPLIT = 2, IBERT_PAGED_PROMPT = 3 };
 void ibert_paged_attention_override(int32_t form);
 
+/* Heads of a row that a team of lanes of ibert_rotary_append_i takes one after the other, where heads are 128 wide and rot_dim is a multiple of 32 (elsewhere one): 1 or 2;
+ * negative: what is faster for the rows (the default).  The result never depends on it.  Process-wide, not thread-safe. */
+void ibert_rotary_override(int32_t heads);
+
 /* Steps 1 to 4 of a layer as one kernel: 0 never; a tile (1000 wavefronts + 100 MFMA rows of one + 10 sequences + stages, one of those ibert_qkv_attention_plan names)
  * wherever its rows hold a sequence and the parameters allow it; negative where it is the faster way (the default).  Process-wide, not thread-safe. */
 void ibert_qkv_attention_override(int32_t tile);

@@ -171,6 +171,7 @@ SIGNATURES = {
     "ibert_layernorm_params_from_float": (C.c_int, [_P, _P, C.c_int32, C.c_double, _P, _P, C.POINTER(C.c_int32)]),
     "ibert_layer_quant_from_scales": (C.c_int, [C.POINTER(LayerScales), C.c_int32, C.c_int32, C.POINTER(LayerQuant)]),
     "ibert_paged_attention_override": (None, [C.c_int32]),
+    "ibert_rotary_override": (None, [C.c_int32]),
     "ibert_kv_cache_bytes": (C.c_size_t, [C.POINTER(KvCache)]),
     "ibert_page_tables_i": (C.c_int, [_P, _P] + [C.c_int32] * 3 + [_P] * 4 + [C.c_int32] * 2 + [_P] * 5),
     "ibert_rotary_append_i": (C.c_int, [C.POINTER(RotaryDesc), C.POINTER(KvCache), _P, C.c_int64] + [_P] * 5 +
@@ -467,6 +468,10 @@ PAGED_TWICE, PAGED_ONE, PAGED_SPLIT, PAGED_PROMPT = 0, 1, 2, 3
 
 def ibert_paged_attention_override(form: int):
     lib().ibert_paged_attention_override(form)
+
+
+def ibert_rotary_override(heads: int):
+    lib().ibert_rotary_override(heads)
 
 
 def ibert_kv_cache_bytes(cache: KvCache) -> int:

@@ -13,6 +13,7 @@
 // Bound: HBM, and with norms the vector ALU next to it.  16384 rows of 32 + 8 + 8 heads of width 128: 206 MB in 49 us without norms (4.2 TB/s), in 60 us with them
 // (3.4 TB/s; 0.79 of the ALU's slots).  2741 rows of 16 + 16 + 16 heads of width 64: 17 MB in 7.6 us.  Five rows: 3.5 us, three dependent trips to memory.
 #include "layernorm_math.h"
+#include "ibert_testing.h"
 
 namespace ibert {
 
@@ -300,21 +301,26 @@ static int launch_rotary(RotaryArgs& a, hipStream_t stream)
     a.wgs[2] = (int32_t)((a.rows + 63) / 64 * a.heads_kv);
     hipLaunchKernelGGL((rotary_append_kernel<D, INTERLEAVED, P, NH>), dim3((unsigned)(a.wgs[0] + a.wgs[1] + a.wgs[2])), dim3(RO_THREADS), 0, stream, a);
     IBERT_LAUNCH_CHECK("rotary_append_kernel");
-    g_last_kernel = "rotary_append_kernel";
+    static const KernelName name("rotary_append_kernel<%d, %s, %d, %d>", D, INTERLEAVED ? "true" : "false", P, NH);
+    g_last_kernel = name.text;
     return IBERT_OK;
 }
+
+static int g_rotary_heads = -1;         // see ibert_rotary_override
 
 template <int D>
 static int launch_rotary(RotaryArgs& a, bool interleaved, hipStream_t stream)
 {
     if (a.rot % 32) return interleaved ? launch_rotary<D, true, 8, 1>(a, stream) : launch_rotary<D, false, 8, 1>(a, stream);
     if constexpr (D == 128) {
-        if (a.rows * a.heads_q >= RO_TEAM_HEADS) return interleaved ? launch_rotary<D, true, 16, 2>(a, stream) : launch_rotary<D, false, 16, 2>(a, stream);
+        if (g_rotary_heads < 0 ? a.rows * a.heads_q >= RO_TEAM_HEADS : g_rotary_heads == 2) return interleaved ? launch_rotary<D, true, 16, 2>(a, stream) : launch_rotary<D, false, 16, 2>(a, stream);
     }
     return interleaved ? launch_rotary<D, true, 16, 1>(a, stream) : launch_rotary<D, false, 16, 1>(a, stream);
 }
 
 }  // namespace ibert
+
+extern "C" void ibert_rotary_override(int32_t heads) { ibert::g_rotary_heads = heads; }
 
 extern "C" int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* cache, const int8_t* qkv, int64_t ld_qkv,
                                      const int16_t* table, const int32_t* positions, const int32_t* slots, const int32_t* q_gamma,

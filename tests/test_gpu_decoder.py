@@ -176,6 +176,51 @@ def test_rotary_append_of_many_rows(gpu):
             same(got, want, what)
 
 
+TEAMS = ROTARY + [  # the same, of heads of 128 whose pieces are whole: odd numbers of heads, one norm, none or a part rotated, rows that leave the last workgroup partly filled
+    (67, 7, 1, 128, 128, False, 64, True, False, 16, (0, 5, 66)), (129, 9, 3, 128, 64, True, 128, False, True, 0, ()), (257, 5, 5, 128, 32, False, 64, True, True, 32, range(0, 257, 9)),
+    (63, 3, 3, 128, 0, False, 64, False, False, 0, ()), (95, 15, 5, 128, 96, True, 256, True, True, 0, (94,)), (1, 1, 1, 128, 96, False, 64, True, True, 0, ()),
+    (2, 2, 2, 128, 128, True, 64, False, False, 0, (1,)), (65, 33, 11, 128, 128, True, 64, True, False, 0, ()), (40, 64, 2, 128, 64, False, 64, False, True, 48, ())]
+
+
+@pytest.mark.parametrize("args", TEAMS, ids=lambda a: "t%d_q%d_k%d_d%d_r%d_%s_n%d%d" % (a[0], a[1], a[2], a[3], a[4], "il" if a[5] else "half", a[7], a[8]))
+def test_rotary_append_of_one_and_two_heads_a_team(gpu, args):
+    torch, G, B = libs()
+    rows, hq, hk, D, R, inter, page, qn, kn, ld, skip = args
+    case = U.Rotary(rows + R + 1, rows, hq, hk, D, R, inter, page, qn, kn, ld, skip)
+    # heads whose roots are far apart beside each other: nothing, one unit, the most there is
+    case.qkv[0, D:2 * D] = 0
+    case.qkv[0, 2 * D - 1] = 1
+    case.qkv[rows // 2, :D] = -128
+    want = case.oracle()
+    for heads in (1, 2):
+        G.say("rotary %s, %d heads a team" % (args, heads))
+        B.ibert_rotary_override(heads)
+        try:
+            got = run_rotary(case)
+        finally:
+            B.ibert_rotary_override(-1)
+        assert B.lib().ibert_last_kernel().decode().endswith(", %d>" % (heads if D == 128 and R % 32 == 0 else 1))
+        for g, w, what in zip(got, want, "qkv"):
+            same(g, w, "%s, %d heads a team" % (what, heads))
+
+
+@pytest.mark.parametrize("rows,hq,hk,R,inter,qn,kn,heads", [
+    (8192, 32, 8, 128, False, True, True, 2), (8191, 32, 8, 128, True, True, True, 1), (37450, 7, 1, 64, True, True, False, 2), (29128, 9, 3, 32, False, False, True, 2),
+    (20165, 13, 1, 0, False, False, False, 2), (2033, 129, 1, 96, False, True, True, 2), (16384, 16, 4, 112, False, False, True, 1)])
+def test_rotary_append_by_its_rule_for_many_rows(gpu, rows, hq, hk, R, inter, qn, kn, heads):
+    # on both sides of 262144 heads of queries; half of the rows in runs as a prompt has them, the others anywhere, some without a slot
+    torch, G, B = libs()
+    case = U.Rotary(rows + hq, rows, hq, hk, 128, R, inter, 64, qn, kn, 16, range(5, rows, 997))
+    free = np.setdiff1d(np.arange(case.pages * 64, dtype=np.int32), case.slots[rows // 2:])
+    run = case.slots[:rows // 2] >= 0
+    case.slots[:rows // 2][run] = free[:int(run.sum())]
+    G.say("rotary by rule: %d rows, %d + %d heads, R %d" % (rows, hq, hk, R))
+    got = run_rotary(case)
+    assert B.lib().ibert_last_kernel().decode().endswith(", %d>" % heads)
+    for g, w, what in zip(got, case.oracle(), "qkv"):
+        same(g, w, what)
+
+
 # ------------------------------------------------------------------------------------------- attention
 class DeviceAttention:
     def __init__(self, case, max_q=None, max_kv=None, plain_rows=False):
