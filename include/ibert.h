@@ -469,11 +469,11 @@ size_t ibert_kv_cache_bytes(const ibert_kv_cache* cache);
  * head on, and pages that come back stand behind the count.  ring_out = {head, count, sequences not granted} afterwards (pages that come
  * back are taken by a later call).
  * Pointers: device int32; len_before, len_after, kv_len [batch], q_start [batch + 1], block_table [batch, max_pages],
- * free_ring [num_pages], ring_in [2], ring_out [3], slots, positions [rows].  What is written must not be one of the
- * other arrays (ring_out is not ring_in, kv_len neither of the two lengths): programs keep two of each and swap them.
+ * free_ring [num_pages], ring_in [2], ring_out [3], slots, positions [rows].  What is written must not overlap
+ * another of the arrays (ring_out not ring_in, kv_len neither of the two lengths): programs keep two of each and swap them.
  * Values of ring_in outside [0, num_pages) / [0, num_pages] are clamped into it.
  * Errors: IBERT_ERR_SHAPE (batch outside [0, 8192], page_size no 64 * 2^i, num_pages or max_pages < 1, rows < 0,
- * num_pages * page_size or max_pages * page_size or batch * max_pages >= 2^31, an output that is its input), IBERT_ERR_NULL.
+ * num_pages * page_size or max_pages * page_size or batch * max_pages >= 2^31, a written array that overlaps another), IBERT_ERR_NULL.
  * ---------------------------------------------------------------------------------------------- */
 int ibert_page_tables_i(const int32_t* len_before, const int32_t* len_after, int32_t batch, int32_t page_size,
                         int32_t num_pages, const int32_t* ring_in, int32_t* free_ring, int32_t* ring_out,

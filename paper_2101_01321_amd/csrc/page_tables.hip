@@ -195,7 +195,17 @@ extern "C" int ibert_page_tables_i(const int32_t* len_before, const int32_t* len
     if (!ring_in || !free_ring || !ring_out || !q_start) return IBERT_ERR_NULL;
     if (batch > 0 && (!len_before || !len_after || !block_table || !kv_len)) return IBERT_ERR_NULL;
     if (rows > 0 && (!slots || !positions)) return IBERT_ERR_NULL;
-    if (ring_in == ring_out || (batch > 0 && (kv_len == len_before || kv_len == len_after))) return IBERT_ERR_SHAPE;
+    // (workgroups read what the inputs were while others write: no written array may share a word with another)
+    const int64_t n = batch, r = rows;
+    const struct { const int32_t* p; int64_t words; } arrays[] = {
+        {free_ring, num_pages}, {ring_out, 3}, {block_table, n * max_pages}, {q_start, n + 1}, {kv_len, n}, {slots, r}, {positions, r},        // written
+        {len_before, n}, {len_after, n}, {ring_in, 2}};
+    for (int w = 0; w < 7; ++w)
+        for (int o = w + 1; o < 10; ++o) {
+            const auto &x = arrays[w], &y = arrays[o];
+            const uintptr_t px = reinterpret_cast<uintptr_t>(x.p), py = reinterpret_cast<uintptr_t>(y.p);
+            if (x.words > 0 && y.words > 0 && px < py + 4 * (uint64_t)y.words && py < px + 4 * (uint64_t)x.words) return IBERT_ERR_SHAPE;
+        }
     ibert::PageArgs a;
     a.before = len_before; a.after = len_after; a.ring_in = ring_in;
     a.ring = free_ring; a.ring_out = ring_out; a.table = block_table; a.q_start = q_start; a.kv_len = kv_len; a.slots = slots; a.positions = positions;

@@ -290,3 +290,21 @@ def test_single_rows_among_prompts_ask_for_the_room_of_single_rows():
     assert need(3, 3 * 1024, 1024, 60000) == 0                         # three prompts
     assert need(2, 41, 40, 500) == need(2, 80, 40, 500) == 0           # short ones
     assert B.lib().ibert_paged_attention_i(C.byref(d), C.byref(c), DUMMY, 4096, DUMMY, 1000, DUMMY, DUMMY, 3, 1026, 1024, 60000, DUMMY, 4096, None, 0, None) == -5
+
+
+def test_page_tables_refuse_what_overlaps():
+    # every written array with every other: the same address, and the last word of one on the first of the other
+    batch, num, width, rows = 3, 10, 4, 5
+    words = dict(ring=num, ring_out=3, table=batch * width, q_start=batch + 1, kv_len=batch, slots=rows, positions=rows, before=batch, after=batch, ring_in=2)
+    written = ("ring", "ring_out", "table", "q_start", "kv_len", "slots", "positions")
+
+    def call(batch=batch, rows=rows, **kw):
+        p = {k: 1 << 20 | 4096 * i for i, k in enumerate(words)}
+        p.update(kw)
+        return B.lib().ibert_page_tables_i(p["before"], p["after"], batch, 64, num, p["ring_in"], p["ring"], p["ring_out"], p["table"], width, rows, p["q_start"], p["kv_len"],
+                                           p["slots"], p["positions"], None)
+    for w in written:
+        for o in words:
+            if o != w:
+                for at in (0, 4 * (words[o] - 1), -4 * (words[w] - 1)):
+                    assert call(**{o: 1 << 24, w: (1 << 24) + at}) == -2, (w, o, at)
