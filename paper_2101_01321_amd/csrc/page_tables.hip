@@ -18,13 +18,9 @@ struct PageArgs {
     int32_t batch, log_page, num_pages, max_pages, rows;
 };
 
-// Sums of what is asked for may pass 32 bits: they stop at 2^31 - 1, above everything they are compared with.  (Addition that
-// stops there is associative, so a scan may group it as it likes.)
-__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b)
-{
-    const uint32_t s = a + b;
-    return s > 0x7fffffffu ? 0x7fffffffu : s;
-}
+// Sums of what is asked for may pass 32 bits: they stop at 2^32 - 1, above everything they are compared with (rows and pages,
+// at most 2^31 - 1).  (Addition that stops there is associative, so a scan may group it as it likes.)
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
 // The value some lanes before this one in its row of 16 (or the last of the rows before it), 0 where there is none.
 template <int CTRL, int ROWS>

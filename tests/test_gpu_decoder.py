@@ -81,6 +81,24 @@ def test_page_tables(gpu, name, case):
         assert want["ring_out"][2] > 0
 
 
+def test_page_tables_of_the_most_rows_there_can_be(gpu):
+    # 2^31 - 1 rows, and asked for one more: who asked first is refused for want of pages, who asks next, without a page, for want of rows; who asks for none is not
+    torch, G, B = libs()
+    most, i32 = 2 ** 31 - 1, lambda a: torch.tensor(a, dtype=torch.int32, device=G.DEV)     # noqa: E731
+    before, after, ring_in, ring = i32([0, 1, 70, 5]), i32([most, 2, 3, 5]), i32([1, 4]), i32([0, 4, 5, 6, 7, 0, 0, 0])
+    table = i32([[0, 0], [0, 0], [1, 2], [3, 0]])
+    ring_out, q_start, kv_len = i32([77] * 3), i32([77] * 5), i32([77] * 4)
+    slots, positions = (torch.full((most,), 77, dtype=torch.int32, device=G.DEV) for _ in range(2))
+    G.say("page tables: %d rows" % most)
+    B.ibert_page_tables_i(before, after, 4, 64, 8, ring_in, ring, ring_out, table, 2, most, q_start, kv_len, slots, positions)
+    torch.cuda.synchronize()
+    assert ring_out.tolist() == [1, 5, 2] and q_start.tolist() == [0] * 5 and kv_len.tolist() == [0, 1, 3, 5]
+    assert ring.tolist() == [0, 4, 5, 6, 7, 2, 0, 0] and table.tolist() == [[0, 0], [0, 0], [1, 2], [3, 0]]
+    for t, want in ((slots, -1), (positions, 0)):
+        for part in t.split(1 << 28):
+            assert bool((part == want).all())
+
+
 def test_page_tables_clamp_what_the_ring_says(gpu):
     # a head and a count outside the ring are taken as the nearest inside; nothing else is touched
     torch, G, B = libs()
