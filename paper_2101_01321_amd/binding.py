@@ -200,6 +200,12 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("libibert.so is missing: build it with `python -m paper_2101_01321_amd.build` "
                                "(or __graft_entry__.build()); there is no fallback path")
+        # torch brings a HIP runtime of its own.  Loaded first, it serves this library too; loaded second, behind a host helper that
+        # was called before torch was imported, it would be a second runtime in the process, and the first has no device then.
+        try:
+            import torch  # noqa: F401
+        except ImportError:
+            pass                             # (the host helpers need none)
         L = C.CDLL(LIB_PATH)
         for name, (res, args) in SIGNATURES.items():
             fn = getattr(L, name)

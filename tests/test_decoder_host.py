@@ -308,3 +308,15 @@ def test_page_tables_refuse_what_overlaps():
             if o != w:
                 for at in (0, 4 * (words[o] - 1), -4 * (words[w] - 1)):
                     assert call(**{o: 1 << 24, w: (1 << 24) + at}) == -2, (w, o, at)
+
+
+@pytest.mark.parametrize("first", ["B.ibert_rotary_table_from_freqs(np.ones(4), 3)", "B.lib()", "import torch"])
+def test_one_hip_runtime_whatever_is_called_first(first):
+    # a process with torch's runtime and the system's beside it has no device for the second of them
+    import os
+    import subprocess
+    import sys
+    code = ("import numpy as np\nfrom paper_2101_01321_amd import binding as B\n%s\nimport torch\nB.lib()\n"
+            "print(len({line.split()[-1] for line in open('/proc/self/maps') if 'libamdhip64' in line}))" % first)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert subprocess.run([sys.executable, "-c", code], cwd=root, check=True, capture_output=True, text=True).stdout.split() == ["1"]
