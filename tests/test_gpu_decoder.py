@@ -81,6 +81,31 @@ def test_page_tables(gpu, name, case):
         assert want["ring_out"][2] > 0
 
 
+def _pages_of_many_rounds():
+    rng = np.random.default_rng(14)
+    yield "150000 rows of wide pages", U.Pages(20, [0, 5, 1024, 0, 100], [30000, 30005, 31024, 30000, 30100], 1024, extra_rows=300)
+    yield "8.8 million rows, 137500 pages", U.Pages(21, [0] * 20 + [7000], [440000] * 20 + [0], 64, extra_rows=7)
+    yield "no rows, 38998 pages back", U.Pages(22, rng.integers(129 * 64, 130 * 64, 300), np.zeros(300), 64, rows=0)
+    yield "one row, pages back from every other sequence", U.Pages(23, [9000, 64] * 400 + [64], [100, 64] * 400 + [65], 64)
+    yield "three rows for many, pages back", U.Pages(24, [5000, 63] * 700, [0, 65] * 700, 64, rows=3)
+
+
+@pytest.mark.parametrize("name,case", list(_pages_of_many_rounds()), ids=lambda v: v.replace(" ", "_") if isinstance(v, str) else "")
+def test_page_tables_of_more_than_one_round(gpu, name, case):
+    # more rows than 256 workgroups have threads, and more pages than a launch that is sized by few rows has
+    torch, G, B = libs()
+    G.say("page tables: " + name)
+    d = DevicePages(case)
+    for _ in range(2):
+        d.call()
+        torch.cuda.synchronize()
+        want = d.check()
+        if _ == 0:                           # once more from what was there before
+            for k in ("ring", "table"):
+                d.t[k].copy_(torch.from_numpy(getattr(case, k)))
+    assert (want["ring_out"][2] > 0) == name.startswith("three")
+
+
 def test_page_tables_of_the_most_rows_there_can_be(gpu):
     # 2^31 - 1 rows, and asked for one more: who asked first is refused for want of pages, who asks next, without a page, for want of rows; who asks for none is not
     torch, G, B = libs()
