@@ -473,6 +473,39 @@ def test_attention_leaves_rows_beyond_max_q_len(gpu):
         same(d.result(), np.where(seen[:, None], want, case.out), "out")
 
 
+def _rows_beyond_the_bound():
+    rng = np.random.default_rng(81)
+    yield "few", U.Attention(82, 3, 1, 64, 64, [40, 10, 21, 1, 0], [60, 10, 90, 70, 5], pad=3), (1, 7, 20, 30)
+    yield "few, width 128, a window", U.Attention(83, 8, 2, 128, 64, [5, 130, 64, 17], [200, 400, 64, 30], 50, 5), (3, 5, 16, 65, 129)
+    n = np.zeros(200, np.int64)
+    n[rng.permutation(200)[:20]] = rng.integers(100, 200, 20)
+    yield "tiles that are counted", U.Attention(84, 8, 2, 64, 64, n, n + rng.integers(0, 90, 200), pad=4), (131,)
+    n = np.where(rng.random(200) < 0.5, 1, 0)
+    n[[7, 150]], n[60:64] = 500, 90
+    yield "tiles that are counted, single rows apart", U.Attention(85, 8, 2, 64, 64, n, n + rng.integers(0, 300, 200), pad=4), (301, 77)
+    yield "single rows apart", U.Attention(86, 8, 2, 128, 64, [1] * 20 + [600] + [1] * 10, [700] * 20 + [650] + [300] * 10), (333,)
+
+
+@pytest.mark.parametrize("name,case,bounds", list(_rows_beyond_the_bound()), ids=lambda v: v.replace(" ", "_") if isinstance(v, str) else "")
+def test_attention_of_every_form_leaves_rows_beyond_max_q_len(gpu, name, case, bounds):
+    torch, G, B = libs()
+    want = case.oracle()
+    for most in bounds:
+        seen = np.zeros(case.rows, bool)
+        seen[:int(case.n.sum())] = np.concatenate([np.arange(k) < most for k in case.n])
+        for form in (B.PAGED_TWICE, B.PAGED_ONE, B.PAGED_SPLIT, B.PAGED_PROMPT, -1):
+            G.say("attention, %s: at most %d rows of each sequence, form %d" % (name, most, form))
+            B.ibert_paged_attention_override(form)
+            try:
+                d = DeviceAttention(case, max_q=most)
+                d.call()
+                same(d.result(), np.where(seen[:, None], want, case.out), "out, form %d, at most %d" % (form, most))
+            finally:
+                B.ibert_paged_attention_override(-1)
+        if not name.startswith("few"):
+            assert B.lib().ibert_last_kernel().decode().startswith("paged_prompt_kernel")
+
+
 def test_attention_clamps_lengths_and_pages(gpu):
     torch, G, B = libs()
     case = U.Attention(32, 4, 2, 64, 64, [1, 1, 1], [100, 128, 70])
