@@ -320,3 +320,14 @@ def test_one_hip_runtime_whatever_is_called_first(first):
             "print(len({line.split()[-1] for line in open('/proc/self/maps') if 'libamdhip64' in line}))" % first)
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     assert subprocess.run([sys.executable, "-c", code], cwd=root, check=True, capture_output=True, text=True).stdout.split() == ["1"]
+
+
+@pytest.mark.parametrize("hq,hk,D,batch,rows,max_q,max_kv", [(4, 2, 128, 1, 1, 1, 131072), (12, 12, 64, 1, 1, 1, 4000), (32, 8, 128, 1, 4, 4, 20000), (32, 8, 128, 3, 1026, 1024, 60000)])
+def test_a_workspace_that_does_not_do_is_refused(hq, hk, D, batch, rows, max_q, max_kv):
+    # one row and a few on many keys, and single rows beside a prompt: without one, a byte short, off its alignment
+    d = B.PagedAttentionDesc(hq, 0, 0, B.Dyadic(1, 30), B.Dyadic(1, 16))
+    c = cache(heads_kv=hk, num_pages=100000, head_dim=D)
+    need = B.ibert_paged_attention_workspace_bytes(d, c, batch, rows, max_q, max_kv)
+    assert need > 0
+    for at, size in ((None, 0), (None, need), (DUMMY, need - 1), (DUMMY, 0), (DUMMY + 16, need), (DUMMY + 128, need + 256)):
+        assert B.lib().ibert_paged_attention_i(C.byref(d), C.byref(c), DUMMY, hq * D, DUMMY, 4096, DUMMY, DUMMY, batch, rows, max_q, max_kv, DUMMY, hq * D, at, size, None) == -5, (at, size)
