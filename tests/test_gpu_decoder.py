@@ -686,6 +686,74 @@ def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
     same(devs[0].result(), cases[0].oracle(), "after other lengths")
 
 
+def test_attention_under_bounds_far_above_the_lengths(gpu):
+    # what a captured step hands over: the longest context and the most rows that may come
+    for n, kv, hq, hk, D, max_q in (([1] * 3, [70, 0, 4000], 8, 2, 128, 1), ([1, 3, 1], [700, 64, 5], 4, 4, 64, 16), ([1] * 40, [100] * 39 + [9000], 16, 16, 64, 1), ([90, 1], [100, 2], 8, 2, 128, 2048)):
+        check_attention(U.Attention(87 + D, hq, hk, D, 128, n, kv, pad=max_q), max_q=max_q, max_kv=131072)
+    # without starts every sequence has one row, whatever the bound says
+    check_attention(U.Attention(88, 8, 2, 128, 64, [1] * 20, [700] * 19 + [65], pad=9), plain_rows=True, max_q=600, max_kv=5000)
+
+
+def test_decoder_calls_on_two_streams_at_once(gpu):
+    # a workspace, page tables and cache for each; keys split on both, single rows beside a prompt on one of them
+    torch, G, B = libs()
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    cases = [U.Attention(89, 8, 2, 128, 64, [1, 1], [9000, 700]), U.Attention(90, 16, 4, 128, 64, [1, 1, 600, 1], [9000, 3000, 650, 300])]
+    pages = [U.Pages(91 + i, *U.mixed_lengths(np.random.default_rng(91 + i), 300, 900), 64) for i in range(2)]
+    want = [c.oracle() for c in cases]
+    devs, tables = [DeviceAttention(c) for c in cases], [[DevicePages(p) for _ in range(6)] for p in pages]
+    assert all(d.size > 0 for d in devs)
+    torch.cuda.synchronize()
+    G.say("decoder calls on two streams")
+    for k in range(6):
+        for d, t, s in zip(devs, tables, sides):
+            t[k].call(s)
+            for _ in range(3):
+                d.call(s)
+    for d, w in zip(devs, want):
+        same(d.result(), w, "out")
+    for t in tables:
+        for p in t:
+            p.check()
+
+
+def test_single_rows_among_prompts_in_a_graph(gpu):
+    # two plans in one call, and lengths that change between replays: the same launches then take other rows
+    torch, G, B = libs()
+    case = U.Attention(93, 16, 4, 128, 64, [1, 1, 600, 1], [9000, 3000, 650, 300], pad=40)
+    rot = U.Rotary(94, 100, 5, 5, 128, 128, True, 64, True, True, 16, range(90, 100))
+    tk, tv, tq, tx, tc, tp, ts, gq, gk = (G.to_dev(a) for a in (rot.k0, rot.v0, rot.q0, rot.qkv, rot.cs, rot.positions, rot.slots, rot.gq, rot.gk))
+    desc, cache = rot.descs(tk, tv)
+    d = DeviceAttention(case)
+    assert d.size > 0
+    B.ibert_rotary_override(2)
+    try:
+        graph = torch.cuda.CUDAGraph()
+        d.call()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            d.call()
+            B.ibert_rotary_append_i(desc, cache, tx, rot.qkv.shape[1], tc, tp, ts, gq, gk, rot.rows, tq, rot.q0.shape[1])
+    finally:
+        B.ibert_rotary_override(-1)
+    rot_want = rot.oracle()
+    for k, (n, kv) in enumerate([(case.n, case.kv), ([2, 1, 599, 1], [8999, 1, 9000, 64]), ([1] * 4, [2000, 0, 5000, 77]), ([0, 600, 1, 40], [5, 600, 8000, 39])]):
+        case.n, case.kv = np.array(n), np.array(kv)
+        case.q_start, case.kv_len = np.concatenate([[0], np.cumsum(n)]).astype(np.int32), np.array(kv, np.int32)
+        for _ in range(2):
+            G.say("single rows among prompts, replay %d" % k)
+            d.start.copy_(torch.from_numpy(case.q_start))
+            d.kv.copy_(torch.from_numpy(case.kv_len))
+            d.out[:-64].copy_(torch.from_numpy(case.out.reshape(-1)))
+            d.ws.fill_(-1)
+            for t, old in ((tq, rot.q0), (tk, rot.k0), (tv, rot.v0)):
+                t.copy_(torch.from_numpy(old))
+            graph.replay()
+            same(d.result(), case.oracle(), "out of replay %d" % k)
+            for got, w, what in zip((tq, tk, tv), rot_want, "qkv"):
+                same(got, w, what)
+
+
 # ------------------------------------------------------------------------------------------- as a decoder runs them
 @pytest.mark.parametrize("hq,hk,D,R,inter,norm,window,sinks", [(12, 12, 64, 64, False, False, 0, 0), (8, 2, 128, 64, True, True, 100, 4)])
 def test_a_decoder_layer_step_by_step(gpu, hq, hk, D, R, inter, norm, window, sinks):
