@@ -535,7 +535,9 @@ int ibert_rotary_append_i(const ibert_rotary_desc* desc, const ibert_kv_cache* c
  * first max_q_len, are left as they were.  max_q_len, max_kv_len: bounds of the batch that the host knows; they size the launch and the workspace, and say with
  * rows whether single rows stand among prompts, which are then worked on apart.
  * workspace: device, 256-byte aligned, ibert_paged_attention_workspace_bytes() bytes for the same arguments (smaller bounds, or fewer rows, may ask
- * for more; else IBERT_ERR_WORKSPACE; may be NULL where that is 0); calls that may overlap in time need one each.
+ * for more; else IBERT_ERR_WORKSPACE; may be NULL where that is 0); calls that may overlap in time need one each.  A program that keeps one workspace
+ * asks for every set of bounds that it calls with (batch, rows, max_q_len, max_kv_len) and keeps the largest.  What is asked for grows with batch * max_kv_len up to
+ * 2 GiB; a call that would ask for more asks for none and takes a slower form.
  * Preconditions: max_kv_len <= 131072 and scores_dy.m >= 0, its shift in [24, 62], out_dy's in [0, 62], window, sinks >= 0
  * (IBERT_ERR_PARAM_RANGE); heads_q a multiple of heads_kv, leading dimensions >= heads_q * head_dim, batch <= 65535, max_q_len >= 1,
  * max_q_len * heads_q / heads_kv <= 64 * 65535, rows >= batch where q_start is NULL (IBERT_ERR_SHAPE); q and ld_q 16-byte, out and ld_out 4-byte aligned (IBERT_ERR_ALIGN).  The cache's V holds values in

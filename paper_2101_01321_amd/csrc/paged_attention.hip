@@ -576,8 +576,9 @@ __global__ __launch_bounds__(PJ_THREADS) void paged_join_kernel(SplitArgs a)
 // waits for another before the end.  Then weights and sums, which stay in registers: K and V come a block of 64 keys at a time into
 // LDS, one block ahead, for all four.  A weight's two halves are read from a table in LDS, entry DY(m - s): the maximum goes into the
 // addend of the score's own 64-bit multiply-add.
-// Bound: issue.  A score costs a multiply-add, a shift, a cap, an address, a read of 16 bits and a permute, and an MFMA takes the
-// place of two and a half vector instructions, so that four wavefronts a SIMD, which is what 16 rows each allow, beat two of 32 rows: those
+// Bound: LDS, and issue next to it.  4096 rows of 32 heads of width 128 (153 us): LDS works 0.58 of the cycles as counted, and some 0.8 of them as a 16-byte read takes 8 where it
+// counts 4; 0.24 of the cycles are bank conflicts of the table's reads.  Matrix cores 0.48, vector ALU 0.45.  A score costs a multiply-add, a shift, a cap, an address, a read of 16 bits
+// and a permute, and an MFMA takes the place of two and a half vector instructions.  Four wavefronts a SIMD, which is what 16 rows each allow, beat two of 32 rows: those
 // read every key from LDS half as often, but two wavefronts issue only every 5.8 cycles.  us, 4096 rows of 32 heads of width 128, 16 rows a wavefront / 32:
 // 176 / 194; 32 x 200 rows of 12 heads of width 64 23.0 / 22.6, 4096 of 16 75.8 / 101.
 constexpr int PP_TABLE = 1025, PP_NW = 4, PP_ROWS = 64;

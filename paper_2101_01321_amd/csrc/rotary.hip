@@ -10,7 +10,7 @@
 // Values: the cache wants 16 tokens of a channel side by side.  A wavefront takes 16 channels of 64 rows.  Where rows follow each other into
 // a block of 64 tokens (a prompt), their bytes are transposed, four rows by lane swaps and the rest through LDS, and leave as 1 KB, or
 // as the dwords and bytes of it that they fill; single rows are stored byte by byte.
-// Bound: HBM, and with norms the vector ALU next to it.  16384 rows of 32 + 8 + 8 heads of width 128: 206 MB in 49 us without norms (4.2 TB/s), in 60 us with them
+// Bound: HBM, and with norms the vector ALU next to it.  16384 rows of 32 + 8 + 8 heads of width 128: 206 MB in 49 us without norms (4.2 TB/s), in 61 us with them
 // (3.4 TB/s; 0.79 of the ALU's slots).  2741 rows of 16 + 16 + 16 heads of width 64: 17 MB in 7.6 us.  Five rows: 3.5 us, three dependent trips to memory.
 #include "layernorm_math.h"
 #include "ibert_testing.h"
@@ -40,8 +40,10 @@ __device__ __forceinline__ int32_t byte_of(uint32_t p, int i) { return (int32_t)
 
 // NH: heads of a row that a team of lanes takes one after the other.  With two the table's row, the row's slot and what else is the same for both is
 // fetched once, and each lane finds the root and the reciprocal of one head for all; it halves the wavefronts, so it is for many rows.  us, one head /
-// two, 32 query heads of width 128: 1024 rows with norms 7.4 / 8.4, 2048 12.9 / 13.0, 4096 without 14.0 / 14.5, 16384 without 55.5 / 48.9, with 74.6 / 66.9.
-// (Four heads: 132 registers, 69.7.  Width 64, 2 lanes a head: no change at 16384 rows.)
+// two, 32 + 8 heads of queries and keys of width 128: 1024 rows with norms 7.4 / 8.4, 2048 12.9 / 13.0, 4096 without 13.7 / 14.1, with 18.6 / 18.7, 6144 without 18.0 / 18.1, with
+// 24.5 / 24.2, 8192 (the line, RO_TEAM_HEADS) without 27.7 / 25.8, with 37.2 / 35.1, 16384 without 56.2 / 49.2, with 70.3 / 62.8; 64 + 8 heads, 3072 rows without 15.3 / 15.9, 4096 (the line)
+// 20.0 / 20.0, with 28.3 / 26.9.  As many keys as queries gain below the line too: 16 + 16 heads, 8192 rows without 34.0 / 29.0, with 40.5 / 35.8.
+// (Four heads: 132 registers, 69.7 where two took 66.9.  Width 64, 2 lanes a head: no change at 16384 rows.)
 template <int D, bool INTERLEAVED, int P, int NH>
 __device__ __forceinline__ void rotate_heads(const RotaryArgs& a, int32_t wg, int kind)
 {
