@@ -686,6 +686,19 @@ def test_decoder_calls_in_graphs_and_on_another_stream(gpu):
     same(devs[0].result(), cases[0].oracle(), "after other lengths")
 
 
+def test_attention_at_the_largest_batch_and_bound_of_rows(gpu):
+    # 65535 sequences, most of them empty, in every form; 65535 tiles of 64 rows as the bound of a few, with starts (tiles are counted) and without
+    n, kv = np.ones(65535, np.int64), np.zeros(65535, np.int64)
+    kv[[0, 1, 511, 512, 40000, 65533, 65534]] = (64, 1, 65, 300, 128, 7, 200)
+    check_attention(U.Attention(95, 2, 1, 64, 64, n, kv))
+    n[[3, 65534]], n[100:200] = (0, 70), 0
+    check_attention(U.Attention(96, 2, 1, 64, 64, n, kv))
+    case = U.Attention(97, 1, 1, 64, 64, [1, 70, 1], [200, 130, 64])
+    check_attention(case, max_q=64 * 65535)
+    check_attention(U.Attention(98, 2, 1, 64, 64, [1, 1], [70, 1]), plain_rows=True, max_q=32 * 65535)
+    check_attention(U.Attention(99, 1024, 1024, 64, 64, [1, 20], [70, 130]))
+
+
 def test_attention_under_bounds_far_above_the_lengths(gpu):
     # what a captured step hands over: the longest context and the most rows that may come
     for n, kv, hq, hk, D, max_q in (([1] * 3, [70, 0, 4000], 8, 2, 128, 1), ([1, 3, 1], [700, 64, 5], 4, 4, 64, 16), ([1] * 40, [100] * 39 + [9000], 16, 16, 64, 1), ([90, 1], [100, 2], 8, 2, 128, 2048)):
