@@ -214,8 +214,10 @@ int ibert_rotary_freqs(const ibert_rotary_scaling* sc, int32_t rot_dim, double* 
                                         !std::isfinite(sc->first_len) || !std::isfinite(sc->fast))) return IBERT_ERR_PARAM_RANGE;
     const double two_pi = 6.283185307179586;
     const double base = sc->kind == IBERT_ROPE_BASE ? sc->base * std::pow(sc->factor, (double)rot_dim / (rot_dim - 2)) : sc->base;
+    if (!std::isfinite(base)) return IBERT_ERR_PARAM_RANGE;
     for (int i = 0; i < rot_dim / 2; ++i) {
         double f = std::pow(base, -2.0 * i / rot_dim);
+        if (!std::isfinite(f)) return IBERT_ERR_PARAM_RANGE;
         if (sc->kind == IBERT_ROPE_LINEAR) f /= sc->factor;
         if (sc->kind == IBERT_ROPE_RAMP) {
             double keep = (f * sc->first_len / two_pi - sc->slow) / (sc->fast - sc->slow);
