@@ -560,7 +560,7 @@ int ibert_paged_attention_i(const ibert_paged_attention_desc* desc, const ibert_
  *   IBERT_ROPE_LINEAR  freqs / factor;   IBERT_ROPE_BASE  base * factor^(R/(R-2)) in place of base (R > 2);
  *   IBERT_ROPE_RAMP    turns = freqs * first_len / 2 pi;  keep = clamp((turns - slow) / (fast - slow), 0, 1);
  *                      freqs * (keep + (1 - keep) / factor)                            (first_len >= 1, 0 <= slow < fast)
- *   A base or a frequency that binary64 does not hold is refused (IBERT_ERR_PARAM_RANGE).
+ *   A base or a frequency that binary64 does not hold is refused (IBERT_ERR_PARAM_RANGE), and by the table an angle.
  * ibert_rotary_table_from_freqs: table[p][i] = {rint(2^14 cos(p freqs[i])), rint(2^14 sin(p freqs[i]))}, p < max_pos, to a host array.
  * ibert_head_norm_from_float: gamma_q[i] = rint(gamma[i] / S_out * 2^(shift-10)) with the largest shift in [1, 30] such that
  *   max |gamma_q| < 2^14; u then has the scale S_out.

@@ -236,7 +236,7 @@ int ibert_rotary_table_from_freqs(const double* freqs, int32_t rot_dim, int32_t 
     if (!freqs || !table) return IBERT_ERR_NULL;
     const int n = rot_dim / 2;
     for (int i = 0; i < n; ++i)
-        if (!std::isfinite(freqs[i])) return IBERT_ERR_PARAM_RANGE;
+        if (!std::isfinite(freqs[i]) || !std::isfinite(freqs[i] * (max_pos - 1))) return IBERT_ERR_PARAM_RANGE;
     for (int64_t p = 0; p < max_pos; ++p)
         for (int i = 0; i < n; ++i) {
             const double angle = (double)p * freqs[i];

@@ -339,3 +339,10 @@ def test_frequencies_that_binary64_does_not_hold_are_refused(scaling, rot_dim):
     with pytest.raises(B.IbertError) as e:
         B.ibert_rotary_freqs(scaling, rot_dim)
     assert e.value.code == -3
+
+
+def test_a_table_of_angles_that_binary64_does_not_hold_is_refused():
+    with pytest.raises(B.IbertError) as e:
+        B.ibert_rotary_table_from_freqs(np.array([1.0, 1e308]), 100)
+    assert e.value.code == -3
+    assert tuple(B.ibert_rotary_table_from_freqs(np.array([1e308]), 1)[0, 0]) == (16384, 0)         # position 0 alone has an angle
