@@ -580,6 +580,135 @@ int ibert_paged_attention_from_scales(double S_q, double S_k, double S_v, double
                                       ibert_paged_attention_desc* out);
 
 /* ------------------------------------------------------------------------------------------------
+ * Gated feed-forward block: act(x W_gate) * (x W_up), the decoder's counterpart of ibert_gemm_i8_gelu, in one kernel.  The paper's
+ * encoder has none; reading, with the same pieces (INT32 sums, dyadic requantization, the integer non-linearities), per token i and
+ * channel f < F:
+ *   g = clamp(DY(sum_k A[i,k] W[f,k] + bias[f]; mult[f], shift[f]), -G, G)
+ *   u = clamp(DY(sum_k A[i,k] W[F+f,k] + bias[F+f]; mult[F+f], shift[F+f]), -32767, 32767)
+ *   IBERT_GATE_SILU: G = 65535, g on the scale IBERT_SILU_SCALE = ln2/1024 (the multipliers bring it there):
+ *       d = min((|g| + 8) >> 4, 1024), z = d >> 6, f = d & 63       (distance in steps of ln2/64)
+ *       e = floor(((124 - f)^2 + 8180) / 2^z + 1/2), 0 from z = 16 on        (I-Exp of Alg. 3, constants of Eq. 13 at S = ln2/64)
+ *       p = floor((23556 * 2^15 + floor((23556 + e) / 2)) / (23556 + e))     (sigmoid of |g|, 15 bits; 23556 = e at d = 0)
+ *       a = (g * (g < 0 ? 2^15 - p : p) + 2^14) >> 15                        (scale of g)
+ *   IBERT_GATE_GELU: G = gelu.q_max; t as in ibert_gelu_i; a = clamp(DY(t; gelu.out), -32767, 32767)   (gelu.out to a scale of 16 bits)
+ *   C[i,f] = clamp(DY(a * u; out_dy), -127, 127)
+ * ibert_gemm_i8_gated: W: device int8 [2F, K] (the gate's rows, then the up projection's), bias (may be NULL), mult, shift: device int32
+ * [2F], shifts in [0, 62].  A: device int8 [M, lda]; C: device int8 [M, ldc], must not overlap A or W.  desc: host.  Single tokens and prompts
+ * alike; no alignment is required; 16-byte aligned A and W (pointers and leading dimensions) with K a multiple of 16 are the fast path.
+ * Errors: IBERT_ERR_SHAPE (M or F < 0, K outside [1, 2^17], F > 2^24, a leading dimension below its row), IBERT_ERR_PARAM_RANGE (activation,
+ * gelu's preconditions with IBERT_GATE_GELU, out_dy's shift), IBERT_ERR_NULL.  M = 0 or F = 0: nothing to do.
+ * |bias| + K * 16129 < 2^31 is the caller's responsibility, as for ibert_gemm_i8_requant.
+ * ---------------------------------------------------------------------------------------------- */
+enum { IBERT_GATE_SILU = 0, IBERT_GATE_GELU = 1 };
+#define IBERT_SILU_SCALE (0.69314718055994530942 / 1024)
+
+typedef struct {
+    int32_t activation;
+    ibert_gelu_params gelu;      /* used iff activation == IBERT_GATE_GELU */
+    ibert_dyadic out_dy;
+} ibert_gate_params;
+
+typedef struct {
+    int32_t M, F, K;
+    int64_t lda, ldw, ldc;       /* ldw: INT8 weights only */
+    ibert_gate_params gate;
+} ibert_gated_desc;
+
+int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A, const int8_t* W, const int32_t* bias,
+                        const int32_t* mult, const int32_t* shift, int8_t* C, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Products with 4-bit weights and group scales, for steps of few tokens, whose time is that of reading the weights.
+ * The real weight of channel n at k is S_w[n] * scale[n, k / group] * (w[n,k] - zero[n, k / group]): w in [-8, 7], an integer scale in
+ * [0, 255] and, optionally, a zero point in [-8, 7] for each group of `group` = 32, 64 or 128 values of K; S_w[n] goes into mult and shift.
+ *   acc[i,n] = clamp(sum_k A[i,k] scale (w - zero) + bias[n]) into INT32     (the sum is exact, however large)
+ *   v        = DY(acc; mult[n], shift[n]) (+ DY(residual[i,n]; residual_dy) iff residual != NULL)
+ *   C[i,n]   = clamp(v, -out_clamp, +out_clamp), stored as IBERT_I8, IBERT_I16 or IBERT_I32
+ * ibert_gemm_w4_gated: the gated block above on such weights, both matrices [F, K], with the same group; desc->ldw is ignored.
+ *
+ * The weights are laid out once (ibert_w4_pack), N in tiles of 16 channels, K in chunks of 128, both padded:
+ *   w[n/16][k/128][k%32/8][n%16][k%64/32][k%8], one byte: k%128 < 64 in the low four bits, k + 64 in the high four (two's complement)
+ *   scales (uint8), zeros (int8; their low four bits count): [n/16][k/128][n%16][k%128/group]
+ * What stands past N and K is never looked at.  w, scales, zeros, bias, mult, shift, A, residual, C: device; the structs: host.
+ * w: 16-byte aligned; scales and zeros: 4-byte aligned (IBERT_ERR_ALIGN).  bias, residual, zeros may be NULL.  A, C, residual: any alignment.
+ * Errors: IBERT_ERR_SHAPE (M or N < 0, K outside [1, 2^17], N > 2^24, a leading dimension below its row), IBERT_ERR_PARAM_RANGE (group, out_dtype,
+ * out_clamp as for ibert_gemm_i8_requant, a dyadic's shift, gate), IBERT_ERR_NULL.  M = 0 or N = 0: nothing to do.  C must not overlap the inputs.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    const uint8_t* w;
+    const uint8_t* scales;
+    const int8_t* zeros;         /* or NULL: all 0 */
+    int32_t group;
+} ibert_w4_weights;
+
+typedef struct {
+    int32_t M, N, K;
+    int32_t out_dtype;           /* IBERT_I8 | IBERT_I32 | IBERT_I16 */
+    int64_t lda, ldc, ldr;
+    int32_t out_clamp;
+    ibert_dyadic residual_dy;    /* used iff residual != NULL */
+} ibert_w4_desc;
+
+int ibert_gemm_w4_requant(const ibert_w4_desc* desc, const int8_t* A, const ibert_w4_weights* weights, const int32_t* bias,
+                          const int32_t* mult, const int32_t* shift, const int8_t* residual, void* C, void* stream);
+int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A, const ibert_w4_weights* gate, const ibert_w4_weights* up,
+                        const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, void* stream);
+
+/* Bytes of w, and of scales or zeros (0 for sizes that are refused). */
+size_t ibert_w4_bytes(int32_t N, int32_t K);
+size_t ibert_w4_scale_bytes(int32_t N, int32_t K, int32_t group);
+
+/* Host: lays out w [N, K] (values in [-8, 7], else IBERT_ERR_PARAM_RANGE), scales and zeros (NULL: none) [N, ceil(K / group)]; padding becomes 0. */
+int ibert_w4_pack(const int8_t* w, const uint8_t* scales, const int8_t* zeros, int32_t N, int32_t K, int32_t group,
+                  uint8_t* w_out, uint8_t* scales_out, int8_t* zeros_out);
+
+/* Host: real weights [N, K] -> w, scales as ibert_w4_pack takes them, and S_w [N], without zero points (binary64):
+ *   top_g = max |x| in group g;  S_w[n] = max_g top_g / (7 * 255)  (1 where the row is all zeros);
+ *   scale = max(1, rint(top_g / 7 / S_w)) or 0 where top_g = 0;  w = clamp(rint(x / (scale S_w)), -7, 7).
+ * A value that is not finite, or a row so small that S_w is 0 or denormal: IBERT_ERR_PARAM_RANGE. */
+int ibert_w4_from_float(const double* x, int32_t N, int32_t K, int32_t group, int8_t* w, uint8_t* scales, double* S_w);
+
+/* Host: the gated block's constants from real scales: with IBERT_GATE_SILU S_gate is not used (it is IBERT_SILU_SCALE), with IBERT_GATE_GELU gelu is that of
+ * ibert_gelu_params_from_scale(S_gate, S_gate / 4);  out_dy = dyadic(S_a * S_up / S_out), S_a the scale of a. */
+int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up, double S_out, ibert_gate_params* out);
+
+/* ------------------------------------------------------------------------------------------------
+ * ibert_logits_adjust_i -- what is done to the INT32 logits of the vocabulary before Softmax or a choice: penalties for repeated
+ * tokens, biases, and masks of a grammar.  For row r (a request) and token t, with n = how often t stands in
+ * tokens[out_start[r] .. token_start[r+1]) (what has been produced) and `seen` = whether it stands anywhere in
+ * tokens[token_start[r] .. token_start[r+1]) (the prompt too):
+ *   v = x[r,t];  INT32_MIN ("minus infinity") stays what it is
+ *   if seen: v = clamp(DY(v; v > 0 ? up : down)) into INT32                      (repetition penalty p: up ~ 1/p, down ~ p)
+ *   v = v - (n > 0 ? presence : 0) - frequency * n + (sum of the values of row r's biases for t)
+ *   y[r,t] = clamp(v) into [INT32_MIN + 1, INT32_MAX], or INT32_MIN where the row's mask has bit t clear
+ * x, y: device int32 [rows, ldx], [rows, ldy]; y may be x (with ldy = ldx) and must not overlap it otherwise.  params: device
+ * ibert_logits_row [rows]; a row whose mask is negative has none, one at or above num_masks is taken as the last.  tokens: device int32
+ * [num_tokens]; token_start: device int32 [rows + 1]; out_start: device int32 [rows]; both NULL where num_tokens = 0.  bias_ids, bias_values: device int32
+ * [num_biases], bias_start: device int32 [rows + 1]; a token may be named more than once.  masks: device uint32 [num_masks, ld_mask], bit t % 32 of word t / 32.
+ * Starts are clamped into [0, num_tokens] ([0, num_biases]) and into order; token numbers outside [0, vocab) are ignored; shifts outside [0, 62] are clamped into it.
+ * Errors: IBERT_ERR_SHAPE (negative sizes, num_tokens or num_biases > 2^30, vocab > 2^26, ldx or ldy < vocab, ld_mask < ceil(vocab / 32), x and y overlap), IBERT_ERR_NULL.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+    ibert_dyadic up, down;
+    int32_t presence, frequency;
+    int32_t mask;
+} ibert_logits_row;
+
+typedef struct {
+    int32_t rows, vocab;
+    int64_t ldx, ldy;
+    int32_t num_tokens, num_biases, num_masks, ld_mask;
+} ibert_logits_desc;
+
+int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_t* x, const ibert_logits_row* params, const int32_t* tokens,
+                          const int32_t* token_start, const int32_t* out_start, const int32_t* bias_ids, const int32_t* bias_values,
+                          const int32_t* bias_start, const uint32_t* masks, int32_t* y, void* stream);
+
+/* Host: a row's parameters at logits of scale S: up = dyadic(1 / repetition), down = dyadic(repetition), presence and frequency = rint(. / S), which must fit
+ * 31 bits; repetition > 0. */
+int ibert_logits_row_from_reals(double S, double repetition, double presence, double frequency, int32_t mask, ibert_logits_row* out);
+
+/* ------------------------------------------------------------------------------------------------
  * Optional instrumentation for benchmarks (not part of the method): while a profile is open,
  * ibert_encoder_layer_i / ibert_encoder_i bracket each of the ten steps with HIP events on the caller's
  * stream.  ibert_profile_begin creates the events (host objects; no device memory) for up to `capacity`

@@ -112,6 +112,37 @@ class PagedAttentionDesc(C.Structure):
                 ("out_dy", Dyadic)]
 
 
+GATE_SILU, GATE_GELU = 0, 1
+SILU_SCALE = 0.69314718055994530942 / 1024
+
+
+class GateParams(C.Structure):
+    _fields_ = [("activation", C.c_int32), ("gelu", GeluParams), ("out_dy", Dyadic)]
+
+
+class GatedDesc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("F", C.c_int32), ("K", C.c_int32), ("lda", C.c_int64), ("ldw", C.c_int64), ("ldc", C.c_int64),
+                ("gate", GateParams)]
+
+
+class W4Weights(C.Structure):
+    _fields_ = [("w", _P), ("scales", _P), ("zeros", _P), ("group", C.c_int32)]
+
+
+class W4Desc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("out_dtype", C.c_int32), ("lda", C.c_int64), ("ldc", C.c_int64),
+                ("ldr", C.c_int64), ("out_clamp", C.c_int32), ("residual_dy", Dyadic)]
+
+
+class LogitsRow(C.Structure):
+    _fields_ = [("up", Dyadic), ("down", Dyadic), ("presence", C.c_int32), ("frequency", C.c_int32), ("mask", C.c_int32)]
+
+
+class LogitsDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64), ("num_tokens", C.c_int32),
+                ("num_biases", C.c_int32), ("num_masks", C.c_int32), ("ld_mask", C.c_int32)]
+
+
 class ProfileRecord(C.Structure):
     _fields_ = [("step", C.c_int32), ("ms", C.c_float), ("ops", C.c_double), ("bytes", C.c_double),
                 ("kernel", C.c_char * 96)]
@@ -183,6 +214,17 @@ SIGNATURES = {
     "ibert_rotary_table_from_freqs": (C.c_int, [_P, C.c_int32, C.c_int32, _P]),
     "ibert_head_norm_from_float": (C.c_int, [_P, C.c_int32, C.c_double, _P, C.POINTER(C.c_int32)]),
     "ibert_paged_attention_from_scales": (C.c_int, [C.c_double] * 4 + [C.c_int32, C.POINTER(PagedAttentionDesc)]),
+    "ibert_rows_override": (None, [C.c_int32] * 2),
+    "ibert_gemm_i8_gated": (C.c_int, [C.POINTER(GatedDesc)] + [_P] * 7),
+    "ibert_gemm_w4_requant": (C.c_int, [C.POINTER(W4Desc), _P, C.POINTER(W4Weights)] + [_P] * 6),
+    "ibert_gemm_w4_gated": (C.c_int, [C.POINTER(GatedDesc), _P] + [C.POINTER(W4Weights)] * 2 + [_P] * 5),
+    "ibert_w4_bytes": (C.c_size_t, [C.c_int32] * 2),
+    "ibert_w4_scale_bytes": (C.c_size_t, [C.c_int32] * 3),
+    "ibert_w4_pack": (C.c_int, [_P] * 3 + [C.c_int32] * 3 + [_P] * 3),
+    "ibert_w4_from_float": (C.c_int, [_P] + [C.c_int32] * 3 + [_P] * 3),
+    "ibert_gate_params_from_scales": (C.c_int, [C.c_int32] + [C.c_double] * 3 + [C.POINTER(GateParams)]),
+    "ibert_logits_adjust_i": (C.c_int, [C.POINTER(LogitsDesc)] + [_P] * 11),
+    "ibert_logits_row_from_reals": (C.c_int, [C.c_double] * 4 + [C.c_int32, C.POINTER(LogitsRow)]),
     "ibert_profile_begin": (C.c_int, [C.c_int32]),
     "ibert_profile_end": (C.c_int, [C.POINTER(ProfileRecord), C.c_int32, C.POINTER(C.c_int32)]),
     "ibert_status_string": (C.c_char_p, [C.c_int]),
@@ -510,6 +552,80 @@ def ibert_paged_attention_i(desc: PagedAttentionDesc, cache: KvCache, q, ld_q: i
     _chk(lib().ibert_paged_attention_i(C.byref(desc), C.byref(cache), _dp(q), ld_q, _dp(block_table), max_pages, _dp(q_start),
                                        _dp(kv_len), batch, rows, max_q_len, max_kv_len, _dp(out), ld_out, _dp(workspace),
                                        nbytes, _stream(stream)), "ibert_paged_attention_i")
+
+
+def ibert_rows_override(tiles: int, groups: int):
+    lib().ibert_rows_override(tiles, groups)
+
+
+def ibert_gemm_i8_gated(desc: GatedDesc, A, W, bias, mult, shift, out, stream=None):
+    _chk(lib().ibert_gemm_i8_gated(C.byref(desc), _dp(A), _dp(W), _dp(bias), _dp(mult), _dp(shift), _dp(out), _stream(stream)),
+         "ibert_gemm_i8_gated")
+
+
+def ibert_gemm_w4_requant(desc: W4Desc, A, weights: W4Weights, bias, mult, shift, residual, out, stream=None):
+    _chk(lib().ibert_gemm_w4_requant(C.byref(desc), _dp(A), C.byref(weights), _dp(bias), _dp(mult), _dp(shift), _dp(residual), _dp(out),
+                                     _stream(stream)), "ibert_gemm_w4_requant")
+
+
+def ibert_gemm_w4_gated(desc: GatedDesc, A, gate: W4Weights, up: W4Weights, bias, mult, shift, out, stream=None):
+    _chk(lib().ibert_gemm_w4_gated(C.byref(desc), _dp(A), C.byref(gate), C.byref(up), _dp(bias), _dp(mult), _dp(shift), _dp(out),
+                                   _stream(stream)), "ibert_gemm_w4_gated")
+
+
+def _np_ptr(a) -> Optional[int]:
+    return None if a is None else a.ctypes.data
+
+
+def ibert_w4_bytes(N: int, K: int) -> int:
+    return int(lib().ibert_w4_bytes(N, K))
+
+
+def ibert_w4_scale_bytes(N: int, K: int, group: int) -> int:
+    return int(lib().ibert_w4_scale_bytes(N, K, group))
+
+
+def ibert_w4_pack(w, scales, zeros, group: int):
+    """w: [N, K] in [-8, 7]; scales, zeros (or None): [N, ceil(K / group)].  Returns the three arrays in the layout of the kernels."""
+    w, scales = np.ascontiguousarray(w, np.int8), np.ascontiguousarray(scales, np.uint8)
+    zeros = None if zeros is None else np.ascontiguousarray(zeros, np.int8)
+    N, K = w.shape
+    for x in (scales, zeros):
+        if x is not None and x.shape != (N, -(-K // max(group, 1))):
+            raise ValueError("scales and zeros have the shape (N, ceil(K / group))")
+    w_out, s_out = np.empty(ibert_w4_bytes(N, K), np.uint8), np.empty(ibert_w4_scale_bytes(N, K, group), np.uint8)
+    z_out = None if zeros is None else np.empty(s_out.size, np.int8)
+    _chk(lib().ibert_w4_pack(_np_ptr(w), _np_ptr(scales), _np_ptr(zeros), N, K, group, _np_ptr(w_out), _np_ptr(s_out), _np_ptr(z_out)),
+         "ibert_w4_pack")
+    return w_out, s_out, z_out
+
+
+def ibert_w4_from_float(x, group: int):
+    """x: [N, K] reals.  Returns (w, scales, S_w)."""
+    x = np.ascontiguousarray(x, np.float64)
+    N, K = x.shape
+    w, scales, S_w = np.empty((N, K), np.int8), np.empty((N, -(-K // max(group, 1))), np.uint8), np.empty(N, np.float64)
+    _chk(lib().ibert_w4_from_float(_np_ptr(x), N, K, group, _np_ptr(w), _np_ptr(scales), _np_ptr(S_w)), "ibert_w4_from_float")
+    return w, scales, S_w
+
+
+def ibert_gate_params_from_scales(activation: int, S_gate: float, S_up: float, S_out: float) -> GateParams:
+    p = GateParams()
+    _chk(lib().ibert_gate_params_from_scales(activation, float(S_gate), float(S_up), float(S_out), C.byref(p)), "ibert_gate_params_from_scales")
+    return p
+
+
+def ibert_logits_adjust_i(desc: LogitsDesc, x, params, tokens, token_start, out_start, bias_ids, bias_values, bias_start, masks, y, stream=None):
+    """params: device int32 [rows, 7], the fields of LogitsRow in order."""
+    _chk(lib().ibert_logits_adjust_i(C.byref(desc), _dp(x), _dp(params), _dp(tokens), _dp(token_start), _dp(out_start), _dp(bias_ids),
+                                     _dp(bias_values), _dp(bias_start), _dp(masks), _dp(y), _stream(stream)), "ibert_logits_adjust_i")
+
+
+def ibert_logits_row_from_reals(S: float, repetition: float, presence: float, frequency: float, mask: int = -1) -> LogitsRow:
+    p = LogitsRow()
+    _chk(lib().ibert_logits_row_from_reals(float(S), float(repetition), float(presence), float(frequency), mask, C.byref(p)),
+         "ibert_logits_row_from_reals")
+    return p
 
 
 def ibert_profile_begin(capacity: int):

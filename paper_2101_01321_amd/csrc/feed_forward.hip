@@ -1,0 +1,167 @@
+// The gated feed-forward block and the products with 4-bit weights: argument checks, the choice of the kernel, and the INT8 gated block's
+// kernels for few rows.
+#include "rows_launch.h"
+
+namespace ibert {
+
+template <> int launch_rows<true, 32>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream);
+template <> int launch_rows<true, 64>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream);
+template <> int launch_rows<true, 128>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream);
+IBERT_ROWS_UNIT(false, 128)
+
+static int g_rows_tiles = -1, g_rows_groups = -1;
+
+static RowsPlan plan_rows(int32_t M, int32_t N, int32_t K, bool gated)
+{
+    RowsPlan p;
+    p.mt = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
+    p.nt = g_rows_tiles >= 1 ? (g_rows_tiles > 2 ? 2 : g_rows_tiles) : 1;
+    p.cg = 0;
+    if (g_rows_groups >= 0) p.cg = g_rows_groups > 3 ? 3 : g_rows_groups;
+    else {
+        const int64_t down = (M + 16 * p.mt - 1) / (16 * p.mt);
+        while (p.cg < 3 && down * ((N + (32 * p.nt << p.cg) - 1) / (32 * p.nt << p.cg)) >= 512) ++p.cg;
+    }
+    (void)K;
+    (void)gated;
+    return p;
+}
+
+static int launch_w4(const RowsArgs& g, int32_t group, bool zeros, bool gated, hipStream_t stream)
+{
+    const RowsPlan p = plan_rows(g.M, g.N, g.K, gated);
+    if (group == 32) return launch_rows<true, 32>(g, p, zeros, gated, stream);
+    if (group == 64) return launch_rows<true, 64>(g, p, zeros, gated, stream);
+    return launch_rows<true, 128>(g, p, zeros, gated, stream);
+}
+
+static bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
+}
+// bytes from the first to the last element of `rows` rows of n elements
+static int64_t span(int64_t rows, int64_t ld, int64_t n, int64_t elem) { return ((rows - 1) * ld + n) * elem; }
+
+static int check_gate(const ibert_gate_params& p)
+{
+    if (p.activation != IBERT_GATE_SILU && p.activation != IBERT_GATE_GELU) return IBERT_ERR_PARAM_RANGE;
+    if (p.activation == IBERT_GATE_GELU) {
+        const int rc = check_gelu(p.gelu);
+        if (rc) return rc;
+    }
+    return dyadic_ok(p.out_dy) ? IBERT_OK : IBERT_ERR_PARAM_RANGE;
+}
+
+// Sizes and constants of a gated block; *empty: there is nothing to do.
+static int check_gated(const ibert_gated_desc* d, const int8_t* A, const int32_t* mult, const int32_t* shift, const int8_t* C, bool* empty)
+{
+    *empty = false;
+    if (!d) return IBERT_ERR_NULL;
+    if (d->M < 0 || d->F < 0 || d->K < 1 || d->K > (1 << 17) || d->F > (1 << 24)) return IBERT_ERR_SHAPE;
+    const int rc = check_gate(d->gate);
+    if (rc) return rc;
+    if (d->lda < d->K || d->ldc < d->F) return IBERT_ERR_SHAPE;
+    *empty = d->M == 0 || d->F == 0;
+    if (*empty) return IBERT_OK;
+    if (!A || !mult || !shift || !C) return IBERT_ERR_NULL;
+    if (overlap(C, span(d->M, d->ldc, d->F, 1), A, span(d->M, d->lda, d->K, 1))) return IBERT_ERR_SHAPE;
+    return IBERT_OK;
+}
+
+static int check_w4(const ibert_w4_weights* w)
+{
+    if (!w) return IBERT_ERR_NULL;
+    if (w->group != 32 && w->group != 64 && w->group != 128) return IBERT_ERR_PARAM_RANGE;
+    if (!w->w || !w->scales) return IBERT_ERR_NULL;
+    if (!aligned(w->w, 16) || !aligned(w->scales, 4) || (w->zeros && !aligned(w->zeros, 4))) return IBERT_ERR_ALIGN;
+    return IBERT_OK;
+}
+
+static RowsArgs rows_args(const int8_t* A, int64_t lda, int32_t M, int32_t N, int32_t K, const int32_t* bias, const int32_t* mult, const int32_t* shift,
+                          void* C, int64_t ldc)
+{
+    RowsArgs g{};
+    g.A = A; g.lda = lda; g.M = M; g.N = N; g.K = K;
+    g.bias = bias; g.mult = mult; g.shift = shift;
+    g.C = C; g.ldc = ldc;
+    g.a_vec = aligned(A, 16) && lda % 16 == 0;
+    return g;
+}
+
+}  // namespace ibert
+
+extern "C" void ibert_rows_override(int32_t tiles, int32_t groups)
+{
+    ibert::g_rows_tiles = tiles;
+    ibert::g_rows_groups = groups;
+}
+
+extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A, const int8_t* W, const int32_t* bias,
+                                   const int32_t* mult, const int32_t* shift, int8_t* C, void* stream)
+{
+    bool empty;
+    const int rc = ibert::check_gated(desc, A, mult, shift, C, &empty);
+    if (rc) return rc;
+    if (desc->ldw < desc->K) return IBERT_ERR_SHAPE;
+    if (empty) return IBERT_OK;
+    if (!W) return IBERT_ERR_NULL;
+    const ibert_gated_desc& d = *desc;
+    if (ibert::overlap(C, ibert::span(d.M, d.ldc, d.F, 1), W, ibert::span(2 * (int64_t)d.F, d.ldw, d.K, 1))) return IBERT_ERR_SHAPE;
+    ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
+    g.w[0] = W;
+    g.ldw = d.ldw;
+    g.w_vec = ibert::aligned(W, 16) && d.ldw % 16 == 0 && d.K % 16 == 0 && d.ldw <= (1 << 26);
+    g.gate = ibert::gate_const(d.gate);
+    return ibert::launch_rows<false, 128>(g, ibert::plan_rows(d.M, d.F, d.K, true), false, true, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A, const ibert_w4_weights* gate, const ibert_w4_weights* up,
+                                   const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, void* stream)
+{
+    bool empty;
+    int rc = ibert::check_gated(desc, A, mult, shift, C, &empty);
+    if (rc) return rc;
+    if (empty) return IBERT_OK;
+    rc = ibert::check_w4(gate);
+    if (rc) return rc;
+    rc = ibert::check_w4(up);
+    if (rc) return rc;
+    if (gate->group != up->group || (gate->zeros != nullptr) != (up->zeros != nullptr)) return IBERT_ERR_PARAM_RANGE;
+    const ibert_gated_desc& d = *desc;
+    const int64_t wbytes = (int64_t)ibert_w4_bytes(d.F, d.K), cbytes = ibert::span(d.M, d.ldc, d.F, 1);
+    if (ibert::overlap(C, cbytes, gate->w, wbytes) || ibert::overlap(C, cbytes, up->w, wbytes)) return IBERT_ERR_SHAPE;
+    ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
+    g.w[0] = gate->w; g.w[1] = up->w;
+    g.scales[0] = gate->scales; g.scales[1] = up->scales;
+    g.zeros[0] = gate->zeros; g.zeros[1] = up->zeros;
+    g.gate = ibert::gate_const(d.gate);
+    return ibert::launch_w4(g, gate->group, gate->zeros != nullptr, true, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int ibert_gemm_w4_requant(const ibert_w4_desc* desc, const int8_t* A, const ibert_w4_weights* weights, const int32_t* bias,
+                                     const int32_t* mult, const int32_t* shift, const int8_t* residual, void* C, void* stream)
+{
+    if (!desc) return IBERT_ERR_NULL;
+    const ibert_w4_desc& d = *desc;
+    if (d.M < 0 || d.N < 0 || d.K < 1 || d.K > (1 << 17) || d.N > (1 << 24)) return IBERT_ERR_SHAPE;
+    if (d.out_dtype != IBERT_I8 && d.out_dtype != IBERT_I32 && d.out_dtype != IBERT_I16) return IBERT_ERR_PARAM_RANGE;
+    if (d.out_clamp < 0 || (d.out_dtype == IBERT_I8 && d.out_clamp > 127) || (d.out_dtype == IBERT_I16 && d.out_clamp > 32767)) return IBERT_ERR_PARAM_RANGE;
+    if (residual && !ibert::dyadic_ok(d.residual_dy)) return IBERT_ERR_PARAM_RANGE;
+    if (d.lda < d.K || d.ldc < d.N || (residual && d.ldr < d.N)) return IBERT_ERR_SHAPE;
+    if (d.M == 0 || d.N == 0) return IBERT_OK;
+    if (!A || !mult || !shift || !C) return IBERT_ERR_NULL;
+    const int rc = ibert::check_w4(weights);
+    if (rc) return rc;
+    const int64_t elem = d.out_dtype == IBERT_I8 ? 1 : (d.out_dtype == IBERT_I16 ? 2 : 4), cbytes = ibert::span(d.M, d.ldc, d.N, elem);
+    if (ibert::overlap(C, cbytes, A, ibert::span(d.M, d.lda, d.K, 1)) || ibert::overlap(C, cbytes, weights->w, (int64_t)ibert_w4_bytes(d.N, d.K)) ||
+        (residual && ibert::overlap(C, cbytes, residual, ibert::span(d.M, d.ldr, d.N, 1)))) return IBERT_ERR_SHAPE;
+    ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.N, d.K, bias, mult, shift, C, d.ldc);
+    g.w[0] = weights->w;
+    g.scales[0] = weights->scales;
+    g.zeros[0] = weights->zeros;
+    g.R = residual; g.ldr = d.ldr;
+    g.res_m = d.residual_dy.m; g.res_s = d.residual_dy.s;
+    g.out_dtype = d.out_dtype; g.out_clamp = d.out_clamp;
+    return ibert::launch_w4(g, weights->group, weights->zeros != nullptr, false, static_cast<hipStream_t>(stream));
+}

@@ -276,4 +276,113 @@ int ibert_paged_attention_from_scales(double S_q, double S_k, double S_v, double
     return ibert_dyadic_from_double(S_v / S_out / 65536.0, &out->out_dy);
 }
 
+size_t ibert_w4_bytes(int32_t N, int32_t K)
+{
+    if (N < 1 || N > (1 << 24) || K < 1 || K > (1 << 17)) return 0;
+    return (size_t)((N + 15) / 16) * ((K + 127) / 128) * 1024;
+}
+
+size_t ibert_w4_scale_bytes(int32_t N, int32_t K, int32_t group)
+{
+    if (group != 32 && group != 64 && group != 128) return 0;
+    return ibert_w4_bytes(N, K) / 1024 * 16 * (128 / group);
+}
+
+int ibert_w4_pack(const int8_t* w, const uint8_t* scales, const int8_t* zeros, int32_t N, int32_t K, int32_t group,
+                  uint8_t* w_out, uint8_t* scales_out, int8_t* zeros_out)
+{
+    const size_t bytes = ibert_w4_bytes(N, K), sbytes = ibert_w4_scale_bytes(N, K, group);
+    if (bytes == 0) return IBERT_ERR_SHAPE;
+    if (sbytes == 0) return IBERT_ERR_PARAM_RANGE;
+    if (!w || !scales || !w_out || !scales_out || (zeros && !zeros_out)) return IBERT_ERR_NULL;
+    const int64_t groups = (K + group - 1) / group, chunks = (K + 127) / 128, per = 128 / group;
+    for (int64_t i = 0; i < (int64_t)N * K; ++i)
+        if (w[i] < -8 || w[i] > 7) return IBERT_ERR_PARAM_RANGE;
+    if (zeros)
+        for (int64_t i = 0; i < (int64_t)N * groups; ++i)
+            if (zeros[i] < -8 || zeros[i] > 7) return IBERT_ERR_PARAM_RANGE;
+    std::memset(w_out, 0, bytes);
+    std::memset(scales_out, 0, sbytes);
+    if (zeros) std::memset(zeros_out, 0, sbytes);
+    for (int64_t n = 0; n < N; ++n) {
+        const int64_t tile = n / 16 * chunks, r = n % 16;
+        for (int64_t k = 0; k < K; ++k) {
+            uint8_t* const b = w_out + (tile + k / 128) * 1024 + k % 32 / 8 * 256 + r * 16 + k % 64 / 32 * 8 + k % 8;
+            *b = (uint8_t)(*b | ((uint32_t)(w[n * K + k] & 15) << (k % 128 < 64 ? 0 : 4)));
+        }
+        for (int64_t gi = 0; gi < groups; ++gi) {
+            const int64_t at = ((tile + gi / per) * 16 + r) * per + gi % per;
+            scales_out[at] = scales[n * groups + gi];
+            if (zeros) zeros_out[at] = zeros[n * groups + gi];
+        }
+    }
+    return IBERT_OK;
+}
+
+int ibert_w4_from_float(const double* x, int32_t N, int32_t K, int32_t group, int8_t* w, uint8_t* scales, double* S_w)
+{
+    if (ibert_w4_bytes(N, K) == 0) return IBERT_ERR_SHAPE;
+    if (ibert_w4_scale_bytes(N, K, group) == 0) return IBERT_ERR_PARAM_RANGE;
+    if (!x || !w || !scales || !S_w) return IBERT_ERR_NULL;
+    const int64_t groups = (K + group - 1) / group;
+    for (int64_t i = 0; i < (int64_t)N * K; ++i)
+        if (!std::isfinite(x[i])) return IBERT_ERR_PARAM_RANGE;
+    for (int64_t n = 0; n < N; ++n) {
+        const double* const row = x + n * K;
+        auto top_of = [&](int64_t g) {
+            double top = 0.0;
+            for (int64_t k = g * group; k < K && k < (g + 1) * group; ++k) top = std::fmax(top, std::fabs(row[k]));
+            return top;
+        };
+        double top = 0.0;
+        for (int64_t g = 0; g < groups; ++g) top = std::fmax(top, top_of(g));
+        const double S = top == 0.0 ? 1.0 : top / (7.0 * 255.0);
+        if (!std::isnormal(S)) return IBERT_ERR_PARAM_RANGE;
+        S_w[n] = S;
+        for (int64_t g = 0; g < groups; ++g) {
+            const double t = top_of(g);
+            const double s = t == 0.0 ? 0.0 : std::fmin(255.0, std::fmax(1.0, std::nearbyint(t / 7.0 / S)));
+            scales[n * groups + g] = (uint8_t)s;
+            for (int64_t k = g * group; k < K && k < (g + 1) * group; ++k) {
+                const double q = s == 0.0 ? 0.0 : std::nearbyint(row[k] / (s * S));
+                w[n * K + k] = (int8_t)std::fmax(-7.0, std::fmin(7.0, q));
+            }
+        }
+    }
+    return IBERT_OK;
+}
+
+int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up, double S_out, ibert_gate_params* out)
+{
+    if (!out) return IBERT_ERR_NULL;
+    if (activation != IBERT_GATE_SILU && activation != IBERT_GATE_GELU) return IBERT_ERR_PARAM_RANGE;
+    if (!(S_up > 0.0) || !(S_out > 0.0)) return IBERT_ERR_PARAM_RANGE;
+    std::memset(out, 0, sizeof *out);
+    out->activation = activation;
+    double S_a = IBERT_SILU_SCALE;
+    if (activation == IBERT_GATE_GELU) {
+        if (!(S_gate > 0.0)) return IBERT_ERR_PARAM_RANGE;
+        S_a = S_gate / 4.0;
+        const int rc = ibert_gelu_params_from_scale(S_gate, S_a, &out->gelu);
+        if (rc) return rc;
+    }
+    return ibert_dyadic_from_double(S_a * S_up / S_out, &out->out_dy);
+}
+
+int ibert_logits_row_from_reals(double S, double repetition, double presence, double frequency, int32_t mask, ibert_logits_row* out)
+{
+    if (!out) return IBERT_ERR_NULL;
+    if (!(S > 0.0) || !std::isfinite(S) || !(repetition > 0.0) || !std::isfinite(repetition)) return IBERT_ERR_PARAM_RANGE;
+    const double p = std::nearbyint(presence / S), f = std::nearbyint(frequency / S);
+    if (!(std::fabs(p) < 2147483648.0) || !(std::fabs(f) < 2147483648.0)) return IBERT_ERR_PARAM_RANGE;
+    int rc = ibert_dyadic_from_double(1.0 / repetition, &out->up);
+    if (rc) return rc;
+    rc = ibert_dyadic_from_double(repetition, &out->down);
+    if (rc) return rc;
+    out->presence = (int32_t)p;
+    out->frequency = (int32_t)f;
+    out->mask = mask;
+    return IBERT_OK;
+}
+
 }  // extern "C"

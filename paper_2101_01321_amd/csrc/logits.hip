@@ -1,0 +1,147 @@
+// Logits of the vocabulary before Softmax or a choice: penalties for repeated tokens, biases, grammar masks.
+//
+// A workgroup takes a slice of one row's vocabulary.  It counts the row's tokens that fall into the slice, and adds up the biases there, in
+// LDS (integer atomics: any order gives the same), then passes over the logits once.  The history is read once per slice, from L2.
+#include "common.h"
+
+namespace ibert {
+
+struct LogitsArgs {
+    const int32_t* x;
+    int32_t* y;
+    const ibert_logits_row* params;
+    const int32_t* tokens;
+    const int32_t* token_start;
+    const int32_t* out_start;
+    const int32_t* bias_ids;
+    const int32_t* bias_values;
+    const int32_t* bias_start;
+    const uint32_t* masks;
+    int64_t ldx, ldy;
+    int32_t vocab, num_tokens, num_biases, num_masks, ld_mask;
+    int32_t slice, slices;         // tokens of a slice (a multiple of 32); slices of a row
+    int32_t vec;                   // rows allow 16-byte loads and stores
+};
+
+constexpr int LOGITS_THREADS = 256;
+constexpr uint32_t SEEN = 0x80000000u;         // in the prompt; the low bits count what has been produced
+
+__device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t bias, const ibert_logits_row& p, int32_t us, int32_t ds)
+{
+    if (x == INT32_MIN) return x;
+    int64_t v = x;
+    if (count) {
+        v = dyadic64(x, x > 0 ? p.up.m : p.down.m, x > 0 ? us : ds);
+        v = v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v);
+        const int64_t n = count & ~SEEN;
+        v -= (n ? (int64_t)p.presence : 0) + p.frequency * n;
+    }
+    v += bias;
+    return (int32_t)(v <= INT32_MIN ? INT32_MIN + 1 : (v > INT32_MAX ? INT32_MAX : v));
+}
+
+__global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArgs g)
+{
+    extern __shared__ __align__(16) unsigned long long room[];
+    const int tid = threadIdx.x, row = blockIdx.x / g.slices, t0 = (blockIdx.x - row * g.slices) * g.slice;
+    const int n = min(g.slice, g.vocab - t0);
+    const ibert_logits_row p = g.params[row];
+    int ts = 0, te = 0, made = 0, bs = 0, be = 0;
+    if (g.num_tokens > 0) {
+        ts = clamp_i32(g.token_start[row], 0, g.num_tokens);
+        te = clamp_i32(g.token_start[row + 1], ts, g.num_tokens);
+        made = clamp_i32(g.out_start[row], ts, te);
+    }
+    if (g.num_biases > 0) {
+        bs = clamp_i32(g.bias_start[row], 0, g.num_biases);
+        be = clamp_i32(g.bias_start[row + 1], bs, g.num_biases);
+    }
+    const bool biased = be > bs;
+    unsigned long long* const bias = room;                          // [slice], where there are biases at all
+    uint32_t* const count = reinterpret_cast<uint32_t*>(room + (g.num_biases > 0 ? g.slice : 0));
+    for (int i = tid; i < n; i += LOGITS_THREADS) {
+        count[i] = 0;
+        if (biased) bias[i] = 0;
+    }
+    __syncthreads();
+    for (int i = ts + tid; i < te; i += LOGITS_THREADS) {
+        const uint32_t t = (uint32_t)(g.tokens[i] - t0);
+        if (t < (uint32_t)n) {
+            if (i >= made) atomicAdd(&count[t], 1u);
+            else atomicOr(&count[t], SEEN);
+        }
+    }
+    for (int i = bs + tid; i < be; i += LOGITS_THREADS) {
+        const uint32_t t = (uint32_t)(g.bias_ids[i] - t0);
+        if (t < (uint32_t)n) atomicAdd(&bias[t], (unsigned long long)(int64_t)g.bias_values[i]);
+    }
+    __syncthreads();
+    const int32_t us = clamp_i32(p.up.s, 0, 62), ds = clamp_i32(p.down.s, 0, 62);
+    const uint32_t* const mask = g.num_masks > 0 && p.mask >= 0 ? g.masks + (int64_t)min(p.mask, g.num_masks - 1) * g.ld_mask : nullptr;
+    const int32_t* const x = g.x + (int64_t)row * g.ldx + t0;
+    int32_t* const y = g.y + (int64_t)row * g.ldy + t0;
+    auto one = [&](int i, int32_t v, uint32_t word) {
+        return mask && !((word >> ((t0 + i) & 31)) & 1u) ? INT32_MIN : adjusted(v, count[i], biased ? (int64_t)bias[i] : 0, p, us, ds);
+    };
+    typedef int v4i __attribute__((ext_vector_type(4)));
+    if (g.vec) {
+        for (int i = 4 * tid; i + 4 <= n; i += 4 * LOGITS_THREADS) {
+            const uint32_t word = mask ? mask[(t0 + i) >> 5] : 0;
+            v4i v = *reinterpret_cast<const v4i*>(x + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = one(i + e, v[e], word);
+            *reinterpret_cast<v4i*>(y + i) = v;
+        }
+    }
+    for (int i = (g.vec ? n & ~3 : 0) + tid; i < n; i += LOGITS_THREADS) y[i] = one(i, x[i], mask ? mask[(t0 + i) >> 5] : 0);
+}
+
+static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
+{
+    g.slice = 2048;
+    g.slices = (g.vocab + g.slice - 1) / g.slice;
+    const size_t lds = (size_t)g.slice * (g.num_biases > 0 ? 12 : 4);
+    // (a launch may have 2^32 threads at most: pieces of rows)
+    const int64_t most = (1 << 23) / g.slices < 1 ? 1 : (1 << 23) / g.slices;
+    for (int64_t r0 = 0; r0 < rows; r0 += most) {
+        const int64_t n = rows - r0 < most ? rows - r0 : most;
+        LogitsArgs a = g;
+        a.x += r0 * g.ldx;
+        a.y += r0 * g.ldy;
+        a.params += r0;
+        if (a.token_start) a.token_start += r0;
+        if (a.out_start) a.out_start += r0;
+        if (a.bias_start) a.bias_start += r0;
+        hipLaunchKernelGGL(logits_adjust_kernel, dim3((unsigned)(n * g.slices)), dim3(LOGITS_THREADS), lds, stream, a);
+        IBERT_LAUNCH_CHECK("logits_adjust_kernel");
+    }
+    g_last_kernel = "logits_adjust_kernel";
+    return IBERT_OK;
+}
+
+}  // namespace ibert
+
+extern "C" int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_t* x, const ibert_logits_row* params, const int32_t* tokens,
+                                     const int32_t* token_start, const int32_t* out_start, const int32_t* bias_ids, const int32_t* bias_values,
+                                     const int32_t* bias_start, const uint32_t* masks, int32_t* y, void* stream)
+{
+    if (!desc) return IBERT_ERR_NULL;
+    const ibert_logits_desc& d = *desc;
+    if (d.rows < 0 || d.vocab < 0 || d.vocab > (1 << 26) || d.num_tokens < 0 || d.num_tokens > (1 << 30) || d.num_biases < 0 || d.num_biases > (1 << 30) ||
+        d.num_masks < 0 || d.ldx < d.vocab || d.ldy < d.vocab || (d.num_masks > 0 && d.ld_mask < (d.vocab + 31) / 32)) return IBERT_ERR_SHAPE;
+    if (d.rows == 0 || d.vocab == 0) return IBERT_OK;
+    if (!x || !y || !params || (d.num_tokens > 0 && (!tokens || !token_start || !out_start)) ||
+        (d.num_biases > 0 && (!bias_ids || !bias_values || !bias_start)) || (d.num_masks > 0 && !masks)) return IBERT_ERR_NULL;
+    const uintptr_t px = reinterpret_cast<uintptr_t>(x), py = reinterpret_cast<uintptr_t>(y);
+    const uint64_t sx = 4 * ((uint64_t)(d.rows - 1) * (uint64_t)d.ldx + d.vocab), sy = 4 * ((uint64_t)(d.rows - 1) * (uint64_t)d.ldy + d.vocab);
+    if (!(px == py && d.ldx == d.ldy) && px < py + sy && py < px + sx) return IBERT_ERR_SHAPE;
+    ibert::LogitsArgs g{};
+    g.x = x; g.y = y; g.params = params;
+    if (d.num_tokens > 0) { g.tokens = tokens; g.token_start = token_start; g.out_start = out_start; }
+    if (d.num_biases > 0) { g.bias_ids = bias_ids; g.bias_values = bias_values; g.bias_start = bias_start; }
+    g.masks = masks;
+    g.ldx = d.ldx; g.ldy = d.ldy;
+    g.vocab = d.vocab; g.num_tokens = d.num_tokens; g.num_biases = d.num_biases; g.num_masks = d.num_masks; g.ld_mask = d.ld_mask;
+    g.vec = ibert::aligned(x, 16) && ibert::aligned(y, 16) && d.ldx % 4 == 0 && d.ldy % 4 == 0;
+    return ibert::launch_logits(g, d.rows, static_cast<hipStream_t>(stream));
+}

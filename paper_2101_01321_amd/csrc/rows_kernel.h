@@ -1,0 +1,300 @@
+// Products of few activation rows with weight matrices that are read once: 4-bit weights with group scales, and the INT8 weights of
+// a gated block; plain (bias, requantization, residual) or ending in the gated product.
+//
+//   * A wavefront owns 16 NT channels and every KS-th chunk of 128 of K; its weights come straight from memory into registers, a few
+//     chunks ahead, and are used once.  4-bit weights stand in memory as the matrix unit wants them: 1 KB a tile of 16 channels and
+//     chunk, 16 bytes a lane, whose low and high halves are the operands of two MFMAs.  A nibble shifted to the top of its byte is
+//     16 times its signed value, so that two operations on a dword unpack four weights, and the sums of a group (|sum| < 2^18) are
+//     shifted back.
+//   * The rows of A are staged in LDS in operand order, a slab of chunks at a time, bytes past K as zeros: what weights hold there
+//     does not matter.
+//   * sum_g s_g (sum_k a w - z_g sum_k a): the sum of a group's activations comes from an MFMA with ones, which leaves it in the lanes
+//     that need it.  Group terms are added by 24-bit multiply-adds in 32 bits, which hold 4096 values of K
+//     (4096 * 128 * 15 * 255 < 2^31), then in 64 bits in LDS, where the wavefronts of a workgroup meet: integer sums, any order.
+#pragma once
+#include <type_traits>
+
+#include "gate_math.h"
+
+namespace ibert {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+struct RowsArgs {
+    const int8_t* A;
+    int64_t lda;
+    int32_t M, N, K;               // N: output columns (of a gated block F)
+    const void* w[2];              // INT8 rows, or packed 4-bit weights: [0] all or the gate's, [1] the up projection's
+    const uint8_t* scales[2];
+    const int8_t* zeros[2];
+    int64_t ldw;
+    const int32_t* bias;
+    const int32_t* mult;
+    const int32_t* shift;
+    const int8_t* R;
+    int64_t ldr;
+    int32_t res_m, res_s;
+    void* C;
+    int64_t ldc;
+    int32_t out_dtype, out_clamp;
+    GateConst gate;
+    int32_t chunks, slab;          // chunks of 128 in K; of a slab (a multiple of KS * RING)
+    int32_t cg;                    // log2 of the groups of channels of a workgroup: 2^cg groups by KS = 8 >> cg shares of K
+    int32_t mp;                    // log2 of the rows held in LDS
+    int32_t a_vec, w_vec;          // 16-byte loads of A, of INT8 weights
+    int32_t across, down;          // workgroups over the channels and over the rows
+};
+
+constexpr int ROWS_THREADS = 512;
+// chunks of weights that a wavefront has under way
+constexpr int rows_ring(int mt) { return mt == 4 ? 2 : 4; }
+
+// 16 bytes of a buffer, zeros past its end.
+__device__ __forceinline__ v4i buffer_16(const void* base, uint32_t bytes, uint32_t offset)
+{
+    typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
+    const v4u v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 0);
+    return v4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
+}
+
+// 16 bytes of a row of n bytes at p from byte k on, zeros past its end; any alignment (memory is read unaligned here).
+__device__ __forceinline__ v4i bytes_16(const int8_t* p, int k, int n)
+{
+    union { v4i v; int8_t b[16]; } u;
+    if (k + 16 <= n) {
+        __builtin_memcpy(u.b, p + k, 16);
+        return u.v;
+    }
+    u.v = v4i{0, 0, 0, 0};
+    for (int i = 0; i < 16; ++i)
+        if (k + i < n) u.b[i] = p[k + i];
+    return u.v;
+}
+
+// W4: 4-bit weights in groups of G (ZERO: with zero points), else INT8 rows.  GATED: NT / 2 tiles of gate channels, then as many of the up projection.
+template <bool W4, int MT, int NT, int G, bool ZERO, bool GATED>
+__global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
+{
+    typedef std::conditional_t<W4, unsigned long long, unsigned int> sum_t;
+    constexpr int ROWS_RING = rows_ring(MT), NH = GATED ? NT / 2 : NT, GPC = W4 ? 128 / G : 1, WR = W4 ? 1 : 2;
+    static_assert(!GATED || NT % 2 == 0, "pairs of tiles");
+    extern __shared__ __align__(16) int8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const int cgi = wave & ((1 << g.cg) - 1), kg = wave >> g.cg, ks = 8 >> g.cg;
+    // workgroups go round the XCDs: those of the same channels stand on the same one, whose L2 then holds their weights
+    const int j = blockIdx.x >> 3, jc = j / g.down, bx = jc * 8 + (blockIdx.x & 7);
+    if (bx >= g.across) return;
+    const int cols = 16 * NT << g.cg, m0 = (j - jc * g.down) * (16 * MT), rows = min(16 * MT, g.M - m0);
+    const int b0 = bx * (16 * NH << g.cg), n0 = b0 + cgi * (16 * NH);        // first output column of the workgroup, of the wavefront
+    const int abytes = (g.slab << 7) << g.mp;
+    sum_t* const sums = reinterpret_cast<sum_t*>(lds + abytes);                         // [16 MT][cols]
+
+    // the tiles that lie past the last channel read the last one again: nothing of them is stored
+    const uint8_t *wp[NT], *sp[NT], *zp[NT];
+    uint32_t wbytes[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int half = t / NH, c = n0 + 16 * (t - half * NH);
+        if (W4) {
+            const int tile = min(c, g.N - 1) >> 4;
+            wp[t] = static_cast<const uint8_t*>(g.w[half]) + (int64_t)tile * g.chunks * 1024;
+            wbytes[t] = (uint32_t)g.chunks * 1024u;
+            sp[t] = g.scales[half] + (int64_t)tile * g.chunks * (16 * GPC);
+            zp[t] = ZERO ? reinterpret_cast<const uint8_t*>(g.zeros[half]) + (int64_t)tile * g.chunks * (16 * GPC) : nullptr;
+        } else {
+            const int first = min(c, g.N - 1), left = min(16, g.N - first);
+            wp[t] = static_cast<const uint8_t*>(g.w[0]) + (int64_t)(half * g.N + first) * g.ldw;
+            wbytes[t] = (uint32_t)((left - 1) * g.ldw + g.K);
+            sp[t] = zp[t] = nullptr;
+        }
+    }
+    struct Piece {
+        v4i w[WR];
+        uint32_t s, z;
+    };
+    auto load = [&](int t, int c) {
+        Piece p;
+        if constexpr (W4) {
+            p.w[0] = buffer_16(wp[t], wbytes[t], (uint32_t)c * 1024u + (uint32_t)lane * 16u);      // (zeros from the last chunk on, without a request)
+            const int at = (min(c, g.chunks - 1) * 16 + r) * GPC;
+            if (GPC == 4) p.s = *reinterpret_cast<const uint32_t*>(sp[t] + at);
+            else if (GPC == 2) p.s = *reinterpret_cast<const uint16_t*>(sp[t] + at);
+            else p.s = sp[t][at];
+            if constexpr (ZERO) {
+                if (GPC == 4) p.z = *reinterpret_cast<const uint32_t*>(zp[t] + at);
+                else if (GPC == 2) p.z = *reinterpret_cast<const uint16_t*>(zp[t] + at);
+                else p.z = zp[t][at];
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = 64 * h + 16 * q;
+                if (g.w_vec) p.w[h] = buffer_16(wp[t], wbytes[t], (uint32_t)(r * (int)g.ldw + k + c * 128));
+                else {
+                    const int half = t / NH, n = min(n0 + 16 * (t - half * NH) + r, g.N - 1);
+                    p.w[h] = bytes_16(static_cast<const int8_t*>(g.w[0]) + (int64_t)(half * g.N + n) * g.ldw, c * 128 + k, g.K);
+                }
+            }
+        }
+        return p;
+    };
+
+    Piece ring[ROWS_RING][NT];
+#pragma unroll
+    for (int i = 0; i < ROWS_RING; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) ring[i][t] = load(t, kg + i * ks);
+    for (int i = tid; i < 16 * MT * cols; i += ROWS_THREADS) sums[i] = 0;
+
+    v4i acc[MT][NT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[j][t] = v4i{0, 0, 0, 0};
+    auto flush = [&]() {
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    atomicAdd(&sums[(16 * j + 4 * q + e) * cols + cgi * 16 * NT + 16 * t + r], (sum_t)(int64_t)acc[j][t][e]);
+                acc[j][t] = v4i{0, 0, 0, 0};
+            }
+    };
+
+    int since = 0;                                                 // chunks in the 32-bit sums
+    const int mask = (1 << g.mp) - 1, qstep = 16 << g.mp;
+    for (int s0 = 0; s0 < g.chunks; s0 += g.slab) {
+        const int s1 = min(g.chunks, s0 + g.slab);
+        if (s0) __syncthreads();                                   // the slab before has been read
+        // ---- stage A: 16 bytes of a row at a time
+        for (int u = tid; u < ((s1 - s0) << 3) << g.mp; u += ROWS_THREADS) {
+            const int v = u & 7, row = (u >> 3) & mask, c = u >> (3 + g.mp), k = (s0 + c) * 128 + 16 * v;
+            if (row >= rows) continue;
+            const int8_t* p = g.A + (int64_t)(m0 + row) * g.lda;
+            const v4i x = g.a_vec && k + 16 <= g.K ? *reinterpret_cast<const v4i*>(p + k) : bytes_16(p, k, g.K);
+            int8_t* const at = lds + (c * 8 + (v >> 2) * 4) * qstep + row * 16;
+            if constexpr (W4) {
+                int8_t* const d = at + 2 * (v & 1) * qstep + ((v >> 1) & 1) * 8;
+                *reinterpret_cast<v2i*>(d) = v2i{x[0], x[1]};
+                *reinterpret_cast<v2i*>(d + qstep) = v2i{x[2], x[3]};
+            } else {
+                *reinterpret_cast<v4i*>(at + (v & 3) * qstep) = x;
+            }
+        }
+        __syncthreads();
+        for (int c0 = s0 + kg; c0 < s1; c0 += ks * ROWS_RING) {
+#pragma unroll
+            for (int i = 0; i < ROWS_RING; ++i) {
+                const int c = c0 + i * ks;
+                if (c < s1) {
+                    v4i xa[2][MT];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j)
+                            xa[h][j] = *reinterpret_cast<const v4i*>(lds + ((c - s0) * 8 + h * 4 + q) * qstep + ((16 * j + r) & mask) * 16);
+                    if constexpr (!W4) {
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int j = 0; j < MT; ++j)
+                                    acc[j][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[h][j], ring[i][t].w[h], acc[j][t], 0, 0, 0);
+                    } else {
+                        const v4i zero = {0, 0, 0, 0};
+                        constexpr int ONES = 0x01010101;
+                        // the sums of one group's products (or of its activations): group gi of the chunk, operands lo | hi
+                        auto group = [&](int j, int gi, const v4i& lo, const v4i& hi) {
+                            if (G == 128)
+                                return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[1][j], hi, __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[0][j], lo, zero, 0, 0, 0), 0, 0, 0);
+                            if (G == 64) return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[gi & 1][j], gi & 1 ? hi : lo, zero, 0, 0, 0);
+                            const v4i x = xa[gi >> 1][j], w = gi & 2 ? hi : lo;
+                            const int e = 2 * (gi & 1);
+                            const long xl = (long)(((uint64_t)(uint32_t)x[e + 1] << 32) | (uint32_t)x[e]), wl = (long)(((uint64_t)(uint32_t)w[e + 1] << 32) | (uint32_t)w[e]);
+                            return __builtin_amdgcn_mfma_i32_16x16x32_i8(xl, wl, zero, 0, 0, 0);
+                        };
+                        v4i sa[MT][GPC];
+                        if constexpr (ZERO) {
+                            const v4i ones = {ONES, ONES, ONES, ONES};
+#pragma unroll
+                            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                                for (int gi = 0; gi < GPC; ++gi) sa[j][gi] = group(j, gi, ones, ones);
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const v4i w = ring[i][t].w[0];
+                            v4i lo, hi;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                lo[e] = (int)(((uint32_t)w[e] << 4) & 0xf0f0f0f0u);
+                                hi[e] = (int)((uint32_t)w[e] & 0xf0f0f0f0u);
+                            }
+#pragma unroll
+                            for (int gi = 0; gi < GPC; ++gi) {
+                                const int32_t sc = (int32_t)((ring[i][t].s >> (8 * gi)) & 255u);
+                                int32_t zc = 0;
+                                if constexpr (ZERO) zc = (int32_t)(ring[i][t].z << (28 - 8 * gi)) >> 28;     // (four bits, signed)
+#pragma unroll
+                                for (int j = 0; j < MT; ++j) {
+                                    const v4i p = group(j, gi, lo, hi);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        int32_t d = p[e] >> 4;
+                                        if constexpr (ZERO) d -= smul24(zc, sa[j][gi][e]);
+                                        acc[j][t][e] = smad24(sc, d, acc[j][t][e]);
+                                    }
+                                }
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) ring[i][t] = load(t, c + ROWS_RING * ks);
+            }
+            since += ROWS_RING;
+            if (W4 && since + ROWS_RING > 32) {
+                flush();
+                since = 0;
+            }
+        }
+    }
+    flush();
+    __syncthreads();
+
+    // ---- epilogue: an output a thread and round
+    for (int i = tid; i < rows * (16 * NH << g.cg); i += ROWS_THREADS) {
+        const int m = i / (16 * NH << g.cg), nn = i - m * (16 * NH << g.cg), n = b0 + nn;
+        if (n >= g.N) continue;
+        const sum_t* const row = sums + m * cols;
+        auto value = [&](const sum_t* p, int ch) {
+            const int64_t b = g.bias ? g.bias[ch] : 0;
+            if constexpr (!W4) return (int32_t)((uint32_t)*p + (uint32_t)b);
+            else {
+                const int64_t v = (int64_t)*p + b;
+                return (int32_t)(v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v));
+            }
+        };
+        const int64_t off = (int64_t)(m0 + m) * g.ldc + n;
+        if constexpr (GATED) {
+            const int wv = nn / (16 * NH), in = nn - wv * (16 * NH);
+            const int32_t ag = value(row + wv * 16 * NT + in, n), au = value(row + wv * 16 * NT + 16 * NH + in, g.N + n);
+            static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(ag, au, g.mult[n], g.shift[n], g.mult[g.N + n], g.shift[g.N + n], g.gate);
+        } else {
+            int64_t v = dyadic64(value(row + nn, n), g.mult[n], g.shift[n]);
+            if (g.R) v += dyadic64(g.R[(int64_t)(m0 + m) * g.ldr + n], g.res_m, g.res_s);
+            const int32_t y = clamp_i64_to_i32(v, g.out_clamp);
+            if (g.out_dtype == IBERT_I8) static_cast<int8_t*>(g.C)[off] = (int8_t)y;
+            else if (g.out_dtype == IBERT_I16) static_cast<int16_t*>(g.C)[off] = (int16_t)y;
+            else static_cast<int32_t*>(g.C)[off] = y;
+        }
+    }
+}
+
+}  // namespace ibert

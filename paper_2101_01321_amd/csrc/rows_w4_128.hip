@@ -1,0 +1,8 @@
+// Products with 4-bit weights in groups of 128 values.
+#include "rows_launch.h"
+
+namespace ibert {
+
+IBERT_ROWS_UNIT(true, 128)
+
+}  // namespace ibert

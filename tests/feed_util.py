@@ -1,0 +1,230 @@
+"""Inputs of the gated block, the products with 4-bit weights and the logits' adjustment, and what they are by definition, in 64 bits with numpy."""
+import math
+
+import numpy as np
+
+from paper_2101_01321_amd import binding as B
+
+LOW, HIGH = -2 ** 31, 2 ** 31 - 1
+
+
+def dyadic(real):
+    return B.ibert_dyadic_from_double(real).tuple()
+
+
+def normal8(rng, std, *shape):
+    return np.clip(np.rint(rng.normal(0, std, shape)), -128, 127).astype(np.int8)
+
+
+def dy(x, m, s):
+    """DY of arrays of whole numbers; every product stays below 2^63."""
+    x, m, s = np.asarray(x, np.int64), np.asarray(m, np.int64), np.asarray(s, np.int64)
+    return (x * m + np.where(s > 0, np.int64(1) << np.maximum(s - 1, 0), 0)) >> s
+
+
+def product(a, w):
+    """a w^T of whole numbers, exact: binary64 holds every sum below 2^53."""
+    return np.rint(a.astype(np.float64) @ w.astype(np.float64).T).astype(np.int64)
+
+
+def sigmoid(d):
+    """The sigmoid of d steps of ln2/64, 15 bits, by the definition's own steps."""
+    z, f = d >> 6, d & 63
+    e = (((124 - f) ** 2 + 8180) * 2 + 2 ** z) // 2 ** (z + 1) if z < 16 else 0
+    return (23556 * 2 ** 15 + (23556 + e) // 2) // (23556 + e)
+
+
+SIGMOID = np.array([sigmoid(d) for d in range(1025)], np.int64)
+
+
+def gate(acc_g, acc_u, m, s, p):
+    """p: GateParams; m, s: [2F]."""
+    F = acc_g.shape[1]
+    g, u = dy(acc_g, m[:F], s[:F]), np.clip(dy(acc_u, m[F:], s[F:]), -32767, 32767)
+    if p.activation == B.GATE_SILU:
+        g = np.clip(g, -65535, 65535)
+        sig = SIGMOID[np.minimum((np.abs(g) + 8) >> 4, 1024)]
+        a = (g * np.where(g < 0, 2 ** 15 - sig, sig) + 2 ** 14) >> 15
+    else:
+        c = p.gelu
+        g = np.clip(g, -c.q_max, c.q_max)
+        poly = (np.minimum(np.abs(g), -c.q_b) + c.q_b) ** 2 + c.q_c
+        a = np.clip(dy(g * (np.sign(g) * poly + c.q_1), c.out.m, c.out.s), -32767, 32767)
+    return np.clip(dy(a * u, p.out_dy.m, p.out_dy.s), -127, 127).astype(np.int8)
+
+
+class Channels:
+    """Bias, multipliers and shifts of n channels that bring sums of deviation acc_std to about out_std."""
+
+    def __init__(self, rng, n, acc_std, out_std, bias=True):
+        pairs = [dyadic(out_std / acc_std * f) for f in rng.uniform(0.6, 1.6, n)]
+        self.m, self.s = np.array([p[0] for p in pairs], np.int32), np.array([p[1] for p in pairs], np.int32)
+        self.b = np.rint(rng.normal(0, acc_std / 3, n)).astype(np.int32) if bias else None
+
+    def join(self, other):
+        self.m, self.s = np.concatenate([self.m, other.m]), np.concatenate([self.s, other.s])
+        if self.b is not None:
+            self.b = np.concatenate([self.b, other.b])
+        return self
+
+    def bias(self):
+        return 0 if self.b is None else self.b.astype(np.int64)
+
+
+class W4:
+    """4-bit weights [N, K] with their group scales and zero points."""
+
+    def __init__(self, rng, N, K, group, zeros, std=3.0):
+        self.group, self.N, self.K = group, N, K
+        G = -(-K // group)
+        self.w = np.clip(np.rint(rng.normal(0, std, (N, K))), -8, 7).astype(np.int8)
+        self.s = rng.integers(0, 256, (N, G)).astype(np.uint8)
+        self.z = rng.integers(-8, 8, (N, G)).astype(np.int8) if zeros else None
+
+    def whole(self):
+        up = lambda x: np.repeat(x.astype(np.int64), self.group, 1)[:, :self.K]      # noqa: E731
+        w = self.w.astype(np.int64)
+        return (w - (0 if self.z is None else up(self.z))) * up(self.s)
+
+    def pack(self):
+        return B.ibert_w4_pack(self.w, self.s, self.z, self.group)
+
+
+def gate_params(act, acc_scale=1.0):
+    """Constants of a block whose gates have a deviation of about 2, and what the channels have to bring the sums to."""
+    p = B.ibert_gate_params_from_scales(act, 1 / 200, 1 / 2000, 1 / 16)
+    return p, 2 / (B.SILU_SCALE if act == B.GATE_SILU else 1 / 200), 4000
+
+
+class Gated:
+    """One call of a gated block.  group None: INT8 weights.  ld: bytes behind a row of A, W and C; off: bytes in front."""
+
+    def __init__(self, seed, M, F, K, act, group=None, zeros=False, bias=True, ld=(0, 0, 0)):
+        rng = np.random.default_rng(seed)
+        self.M, self.F, self.K, self.act, self.group, self.ld = M, F, K, act, group, ld
+        self.a = normal8(rng, 40, M, K + ld[0])
+        self.params, gs, us = gate_params(act)
+        if group is None:
+            self.w = normal8(rng, 40, 2 * F, K + ld[1])
+            whole, std = self.w[:, :K], 1600 * math.sqrt(K)
+        else:
+            self.g4, self.u4 = W4(rng, F, K, group, zeros), W4(rng, F, K, group, zeros)
+            whole, std = np.concatenate([self.g4.whole(), self.u4.whole()]), 40 * 150 * (6 if zeros else 3) * math.sqrt(K)
+        self.ch = Channels(rng, F, std, gs, bias).join(Channels(rng, F, std, us, bias))
+        self.acc = np.clip(product(self.a[:, :K], whole) + self.ch.bias(), LOW, HIGH)
+        self.c0 = rng.integers(-127, 128, (M, F + ld[2])).astype(np.int8)
+
+    def expected(self):
+        out = self.c0.copy()
+        if self.M and self.F:
+            out[:, :self.F] = gate(self.acc[:, :self.F], self.acc[:, self.F:], self.ch.m, self.ch.s, self.params)
+        return out
+
+    def desc(self):
+        return B.GatedDesc(self.M, self.F, self.K, self.K + self.ld[0], self.K + self.ld[1], self.F + self.ld[2], self.params)
+
+
+class Rows4:
+    """One call of ibert_gemm_w4_requant."""
+
+    def __init__(self, seed, M, N, K, group, zeros=False, out="i16", residual=False, bias=True, ld=(0, 0, 0), extreme=False):
+        rng = np.random.default_rng(seed)
+        self.M, self.N, self.K, self.ld, self.out = M, N, K, ld, out
+        self.a = normal8(rng, 40, M, K + ld[0])
+        self.w4 = W4(rng, N, K, group, zeros)
+        if extreme:
+            self.a[:] = -128
+            self.w4.w[:] = -8
+            self.w4.s[:] = 255
+            if zeros:
+                self.w4.z[:] = 7
+        std = 40 * 150 * (6 if zeros else 3) * math.sqrt(K)
+        self.clamp, target = {"i8": (127, 40), "i16": (32767, 9000), "i32": (HIGH, 2e6)}[out]
+        self.ch = Channels(rng, N, std, target, bias)
+        self.r = normal8(rng, 40, M, N + ld[2]) if residual else None
+        self.res_dy = dyadic(50.0)
+        self.acc = np.clip(product(self.a[:, :K], self.w4.whole()) + self.ch.bias(), LOW, HIGH)
+        self.dtype = {"i8": np.int8, "i16": np.int16, "i32": np.int32}[out]
+        self.c0 = rng.integers(-99, 99, (M, N + ld[1])).astype(self.dtype)
+
+    def expected(self):
+        v = dy(self.acc, self.ch.m, self.ch.s)
+        if self.r is not None:
+            v = v + dy(self.r[:, :self.N], *self.res_dy)
+        out = self.c0.copy()
+        out[:, :self.N] = np.clip(v, -self.clamp, self.clamp)
+        return out
+
+    def desc(self):
+        return B.W4Desc(self.M, self.N, self.K, {"i8": B.I8, "i16": B.I16, "i32": B.I32}[self.out], self.K + self.ld[0], self.N + self.ld[1], self.N + self.ld[2],
+                        self.clamp, B.Dyadic(*self.res_dy))
+
+
+class Logits:
+    """One call of ibert_logits_adjust_i.  lens, blens: tokens and biases of each row."""
+
+    def __init__(self, seed, lens, vocab, blens=None, masks=0, ld=(0, 0, 0), std=300.0):
+        rng = np.random.default_rng(seed)
+        rows = len(lens)
+        blens = [0] * rows if blens is None else blens
+        self.rows, self.vocab, self.ld, self.num_masks = rows, vocab, ld, masks
+        self.x = np.rint(rng.normal(0, std, (rows, vocab + ld[0]))).astype(np.int32)
+        if vocab > 8:
+            for r in range(rows):                # what a row may hold at its ends
+                self.x[r, rng.choice(vocab, 4, False)] = (LOW, HIGH, LOW + 1, 0)
+        self.start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        self.made = (self.start[:-1] + (np.array(lens) * rng.random(rows)).astype(np.int32)).astype(np.int32)
+        self.tokens = np.minimum(vocab - 1, vocab * rng.random(self.start[-1]) ** 3).astype(np.int32)
+        if self.tokens.size > 3:                 # numbers that are no token
+            self.tokens[rng.integers(0, self.tokens.size, 3)] = (-1, vocab, LOW)
+        self.bstart = np.concatenate([[0], np.cumsum(blens)]).astype(np.int32)
+        self.ids = rng.integers(-2, vocab + 2, self.bstart[-1]).astype(np.int32)
+        if self.ids.size > 2:
+            self.ids[1] = self.ids[0] = rng.integers(0, vocab)      # a token named twice
+        self.values = rng.choice([1, -500, 700, HIGH, LOW, 3], self.bstart[-1]).astype(np.int32)
+        words = -(-vocab // 32) + ld[2]
+        self.masks = rng.integers(0, 2 ** 32, (masks, words)).astype(np.uint32)
+        if masks > 1:
+            self.masks[1] = 0                    # a grammar that leaves nothing
+        pick = [-1, -2 ** 31] + list(range(masks)) + [masks + 3] if masks else [-1, 0, 5]
+        pen = [1.0, 1.2, 0.8, 1e6, 2.0 ** -30]
+        self.params = np.zeros((rows, 7), np.int32)
+        for r in range(rows):
+            q = pen[int(rng.integers(0, len(pen)))]
+            up, down = dyadic(1 / q), dyadic(q)
+            self.params[r] = (*up, *down, rng.choice([0, 50, -20, HIGH]), rng.choice([0, 7, -3, LOW]), pick[(r + seed) % len(pick)])
+        self.y0 = rng.integers(-99, 99, (rows, vocab + ld[1])).astype(np.int32)
+
+    def expected(self, y0=None):
+        out = (self.y0 if y0 is None else y0).copy()
+        for r in range(self.rows):
+            um, us, dm, ds, presence, frequency, mask = (int(v) for v in self.params[r])
+            us, ds = min(max(us, 0), 62), min(max(ds, 0), 62)
+            ts, te = (min(max(int(v), 0), self.tokens.size) for v in self.start[r:r + 2])
+            te = max(te, ts)
+            made = min(max(int(self.made[r]), ts), te)
+            inside = lambda t: t[(t >= 0) & (t < self.vocab)]      # noqa: E731
+            seen = set(inside(self.tokens[ts:te]).tolist())
+            n = np.bincount(inside(self.tokens[made:te]), minlength=self.vocab)
+            bias = {}
+            b0 = min(max(int(self.bstart[r]), 0), self.ids.size)
+            b1 = max(b0, min(max(int(self.bstart[r + 1]), 0), self.ids.size))
+            for t, v in zip(self.ids[b0:b1].tolist(), self.values[b0:b1].tolist()):
+                bias[t] = bias.get(t, 0) + v
+            mask = None if mask < 0 or not self.num_masks else self.masks[min(mask, self.num_masks - 1)]
+            for t in range(self.vocab):
+                v = int(self.x[r, t])
+                if v != LOW:
+                    if t in seen:
+                        m, s = (um, us) if v > 0 else (dm, ds)
+                        v = (v * m + (2 ** s) // 2) // 2 ** s if s else v * m
+                        v = min(max(v, LOW), HIGH) - (presence if n[t] else 0) - frequency * int(n[t])
+                    v = min(max(v + bias.get(t, 0), LOW + 1), HIGH)
+                if mask is not None and not (int(mask[t // 32]) >> (t % 32)) & 1:
+                    v = LOW
+                out[r, t] = v
+        return out
+
+    def desc(self):
+        return B.LogitsDesc(self.rows, self.vocab, self.vocab + self.ld[0], self.vocab + self.ld[1], self.tokens.size, self.ids.size, self.num_masks,
+                            self.masks.shape[1] if self.num_masks else 0)
