@@ -1,5 +1,6 @@
 // The gated feed-forward block and the products with 4-bit weights: argument checks, the choice of the kernel, and the INT8 gated block's
 // kernels for few rows.
+#include "gated_stream.h"
 #include "rows_launch.h"
 
 namespace ibert {
@@ -108,6 +109,8 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     if (!W) return IBERT_ERR_NULL;
     const ibert_gated_desc& d = *desc;
     if (ibert::overlap(C, ibert::span(d.M, d.ldc, d.F, 1), W, ibert::span(2 * (int64_t)d.F, d.ldw, d.K, 1))) return IBERT_ERR_SHAPE;
+    if ((ibert::g_rows_tiles == 0 || (ibert::g_rows_tiles < 0 && d.M > 128)) && ibert::gated_stream_ok(d, A, W))
+        return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, static_cast<hipStream_t>(stream));
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
     g.w[0] = W;
     g.ldw = d.ldw;

@@ -1,0 +1,11 @@
+// The persistent kernel of the INT8 gated block (gated_stream.hip): does it serve these operands, and its launch (validated arguments, M and F >= 1).
+#pragma once
+#include "common.h"
+
+namespace ibert {
+
+bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W);
+int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C,
+                        hipStream_t stream);
+
+}  // namespace ibert

@@ -1,0 +1,432 @@
+// The gated block for many tokens: the persistent workgroups of gemm_stream.h (streamed K steps of 128 bytes, two LDS stages, a step in
+// four phases by quadrants of the wavefront's tile), whose tile is 256 tokens by 128 channels of the gate and the same 128 of the up
+// projection.
+//
+//   * The first two MFMA blocks of a wavefront's four are rows of W_gate and the last two the same rows of W_up, so that the two halves of
+//     a step ("W first", "W second") bring one matrix each, and a lane ends up with gate and up sums of the same two neighbouring channels
+//     in registers: neither product is ever stored.
+//   * Rows of W are dealt to the LDS rows such that lane r of 16 has channels 2 r and 2 r + 1 of its wavefront's 32.
+//   * F and M may be ragged: operands, constants and output are buffers that end with the last row or channel.
+//   * SiLU's sigmoids are a table of 1025 entries of 16 bits in LDS, built once by every workgroup with the function it stands for.
+#include "gate_math.h"
+#include "gemm_stream.h"
+#include "gated_stream.h"
+
+namespace ibert {
+
+struct GatedStreamArgs {
+    const int8_t* A;
+    const int8_t* W;
+    const int32_t* bias;
+    const int32_t* mult;
+    const int32_t* shift;
+    int8_t* C;
+    int32_t M, F, nk;
+    int32_t lda, ldw, ldc;
+    int32_t tiles_m, bn;           // as in StreamArgs
+    uint32_t bn_magic;
+    int32_t xs, gs, per_xcd;
+    int32_t fast;                  // K * 127^2 < 2^30, the product's shift in [33, 62], and gelu_fast_ok where it is GELU
+    int32_t c_vec;                 // rows of C allow 16-byte stores
+    GateConst gate;
+};
+
+constexpr int GS_BM = 256, GS_BF = 128, GS_NW = 8;       // tokens and channels of a tile; wavefronts
+constexpr int GS_STAGE = (GS_BM + 2 * GS_BF) * 128;
+constexpr int GS_PAR = 2 * GS_STAGE;                     // two buffers of 3 x 256 constants
+constexpr int GS_TURN = GS_PAR + 2 * 3 * 256 * 4;        // rows on their way out: 32 rows of 32 bytes a wavefront
+constexpr int GS_PITCH = 48, GS_TURN_WAVE = 32 * GS_PITCH;
+constexpr int GS_SIG = GS_TURN + GS_NW * GS_TURN_WAVE;
+constexpr int GS_LDS = GS_SIG + 2064;
+
+template <bool SILU>
+__global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArgs g)
+{
+    constexpr int BM = GS_BM, BN = 256, NW = GS_NW, NT = 64 * NW, WR = 2, WC = 4;
+    constexpr int WM = BM / WR, WN = BN / WC, FM = WM / 16, FN = 4, FMH = FM / 2, FN0 = 2, FN1 = 2;
+    constexpr int QA = FMH * 2 * WR / NW, QW = FN0 * 2 * WC / NW, NQ = QA + QW;       // requests of a wavefront: A half, W half, a group
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm0 = wave % WR * WM, wn0 = wave / WR * WN;
+    const int frow = lane & 15, fch = lane >> 4;
+
+    // ---- the workgroup's tiles (see stream_run, stream_tile) ------------------------------------
+    const int xcd = blockIdx.x & 7, group = g.tiles_m * g.bn, xm = xcd >> g.xs, t0 = (int)(((int64_t)xm * group) >> g.gs);
+    const int first_col = (xcd & ((1 << g.xs) - 1)) * g.bn, count = (int)(((int64_t)(xm + 1) * group) >> g.gs) - t0;
+    const uint32_t kbytes = (uint32_t)g.nk * 128u;
+    int lt = blockIdx.x >> 3;
+    if (lt >= count) return;
+    auto tile_at = [&](int l, int& m0, int& n0) {
+        const int t = t0 + l, tm = udiv_fix(t, g.bn, g.bn_magic);
+        m0 = tm * BM;
+        n0 = (first_col + t - tm * g.bn) * GS_BF;
+    };
+
+    // ---- requests (see gemm_stream.h) -----------------------------------------------------------
+    const int r8 = lane >> 3;
+    const uint32_t chunk = (uint32_t)(((lane & 7) ^ (((wave & 1) << 2) | (r8 >> 1))) << 4);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
+    auto first_row = [&](int nb, int rows) { return wave / nb * rows + wave % nb * 8; };
+    constexpr int SA = NW / (FMH * 2) * WM, SW = NW / (FN0 * 2) * WN;                // rows of the stage from request to request
+    const int pa = first_row(FMH * 2, WM), pw = first_row(FN0 * 2, WN);              // (the up projection's: 32 rows of the stage on)
+    auto w_row = [&](int p) {                                      // channel, from the tile's first, that belongs in row p of the stage's W part
+        const int w = p / WN, r = p - w * WN, q = (r & 8) + r8;
+        return w * 32 + 2 * q + ((r >> 4) & 1);
+    };
+    uint32_t va[2][QA], vw[QW];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < QA; ++q) va[h][q] = (uint32_t)(pa + h * (WM / 2) + q * SA + r8) * (uint32_t)g.lda + chunk;
+#pragma unroll
+    for (int q = 0; q < QW; ++q) vw[q] = (uint32_t)w_row(pw + q * SW) * (uint32_t)g.ldw + chunk;
+    v4i da, dg, du;                                                // descriptors of the request stream's tile: A, gate, up
+    da[3] = dg[3] = du[3] = 0x00020000;
+    uint32_t koff = 0, kinc = 128, rstage = lds0;
+    int rlt = lt;
+    auto buffer = [](v4i& d, const void* p, uint32_t bytes) {
+        const uint64_t u = (uint64_t)(uintptr_t)p;
+        d[0] = (int32_t)(uint32_t)u;
+        d[1] = (int32_t)((uint32_t)(u >> 32) & 0xffffu);
+        d[2] = (int32_t)bytes;
+    };
+    auto request_tile = [&](int l) {
+        if (l < count) {
+            int m0, n0;
+            tile_at(l, m0, n0);
+            const int rows = g.M - m0 < BM ? g.M - m0 : BM, cols = g.F - n0 < GS_BF ? g.F - n0 : GS_BF;
+            buffer(da, g.A + (int64_t)m0 * g.lda, (uint32_t)rows * (uint32_t)g.lda);
+            buffer(dg, g.W + (int64_t)n0 * g.ldw, (uint32_t)cols * (uint32_t)g.ldw);
+            buffer(du, g.W + ((int64_t)g.F + n0) * g.ldw, (uint32_t)cols * (uint32_t)g.ldw);
+            kinc = 128;
+        } else {
+            da[2] = dg[2] = du[2] = 0;
+            kinc = 0;
+        }
+    };
+    auto request_one = [&](int h, int q) {
+        const bool is_a = q < QA;
+        const int k = is_a ? q : q - QA;
+        const int row = is_a ? h * (WM / 2) + k * SA : h * 32 + k * SW;
+        const uint32_t place = rstage + (uint32_t)((is_a ? pa : BM + pw) * 128);
+        asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
+                     :: "s"(place), "i"(row * 128), "v"(is_a ? va[h][is_a ? k : 0] : vw[is_a ? 0 : k]), "s"(is_a ? da : (h == 0 ? dg : du)), "s"(koff)
+                     : "memory", "m0", "scc");
+    };
+    auto request_advance = [&]() {
+        koff += kinc;
+        rstage = 2 * lds0 + (uint32_t)GS_STAGE - rstage;
+        if (koff == kbytes) {
+            koff = 0;
+            rlt += g.per_xcd;
+            request_tile(rlt);
+        }
+    };
+    // Constants of a tile: [bias, mult, shift][gate, up][128], by DMA, 64 dwords a request; zeros past the last channel.
+    int par_n0 = -1, par_buf = 1;
+    auto request_constants = [&](int n0) {
+        if (n0 == par_n0) return;
+        par_n0 = n0;
+        par_buf ^= 1;
+        const uint32_t base = lds0 + (uint32_t)(GS_PAR + par_buf * 3 * BN * 4);
+#pragma unroll
+        for (int a = 0; a < 3; ++a) {
+            const int32_t* src = a == 0 ? g.bias : (a == 1 ? g.mult : g.shift);
+            if (src) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if ((a * 4 + c) % NW == wave) {
+                        v4i d;
+                        buffer(d, src + (int64_t)(c >> 1) * g.F, (uint32_t)g.F * 4u);
+                        d[3] = 0x00020000;
+                        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                                     :: "s"(base + (uint32_t)((a * BN + c * 64) * 4)), "v"((uint32_t)(n0 + (c & 1) * 64 + lane) * 4u), "s"(d) : "memory", "m0");
+                    }
+            } else {
+                int32_t* p = reinterpret_cast<int32_t*>(lds + GS_PAR + par_buf * 3 * BN * 4) + a * BN;
+                int32_t fill = 0, c0 = tid;
+                asm volatile("" : "+s"(fill), "+v"(c0));
+                for (int c = c0; c < BN; c += NT) p[c] = fill;
+            }
+        }
+    };
+    constexpr auto vm = [](int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); };
+
+    v4i acc[FN][FM];
+    const int rd0 = frow * 128 + ((fch ^ ((frow >> 1) & 7)) << 4);
+    auto operand = [&](int sl, int off) { return *reinterpret_cast<const v4i*>(lds + off + (sl ? rd0 ^ 64 : rd0)); };
+    v4i at[FMH][2], ab[FMH][2], w0[FN0][2], w1[FN1][2];
+    int stage = 0;
+    auto read_a = [&](v4i (&d)[FMH][2], int st, int h, int q) { d[q >> 1][q & 1] = operand(q & 1, st + (wm0 + (h * FMH + (q >> 1)) * 16) * 128); };
+    auto read_w0 = [&](int st, int q) { w0[q >> 1][q & 1] = operand(q & 1, st + BM * 128 + (wn0 + (q >> 1) * 16) * 128); };
+    auto read_w1 = [&](int st, int q) { w1[q >> 1][q & 1] = operand(q & 1, st + BM * 128 + (wn0 + (FN0 + (q >> 1)) * 16) * 128); };
+
+    // ---- prologue -------------------------------------------------------------------------------
+    int m0, n0;
+    tile_at(lt, m0, n0);
+    request_constants(n0);
+    request_tile(lt);
+    auto request_two_steps = [&]() {
+#pragma unroll 1
+        for (int st = 0; st < 2; ++st) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) request_one(0, q);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) request_one(1, q);
+            request_advance();
+        }
+    };
+    request_two_steps();
+    if constexpr (SILU) {
+        uint16_t* const sig = reinterpret_cast<uint16_t*>(lds + GS_SIG);
+        for (int d = tid; d <= SIG_STEPS; d += NT) sig[d] = (uint16_t)sigmoid15((uint32_t)d);
+    }
+    __builtin_amdgcn_s_waitcnt(vm(2 * NQ));
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+    auto quadrant = [&](v4i (&xw)[2][2], int i0, v4i (&xa)[FMH][2], int j0, auto zero_tag, auto&& between) {
+        constexpr bool ZERO = decltype(zero_tag)::value;
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FMH; ++j) {
+                    between((sl * 2 + i) * FMH + j);
+                    __builtin_amdgcn_sched_barrier(0);
+                    acc[i0 + i][j0 + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[j][sl], xw[i][sl], ZERO && sl == 0 ? v4i{0, 0, 0, 0} : acc[i0 + i][j0 + j], 0, 0, 0);
+                }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int MQ = 4 * FMH;                                    // MFMAs of a quadrant
+    // One K step; REQ and wait as in gemm_stream.h.
+    auto step = [&](auto req_tag, bool wait) {
+        constexpr int REQ = decltype(req_tag)::value;
+        using Z = std::integral_constant<bool, REQ == 2>;
+        const int nst = GS_STAGE - stage;
+        auto ask = [&](int h, int n, int idx) {
+#pragma unroll
+            for (int r = 0; r < 2 * NQ; ++r)
+                if (r < n && idx == (2 * r + 1) * (2 * MQ) / (2 * n)) request_one(REQ == 2 ? (r < NQ ? 0 : 1) : h, REQ == 2 && r >= NQ ? r - NQ : r);
+        };
+        quadrant(w0, 0, at, 0, Z{}, [&](int idx) {
+            if (idx < 2 * FN1) read_w1(stage, idx);
+            if (REQ == 1) ask(0, NQ, idx);
+        });
+        quadrant(w1, FN0, at, 0, Z{}, [&](int idx) {
+            if (idx < 2 * FMH) read_a(ab, stage, 1, idx);
+            if (REQ == 1) ask(0, NQ, MQ + idx);
+        });
+        if (wait) __builtin_amdgcn_s_waitcnt(vm(REQ == 1 ? 2 * NQ : NQ));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        quadrant(w0, 0, ab, FMH, Z{}, [&](int idx) {
+            if (idx < 2 * FMH) read_a(at, nst, 0, idx);
+            ask(1, REQ == 2 ? 2 * NQ : NQ, idx);
+        });
+        quadrant(w1, FN0, ab, FMH, Z{}, [&](int idx) {
+            if (idx < 2 * FN0) read_w0(nst, idx);
+            ask(1, REQ == 2 ? 2 * NQ : NQ, MQ + idx);
+        });
+        request_advance();
+        if (wait) __builtin_amdgcn_s_waitcnt(vm(2 * NQ));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        stage = nst;
+    };
+
+    bool first = true;
+    using R1 = std::integral_constant<int, 1>;
+    using R2 = std::integral_constant<int, 2>;
+    for (;;) {
+#pragma unroll
+        for (int q = 0; q < 2 * FMH; ++q) read_a(at, stage, 0, q);
+#pragma unroll
+        for (int q = 0; q < 2 * FN0; ++q) read_w0(stage, q);
+        step(R2{}, first);
+        const int par_own = par_buf;
+        if (lt + g.per_xcd < count) {
+            int next_m0, next_n0;
+            tile_at(lt + g.per_xcd, next_m0, next_n0);
+            request_constants(next_n0);
+        }
+        for (uint32_t kt = 128; kt < kbytes; kt += 128) step(R1{}, true);
+
+        // ---- epilogue ---------------------------------------------------------------------------
+        // acc[i][j][e] (i < 2 gate, else up) = channel n0 + wn0 / 2 + 2 r16 + i % 2 of row m0 + wm0 + 16 j + 4 u + e
+        int el = lane;
+        asm volatile("" : "+v"(el));
+        const int r16 = el & 15, u = el >> 4, wf0 = wn0 / 2;
+        const int32_t* par = reinterpret_cast<const int32_t*>(lds + GS_PAR + par_own * 3 * BN * 4);
+        typedef const __attribute__((address_space(4))) GatedStreamArgs* kernel_args;
+#if defined(__HIP_DEVICE_COMPILE__)
+        kernel_args ga = (kernel_args)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(ga));
+#else
+        kernel_args ga = nullptr;
+#endif
+        const int last = ga->M - 1 - m0, rows = last < BM ? last : BM - 1;
+        const int cols = ga->F - n0 < GS_BF ? ga->F - n0 : GS_BF;
+        const int64_t out0 = (int64_t)m0 * ga->ldc + n0;
+        // Fast form: every shift of the tile's channels in [33, 62], every |bias| below 2^30, and `fast`.
+        bool fast;
+        {
+            bool ok = true;
+#pragma unroll
+            for (int c = 0; c < BN; c += 64) {
+                const int32_t ps = par[2 * BN + c + el], pb = par[c + el];
+                if ((c & 64) + el < cols) ok = ok && ps >= 33 && ps <= 62 && (pb ^ (pb << 1)) >= 0;
+            }
+            fast = __builtin_amdgcn_ballot_w64(!ok) == 0 && ga->fast;
+        }
+        if (fast) {
+            const auto cb = __builtin_amdgcn_make_buffer_rsrc(ga->C + out0, 0, (int)((uint32_t)rows * (uint32_t)ga->ldc + (uint32_t)cols), 0x00020000);
+            int64_t c0[FN];
+            int32_t mm[FN], sh[FN];
+#pragma unroll
+            for (int i = 0; i < FN; ++i) {
+                const int c = (i >> 1) * 128 + wf0 + 2 * r16 + (i & 1);
+                const int32_t b = par[c], s = par[2 * BN + c];
+                mm[i] = par[BN + c];
+                c0[i] = (int64_t)b * mm[i] + ((int64_t)1 << ((s - 1) & 63));
+                sh[i] = (s - 32) & 31;
+            }
+            const GeluConst gl{ga->gate.gelu.q_b, ga->gate.gelu.q_c, ga->gate.gelu.q_1, ga->gate.gelu.q_max, ga->gate.gelu.m, ga->gate.gelu.s};
+            const int32_t gl_rnd = 1 << ((gl.s - 33) & 31), gl_sh = (gl.s - 32) & 31;
+            const int32_t om = ga->gate.m, ornd = 1 << ((ga->gate.s - 33) & 31), osh = (ga->gate.s - 32) & 31;
+            const uint16_t* const sig = reinterpret_cast<const uint16_t*>(lds + GS_SIG);
+            int8_t* const turn = lds + GS_TURN + wave * GS_TURN_WAVE;
+            auto value = [&](int i, int n) { return (int32_t)(((int64_t)acc[i][n >> 2][n & 3] * mm[i] + c0[i]) >> 32) >> sh[i]; };
+            auto fence = []() { __builtin_amdgcn_wave_barrier(); };
+            typedef unsigned v4u __attribute__((ext_vector_type(4)));
+            constexpr int UNITS = FM / 2;
+            v4u mv[UNITS];
+            const int col = wf0 + (el & 1) * 16, mrow = el >> 1;   // piece and row of a unit that the lane moves
+            auto store = [&](int unit) __attribute__((always_inline)) {
+                const int at = (wm0 + unit * 32 + mrow) * ga->ldc + col;
+                if (ga->c_vec && col + 16 <= cols) __builtin_amdgcn_raw_buffer_store_b128(mv[unit], cb, at, 0, 0);
+                else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (col + e < cols) __builtin_amdgcn_raw_buffer_store_b8((uint8_t)(mv[unit][e >> 2] >> (8 * (e & 3))), cb, at + e, 0, 0);
+                }
+            };
+            // the result of token n's channel i (0 or 1)
+            auto result = [&](int n, int i) __attribute__((always_inline)) {
+                const int32_t up = med3_i32(value(2 + i, n), -32767, 32767);
+                int32_t a;
+                if constexpr (SILU) {
+                    const int32_t gt = med3_const<-65535, 65535>(value(i, n));
+                    a = silu_of(gt, sig[silu_step(gt)]);
+                } else {
+                    const int32_t q = med3_i32(value(i, n), -gl.q_max, gl.q_max);
+                    const int32_t v = min(max(q, -q), -gl.q_b) + gl.q_b;
+                    const int32_t poly = smad24(v, v, gl.q_c), sg = q >> 31;
+                    const int32_t t = smul24(q, ((poly ^ sg) - sg) + gl.q_1);
+                    a = med3_const<-32767, 32767>((__mulhi(t, gl.m) + gl_rnd) >> gl_sh);
+                }
+                return med3_const<-127, 127>((__mulhi(smul24(a, up), om) + ornd) >> osh);
+            };
+#pragma unroll
+            for (int unit = 0; unit < UNITS; ++unit) {
+                fence();
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const int32_t y0 = result(8 * unit + t, 0), y1 = result(8 * unit + t, 1);
+                    *reinterpret_cast<uint16_t*>(turn + (16 * (t / 4) + 4 * u + t % 4) * GS_PITCH + 2 * r16) = (uint16_t)((y0 & 0xff) | (y1 << 8));
+                    if (t % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+                }
+                fence();
+                mv[unit] = *reinterpret_cast<const v4u*>(turn + mrow * GS_PITCH + (el & 1) * 16);
+                // before the first store this wavefront's requests have all landed, so that the next tile's first step need not count stores among loads
+                if (unit == 1) __builtin_amdgcn_s_waitcnt(vm(0));
+                if (unit >= 1) store(unit - 1);
+            }
+            store(UNITS - 1);
+        } else {
+            // Any constants: a rolled loop, 16 rows of each row of wavefronts at a time through LDS, where the next tile's first steps had
+            // arrived -- they are requested again afterwards.
+            constexpr int SP = BN + 4;
+            int32_t* const st = reinterpret_cast<int32_t*>(lds);
+            __builtin_amdgcn_s_waitcnt(vm(0));
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 1
+            for (int j = 0; j < FM; ++j) {
+#pragma unroll
+                for (int k = 0; k < FM; ++k)
+                    if (k == j) {
+#pragma unroll
+                        for (int i = 0; i < FN; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) st[(wave % WR * 16 + 4 * u + e) * SP + (i >> 1) * 128 + wf0 + 2 * r16 + (i & 1)] = acc[i][k][e];
+                    }
+                __syncthreads();
+#pragma unroll 1
+                for (int q = wave * 64 + el; q < 16 * WR * GS_BF; q += NT) {
+                    const int r = q / GS_BF, c = q - r * GS_BF, row = (r >> 4) * WM + 16 * j + (r & 15);
+                    if (row > last || c >= cols) continue;
+                    const GateConst gc{ga->gate.silu, GeluConst{ga->gate.gelu.q_b, ga->gate.gelu.q_c, ga->gate.gelu.q_1, ga->gate.gelu.q_max, ga->gate.gelu.m, ga->gate.gelu.s},
+                                       ga->gate.m, ga->gate.s};
+                    ga->C[out0 + (int64_t)row * ga->ldc + c] =
+                        (int8_t)gate_one((int32_t)((uint32_t)st[r * SP + c] + (uint32_t)par[c]), (int32_t)((uint32_t)st[r * SP + 128 + c] + (uint32_t)par[128 + c]),
+                                         par[BN + c], par[2 * BN + c] & 63, par[BN + 128 + c], par[2 * BN + 128 + c] & 63, gc);
+                }
+                __syncthreads();
+            }
+            rlt = lt + g.per_xcd;
+            koff = 0;
+            rstage = lds0 + (uint32_t)stage;
+            request_tile(rlt);
+            request_two_steps();
+            __builtin_amdgcn_s_waitcnt(vm(0));
+            asm volatile("s_barrier" ::: "memory");
+        }
+        lt += g.per_xcd;
+        if (lt >= count) break;
+        tile_at(lt, m0, n0);
+        first = false;
+    }
+}
+
+bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W)
+{
+    return d.K % 128 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
+           (int64_t)((d.M + GS_BM - 1) / GS_BM) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
+}
+
+int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C,
+                        hipStream_t stream)
+{
+    GatedStreamArgs s;
+    s.A = A; s.W = W; s.bias = bias; s.mult = mult; s.shift = shift; s.C = C;
+    s.M = d.M; s.F = d.F; s.nk = d.K / 128;
+    s.lda = (int32_t)d.lda; s.ldw = (int32_t)d.ldw; s.ldc = (int32_t)d.ldc;
+    s.tiles_m = (d.M + GS_BM - 1) / GS_BM;
+    const int tiles_n = (d.F + GS_BF - 1) / GS_BF;
+    // as stream_shares and stream_deal
+    s.xs = 0;
+    while (s.xs < 2 && tiles_n % (2 << s.xs) == 0 && ((2 * (int64_t)d.F * d.K) >> s.xs) > (2 << 20) && s.tiles_m >= (8 >> s.xs)) ++s.xs;
+    s.gs = 3 - s.xs;
+    s.bn = tiles_n >> s.xs;
+    s.bn_magic = udiv_magic(s.bn);
+    const int64_t run = ((int64_t)s.tiles_m * s.bn + (1 << s.gs) - 1) >> s.gs;
+    s.per_xcd = (int32_t)(run < 32 ? run : 32);
+    const ibert_gate_params& p = d.gate;
+    s.gate = gate_const(p);
+    s.fast = (int64_t)d.K * 16129 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (s.gate.silu || gelu_fast_ok(p.gelu));
+    s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
+    static bool attr_done = false;
+    if (!attr_done) {
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(gated_stream_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(gated_stream_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
+        attr_done = true;
+    }
+    static_assert(GS_LDS <= 163840, "LDS of a workgroup");
+    const dim3 grid(8u * (unsigned)s.per_xcd), block(64 * GS_NW);
+    if (s.gate.silu) hipLaunchKernelGGL(gated_stream_kernel<true>, grid, block, GS_LDS, stream, s);
+    else hipLaunchKernelGGL(gated_stream_kernel<false>, grid, block, GS_LDS, stream, s);
+    IBERT_LAUNCH_CHECK("gated_stream_kernel");
+    g_last_kernel = s.gate.silu ? "gated_stream_kernel<true>" : "gated_stream_kernel<false>";
+    return IBERT_OK;
+}
+
+}  // namespace ibert

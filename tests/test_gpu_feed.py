@@ -9,7 +9,7 @@ import feed_util as U
 from test_gpu_decoder import libs, same
 
 
-@pytest.fixture(params=[(-1, -1), (1, 0), (1, 3), (2, 1), (2, 2)], ids=lambda p: "t%d_g%d" % p)
+@pytest.fixture(params=[(-1, -1), (1, 0), (1, 3), (2, 1), (2, 2), (0, 0)], ids=lambda p: "t%d_g%d" % p)
 def form(request, gpu):
     from paper_2101_01321_amd import binding as B
     B.ibert_rows_override(*request.param)
@@ -101,6 +101,54 @@ def test_w4(form, M, N, K, group, zeros):
     run(U.Rows4(M + N + K, M, N, K, group, zeros, out, residual=bool((N + zeros) % 2), bias=M % 3 != 0), "w4 %d x %d x %d, groups of %d, %s" % (M, N, K, group, out))
 
 
+@pytest.fixture
+def persistent(gpu):
+    from paper_2101_01321_amd import binding as B
+    B.ibert_rows_override(0, 0)
+    yield
+    B.ibert_rows_override(-1, -1)
+
+
+def ran(kernel):
+    from paper_2101_01321_amd import binding as B
+    assert B.lib().ibert_last_kernel().decode().startswith(kernel), B.lib().ibert_last_kernel()
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
+@pytest.mark.parametrize("M,F,K", [(256, 128, 128), (257, 129, 256), (300, 400, 384), (1000, 127, 1024), (511, 1, 256), (5150, 2050, 128), (4100, 4096, 384), (9000, 1300, 256)])
+def test_persistent_gated(persistent, M, F, K, act):
+    # ragged tokens and channels; up to two tiles and more to a workgroup, columns shared by XCDs or not
+    run(U.Gated(M + F + K + act, M, F, K, act), "persistent gated %d x %d x %d" % (M, F, K))
+    ran("gated_stream_kernel")
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
+@pytest.mark.parametrize("ld,off", [((16, 32, 16), 0), ((0, 0, 3), 0), ((0, 0, 8), 16), ((112, 0, 16), 16)])
+def test_persistent_gated_strides(persistent, ld, off, act):
+    run(U.Gated(act, 290, 200, 256, act, ld=ld), "persistent gated, strides %s, at %d" % (ld, off), off)
+    ran("gated_stream_kernel")
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
+def test_persistent_gated_any_constants(persistent, act):
+    # shifts below 33, biases of 31 bits and an output shift below 33 take the general epilogue, tile by tile; the tiles beside them do not
+    c = U.Gated(7 + act, 5000, 1400, 128, act)
+    c.ch.m[200], c.ch.s[200] = 3, 1
+    c.ch.b[1400 + 700] = U.HIGH
+    c.ch.m[1300], c.ch.s[1300] = 1, 0
+    c.ch.m[1400 + 5], c.ch.s[1400 + 5] = U.LOW, 62
+    acc = U.product(c.a, c.w) + c.ch.bias()
+    c.acc = (acc + 2 ** 31) % 2 ** 32 - 2 ** 31
+    run(c, "persistent gated, any constants")
+    ran("gated_stream_kernel")
+    c = U.Gated(9 + act, 700, 300, 256, act, bias=False)
+    c.params.out_dy.m, c.params.out_dy.s = 1, 20
+    run(c, "persistent gated, a small shift")
+    if act:
+        c.params.gelu.out.m, c.params.gelu.out.s = -3, 32
+        run(c, "persistent gated, gelu's small shift")
+
+
 @pytest.mark.parametrize("off", [0, 1, 4, 13])
 @pytest.mark.parametrize("ld", [(0, 0, 0), (16, 32, 16), (3, 5, 7), (12, 4, 1)])
 def test_rows_at_any_address(gpu, ld, off):
@@ -175,11 +223,11 @@ def test_dtype_and_rows_that_are_not_there(gpu):
     assert torch.equal(before, d.out)
 
 
-@pytest.mark.parametrize("kind", ["gated", "w4_gated", "w4"])
+@pytest.mark.parametrize("kind", ["gated", "persistent", "w4_gated", "w4"])
 def test_streams_and_graphs(gpu, kind):
     # two calls at once on streams of their own; then both captured, replayed between eager calls with other inputs
     torch, G, B = libs()
-    make = {"gated": lambda i: U.Gated(i, 37, 200, 512, i % 2), "w4_gated": lambda i: U.Gated(i, 3, 200, 512, i % 2, 64, True),
+    make = {"gated": lambda i: U.Gated(i, 37, 200, 512, i % 2), "persistent": lambda i: U.Gated(i, 700, 1000, 256, i % 2), "w4_gated": lambda i: U.Gated(i, 3, 200, 512, i % 2, 64, True),
             "w4": lambda i: U.Rows4(i, 9, 300, 1024, 128, False, "i16", True)}[kind]
     d = [OnDevice(make(i)) for i in range(2)]
     streams = [torch.cuda.Stream() for _ in d]
