@@ -6,6 +6,8 @@
 
 namespace ibert {
 
+typedef int v4i __attribute__((ext_vector_type(4)));
+
 struct LogitsArgs {
     const int32_t* x;
     int32_t* y;
@@ -19,11 +21,12 @@ struct LogitsArgs {
     const uint32_t* masks;
     int64_t ldx, ldy;
     int32_t vocab, num_tokens, num_biases, num_masks, ld_mask;
-    int32_t slice, slices;         // tokens of a slice (a multiple of 32); slices of a row
+    int32_t slices;                // of a row
     int32_t vec;                   // rows allow 16-byte loads and stores
 };
 
-constexpr int LOGITS_THREADS = 256;
+// Threads of a workgroup, tokens of its slice.  The logits of a slice (8 a thread) are requested first and arrive while the history is counted.
+constexpr int LOGITS_THREADS = 512, LOGITS_SLICE = 4096;
 constexpr uint32_t SEEN = 0x80000000u;         // in the prompt; the low bits count what has been produced
 
 __device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t bias, const ibert_logits_row& p, int32_t us, int32_t ds)
@@ -43,9 +46,25 @@ __device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t b
 __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArgs g)
 {
     extern __shared__ __align__(16) unsigned long long room[];
-    const int tid = threadIdx.x, row = blockIdx.x / g.slices, t0 = (blockIdx.x - row * g.slices) * g.slice;
-    const int n = min(g.slice, g.vocab - t0);
+    const int tid = threadIdx.x, row = blockIdx.x / g.slices, t0 = (blockIdx.x - row * g.slices) * LOGITS_SLICE;
+    const int n = min(LOGITS_SLICE, g.vocab - t0);
     const ibert_logits_row p = g.params[row];
+    const uint32_t* const mask = g.num_masks > 0 && p.mask >= 0 ? g.masks + (int64_t)min(p.mask, g.num_masks - 1) * g.ld_mask : nullptr;
+    const int32_t* const x = g.x + (int64_t)row * g.ldx + t0;
+    int32_t* const y = g.y + (int64_t)row * g.ldy + t0;
+    constexpr int PER = LOGITS_SLICE / (4 * LOGITS_THREADS);
+    v4i logits[PER];
+    uint32_t words[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = 4 * (k * LOGITS_THREADS + tid);
+        logits[k] = v4i{0, 0, 0, 0};
+        words[k] = 0;
+        if (g.vec && i + 4 <= n) {
+            logits[k] = *reinterpret_cast<const v4i*>(x + i);
+            if (mask) words[k] = mask[(t0 + i) >> 5];
+        }
+    }
     int ts = 0, te = 0, made = 0, bs = 0, be = 0;
     if (g.num_tokens > 0) {
         ts = clamp_i32(g.token_start[row], 0, g.num_tokens);
@@ -57,19 +76,41 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
         be = clamp_i32(g.bias_start[row + 1], bs, g.num_biases);
     }
     const bool biased = be > bs;
-    unsigned long long* const bias = room;                          // [slice], where there are biases at all
-    uint32_t* const count = reinterpret_cast<uint32_t*>(room + (g.num_biases > 0 ? g.slice : 0));
+    unsigned long long* const bias = room;                          // [LOGITS_SLICE], where there are biases at all
+    uint32_t* const count = reinterpret_cast<uint32_t*>(room + (g.num_biases > 0 ? LOGITS_SLICE : 0));
     for (int i = tid; i < n; i += LOGITS_THREADS) {
         count[i] = 0;
         if (biased) bias[i] = 0;
     }
     __syncthreads();
-    for (int i = ts + tid; i < te; i += LOGITS_THREADS) {
-        const uint32_t t = (uint32_t)(g.tokens[i] - t0);
-        if (t < (uint32_t)n) {
+    // (four tokens to a load, 16-byte aligned ones: what lies in front of the row's first or behind its last is left out)
+    auto token = [&](int i, int32_t id) {
+        const uint32_t t = (uint32_t)(id - t0);
+        if (t < (uint32_t)n && i >= ts && i < te) {
             if (i >= made) atomicAdd(&count[t], 1u);
             else atomicOr(&count[t], SEEN);
         }
+    };
+    const int lead = (int)((reinterpret_cast<uintptr_t>(g.tokens + ts) >> 2) & 3);
+    const int32_t* const tokens = g.tokens + ts - lead;
+    for (int i = 4 * tid; i < te - ts + lead; i += 8 * LOGITS_THREADS) {
+        v4i a[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int at = i + 4 * k * LOGITS_THREADS;
+            a[k] = v4i{-1, -1, -1, -1};
+            // (the words around a row's own are read only where they are tokens of the array)
+            if (ts - lead + at >= 0 && ts - lead + at + 4 <= g.num_tokens) a[k] = *reinterpret_cast<const v4i*>(tokens + at);
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (ts - lead + at + e >= ts && ts - lead + at + e < te) a[k][e] = tokens[at + e];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) token(ts - lead + i + 4 * k * LOGITS_THREADS + e, a[k][e]);
     }
     for (int i = bs + tid; i < be; i += LOGITS_THREADS) {
         const uint32_t t = (uint32_t)(g.bias_ids[i] - t0);
@@ -77,19 +118,17 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
     }
     __syncthreads();
     const int32_t us = clamp_i32(p.up.s, 0, 62), ds = clamp_i32(p.down.s, 0, 62);
-    const uint32_t* const mask = g.num_masks > 0 && p.mask >= 0 ? g.masks + (int64_t)min(p.mask, g.num_masks - 1) * g.ld_mask : nullptr;
-    const int32_t* const x = g.x + (int64_t)row * g.ldx + t0;
-    int32_t* const y = g.y + (int64_t)row * g.ldy + t0;
     auto one = [&](int i, int32_t v, uint32_t word) {
         return mask && !((word >> ((t0 + i) & 31)) & 1u) ? INT32_MIN : adjusted(v, count[i], biased ? (int64_t)bias[i] : 0, p, us, ds);
     };
-    typedef int v4i __attribute__((ext_vector_type(4)));
     if (g.vec) {
-        for (int i = 4 * tid; i + 4 <= n; i += 4 * LOGITS_THREADS) {
-            const uint32_t word = mask ? mask[(t0 + i) >> 5] : 0;
-            v4i v = *reinterpret_cast<const v4i*>(x + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = one(i + e, v[e], word);
+        for (int k = 0; k < PER; ++k) {
+            const int i = 4 * (k * LOGITS_THREADS + tid);
+            if (i + 4 > n) continue;
+            v4i v = logits[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = one(i + e, v[e], words[k]);
             *reinterpret_cast<v4i*>(y + i) = v;
         }
     }
@@ -98,9 +137,8 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
 
 static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
 {
-    g.slice = 2048;
-    g.slices = (g.vocab + g.slice - 1) / g.slice;
-    const size_t lds = (size_t)g.slice * (g.num_biases > 0 ? 12 : 4);
+    g.slices = (g.vocab + LOGITS_SLICE - 1) / LOGITS_SLICE;
+    const size_t lds = (size_t)LOGITS_SLICE * (g.num_biases > 0 ? 12 : 4);
     // (a launch may have 2^32 threads at most: pieces of rows)
     const int64_t most = (1 << 23) / g.slices < 1 ? 1 : (1 << 23) / g.slices;
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
