@@ -686,7 +686,7 @@ int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up
  * [num_tokens]; token_start: device int32 [rows + 1]; out_start: device int32 [rows]; both NULL where num_tokens = 0.  bias_ids, bias_values: device int32
  * [num_biases], bias_start: device int32 [rows + 1]; a token may be named more than once.  masks: device uint32 [num_masks, ld_mask], bit t % 32 of word t / 32.
  * Starts are clamped into [0, num_tokens] ([0, num_biases]) and into order; token numbers outside [0, vocab) are ignored; shifts outside [0, 62] are clamped into it.
- * Errors: IBERT_ERR_SHAPE (negative sizes, num_tokens or num_biases > 2^30, vocab > 2^26, ldx or ldy < vocab, ld_mask < ceil(vocab / 32), x and y overlap), IBERT_ERR_NULL.
+ * Errors: IBERT_ERR_SHAPE (negative sizes, num_tokens or num_biases >= 2^30, vocab > 2^26, ldx or ldy < vocab, ld_mask < ceil(vocab / 32), x and y overlap), IBERT_ERR_NULL.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
     ibert_dyadic up, down;

@@ -237,7 +237,7 @@ def logits_desc(**change):
 
 def test_logits_refuse():
     for change in ({"rows": -1}, {"vocab": -1}, {"vocab": (1 << 26) + 1, "ldx": 1 << 27, "ldy": 1 << 27, "ld_mask": 1 << 23}, {"ldx": 99}, {"ldy": 99}, {"num_tokens": -1},
-                   {"num_tokens": (1 << 30) + 1}, {"num_biases": -1}, {"num_biases": (1 << 30) + 1}, {"num_masks": -1}, {"ld_mask": 3}):
+                   {"num_tokens": 1 << 30}, {"num_biases": -1}, {"num_biases": 1 << 30}, {"num_masks": -1}, {"ld_mask": 3}):
         assert logits(logits_desc(**change)) == -2, change
     assert logits(None) == -1
     for name in ("x", "p", "tok", "ts", "os", "ids", "vals", "bs", "masks", "y"):
