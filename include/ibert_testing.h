@@ -66,9 +66,10 @@ void ibert_paged_attention_override(int32_t form);
  * negative: what is faster for the rows (the default).  The result never depends on it.  Process-wide, not thread-safe. */
 void ibert_rotary_override(int32_t heads);
 
-/* Which kernels the gated block and the products with 4-bit weights run: `tiles` of 16 channels to a wavefront (1 or 2; the gated block takes pairs of them) and
- * 2^`groups` groups of channels to a workgroup (0 to 3), or tiles = 0: the persistent kernel of the INT8 gated block where it can run at all.  Negative: what is faster
- * (the default).  The result never depends on it.  Process-wide, not thread-safe. */
+/* Which kernels the gated block and the products with 4-bit weights run: `tiles` = 1 or 2 tiles of 16 channels to a wavefront (the gated block takes pairs of them) and
+ * 2^`groups` groups of channels to a workgroup (0 to 3); tiles = 9 or 10: the kernel of 4-bit weights whose wavefronts have rings of their own, with one or two tiles and 8 x `groups`
+ * (1, 2, 4, 8) rows to a workgroup, where it can run; tiles = 0: the persistent kernel of the INT8 gated block where it can run.  Negative: what is faster (the default).  The result
+ * never depends on it.  Process-wide, not thread-safe. */
 void ibert_rows_override(int32_t tiles, int32_t groups);
 
 /* Steps 1 to 4 of a layer as one kernel: 0 never; a tile (1000 wavefronts + 100 MFMA rows of one + 10 sequences + stages, one of those ibert_qkv_attention_plan names)

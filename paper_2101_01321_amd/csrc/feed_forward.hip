@@ -12,25 +12,28 @@ IBERT_ROWS_UNIT(false, 128)
 
 static int g_rows_tiles = -1, g_rows_groups = -1;
 
-static RowsPlan plan_rows(int32_t M, int32_t N, int32_t K, bool gated)
+static RowsPlan plan_rows(int32_t M, int32_t N)
 {
-    RowsPlan p;
+    RowsPlan p{};
     p.mt = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
-    p.nt = g_rows_tiles >= 1 ? (g_rows_tiles > 2 ? 2 : g_rows_tiles) : 1;
+    p.nt = g_rows_tiles >= 1 ? ((g_rows_tiles & 3) > 1 ? 2 : 1) : 1;
     p.cg = 0;
     if (g_rows_groups >= 0) p.cg = g_rows_groups > 3 ? 3 : g_rows_groups;
     else {
         const int64_t down = (M + 16 * p.mt - 1) / (16 * p.mt);
         while (p.cg < 3 && down * ((N + (32 * p.nt << p.cg) - 1) / (32 * p.nt << p.cg)) >= 512) ++p.cg;
     }
-    (void)K;
-    (void)gated;
     return p;
 }
 
 static int launch_w4(const RowsArgs& g, int32_t group, bool zeros, bool gated, hipStream_t stream)
 {
-    const RowsPlan p = plan_rows(g.M, g.N, g.K, gated);
+    RowsPlan p = plan_rows(g.M, g.N);
+    int per;
+    size_t lds;
+    p.br = g.M <= 8 ? 1 : (g.M <= 16 ? 2 : 4);
+    if (g_rows_tiles >= 8 && g_rows_groups >= 1) p.br = g_rows_groups;
+    p.ring = (g_rows_tiles < 0 || g_rows_tiles >= 8) && ring_stages(g, p.br, (gated ? 2 : 1) * p.nt, group, zeros, &per, &lds) > 0;
     if (group == 32) return launch_rows<true, 32>(g, p, zeros, gated, stream);
     if (group == 64) return launch_rows<true, 64>(g, p, zeros, gated, stream);
     return launch_rows<true, 128>(g, p, zeros, gated, stream);
@@ -116,7 +119,7 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     g.ldw = d.ldw;
     g.w_vec = ibert::aligned(W, 16) && d.ldw % 16 == 0 && d.K % 16 == 0 && d.ldw <= (1 << 26);
     g.gate = ibert::gate_const(d.gate);
-    return ibert::launch_rows<false, 128>(g, ibert::plan_rows(d.M, d.F, d.K, true), false, true, static_cast<hipStream_t>(stream));
+    return ibert::launch_rows<false, 128>(g, ibert::plan_rows(d.M, d.F), false, true, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A, const ibert_w4_weights* gate, const ibert_w4_weights* up,

@@ -73,6 +73,79 @@ __device__ __forceinline__ v4i bytes_16(const int8_t* p, int k, int n)
     return u.v;
 }
 
+// acc += the products of a chunk: activations xa (two halves of the chunk), packed weights w of NT tiles, their scales and zero points.
+template <int MT, int NT, int G, bool ZERO>
+__device__ __forceinline__ void chunk_products(v4i (&acc)[MT][NT], const v4i (&xa)[2][MT], const v4i (&w)[NT], const uint32_t (&sc)[NT], const uint32_t (&zc)[NT])
+{
+    constexpr int GPC = 128 / G;
+    const v4i zero = {0, 0, 0, 0};
+    // the sums of one group's products (or of its activations): group gi of the chunk, operands lo | hi
+    auto group = [&](int j, int gi, const v4i& lo, const v4i& hi) {
+        if (G == 128)
+            return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[1][j], hi, __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[0][j], lo, zero, 0, 0, 0), 0, 0, 0);
+        if (G == 64) return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[gi & 1][j], gi & 1 ? hi : lo, zero, 0, 0, 0);
+        const v4i x = xa[gi >> 1][j], y = gi & 2 ? hi : lo;
+        const int e = 2 * (gi & 1);
+        const long xl = (long)(((uint64_t)(uint32_t)x[e + 1] << 32) | (uint32_t)x[e]), yl = (long)(((uint64_t)(uint32_t)y[e + 1] << 32) | (uint32_t)y[e]);
+        return __builtin_amdgcn_mfma_i32_16x16x32_i8(xl, yl, zero, 0, 0, 0);
+    };
+    v4i sa[MT][GPC];
+    if constexpr (ZERO) {
+        constexpr int ONES = 0x01010101;
+        const v4i ones = {ONES, ONES, ONES, ONES};
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int gi = 0; gi < GPC; ++gi) sa[j][gi] = group(j, gi, ones, ones);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        v4i lo, hi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            lo[e] = (int)(((uint32_t)w[t][e] << 4) & 0xf0f0f0f0u);
+            hi[e] = (int)((uint32_t)w[t][e] & 0xf0f0f0f0u);
+        }
+#pragma unroll
+        for (int gi = 0; gi < GPC; ++gi) {
+            const int32_t s = (int32_t)((sc[t] >> (8 * gi)) & 255u);
+            int32_t z = 0;
+            if constexpr (ZERO) z = (int32_t)(zc[t] << (28 - 8 * gi)) >> 28;           // (four bits, signed)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const v4i p = group(j, gi, lo, hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    int32_t d = p[e] >> 4;
+                    if constexpr (ZERO) d -= smul24(z, sa[j][gi][e]);
+                    acc[j][t][e] = smad24(s, d, acc[j][t][e]);
+                }
+            }
+        }
+    }
+}
+
+// Output (m, n) from its sums (of a gated block: gate and up projection).
+template <bool GATED>
+__device__ __forceinline__ void rows_finish(const RowsArgs& g, int m, int n, int64_t s0, int64_t s1)
+{
+    auto value = [&](int64_t v, int ch) {
+        v += g.bias ? g.bias[ch] : 0;
+        return (int32_t)(v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v));
+    };
+    const int64_t off = (int64_t)m * g.ldc + n;
+    if constexpr (GATED) {
+        static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(value(s0, n), value(s1, g.N + n), g.mult[n], g.shift[n], g.mult[g.N + n], g.shift[g.N + n], g.gate);
+    } else {
+        int64_t v = dyadic64(value(s0, n), g.mult[n], g.shift[n]);
+        if (g.R) v += dyadic64(g.R[(int64_t)m * g.ldr + n], g.res_m, g.res_s);
+        const int32_t y = clamp_i64_to_i32(v, g.out_clamp);
+        if (g.out_dtype == IBERT_I8) static_cast<int8_t*>(g.C)[off] = (int8_t)y;
+        else if (g.out_dtype == IBERT_I16) static_cast<int16_t*>(g.C)[off] = (int16_t)y;
+        else static_cast<int32_t*>(g.C)[off] = y;
+    }
+}
+
 // W4: 4-bit weights in groups of G (ZERO: with zero points), else INT8 rows.  GATED: NT / 2 tiles of gate channels, then as many of the up projection.
 template <bool W4, int MT, int NT, int G, bool ZERO, bool GATED>
 __global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
@@ -207,52 +280,15 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
                                 for (int j = 0; j < MT; ++j)
                                     acc[j][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[h][j], ring[i][t].w[h], acc[j][t], 0, 0, 0);
                     } else {
-                        const v4i zero = {0, 0, 0, 0};
-                        constexpr int ONES = 0x01010101;
-                        // the sums of one group's products (or of its activations): group gi of the chunk, operands lo | hi
-                        auto group = [&](int j, int gi, const v4i& lo, const v4i& hi) {
-                            if (G == 128)
-                                return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[1][j], hi, __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[0][j], lo, zero, 0, 0, 0), 0, 0, 0);
-                            if (G == 64) return __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[gi & 1][j], gi & 1 ? hi : lo, zero, 0, 0, 0);
-                            const v4i x = xa[gi >> 1][j], w = gi & 2 ? hi : lo;
-                            const int e = 2 * (gi & 1);
-                            const long xl = (long)(((uint64_t)(uint32_t)x[e + 1] << 32) | (uint32_t)x[e]), wl = (long)(((uint64_t)(uint32_t)w[e + 1] << 32) | (uint32_t)w[e]);
-                            return __builtin_amdgcn_mfma_i32_16x16x32_i8(xl, wl, zero, 0, 0, 0);
-                        };
-                        v4i sa[MT][GPC];
-                        if constexpr (ZERO) {
-                            const v4i ones = {ONES, ONES, ONES, ONES};
-#pragma unroll
-                            for (int j = 0; j < MT; ++j)
-#pragma unroll
-                                for (int gi = 0; gi < GPC; ++gi) sa[j][gi] = group(j, gi, ones, ones);
-                        }
+                        v4i w[NT];
+                        uint32_t sc[NT], zc[NT];
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            const v4i w = ring[i][t].w[0];
-                            v4i lo, hi;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                lo[e] = (int)(((uint32_t)w[e] << 4) & 0xf0f0f0f0u);
-                                hi[e] = (int)((uint32_t)w[e] & 0xf0f0f0f0u);
-                            }
-#pragma unroll
-                            for (int gi = 0; gi < GPC; ++gi) {
-                                const int32_t sc = (int32_t)((ring[i][t].s >> (8 * gi)) & 255u);
-                                int32_t zc = 0;
-                                if constexpr (ZERO) zc = (int32_t)(ring[i][t].z << (28 - 8 * gi)) >> 28;     // (four bits, signed)
-#pragma unroll
-                                for (int j = 0; j < MT; ++j) {
-                                    const v4i p = group(j, gi, lo, hi);
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        int32_t d = p[e] >> 4;
-                                        if constexpr (ZERO) d -= smul24(zc, sa[j][gi][e]);
-                                        acc[j][t][e] = smad24(sc, d, acc[j][t][e]);
-                                    }
-                                }
-                            }
+                            w[t] = ring[i][t].w[0];
+                            sc[t] = ring[i][t].s;
+                            if constexpr (ZERO) zc[t] = ring[i][t].z;
                         }
+                        chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
                     }
                 }
 #pragma unroll
@@ -273,27 +309,157 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
         const int m = i / (16 * NH << g.cg), nn = i - m * (16 * NH << g.cg), n = b0 + nn;
         if (n >= g.N) continue;
         const sum_t* const row = sums + m * cols;
-        auto value = [&](const sum_t* p, int ch) {
-            const int64_t b = g.bias ? g.bias[ch] : 0;
-            if constexpr (!W4) return (int32_t)((uint32_t)*p + (uint32_t)b);
-            else {
-                const int64_t v = (int64_t)*p + b;
-                return (int32_t)(v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v));
-            }
+        auto sum = [&](const sum_t& v) { return W4 ? (int64_t)v : (int64_t)(int32_t)v; };
+        const int wv = nn / (16 * NH), in = nn - wv * (16 * NH);
+        rows_finish<GATED>(g, m0 + m, n, sum(row[GATED ? wv * 16 * NT + in : nn]), sum(row[GATED ? wv * 16 * NT + 16 * NH + in : nn]));
+    }
+}
+
+// The same for aligned rows of A and K a multiple of 16: nothing in the loop waits for another wavefront.
+//   * The eight wavefronts of a workgroup share K in contiguous runs of chunks.  Each has a ring of stages of its own in LDS -- 1 KB blocks of eight rows of A by
+//     128 bytes, and of a tile's chunk of weights -- into which it requests straight from memory as many chunks ahead as LDS holds; scales (and zero points) of its
+//     whole run come first.  The sums (a run is at most 4096 values: 32 bits) meet in LDS at the end.
+//   * A's 16-byte units are swizzled by the row (see swz in gemm_kernel.h); a lane's operand is two reads of eight bytes, 32 apart.
+// BR: blocks of eight rows (1, 2, 4 or 8); NT, G, ZERO, GATED: see rows_kernel.
+template <int BR, int NT, int G, bool ZERO, bool GATED>
+__global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
+{
+    constexpr int MT = (BR + 1) / 2, NH = GATED ? NT / 2 : NT, GPC = 128 / G, NL = BR + NT, STAGE = NL * 1024;
+    constexpr int TM = 8 * BR, PITCH = 16 * NT + 4;                // rows of the tile; dwords of a row of sums
+    constexpr int EP = (TM * 16 * NH + ROWS_THREADS - 1) / ROWS_THREADS;
+    constexpr int SUMS = TM * PITCH * 4;                           // bytes of a wavefront's sums, where its stages were
+    static_assert(3 * NL < 64, "outstanding requests");
+    extern __shared__ __align__(16) int8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const int jb = blockIdx.x >> 3, jc = jb / g.down, bx = jc * 8 + (blockIdx.x & 7);
+    if (bx >= g.across) return;
+    const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
+    const int per = g.slab, c0 = wave * per, run = min(per, g.chunks - c0);           // this wavefront's chunks [c0, c0 + run)
+    const int stages = g.mp, scb = (per * 16 * GPC + 255) & ~255;                       // bytes of a tile's scales
+    const int own = (ZERO ? 2 : 1) * NT * scb + max(stages * STAGE, SUMS);
+    int8_t* const home = lds + wave * own;
+    const uint32_t home0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds + (uint32_t)(wave * own);
+    const uint32_t ring0 = home0 + (uint32_t)((ZERO ? 2 : 1) * NT * scb);
+    int8_t* const ring = home + (ZERO ? 2 : 1) * NT * scb;
+
+    if (run > 0) {
+        const uint8_t* wp[NT];
+        const int64_t tbytes = (int64_t)g.chunks * 1024;
+        // (tiles past the last channel read the last one again)
+        auto tile_of = [&](int t) { return min(n0 + 16 * (t % NH), g.N - 1) >> 4; };
+#pragma unroll
+        for (int t = 0; t < NT; ++t) wp[t] = static_cast<const uint8_t*>(g.w[t / NH]) + tile_of(t) * tbytes;
+        // scales of the run, 64 dwords a request; what lies past the tile's last reads as zeros
+        auto buffer = [](const void* p, uint32_t bytes) {
+            const uint64_t u = (uint64_t)(uintptr_t)p;
+            return v4i{(int32_t)(uint32_t)u, (int32_t)((uint32_t)(u >> 32) & 0xffffu), (int32_t)bytes, 0x00020000};
         };
-        const int64_t off = (int64_t)(m0 + m) * g.ldc + n;
-        if constexpr (GATED) {
-            const int wv = nn / (16 * NH), in = nn - wv * (16 * NH);
-            const int32_t ag = value(row + wv * 16 * NT + in, n), au = value(row + wv * 16 * NT + 16 * NH + in, g.N + n);
-            static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(ag, au, g.mult[n], g.shift[n], g.mult[g.N + n], g.shift[g.N + n], g.gate);
-        } else {
-            int64_t v = dyadic64(value(row + nn, n), g.mult[n], g.shift[n]);
-            if (g.R) v += dyadic64(g.R[(int64_t)(m0 + m) * g.ldr + n], g.res_m, g.res_s);
-            const int32_t y = clamp_i64_to_i32(v, g.out_clamp);
-            if (g.out_dtype == IBERT_I8) static_cast<int8_t*>(g.C)[off] = (int8_t)y;
-            else if (g.out_dtype == IBERT_I16) static_cast<int16_t*>(g.C)[off] = (int16_t)y;
-            else static_cast<int32_t*>(g.C)[off] = y;
+        const uint32_t sbytes = (uint32_t)(g.chunks * 16 * GPC);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int z = 0; z < (ZERO ? 2 : 1); ++z) {
+                const void* src = z ? static_cast<const void*>(g.zeros[t / NH]) : static_cast<const void*>(g.scales[t / NH]);
+                const v4i d = buffer(static_cast<const uint8_t*>(src) + (int64_t)tile_of(t) * sbytes, sbytes);
+                for (int k = 0; k < scb; k += 256)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                                 :: "s"(home0 + (uint32_t)((z * NT + t) * scb + k)), "v"((uint32_t)(c0 * 16 * GPC + k + 4 * lane)), "s"(d) : "memory", "m0");
+            }
+        // requests of a chunk: BR blocks of A (rows past the last read that one again; bytes past K zeros), NT of weights
+        const v4i da = buffer(g.A + (int64_t)m0 * g.lda, (uint32_t)((rows - 1) * (int)g.lda + g.K));
+        const int lr8 = lane >> 3, lp = lane & 7;
+        const int unit0 = lp ^ (lr8 >> 1), unit1 = unit0 ^ 4;
+        uint32_t va[BR];
+#pragma unroll
+        for (int b = 0; b < BR; ++b) va[b] = (uint32_t)(min(8 * b + lr8, rows - 1) * (int)g.lda + (b & 1 ? unit1 : unit0) * 16);
+        const int left0 = g.K - unit0 * 16, left1 = g.K - unit1 * 16;
+        auto request = [&](int chunk, int st) {
+            const int c = __builtin_amdgcn_readfirstlane(chunk);   // (the same in every lane: the compiler loses sight of it)
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)ring0 + st * STAGE);
+#pragma unroll
+            for (int b = 0; b < BR; ++b)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                             :: "s"(to + (uint32_t)(b * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? va[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(da)
+                             : "memory", "m0");
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(to + (uint32_t)((BR + t) * 1024)), "v"((uint32_t)lane * 16u), "s"(wp[t] + (int64_t)c * 1024) : "memory", "m0");
+        };
+        for (int i = 0; i < stages; ++i)
+            if (i < run) request(c0 + i, i);
+
+        v4i acc[MT][NT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[j][t] = v4i{0, 0, 0, 0};
+        constexpr auto vm = [](int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); };
+        const int ra = BR == 1 ? r & 7 : r;
+        const int a0 = ra * 128 + (((q >> 1) ^ ((ra >> 1) & 7)) << 4) + (q & 1) * 8;
+        int st = 0;
+        for (int i = 0; i < run; ++i) {
+            const int younger = min(run - 1 - i, stages - 1);
+            if (younger == 0) __builtin_amdgcn_s_waitcnt(vm(0));
+            else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(NL));
+            else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * NL));
+            else __builtin_amdgcn_s_waitcnt(vm(3 * NL));
+            asm volatile("" ::: "memory");
+            const int8_t* const base = ring + st * STAGE;
+            v4i xa[2][MT], w[NT];
+            uint32_t sc[NT], zc[NT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    const v2i lo = *reinterpret_cast<const v2i*>(base + j * 2048 + (a0 ^ (h * 64))), hi = *reinterpret_cast<const v2i*>(base + j * 2048 + (a0 ^ (h * 64 + 32)));
+                    xa[h][j] = v4i{lo[0], lo[1], hi[0], hi[1]};
+                }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                w[t] = *reinterpret_cast<const v4i*>(base + (BR + t) * 1024 + lane * 16);
+                auto scale = [&](const int8_t* p) {
+                    p += (i * 16 + r) * GPC;
+                    return GPC == 4 ? *reinterpret_cast<const uint32_t*>(p) : (GPC == 2 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint8_t*>(p));
+                };
+                sc[t] = scale(home + t * scb);
+                if constexpr (ZERO) zc[t] = scale(home + (NT + t) * scb);
+            }
+            chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
+            if (i + stages < run) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage has been read
+                request(c0 + i + stages, st);
+            }
+            st = st + 1 == stages ? 0 : st + 1;
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        int32_t* const sums = reinterpret_cast<int32_t*>(ring);
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (BR > 1 || q < 2) sums[(16 * j + 4 * q + e) * PITCH + 16 * t + r] = acc[j][t][e];
+    }
+    __syncthreads();
+
+    // ---- epilogue: an output a thread and round
+    const int runs = (g.chunks + per - 1) / per;
+#pragma unroll
+    for (int p = 0; p < EP; ++p) {
+        const int i = p * ROWS_THREADS + tid, m = i / (16 * NH), nn = i - m * (16 * NH), n = n0 + nn;
+        if (m >= rows || n >= g.N) continue;
+        const int8_t* const at = lds + (ZERO ? 2 : 1) * NT * scb + (m * PITCH + nn) * 4;
+        int64_t s0 = 0, s1 = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+            if (w < runs) {
+                s0 += *reinterpret_cast<const int32_t*>(at + w * own);
+                if constexpr (GATED) s1 += *reinterpret_cast<const int32_t*>(at + w * own + 64 * NH);
+            }
+        rows_finish<GATED>(g, m0 + m, n, s0, s1);
     }
 }
 

@@ -4,15 +4,38 @@
 
 namespace ibert {
 
-// rows of a workgroup / 16 (1, 2, 4); tiles of 16 channels to a wavefront, of each matrix of a gated block (1, 2); log2 of its groups of channels
+// ring: rows_ring_kernel, whose workgroups take 8 br rows (br: 1, 2, 4, 8) and nt tiles of channels.  Else rows of a workgroup / 16 (1, 2, 4); tiles of 16 channels to a wavefront, of each matrix of a gated block (1, 2); log2 of its groups of channels
 struct RowsPlan {
-    int32_t mt, nt, cg;
+    int32_t mt, nt, cg, ring, br;
 };
 
 template <bool W4, int G>
 int launch_rows(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream);
 
 constexpr int ROWS_LDS = 163840;
+
+// Launches workgroups of tm rows by tn channels, those of the same channels on the same XCD; in pieces of rows where there would be 2^32 threads.
+template <typename F, typename Name>
+int rows_pieces(F kern, RowsArgs g, int tm, int tn, size_t lds, hipStream_t stream, Name name)
+{
+    const int64_t M = g.M, across = ((int64_t)g.N + tn - 1) / tn, down = (M + tm - 1) / tm, most = (1 << 22) / across < 1 ? 1 : (1 << 22) / across;
+    const int8_t *A = g.A, *R = g.R;
+    char* C = static_cast<char*>(g.C);
+    const int64_t elem = g.out_dtype == IBERT_I8 ? 1 : (g.out_dtype == IBERT_I16 ? 2 : 4);
+    for (int64_t d0 = 0; d0 < down; d0 += most) {
+        const int64_t m0 = d0 * tm, n = down - d0 < most ? down - d0 : most;
+        g.A = A + m0 * g.lda;
+        g.R = R ? R + m0 * g.ldr : nullptr;
+        g.C = C + m0 * g.ldc * elem;
+        g.M = (int32_t)(M - m0 < n * tm ? M - m0 : n * tm);
+        g.down = (int32_t)n;
+        g.across = (int32_t)across;
+        hipLaunchKernelGGL(kern, dim3((unsigned)((across + 7) / 8 * 8 * n)), dim3(ROWS_THREADS), lds, stream, g);
+        IBERT_LAUNCH_CHECK("rows_kernel");
+    }
+    g_last_kernel = name();
+    return IBERT_OK;
+}
 
 template <bool W4, int MT, int NT, int G, bool ZERO, bool GATED>
 int launch_rows_as(RowsArgs g, const RowsPlan& plan, hipStream_t stream)
@@ -24,8 +47,7 @@ int launch_rows_as(RowsArgs g, const RowsPlan& plan, hipStream_t stream)
         attr_done = true;
     }
     constexpr int NH = GATED ? NT / 2 : NT;
-    const int64_t M = g.M;
-    const int32_t rows = M < 16 * MT ? (int32_t)M : 16 * MT;
+    const int32_t rows = g.M < 16 * MT ? g.M : 16 * MT;
     g.mp = 0;
     while ((1 << g.mp) < rows) ++g.mp;
     g.cg = plan.cg;
@@ -40,27 +62,60 @@ int launch_rows_as(RowsArgs g, const RowsPlan& plan, hipStream_t stream)
     if (g.slab > most) g.slab = most < round() ? round() : most;
     const size_t lds = ((size_t)g.slab << 7 << g.mp) + (size_t)sums();
     if (lds > (size_t)ROWS_LDS) return IBERT_ERR_NOT_IMPLEMENTED;
-    const int64_t across = (g.N + (16 * NH << g.cg) - 1) / (16 * NH << g.cg);
-    // (a launch may have 2^32 threads at most: pieces of rows)
-    const int64_t down = (M + 16 * MT - 1) / (16 * MT), most_down = (1 << 22) / across < 1 ? 1 : (1 << 22) / across;
-    const int8_t *A = g.A, *R = g.R;
-    char* C = static_cast<char*>(g.C);
-    const int64_t elem = g.out_dtype == IBERT_I8 ? 1 : (g.out_dtype == IBERT_I16 ? 2 : 4);
-    for (int64_t d0 = 0; d0 < down; d0 += most_down) {
-        const int64_t m0 = d0 * 16 * MT, n = down - d0 < most_down ? down - d0 : most_down;
-        g.A = A + m0 * g.lda;
-        g.R = R ? R + m0 * g.ldr : nullptr;
-        g.C = C + m0 * g.ldc * elem;
-        g.M = (int32_t)(M - m0 < n * 16 * MT ? M - m0 : n * 16 * MT);
-        g.down = (int32_t)n;
-        g.across = (int32_t)across;
-        const int64_t blocks = (across + 7) / 8 * 8 * n;
-        hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(ROWS_THREADS), lds, stream, g);
-        IBERT_LAUNCH_CHECK("rows_kernel");
+    return rows_pieces(kern, g, 16 * MT, 16 * NH << g.cg, lds, stream, [] {
+        static const KernelName name("rows_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", MT, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
+        return name.text;
+    });
+}
+
+// Can rows_ring_kernel serve these operands, and with how many stages (0: it cannot)?
+inline int ring_stages(const RowsArgs& g, int br, int tiles, int group, bool zeros, int* per, size_t* lds)
+{
+    const int chunks = (g.K + 127) / 128;
+    *per = (chunks + 7) / 8;
+    if (!g.a_vec || g.K % 16 != 0 || *per > 32 || g.lda > (1 << 24)) return 0;
+    const size_t sc = (size_t)((*per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1), stage = (size_t)(br + tiles) * 1024, sums = (size_t)32 * br * (16 * tiles + 4);
+    auto bytes = [&](int n) { return 8 * (sc + (n * stage > sums ? n * stage : sums)); };
+    int n = *per < 4 ? *per : 4;
+    while (n > 0 && bytes(n) > (size_t)ROWS_LDS) --n;
+    *lds = bytes(n);
+    return n;
+}
+
+template <int BR, int NT, int G, bool ZERO, bool GATED>
+int launch_ring_as(RowsArgs g, hipStream_t stream)
+{
+    auto kern = rows_ring_kernel<BR, NT, G, ZERO, GATED>;
+    static bool attr_done = false;
+    if (!attr_done) {
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, ROWS_LDS));
+        attr_done = true;
     }
-    static const KernelName name("rows_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", MT, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
-    g_last_kernel = name.text;
-    return IBERT_OK;
+    constexpr int NH = GATED ? NT / 2 : NT, TM = 8 * BR;
+    size_t lds;
+    g.mp = ring_stages(g, BR, NT, G, ZERO, &g.slab, &lds);
+    if (g.mp == 0) return IBERT_ERR_NOT_IMPLEMENTED;
+    g.chunks = (g.K + 127) / 128;
+    return rows_pieces(kern, g, TM, 16 * NH, lds, stream, [] {
+        static const KernelName name("rows_ring_kernel<%d, %d, %d, %s, %s>", BR, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
+        return name.text;
+    });
+}
+
+template <int G, bool ZERO, bool GATED>
+int launch_ring(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
+{
+    constexpr int PER = GATED ? 2 : 1;
+    if (plan.nt == 1) {
+        if (plan.br == 1) return launch_ring_as<1, PER, G, ZERO, GATED>(g, stream);
+        if (plan.br == 2) return launch_ring_as<2, PER, G, ZERO, GATED>(g, stream);
+        if (plan.br == 4) return launch_ring_as<4, PER, G, ZERO, GATED>(g, stream);
+        return launch_ring_as<8, PER, G, ZERO, GATED>(g, stream);
+    }
+    if (plan.br == 1) return launch_ring_as<1, 2 * PER, G, ZERO, GATED>(g, stream);
+    if (plan.br == 2) return launch_ring_as<2, 2 * PER, G, ZERO, GATED>(g, stream);
+    if (plan.br == 4) return launch_ring_as<4, 2 * PER, G, ZERO, GATED>(g, stream);
+    return launch_ring_as<8, 2 * PER, G, ZERO, GATED>(g, stream);
 }
 
 template <bool W4, int G, int MT>
@@ -82,6 +137,10 @@ int launch_rows_of(const RowsArgs& g, const RowsPlan& plan, bool zeros, bool gat
     template <>                                                                                                           \
     int launch_rows<W4_, G_>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream)                \
     {                                                                                                                     \
+        if constexpr (W4_) {                                                                                              \
+            if (plan.ring && gated) return zeros ? launch_ring<G_, true, true>(g, plan, stream) : launch_ring<G_, false, true>(g, plan, stream);      \
+            if (plan.ring) return zeros ? launch_ring<G_, true, false>(g, plan, stream) : launch_ring<G_, false, false>(g, plan, stream);             \
+        }                                                                                                                 \
         if (plan.mt == 1) return launch_rows_of<W4_, G_, 1>(g, plan, zeros, gated, stream);                               \
         if (plan.mt == 2) return launch_rows_of<W4_, G_, 2>(g, plan, zeros, gated, stream);                               \
         return launch_rows_of<W4_, G_, 4>(g, plan, zeros, gated, stream);                                                 \
