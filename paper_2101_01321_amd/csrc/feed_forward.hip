@@ -16,7 +16,7 @@ static RowsPlan plan_rows(int32_t M, int32_t N)
 {
     RowsPlan p{};
     p.mt = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
-    p.nt = g_rows_tiles >= 1 ? ((g_rows_tiles & 3) > 1 ? 2 : 1) : 1;
+    p.nt = g_rows_tiles == 2 ? 2 : 1;
     p.cg = 0;
     if (g_rows_groups >= 0) p.cg = g_rows_groups > 3 ? 3 : g_rows_groups;
     else {
@@ -26,14 +26,50 @@ static RowsPlan plan_rows(int32_t M, int32_t N)
     return p;
 }
 
-static int launch_w4(const RowsArgs& g, int32_t group, bool zeros, bool gated, hipStream_t stream)
+// Tiles of rows_ring_kernel: 8 br rows that hold M, up to 32 (of INT8 weights 64), by nt tiles of 16 channels (pairs of a gated block).  Wider tiles read A less
+// often, and there must be enough of them.  us, tiles x blocks of rows, at N x K:
+//   4 bits   1 row: 50000 x 1024 1x1 12.8 / 2x1 8.9, 12288 x 4096 8.1 / 9.0
+//            64: 4096 x 12288 1x4 19.5 / 2x4 15.3, 4096 x 4096 8.0 / 8.3, 1024 x 4096 5.9 / 7.2
+//            128: 4096 x 4096 2x4 10.3 / 4x4 11.4, 4096 x 12288 22.8 / 19.8;  256: 4096 x 4096 17.5 / 15.4, 50000 x 1024 79 / 83
+//   pairs    64: 11008 x 4096 1x4 24.9 / 2x4 22.5, 4096 x 1024 6.1 / 6.6;  128: 4096 x 1024 9.3 / 8.5, 2730 x 1024 7.2 / 8.3
+//   INT8     64: 8192 x 2048 1x4 14.4 / 2x8 13.0;  128: 11008 x 4096 48.2 / 42.1, 2730 x 1024 7.9 / 8.3;  256: 2730 x 1024 12.1 / 14.6
+static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, bool gated)
 {
-    RowsPlan p = plan_rows(g.M, g.N);
+    auto blocks = [&](int nt, int br) { return ((int64_t)N + 16 * nt - 1) / (16 * nt) * ((M + 8 * br - 1) / (8 * br)); };
+    p.br = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
+    p.nt = 1;
+    if (!w4) {
+        const int64_t b = blocks(2, 8);
+        if (M > 32 && 4 * b >= 3 * 256 * ((b + 255) / 256)) {
+            p.nt = 2;
+            p.br = 8;
+        }
+    } else if (gated) {
+        if (p.br == 4 && blocks(1, 4) >= 1024) p.nt = 2;
+    } else if (p.br == 4) {
+        if (K >= 2048 && blocks(4, 4) >= (K >= 8192 ? 256 : 512)) p.nt = 4;
+        else if (blocks(1, 4) >= 512) p.nt = 2;
+    } else if (blocks(1, p.br) > 1536) p.nt = 2;
+}
+
+static int launch_few_rows(const RowsArgs& g, bool w4, int32_t group, bool zeros, bool gated, hipStream_t stream)
+{
+    RowsArgs r = g;
+    r.a_vec = g.a_vec && g.K % 16 == 0;
+    RowsPlan p{};
+    plan_ring(p, g.M, g.N, g.K, w4, gated);
+    if (g_rows_tiles >= 8) {
+        p.nt = g_rows_tiles == 12 && !gated ? 4 : (g_rows_tiles == 9 ? 1 : 2);
+        if (g_rows_groups >= 1) p.br = g_rows_groups;
+    }
     int per;
     size_t lds;
-    p.br = g.M <= 8 ? 1 : (g.M <= 16 ? 2 : 4);
-    if (g_rows_tiles >= 8 && g_rows_groups >= 1) p.br = g_rows_groups;
-    p.ring = (g_rows_tiles < 0 || g_rows_tiles >= 8) && ring_stages(g, p.br, (gated ? 2 : 1) * p.nt, group, zeros, &per, &lds) > 0;
+    auto fits = [&] { return ring_stages(r, w4, p.br, (gated ? 2 : 1) * p.nt, gated, group, zeros, &per, &lds) > 0; };
+    while (p.nt > 1 && !fits()) p.nt >>= 1;                        // (rows that are held whole leave less room)
+    while (p.br > 1 && !fits()) p.br >>= 1;
+    p.ring = (g_rows_tiles < 0 || g_rows_tiles >= 8) && fits();
+    if (!p.ring) p = plan_rows(g.M, g.N);
+    if (!w4) return launch_rows<false, 128>(g, p, false, true, stream);
     if (group == 32) return launch_rows<true, 32>(g, p, zeros, gated, stream);
     if (group == 64) return launch_rows<true, 64>(g, p, zeros, gated, stream);
     return launch_rows<true, 128>(g, p, zeros, gated, stream);
@@ -119,7 +155,7 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     g.ldw = d.ldw;
     g.w_vec = ibert::aligned(W, 16) && d.ldw % 16 == 0 && d.K % 16 == 0 && d.ldw <= (1 << 26);
     g.gate = ibert::gate_const(d.gate);
-    return ibert::launch_rows<false, 128>(g, ibert::plan_rows(d.M, d.F), false, true, static_cast<hipStream_t>(stream));
+    return ibert::launch_few_rows(g, false, 128, false, true, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A, const ibert_w4_weights* gate, const ibert_w4_weights* up,
@@ -142,7 +178,7 @@ extern "C" int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A
     g.scales[0] = gate->scales; g.scales[1] = up->scales;
     g.zeros[0] = gate->zeros; g.zeros[1] = up->zeros;
     g.gate = ibert::gate_const(d.gate);
-    return ibert::launch_w4(g, gate->group, gate->zeros != nullptr, true, static_cast<hipStream_t>(stream));
+    return ibert::launch_few_rows(g, true, gate->group, gate->zeros != nullptr, true, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int ibert_gemm_w4_requant(const ibert_w4_desc* desc, const int8_t* A, const ibert_w4_weights* weights, const int32_t* bias,
@@ -169,5 +205,5 @@ extern "C" int ibert_gemm_w4_requant(const ibert_w4_desc* desc, const int8_t* A,
     g.R = residual; g.ldr = d.ldr;
     g.res_m = d.residual_dy.m; g.res_s = d.residual_dy.s;
     g.out_dtype = d.out_dtype; g.out_clamp = d.out_clamp;
-    return ibert::launch_w4(g, weights->group, weights->zeros != nullptr, false, static_cast<hipStream_t>(stream));
+    return ibert::launch_few_rows(g, true, weights->group, weights->zeros != nullptr, false, static_cast<hipStream_t>(stream));
 }

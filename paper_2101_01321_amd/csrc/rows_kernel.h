@@ -125,20 +125,28 @@ __device__ __forceinline__ void chunk_products(v4i (&acc)[MT][NT], const v4i (&x
     }
 }
 
-// Output (m, n) from its sums (of a gated block: gate and up projection).
-template <bool GATED>
-__device__ __forceinline__ void rows_finish(const RowsArgs& g, int m, int n, int64_t s0, int64_t s1)
+struct RowsChannel {
+    int32_t b, m, s;
+};
+__device__ __forceinline__ RowsChannel rows_channel(const RowsArgs& g, int ch)
 {
-    auto value = [&](int64_t v, int ch) {
-        v += g.bias ? g.bias[ch] : 0;
+    return RowsChannel{g.bias ? g.bias[ch] : 0, g.mult[ch], g.shift[ch]};
+}
+
+// Output (m, n) from its sums (of a gated block: gate and up projection), its channels' constants and its residual.
+template <bool GATED>
+__device__ __forceinline__ void rows_finish(const RowsArgs& g, int m, int n, int64_t s0, int64_t s1, const RowsChannel& c0, const RowsChannel& c1, int32_t res)
+{
+    auto value = [&](int64_t v, int32_t b) {
+        v += b;
         return (int32_t)(v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v));
     };
     const int64_t off = (int64_t)m * g.ldc + n;
     if constexpr (GATED) {
-        static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(value(s0, n), value(s1, g.N + n), g.mult[n], g.shift[n], g.mult[g.N + n], g.shift[g.N + n], g.gate);
+        static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(value(s0, c0.b), value(s1, c1.b), c0.m, c0.s, c1.m, c1.s, g.gate);
     } else {
-        int64_t v = dyadic64(value(s0, n), g.mult[n], g.shift[n]);
-        if (g.R) v += dyadic64(g.R[(int64_t)m * g.ldr + n], g.res_m, g.res_s);
+        int64_t v = dyadic64(value(s0, c0.b), c0.m, c0.s);
+        if (g.R) v += dyadic64(res, g.res_m, g.res_s);
         const int32_t y = clamp_i64_to_i32(v, g.out_clamp);
         if (g.out_dtype == IBERT_I8) static_cast<int8_t*>(g.C)[off] = (int8_t)y;
         else if (g.out_dtype == IBERT_I16) static_cast<int16_t*>(g.C)[off] = (int16_t)y;
@@ -311,24 +319,34 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
         const sum_t* const row = sums + m * cols;
         auto sum = [&](const sum_t& v) { return W4 ? (int64_t)v : (int64_t)(int32_t)v; };
         const int wv = nn / (16 * NH), in = nn - wv * (16 * NH);
-        rows_finish<GATED>(g, m0 + m, n, sum(row[GATED ? wv * 16 * NT + in : nn]), sum(row[GATED ? wv * 16 * NT + 16 * NH + in : nn]));
+        RowsChannel c0 = rows_channel(g, n), c1 = rows_channel(g, GATED ? g.N + n : n);
+        int64_t s0 = sum(row[GATED ? wv * 16 * NT + in : nn]), s1 = sum(row[GATED ? wv * 16 * NT + 16 * NH + in : nn]);
+        if constexpr (!W4) {                                       // (INT8 sums have 32 bits, and so has what the bias makes of them)
+            s0 = (int32_t)((uint32_t)s0 + (uint32_t)c0.b);
+            s1 = (int32_t)((uint32_t)s1 + (uint32_t)c1.b);
+            c0.b = c1.b = 0;
+        }
+        rows_finish<GATED>(g, m0 + m, n, s0, s1, c0, c1, !GATED && g.R ? g.R[(int64_t)(m0 + m) * g.ldr + n] : 0);
     }
 }
 
-// The same for aligned rows of A and K a multiple of 16: nothing in the loop waits for another wavefront.
+// The same where nothing in the loop waits for another wavefront.
 //   * The eight wavefronts of a workgroup share K in contiguous runs of chunks.  Each has a ring of stages of its own in LDS -- 1 KB blocks of eight rows of A by
 //     128 bytes, and of a tile's chunk of weights -- into which it requests straight from memory as many chunks ahead as LDS holds; scales (and zero points) of its
-//     whole run come first.  The sums (a run is at most 4096 values: 32 bits) meet in LDS at the end.
+//     whole run come first.  Rows of A that are not aligned (or K, to 16) are copied there whole before the loop, through registers, behind the first requests
+//     of weights.  The sums (a run is at most 4096 values: 32 bits) meet in LDS at the end.
 //   * A's 16-byte units are swizzled by the row (see swz in gemm_kernel.h); a lane's operand is two reads of eight bytes, 32 apart.
 // BR: blocks of eight rows (1, 2, 4 or 8); NT, G, ZERO, GATED: see rows_kernel.
-template <int BR, int NT, int G, bool ZERO, bool GATED>
+template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
 __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
 {
-    constexpr int MT = (BR + 1) / 2, NH = GATED ? NT / 2 : NT, GPC = 128 / G, NL = BR + NT, STAGE = NL * 1024;
+    // (blocks of a tile's chunk of weights: 1, or 2 of eight INT8 rows; requests of a chunk)
+    constexpr int WB = W4 ? 1 : 2, NLW = WB * NT;
+    constexpr int MT = (BR + 1) / 2, NH = GATED ? NT / 2 : NT, GPC = W4 ? 128 / G : 0;
     constexpr int TM = 8 * BR, PITCH = 16 * NT + 4;                // rows of the tile; dwords of a row of sums
     constexpr int EP = (TM * 16 * NH + ROWS_THREADS - 1) / ROWS_THREADS;
     constexpr int SUMS = TM * PITCH * 4;                           // bytes of a wavefront's sums, where its stages were
-    static_assert(3 * NL < 64, "outstanding requests");
+    static_assert(3 * (BR + NLW) < 64, "outstanding requests");
     extern __shared__ __align__(16) int8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
@@ -336,20 +354,40 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
     if (bx >= g.across) return;
     const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
     const int per = g.slab, c0 = wave * per, run = min(per, g.chunks - c0);           // this wavefront's chunks [c0, c0 + run)
+    const bool direct = g.a_vec;                                   // A through the ring
+    const int STAGE = ((direct ? BR : 0) + NLW) * 1024, held = direct ? 0 : per * BR * 1024;
     const int stages = g.mp, scb = (per * 16 * GPC + 255) & ~255;                       // bytes of a tile's scales
-    const int own = (ZERO ? 2 : 1) * NT * scb + max(stages * STAGE, SUMS);
+    const int own = (ZERO ? 2 : 1) * NT * scb + max(held + stages * STAGE, SUMS);
     int8_t* const home = lds + wave * own;
     const uint32_t home0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds + (uint32_t)(wave * own);
     const uint32_t ring0 = home0 + (uint32_t)((ZERO ? 2 : 1) * NT * scb);
     int8_t* const ring = home + (ZERO ? 2 : 1) * NT * scb;
 
-    if (run > 0) {
-        const uint8_t* wp[NT];
+    // what the epilogue needs of its outputs' channels, behind the first requests: an output a thread and round
+    RowsChannel ch[EP][GATED ? 2 : 1];
+    int32_t res[EP];
+    auto ends = [&]() {
+#pragma unroll
+        for (int p = 0; p < EP; ++p) {
+            const int i = p * ROWS_THREADS + tid, m = i / (16 * NH), n = min(n0 + i - m * (16 * NH), g.N - 1);
+            res[p] = 0;
+            if (m < rows) {
+                ch[p][0] = rows_channel(g, n);
+                if constexpr (GATED) ch[p][1] = rows_channel(g, g.N + n);
+                if (!GATED && g.R) res[p] = g.R[(int64_t)(m0 + m) * g.ldr + n];
+            }
+        }
+    };
+    if (run <= 0) ends();
+    else {
+        const uint8_t* wp[W4 ? NT : 1];
         const int64_t tbytes = (int64_t)g.chunks * 1024;
         // (tiles past the last channel read the last one again)
         auto tile_of = [&](int t) { return min(n0 + 16 * (t % NH), g.N - 1) >> 4; };
+        if constexpr (W4) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) wp[t] = static_cast<const uint8_t*>(g.w[t / NH]) + tile_of(t) * tbytes;
+            for (int t = 0; t < NT; ++t) wp[t] = static_cast<const uint8_t*>(g.w[t / NH]) + tile_of(t) * tbytes;
+        }
         // scales of the run, 64 dwords a request; what lies past the tile's last reads as zeros
         auto buffer = [](const void* p, uint32_t bytes) {
             const uint64_t u = (uint64_t)(uintptr_t)p;
@@ -357,7 +395,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
         };
         const uint32_t sbytes = (uint32_t)(g.chunks * 16 * GPC);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < (W4 ? NT : 0); ++t)
 #pragma unroll
             for (int z = 0; z < (ZERO ? 2 : 1); ++z) {
                 const void* src = z ? static_cast<const void*>(g.zeros[t / NH]) : static_cast<const void*>(g.scales[t / NH]);
@@ -374,21 +412,62 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
 #pragma unroll
         for (int b = 0; b < BR; ++b) va[b] = (uint32_t)(min(8 * b + lr8, rows - 1) * (int)g.lda + (b & 1 ? unit1 : unit0) * 16);
         const int left0 = g.K - unit0 * 16, left1 = g.K - unit1 * 16;
+        // INT8 weights: blocks of eight rows as those of A, channels past the last as that one again
+        v4i dw[W4 ? 1 : NT];
+        uint32_t vw[W4 ? 1 : 2 * NT];
+        if constexpr (!W4) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int first = min(n0 + 16 * (t % NH), g.N - 1), left = min(16, g.N - first);
+                dw[t] = buffer(static_cast<const int8_t*>(g.w[0]) + ((int64_t)(t / NH) * g.N + first) * g.ldw, (uint32_t)((left - 1) * (int)g.ldw + g.K));
+#pragma unroll
+                for (int b = 0; b < 2; ++b) vw[2 * t + b] = (uint32_t)(min(8 * b + lr8, left - 1) * (int)g.ldw + (b ? unit1 : unit0) * 16);
+            }
+        }
+        const int ahead = direct ? BR * 1024 : 0;                  // where a stage's weights begin
         auto request = [&](int chunk, int st) {
             const int c = __builtin_amdgcn_readfirstlane(chunk);   // (the same in every lane: the compiler loses sight of it)
-            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)ring0 + st * STAGE);
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)ring0 + held + st * STAGE);
+            if (direct) {
 #pragma unroll
-            for (int b = 0; b < BR; ++b)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                for (int b = 0; b < BR; ++b)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                              :: "s"(to + (uint32_t)(b * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? va[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(da)
                              : "memory", "m0");
+            }
+            if constexpr (W4) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             :: "s"(to + (uint32_t)((BR + t) * 1024)), "v"((uint32_t)lane * 16u), "s"(wp[t] + (int64_t)c * 1024) : "memory", "m0");
+                for (int t = 0; t < NT; ++t)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                                 :: "s"(to + (uint32_t)(ahead + t * 1024)), "v"((uint32_t)lane * 16u), "s"(wp[t] + (int64_t)c * 1024) : "memory", "m0");
+            } else {
+#pragma unroll
+                for (int b = 0; b < 2 * NT; ++b)
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                                 :: "s"(to + (uint32_t)(ahead + b * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? vw[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(dw[b / 2])
+                                 : "memory", "m0");
+            }
         };
         for (int i = 0; i < stages; ++i)
             if (i < run) request(c0 + i, i);
+        if (!direct) {
+            constexpr int U = BR >= 4 ? 1 : 4 / BR;                // chunks whose loads are under way together
+            for (int i0 = 0; i0 < run; i0 += U) {
+                v4i x[U][BR];
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+#pragma unroll
+                    for (int b = 0; b < BR; ++b)
+                        if (i0 + i < run)
+                            x[i][b] = bytes_16(g.A + (int64_t)(m0 + min(8 * b + lr8, rows - 1)) * g.lda, (c0 + i0 + i) * 128 + (b & 1 ? unit1 : unit0) * 16, g.K);
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+#pragma unroll
+                    for (int b = 0; b < BR; ++b)
+                        if (i0 + i < run) *reinterpret_cast<v4i*>(ring + ((i0 + i) * BR + b) * 1024 + lane * 16) = x[i][b];
+            }
+        }
+        ends();
 
         v4i acc[MT][NT];
 #pragma unroll
@@ -398,35 +477,63 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
         constexpr auto vm = [](int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); };
         const int ra = BR == 1 ? r & 7 : r;
         const int a0 = ra * 128 + (((q >> 1) ^ ((ra >> 1) & 7)) << 4) + (q & 1) * 8;
+        const int a8 = ra * 128 + ((q ^ ((ra >> 1) & 7)) << 4), w8 = r * 128 + ((q ^ ((r >> 1) & 7)) << 4);
         int st = 0;
         for (int i = 0; i < run; ++i) {
             const int younger = min(run - 1 - i, stages - 1);
-            if (younger == 0) __builtin_amdgcn_s_waitcnt(vm(0));
-            else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(NL));
-            else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * NL));
-            else __builtin_amdgcn_s_waitcnt(vm(3 * NL));
+            if (younger == 0 || !direct) {
+                if (younger == 0) __builtin_amdgcn_s_waitcnt(vm(0));
+                else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(NLW));
+                else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * NLW));
+                else __builtin_amdgcn_s_waitcnt(vm(3 * NLW));
+            } else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(BR + NLW));
+            else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * (BR + NLW)));
+            else __builtin_amdgcn_s_waitcnt(vm(3 * (BR + NLW)));
             asm volatile("" ::: "memory");
-            const int8_t* const base = ring + st * STAGE;
-            v4i xa[2][MT], w[NT];
-            uint32_t sc[NT], zc[NT];
+            const int8_t* const wbase = ring + held + st * STAGE + ahead;
+            const int8_t* const base = direct ? ring + st * STAGE : ring + i * BR * 1024;
+            v4i xa[2][MT];
+            if constexpr (!W4) {
+                v4i w[2][NT];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    const v2i lo = *reinterpret_cast<const v2i*>(base + j * 2048 + (a0 ^ (h * 64))), hi = *reinterpret_cast<const v2i*>(base + j * 2048 + (a0 ^ (h * 64 + 32)));
-                    xa[h][j] = v4i{lo[0], lo[1], hi[0], hi[1]};
+                    for (int j = 0; j < MT; ++j) xa[h][j] = *reinterpret_cast<const v4i*>(base + j * 2048 + (a8 ^ (h * 64)));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) w[h][t] = *reinterpret_cast<const v4i*>(wbase + 2 * t * 1024 + (w8 ^ (h * 64)));
                 }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                w[t] = *reinterpret_cast<const v4i*>(base + (BR + t) * 1024 + lane * 16);
-                auto scale = [&](const int8_t* p) {
-                    p += (i * 16 + r) * GPC;
-                    return GPC == 4 ? *reinterpret_cast<const uint32_t*>(p) : (GPC == 2 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint8_t*>(p));
-                };
-                sc[t] = scale(home + t * scb);
-                if constexpr (ZERO) zc[t] = scale(home + (NT + t) * scb);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j) acc[j][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[h][j], w[h][t], acc[j][t], 0, 0, 0);
+            } else {
+                v4i w[NT];
+                uint32_t sc[NT], zc[NT];
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    // (the rows' addresses apart: read in pairs of rows the operands would have to be put together by moves)
+                    int aj = a0 + j * 2048;
+                    asm volatile("" : "+v"(aj));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const v2i lo = *reinterpret_cast<const v2i*>(base + (aj ^ (h * 64))), hi = *reinterpret_cast<const v2i*>(base + (aj ^ (h * 64 + 32)));
+                        xa[h][j] = v4i{lo[0], lo[1], hi[0], hi[1]};
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    w[t] = *reinterpret_cast<const v4i*>(wbase + t * 1024 + lane * 16);
+                    auto scale = [&](const int8_t* p) {
+                        p += (i * 16 + r) * GPC;
+                        return GPC == 4 ? *reinterpret_cast<const uint32_t*>(p) : (GPC == 2 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint8_t*>(p));
+                    };
+                    sc[t] = scale(home + t * scb);
+                    if constexpr (ZERO) zc[t] = scale(home + (NT + t) * scb);
+                }
+                chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
             }
-            chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
             if (i + stages < run) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage has been read
                 request(c0 + i + stages, st);
@@ -459,7 +566,12 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
                 s0 += *reinterpret_cast<const int32_t*>(at + w * own);
                 if constexpr (GATED) s1 += *reinterpret_cast<const int32_t*>(at + w * own + 64 * NH);
             }
-        rows_finish<GATED>(g, m0 + m, n, s0, s1);
+        if constexpr (!W4) {                                       // (INT8 sums have 32 bits, and so has what the bias makes of them)
+            s0 = (int32_t)((uint32_t)s0 + (uint32_t)ch[p][0].b);
+            s1 = (int32_t)((uint32_t)s1 + (uint32_t)ch[p][GATED ? 1 : 0].b);
+            ch[p][0].b = ch[p][GATED ? 1 : 0].b = 0;
+        }
+        rows_finish<GATED>(g, m0 + m, n, s0, s1, ch[p][0], ch[p][GATED ? 1 : 0], res[p]);
     }
 }
 

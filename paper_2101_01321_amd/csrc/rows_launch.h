@@ -68,24 +68,29 @@ int launch_rows_as(RowsArgs g, const RowsPlan& plan, hipStream_t stream)
     });
 }
 
-// Can rows_ring_kernel serve these operands, and with how many stages (0: it cannot)?
-inline int ring_stages(const RowsArgs& g, int br, int tiles, int group, bool zeros, int* per, size_t* lds)
+// Can rows_ring_kernel serve these operands, and with how many stages (0: it cannot)?  As many as there is use for, at most four, of what LDS holds beside two
+// more workgroups where there are that many for a unit: us, [1,4096] x 12288 pairs of 4 bits, 768 workgroups, with one stage 13.3, two (three workgroups) 12.3, three
+// (two workgroups) 13.2, four (one) 19.8.
+inline int ring_stages(const RowsArgs& g, bool w4, int br, int tiles, bool gated, int group, bool zeros, int* per, size_t* lds)
 {
-    const int chunks = (g.K + 127) / 128;
+    const int chunks = (g.K + 127) / 128, tn = 16 * (gated ? tiles / 2 : tiles);
     *per = (chunks + 7) / 8;
-    if (!g.a_vec || g.K % 16 != 0 || *per > 32 || g.lda > (1 << 24)) return 0;
-    const size_t sc = (size_t)((*per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1), stage = (size_t)(br + tiles) * 1024, sums = (size_t)32 * br * (16 * tiles + 4);
-    auto bytes = [&](int n) { return 8 * (sc + (n * stage > sums ? n * stage : sums)); };
+    if (g.lda > (1 << 24) || (w4 ? *per > 32 : !g.w_vec)) return 0;
+    const size_t sc = w4 ? (size_t)((*per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1) : 0, sums = (size_t)32 * br * (16 * tiles + 4);
+    const size_t held = g.a_vec ? 0 : (size_t)*per * br * 1024, stage = (size_t)((g.a_vec ? br : 0) + tiles * (w4 ? 1 : 2)) * 1024;
+    auto bytes = [&](int n) { return 8 * (sc + (held + n * stage > sums ? held + n * stage : sums)); };
+    const int64_t blocks = (((int64_t)g.N + tn - 1) / tn) * ((g.M + 8 * br - 1) / (8 * br));
+    const size_t side = blocks <= 256 ? 1 : (blocks <= 512 ? 2 : 3);
     int n = *per < 4 ? *per : 4;
-    while (n > 0 && bytes(n) > (size_t)ROWS_LDS) --n;
+    while (n > 1 && bytes(n) > ROWS_LDS / side) --n;
     *lds = bytes(n);
-    return n;
+    return *lds <= (size_t)ROWS_LDS ? n : 0;
 }
 
-template <int BR, int NT, int G, bool ZERO, bool GATED>
+template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
 int launch_ring_as(RowsArgs g, hipStream_t stream)
 {
-    auto kern = rows_ring_kernel<BR, NT, G, ZERO, GATED>;
+    auto kern = rows_ring_kernel<W4, BR, NT, G, ZERO, GATED>;
     static bool attr_done = false;
     if (!attr_done) {
         IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, ROWS_LDS));
@@ -93,29 +98,35 @@ int launch_ring_as(RowsArgs g, hipStream_t stream)
     }
     constexpr int NH = GATED ? NT / 2 : NT, TM = 8 * BR;
     size_t lds;
-    g.mp = ring_stages(g, BR, NT, G, ZERO, &g.slab, &lds);
+    g.a_vec = g.a_vec && g.K % 16 == 0;
+    g.mp = ring_stages(g, W4, BR, NT, GATED, G, ZERO, &g.slab, &lds);
     if (g.mp == 0) return IBERT_ERR_NOT_IMPLEMENTED;
     g.chunks = (g.K + 127) / 128;
     return rows_pieces(kern, g, TM, 16 * NH, lds, stream, [] {
-        static const KernelName name("rows_ring_kernel<%d, %d, %d, %s, %s>", BR, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
+        static const KernelName name("rows_ring_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", BR, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
         return name.text;
     });
 }
 
-template <int G, bool ZERO, bool GATED>
+template <bool W4, int G, bool ZERO, bool GATED>
 int launch_ring(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
 {
     constexpr int PER = GATED ? 2 : 1;
     if (plan.nt == 1) {
-        if (plan.br == 1) return launch_ring_as<1, PER, G, ZERO, GATED>(g, stream);
-        if (plan.br == 2) return launch_ring_as<2, PER, G, ZERO, GATED>(g, stream);
-        if (plan.br == 4) return launch_ring_as<4, PER, G, ZERO, GATED>(g, stream);
-        return launch_ring_as<8, PER, G, ZERO, GATED>(g, stream);
+        if (plan.br == 1) return launch_ring_as<W4, 1, PER, G, ZERO, GATED>(g, stream);
+        if (plan.br == 2) return launch_ring_as<W4, 2, PER, G, ZERO, GATED>(g, stream);
+        if (plan.br == 4) return launch_ring_as<W4, 4, PER, G, ZERO, GATED>(g, stream);
+        return launch_ring_as<W4, 8, PER, G, ZERO, GATED>(g, stream);
     }
-    if (plan.br == 1) return launch_ring_as<1, 2 * PER, G, ZERO, GATED>(g, stream);
-    if (plan.br == 2) return launch_ring_as<2, 2 * PER, G, ZERO, GATED>(g, stream);
-    if (plan.br == 4) return launch_ring_as<4, 2 * PER, G, ZERO, GATED>(g, stream);
-    return launch_ring_as<8, 2 * PER, G, ZERO, GATED>(g, stream);
+    if constexpr (W4 && !GATED) if (plan.nt == 4) {
+        if (plan.br == 1) return launch_ring_as<W4, 1, 4, G, ZERO, GATED>(g, stream);
+        if (plan.br == 2) return launch_ring_as<W4, 2, 4, G, ZERO, GATED>(g, stream);
+        return launch_ring_as<W4, 4, 4, G, ZERO, GATED>(g, stream);       // (8 rows' blocks: see launch_few_rows)
+    }
+    if (plan.br == 1) return launch_ring_as<W4, 1, 2 * PER, G, ZERO, GATED>(g, stream);
+    if (plan.br == 2) return launch_ring_as<W4, 2, 2 * PER, G, ZERO, GATED>(g, stream);
+    if (plan.br == 4) return launch_ring_as<W4, 4, 2 * PER, G, ZERO, GATED>(g, stream);
+    return launch_ring_as<W4, 8, 2 * PER, G, ZERO, GATED>(g, stream);
 }
 
 template <bool W4, int G, int MT>
@@ -138,9 +149,9 @@ int launch_rows_of(const RowsArgs& g, const RowsPlan& plan, bool zeros, bool gat
     int launch_rows<W4_, G_>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream)                \
     {                                                                                                                     \
         if constexpr (W4_) {                                                                                              \
-            if (plan.ring && gated) return zeros ? launch_ring<G_, true, true>(g, plan, stream) : launch_ring<G_, false, true>(g, plan, stream);      \
-            if (plan.ring) return zeros ? launch_ring<G_, true, false>(g, plan, stream) : launch_ring<G_, false, false>(g, plan, stream);             \
-        }                                                                                                                 \
+            if (plan.ring && gated) return zeros ? launch_ring<W4_, G_, true, true>(g, plan, stream) : launch_ring<W4_, G_, false, true>(g, plan, stream);      \
+            if (plan.ring) return zeros ? launch_ring<W4_, G_, true, false>(g, plan, stream) : launch_ring<W4_, G_, false, false>(g, plan, stream);             \
+        } else if (plan.ring) return launch_ring<W4_, G_, false, true>(g, plan, stream);                                  \
         if (plan.mt == 1) return launch_rows_of<W4_, G_, 1>(g, plan, zeros, gated, stream);                               \
         if (plan.mt == 2) return launch_rows_of<W4_, G_, 2>(g, plan, zeros, gated, stream);                               \
         return launch_rows_of<W4_, G_, 4>(g, plan, zeros, gated, stream);                                                 \
