@@ -68,7 +68,7 @@ void ibert_rotary_override(int32_t heads);
 
 /* Which kernels the gated block and the products with 4-bit weights run: `tiles` = 1 or 2 tiles of 16 channels to a wavefront (the gated block takes pairs of them) and
  * 2^`groups` groups of channels to a workgroup (0 to 3); tiles = 9, 10 or 12: the kernel whose wavefronts have rings of their own, with one, two or four tiles (four: of products alone, at most 32 rows) and
- * 8 x `groups` (1, 2, 4, 8) rows to a workgroup, where it can run; tiles = 0: the persistent kernel of the INT8 gated block where it can run.  Negative: what is faster (the default).  The result
+ * 8 x `groups` (1, 2, 4, 8) rows to a workgroup, where it can run; tiles = 0: the persistent kernel of the INT8 gated block where it can run, its tiles 256 tokens high, or 128 with groups = 1.  Negative: what is faster (the default).  The result
  * never depends on it.  Process-wide, not thread-safe. */
 void ibert_rows_override(int32_t tiles, int32_t groups);
 

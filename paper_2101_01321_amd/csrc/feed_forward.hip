@@ -52,6 +52,21 @@ static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, boo
     } else if (blocks(1, p.br) > 1536) p.nt = 2;
 }
 
+// The kernel of an INT8 gated block: 0 rows_ring_kernel, 1 and 2 the persistent one with tiles of 128 and 256 tokens; by what rounds of its workgroups over the chip's 256 units
+// are expected to take, us, from K / 1024 = k: a round of 64 x 32 rings 4.5 + 2 k behind the first 4, of 128 x 128 tiles 5.5 + 6.3 k, of 256 x 128 tiles 9.3 + 8.4 k.
+// Measured, us, rings / low / tall: 128 x 1024 x 4096 8.7 / 12.0 / 17.7, 256 x 1024 x 4096 14.9 / 12.3 / 17.8, 128 x 2048 x 8192 20.2 / 19 / 28, 1024 x 4096 x 4096 - / 36.2 / 45.7,
+// 2741 x 1024 x 4096 - / 34.4 / 36.7, 8192 x 4096 x 12288 - / 780 / 639.
+static int plan_gated(int32_t M, int32_t F, int32_t K)
+{
+    const double k = K / 1024.0;
+    auto rounds = [&](int rows, int channels) {
+        const int64_t tiles = (((int64_t)M + rows - 1) / rows) * (((int64_t)F + channels - 1) / channels);
+        return (double)((tiles + 255) / 256);
+    };
+    const double ring = 4.0 + rounds(64, 32) * (4.5 + 2.0 * k), low = rounds(128, 128) * (5.5 + 6.3 * k), tall = rounds(256, 128) * (9.3 + 8.4 * k);
+    return M <= 32 || (ring <= low && ring <= tall) ? 0 : (low <= tall ? 1 : 2);
+}
+
 static int launch_few_rows(const RowsArgs& g, bool w4, int32_t group, bool zeros, bool gated, hipStream_t stream)
 {
     RowsArgs r = g;
@@ -148,8 +163,9 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     if (!W) return IBERT_ERR_NULL;
     const ibert_gated_desc& d = *desc;
     if (ibert::overlap(C, ibert::span(d.M, d.ldc, d.F, 1), W, ibert::span(2 * (int64_t)d.F, d.ldw, d.K, 1))) return IBERT_ERR_SHAPE;
-    if ((ibert::g_rows_tiles == 0 || (ibert::g_rows_tiles < 0 && d.M > 128)) && ibert::gated_stream_ok(d, A, W))
-        return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, static_cast<hipStream_t>(stream));
+    const int persistent = ibert::g_rows_tiles == 0 ? (ibert::g_rows_groups == 1 ? 1 : 2) : (ibert::g_rows_tiles < 0 ? ibert::plan_gated(d.M, d.F, d.K) : 0);
+    if (persistent && ibert::gated_stream_ok(d, A, W))
+        return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, persistent == 2, static_cast<hipStream_t>(stream));
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
     g.w[0] = W;
     g.ldw = d.ldw;

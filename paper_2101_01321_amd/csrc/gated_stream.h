@@ -1,11 +1,12 @@
-// The persistent kernel of the INT8 gated block (gated_stream.hip): does it serve these operands, and its launch (validated arguments, M and F >= 1).
+// The persistent kernel of the INT8 gated block (gated_stream.hip): does it serve these operands, and its launch (validated arguments, M and F >= 1;
+// tall: tiles of 256 tokens, else 128).
 #pragma once
 #include "common.h"
 
 namespace ibert {
 
 bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W);
-int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C,
+int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, int tall,
                         hipStream_t stream);
 
 }  // namespace ibert

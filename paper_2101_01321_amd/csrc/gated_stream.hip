@@ -1,5 +1,5 @@
 // The gated block for many tokens: the persistent workgroups of gemm_stream.h (streamed K steps of 128 bytes, two LDS stages, a step in
-// four phases by quadrants of the wavefront's tile), whose tile is 256 tokens by 128 channels of the gate and the same 128 of the up
+// four phases by quadrants of the wavefront's tile), whose tile is 256 or 128 tokens by 128 channels of the gate and the same 128 of the up
 // projection.
 //
 //   * The first two MFMA blocks of a wavefront's four are rows of W_gate and the last two the same rows of W_up, so that the two halves of
@@ -7,7 +7,7 @@
 //     in registers: neither product is ever stored.
 //   * Rows of W are dealt to the LDS rows such that lane r of 16 has channels 2 r and 2 r + 1 of its wavefront's 32.
 //   * F and M may be ragged: operands, constants and output are buffers that end with the last row or channel.
-//   * SiLU's sigmoids are a table of 1025 entries of 16 bits in LDS, built once by every workgroup with the function it stands for.
+//   * SiLU's sigmoids, and GELU's erf where it has room, are tables in LDS, built once by every workgroup with the function they stand for.
 #include "gate_math.h"
 #include "gemm_stream.h"
 #include "gated_stream.h"
@@ -31,18 +31,28 @@ struct GatedStreamArgs {
     GateConst gate;
 };
 
-constexpr int GS_BM = 256, GS_BF = 128, GS_NW = 8;       // tokens and channels of a tile; wavefronts
-constexpr int GS_STAGE = (GS_BM + 2 * GS_BF) * 128;
-constexpr int GS_PAR = 2 * GS_STAGE;                     // two buffers of 3 x 256 constants
-constexpr int GS_TURN = GS_PAR + 2 * 3 * 256 * 4;        // rows on their way out: 32 rows of 32 bytes a wavefront
+constexpr int GS_BF = 128, GS_NW = 8;                    // channels of a tile; wavefronts
 constexpr int GS_PITCH = 48, GS_TURN_WAVE = 32 * GS_PITCH;
-constexpr int GS_SIG = GS_TURN + GS_NW * GS_TURN_WAVE;
-constexpr int GS_LDS = GS_SIG + 2064;
+constexpr int GS_ERF = 3400;                             // entries that GELU's table may have
 
-template <bool SILU>
+// BM: tokens of a tile.
+template <int BM>
+struct GatedLayout {
+    static constexpr int STAGE = (BM + 2 * GS_BF) * 128;
+    static constexpr int PAR = 2 * STAGE;                // two buffers of 3 x 256 constants
+    static constexpr int TURN = PAR + 2 * 3 * 256 * 4;   // rows on their way out: 32 rows of 32 bytes a wavefront
+    static constexpr int TABLE = TURN + GS_NW * GS_TURN_WAVE;
+    static constexpr int LDS = TABLE + 4 * GS_ERF;
+    static_assert(LDS <= 163840 && 2 * (2 * SIG_STEPS + 1) <= 4 * GS_ERF, "LDS of a workgroup");
+};
+
+enum { GS_GELU = 0, GS_SILU = 1, GS_GELU_TABLE = 2 };
+
+template <int ACT, int BM>
 __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArgs g)
 {
-    constexpr int BM = GS_BM, BN = 256, NW = GS_NW, NT = 64 * NW, WR = 2, WC = 4;
+    using GL = GatedLayout<BM>;
+    constexpr int GS_STAGE = GL::STAGE, GS_PAR = GL::PAR, BN = 256, NW = GS_NW, NT = 64 * NW, WR = 2, WC = 4;
     constexpr int WM = BM / WR, WN = BN / WC, FM = WM / 16, FN = 4, FMH = FM / 2, FN0 = 2, FN1 = 2;
     constexpr int QA = FMH * 2 * WR / NW, QW = FN0 * 2 * WC / NW, NQ = QA + QW;       // requests of a wavefront: A half, W half, a group
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
@@ -178,9 +188,20 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
         }
     };
     request_two_steps();
-    if constexpr (SILU) {
-        uint16_t* const sig = reinterpret_cast<uint16_t*>(lds + GS_SIG);
-        for (int d = tid; d <= SIG_STEPS; d += NT) sig[d] = (uint16_t)sigmoid15((uint32_t)d);
+    // SiLU: the factor of a gate in step i - 1024 of either sign, 15 bits.  GELU: erf + q_1 of Alg. 2 over [q_b, -q_b], outside of which it stays the same.
+    if constexpr (ACT == GS_SILU) {
+        uint16_t* const sig = reinterpret_cast<uint16_t*>(lds + GL::TABLE);
+        for (int d = tid; d <= 2 * SIG_STEPS; d += NT) {
+            const int i = d - SIG_STEPS;
+            const uint32_t p = sigmoid15((uint32_t)(i < 0 ? -i : i));
+            sig[d] = (uint16_t)(i < 0 ? 32768u - p : p);
+        }
+    } else if constexpr (ACT == GS_GELU_TABLE) {
+        int32_t* const erf = reinterpret_cast<int32_t*>(lds + GL::TABLE);
+        for (int d = tid; d <= -2 * g.gate.gelu.q_b; d += NT) {
+            const int q = d + g.gate.gelu.q_b, v = (q < 0 ? -q : q) + g.gate.gelu.q_b, poly = smad24(v, v, g.gate.gelu.q_c);
+            erf[d] = (q < 0 ? -poly : (q == 0 ? 0 : poly)) + g.gate.gelu.q_1;
+        }
     }
     __builtin_amdgcn_s_waitcnt(vm(2 * NQ));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -291,48 +312,69 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
                 sh[i] = (s - 32) & 31;
             }
             const GeluConst gl{ga->gate.gelu.q_b, ga->gate.gelu.q_c, ga->gate.gelu.q_1, ga->gate.gelu.q_max, ga->gate.gelu.m, ga->gate.gelu.s};
-            const int32_t gl_rnd = 1 << ((gl.s - 33) & 31), gl_sh = (gl.s - 32) & 31;
-            const int32_t om = ga->gate.m, ornd = 1 << ((ga->gate.s - 33) & 31), osh = (ga->gate.s - 32) & 31;
-            const uint16_t* const sig = reinterpret_cast<const uint16_t*>(lds + GS_SIG);
-            int8_t* const turn = lds + GS_TURN + wave * GS_TURN_WAVE;
+            // (x m + 2^(s-1)) >> s of a 32-bit x, s in [33, 62]: the high half of one 64-bit multiply-add, shifted
+            const int64_t gl_rnd = (int64_t)1 << ((gl.s - 1) & 63), ornd = (int64_t)1 << ((ga->gate.s - 1) & 63);
+            const int32_t gl_sh = (gl.s - 32) & 31, om = ga->gate.m, osh = (ga->gate.s - 32) & 31;
+            const uint32_t table = lds0 + (uint32_t)GL::TABLE;
+            int8_t* const turn = lds + GL::TURN + wave * GS_TURN_WAVE;
             auto value = [&](int i, int n) { return (int32_t)(((int64_t)acc[i][n >> 2][n & 3] * mm[i] + c0[i]) >> 32) >> sh[i]; };
             auto fence = []() { __builtin_amdgcn_wave_barrier(); };
             typedef unsigned v4u __attribute__((ext_vector_type(4)));
+            typedef const __attribute__((address_space(3))) uint16_t* lds_halves;
+            typedef const __attribute__((address_space(3))) int32_t* lds_words;
             constexpr int UNITS = FM / 2;
             v4u mv[UNITS];
             const int col = wf0 + (el & 1) * 16, mrow = el >> 1;   // piece and row of a unit that the lane moves
             auto store = [&](int unit) __attribute__((always_inline)) {
-                const int at = (wm0 + unit * 32 + mrow) * ga->ldc + col;
+                const int row = wm0 + unit * 32 + mrow, at = row * ga->ldc + col;
                 if (ga->c_vec && col + 16 <= cols) __builtin_amdgcn_raw_buffer_store_b128(mv[unit], cb, at, 0, 0);
-                else {
+                else if (row <= last) {
+                    int8_t* const p = ga->C + out0 + at;
+                    if (col + 16 <= cols) __builtin_memcpy(p, &mv[unit], 16);
+                    else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (col + e < cols) __builtin_amdgcn_raw_buffer_store_b8((uint8_t)(mv[unit][e >> 2] >> (8 * (e & 3))), cb, at + e, 0, 0);
+                        for (int e = 0; e < 16; ++e)
+                            if (col + e < cols) p[e] = (int8_t)(mv[unit][e >> 2] >> (8 * (e & 3)));
+                    }
                 }
             };
-            // the result of token n's channel i (0 or 1)
-            auto result = [&](int n, int i) __attribute__((always_inline)) {
-                const int32_t up = med3_i32(value(2 + i, n), -32767, 32767);
-                int32_t a;
-                if constexpr (SILU) {
-                    const int32_t gt = med3_const<-65535, 65535>(value(i, n));
-                    a = silu_of(gt, sig[silu_step(gt)]);
-                } else {
-                    const int32_t q = med3_i32(value(i, n), -gl.q_max, gl.q_max);
-                    const int32_t v = min(max(q, -q), -gl.q_b) + gl.q_b;
-                    const int32_t poly = smad24(v, v, gl.q_c), sg = q >> 31;
-                    const int32_t t = smul24(q, ((poly ^ sg) - sg) + gl.q_1);
-                    a = med3_const<-32767, 32767>((__mulhi(t, gl.m) + gl_rnd) >> gl_sh);
+            // the results of token n: table reads of both channels first
+            auto results = [&](int n) __attribute__((always_inline)) {
+                int32_t gt[2], f[2], up[2], y[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (ACT == GS_SILU) {
+                        gt[i] = med3_const<-65535, 65535>(value(i, n));
+                        // (|g| + 8) >> 4 with g's sign: below zero the shift rounds the other way
+                        const int32_t d = med3_const<-SIG_STEPS, SIG_STEPS>((gt[i] + 8 + (gt[i] >> 31)) >> 4);
+                        f[i] = *(lds_halves)(uintptr_t)(table + 2 * SIG_STEPS + (uint32_t)(d << 1));
+                    } else {
+                        gt[i] = med3_i32(value(i, n), -gl.q_max, gl.q_max);
+                        if constexpr (ACT == GS_GELU_TABLE) f[i] = *(lds_words)(uintptr_t)(table + (uint32_t)((med3_i32(gt[i], gl.q_b, -gl.q_b) - gl.q_b) << 2));
+                        else {
+                            const int32_t v = min(max(gt[i], -gt[i]), -gl.q_b) + gl.q_b;
+                            const int32_t poly = smad24(v, v, gl.q_c), sg = gt[i] >> 31;
+                            f[i] = ((poly ^ sg) - sg) + gl.q_1;
+                        }
+                    }
                 }
-                return med3_const<-127, 127>((__mulhi(smul24(a, up), om) + ornd) >> osh);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) up[i] = med3_i32(value(2 + i, n), -32767, 32767);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    int32_t a;
+                    if constexpr (ACT == GS_SILU) a = smad24(gt[i], f[i], 16384) >> 15;
+                    else a = med3_const<-32767, 32767>((int32_t)(((int64_t)smul24(gt[i], f[i]) * gl.m + gl_rnd) >> 32) >> gl_sh);
+                    y[i] = med3_const<-127, 127>((int32_t)(((int64_t)smul24(a, up[i]) * om + ornd) >> 32) >> osh);
+                }
+                return (uint16_t)__builtin_amdgcn_perm((uint32_t)y[1], (uint32_t)y[0], 0x0c0c0400u);
             };
 #pragma unroll
             for (int unit = 0; unit < UNITS; ++unit) {
                 fence();
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    const int32_t y0 = result(8 * unit + t, 0), y1 = result(8 * unit + t, 1);
-                    *reinterpret_cast<uint16_t*>(turn + (16 * (t / 4) + 4 * u + t % 4) * GS_PITCH + 2 * r16) = (uint16_t)((y0 & 0xff) | (y1 << 8));
+                    *reinterpret_cast<uint16_t*>(turn + (16 * (t / 4) + 4 * u + t % 4) * GS_PITCH + 2 * r16) = results(8 * unit + t);
                     if (t % 2 == 1) __builtin_amdgcn_sched_barrier(0);
                 }
                 fence();
@@ -390,43 +432,52 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W)
 {
     return d.K % 128 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
-           (int64_t)((d.M + GS_BM - 1) / GS_BM) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
+           (int64_t)((d.M + 127) / 128) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
 }
 
-int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C,
-                        hipStream_t stream)
+template <int ACT, int BM>
+static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipStream_t stream)
 {
-    GatedStreamArgs s;
-    s.A = A; s.W = W; s.bias = bias; s.mult = mult; s.shift = shift; s.C = C;
-    s.M = d.M; s.F = d.F; s.nk = d.K / 128;
-    s.lda = (int32_t)d.lda; s.ldw = (int32_t)d.ldw; s.ldc = (int32_t)d.ldc;
-    s.tiles_m = (d.M + GS_BM - 1) / GS_BM;
-    const int tiles_n = (d.F + GS_BF - 1) / GS_BF;
+    s.tiles_m = (s.M + BM - 1) / BM;
+    const int tiles_n = (s.F + GS_BF - 1) / GS_BF;
     // as stream_shares and stream_deal
     s.xs = 0;
-    while (s.xs < 2 && tiles_n % (2 << s.xs) == 0 && ((2 * (int64_t)d.F * d.K) >> s.xs) > (2 << 20) && s.tiles_m >= (8 >> s.xs)) ++s.xs;
+    while (s.xs < 2 && tiles_n % (2 << s.xs) == 0 && (weight_bytes >> s.xs) > (2 << 20) && s.tiles_m >= (8 >> s.xs)) ++s.xs;
     s.gs = 3 - s.xs;
     s.bn = tiles_n >> s.xs;
     s.bn_magic = udiv_magic(s.bn);
     const int64_t run = ((int64_t)s.tiles_m * s.bn + (1 << s.gs) - 1) >> s.gs;
     s.per_xcd = (int32_t)(run < 32 ? run : 32);
-    const ibert_gate_params& p = d.gate;
-    s.gate = gate_const(p);
-    s.fast = (int64_t)d.K * 16129 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (s.gate.silu || gelu_fast_ok(p.gelu));
-    s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
+    auto kern = gated_stream_kernel<ACT, BM>;
     static bool attr_done = false;
     if (!attr_done) {
-        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(gated_stream_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
-        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(gated_stream_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
         attr_done = true;
     }
-    static_assert(GS_LDS <= 163840, "LDS of a workgroup");
-    const dim3 grid(8u * (unsigned)s.per_xcd), block(64 * GS_NW);
-    if (s.gate.silu) hipLaunchKernelGGL(gated_stream_kernel<true>, grid, block, GS_LDS, stream, s);
-    else hipLaunchKernelGGL(gated_stream_kernel<false>, grid, block, GS_LDS, stream, s);
+    hipLaunchKernelGGL(kern, dim3(8u * (unsigned)s.per_xcd), dim3(64 * GS_NW), GatedLayout<BM>::LDS, stream, s);
     IBERT_LAUNCH_CHECK("gated_stream_kernel");
-    g_last_kernel = s.gate.silu ? "gated_stream_kernel<true>" : "gated_stream_kernel<false>";
+    static const KernelName name("gated_stream_kernel<%d, %d>", ACT, BM);
+    g_last_kernel = name.text;
     return IBERT_OK;
+}
+
+int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, int tall,
+                        hipStream_t stream)
+{
+    GatedStreamArgs s{};
+    s.A = A; s.W = W; s.bias = bias; s.mult = mult; s.shift = shift; s.C = C;
+    s.M = d.M; s.F = d.F; s.nk = d.K / 128;
+    s.lda = (int32_t)d.lda; s.ldw = (int32_t)d.ldw; s.ldc = (int32_t)d.ldc;
+    const ibert_gate_params& p = d.gate;
+    s.gate = gate_const(p);
+    const bool gelu = !s.gate.silu, gelu_fast = gelu && gelu_fast_ok(p.gelu);
+    s.fast = (int64_t)d.K * 16129 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
+    s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
+    const int64_t w = 2 * (int64_t)d.F * d.K;
+    if (!gelu) return tall ? launch_gated_stream_as<GS_SILU, 256>(s, w, stream) : launch_gated_stream_as<GS_SILU, 128>(s, w, stream);
+    if (gelu_fast && -2 * (int64_t)p.gelu.q_b < GS_ERF)
+        return tall ? launch_gated_stream_as<GS_GELU_TABLE, 256>(s, w, stream) : launch_gated_stream_as<GS_GELU_TABLE, 128>(s, w, stream);
+    return tall ? launch_gated_stream_as<GS_GELU, 256>(s, w, stream) : launch_gated_stream_as<GS_GELU, 128>(s, w, stream);
 }
 
 }  // namespace ibert

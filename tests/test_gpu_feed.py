@@ -9,7 +9,7 @@ import feed_util as U
 from test_gpu_decoder import libs, same
 
 
-@pytest.fixture(params=[(-1, -1), (1, 0), (1, 3), (2, 1), (2, 2), (0, 0), (9, 1), (9, 4), (10, 2), (10, 8), (12, 1), (12, 4)], ids=lambda p: "t%d_g%d" % p)
+@pytest.fixture(params=[(-1, -1), (1, 0), (1, 3), (2, 1), (2, 2), (0, 0), (0, 1), (9, 1), (9, 4), (10, 2), (10, 8), (12, 1), (12, 4)], ids=lambda p: "t%d_g%d" % p)
 def form(request, gpu):
     from paper_2101_01321_amd import binding as B
     B.ibert_rows_override(*request.param)
@@ -101,10 +101,10 @@ def test_w4(form, M, N, K, group, zeros):
     run(U.Rows4(M + N + K, M, N, K, group, zeros, out, residual=bool((N + zeros) % 2), bias=M % 3 != 0), "w4 %d x %d x %d, groups of %d, %s" % (M, N, K, group, out))
 
 
-@pytest.fixture
-def persistent(gpu):
+@pytest.fixture(params=[0, 1], ids=["tall", "low"])
+def persistent(request, gpu):
     from paper_2101_01321_amd import binding as B
-    B.ibert_rows_override(0, 0)
+    B.ibert_rows_override(0, request.param)
     yield
     B.ibert_rows_override(-1, -1)
 
@@ -131,6 +131,7 @@ def test_persistent_gated_strides(persistent, ld, off, act):
 
 @pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
 def test_persistent_gated_any_constants(persistent, act):
+    from paper_2101_01321_amd import binding as B
     # shifts below 33, biases of 31 bits and an output shift below 33 take the general epilogue, tile by tile; the tiles beside them do not
     c = U.Gated(7 + act, 5000, 1400, 128, act)
     c.ch.m[200], c.ch.s[200] = 3, 1
@@ -147,6 +148,13 @@ def test_persistent_gated_any_constants(persistent, act):
     if act:
         c.params.gelu.out.m, c.params.gelu.out.s = -3, 32
         run(c, "persistent gated, gelu's small shift")
+        # a scale so fine that erf's table finds no room
+        c = U.Gated(11, 700, 300, 256, act)
+        c.params.gelu = B.ibert_gelu_params_from_scale(1 / 1500, 1 / 6000)
+        assert c.params.gelu.q_b < -1700
+        c.ch.m[:300] = c.ch.m[:300] // 8
+        run(c, "persistent gated, gelu computed")
+        ran("gated_stream_kernel<0")
 
 
 @pytest.mark.parametrize("off", [0, 1, 4, 13])
