@@ -2,6 +2,9 @@
 //
 // A workgroup takes a slice of one row's vocabulary.  It counts the row's tokens that fall into the slice, and adds up the biases there, in
 // LDS (integer atomics: any order gives the same), then passes over the logits once.  The history is read once per slice, from L2.
+// What bounds it: the logits' way through HBM (64 x 128000, 65.5 MB: 16.0 us without a history, 4.1 TB/s with the launch), and behind it the trips to memory of a workgroup
+// whose row has a history (where its tokens are, the tokens): 22.9 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
+// slice (workgroups that go through several slices) or dealt to wavefronts of their own, the loads cost so many registers that fewer workgroups fit: 35.7 and 42.4 us.
 #include "common.h"
 
 namespace ibert {
@@ -26,7 +29,7 @@ struct LogitsArgs {
 };
 
 // Threads of a workgroup, tokens of its slice.  The logits of a slice (8 a thread) are requested first and arrive while the history is counted.
-constexpr int LOGITS_THREADS = 512, LOGITS_SLICE = 4096;
+constexpr int LOGITS_THREADS = 512;
 constexpr uint32_t SEEN = 0x80000000u, BIASED = 0x40000000u;     // in the prompt; has biases; the low bits count what has been produced
 
 __device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t bias, const ibert_logits_row& p, int32_t us, int32_t ds)
@@ -43,13 +46,14 @@ __device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t b
     return (int32_t)(v <= INT32_MIN ? INT32_MIN + 1 : (v > INT32_MAX ? INT32_MAX : v));
 }
 
-__global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArgs g)
+template <int LOGITS_SLICE>
+__global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(LogitsArgs g)
 {
-    extern __shared__ __align__(16) unsigned long long room[];
+    extern __shared__ __align__(16) int32_t room[];
     const int tid = threadIdx.x, row = blockIdx.x / g.slices, t0 = (blockIdx.x - row * g.slices) * LOGITS_SLICE;
     const int n = min(LOGITS_SLICE, g.vocab - t0);
-    unsigned long long* const bias = room;                          // [LOGITS_SLICE], where there are biases at all
-    uint32_t* const count = reinterpret_cast<uint32_t*>(room + (g.num_biases > 0 ? LOGITS_SLICE : 0));
+    uint32_t* const count = reinterpret_cast<uint32_t*>(room);
+    int32_t* const bias = room + LOGITS_SLICE;                      // where there are biases at all
     const ibert_logits_row p = g.params[row];
     int ts = 0, te = 0, made = 0, bs = 0, be = 0;
     if (g.num_tokens > 0) {
@@ -62,9 +66,13 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
         be = clamp_i32(g.bias_start[row + 1], bs, g.num_biases);
     }
     const bool biased = be > bs;
+    // Sums of biases have 32 bits where every value is below 2^31 / (be - bs) in size, so that none can overflow; where one is not, who finds a biased token adds up
+    // the row's list in 64 bits.  (With 64 bits for every token a unit holds three workgroups in place of four.)
+    const uint32_t small = biased ? 0x7fffffffu / (uint32_t)(be - bs) : 0;
+    __shared__ int32_t wide;
 
     // Loads arrive in the order in which they are asked for: first what is counted, then the logits.  (The other way round nothing is counted before the
-    // logits are there, and every workgroup takes two trips to memory one after the other: 64 x 128000 with 262 thousand tokens 26.5 us.)
+    // logits are there, and every workgroup takes two trips to memory one after the other: 64 x 128000 with 262 thousand tokens 26.5 / 24.9 us.)
     constexpr int LV = 4, ROUND = 4 * LV * LOGITS_THREADS;          // loads of four tokens under way; tokens of a round
     // four tokens from an aligned place on, none (-1) outside the row's; words of other rows are not read
     auto load4 = [&](int at) {
@@ -104,11 +112,9 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
     }
     for (int i = 4 * tid; i < n; i += 4 * LOGITS_THREADS) {
         *reinterpret_cast<v4i*>(count + i) = v4i{0, 0, 0, 0};
-        if (biased) {
-            *reinterpret_cast<v4i*>(bias + i) = v4i{0, 0, 0, 0};
-            *reinterpret_cast<v4i*>(bias + i + 2) = v4i{0, 0, 0, 0};
-        }
+        if (biased) *reinterpret_cast<v4i*>(bias + i) = v4i{0, 0, 0, 0};
     }
+    if (tid == 0) wide = 0;
     __syncthreads();
     for (int i = first;; i += ROUND) {
 #pragma unroll
@@ -133,14 +139,23 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
         const uint32_t t = (uint32_t)bid - (uint32_t)t0;
         if (t < (uint32_t)n) {
             atomicOr(&count[t], BIASED);
-            atomicAdd(&bias[t], (unsigned long long)(int64_t)bval);
+            atomicAdd(&bias[t], bval);
+            if ((uint32_t)(bval < 0 ? 0u - (uint32_t)bval : (uint32_t)bval) > small) wide = 1;
         }
     }
     __syncthreads();
+    const bool whole = biased && wide;
+    auto bias_of = [&](int i) {
+        if (!whole) return (int64_t)bias[i];
+        int64_t sum = 0;
+        for (int k = bs; k < be; ++k)
+            if (g.bias_ids[k] == t0 + i) sum += g.bias_values[k];
+        return sum;
+    };
     const int32_t us = clamp_i32(p.up.s, 0, 62), ds = clamp_i32(p.down.s, 0, 62);
     auto plain = [&](int i, int32_t v) {
         const uint32_t c = count[i];
-        return c ? adjusted(v, c, c & BIASED ? (int64_t)bias[i] : 0, p, us, ds) : v;
+        return c ? adjusted(v, c, c & BIASED ? bias_of(i) : 0, p, us, ds) : v;
     };
     auto one = [&](int i, int32_t v, uint32_t word) {
         return mask && !((word >> ((t0 + i) & 31)) & 1u) ? INT32_MIN : plain(i, v);
@@ -159,12 +174,21 @@ __global__ __launch_bounds__(LOGITS_THREADS) void logits_adjust_kernel(LogitsArg
     for (int i = (g.vec ? n & ~3 : 0) + tid; i < n; i += LOGITS_THREADS) y[i] = one(i, x[i], mask ? mask[(t0 + i) >> 5] : 0);
 }
 
+template <int LOGITS_SLICE>
 static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
 {
+    auto kern = logits_adjust_kernel<LOGITS_SLICE>;
+    const size_t lds = (size_t)LOGITS_SLICE * (g.num_biases > 0 ? 8 : 4);
+    if (lds > 60000) {
+        static bool attr_done = false;
+        if (!attr_done) {
+            IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 8 * LOGITS_SLICE));
+            attr_done = true;
+        }
+    }
     g.slices = (g.vocab + LOGITS_SLICE - 1) / LOGITS_SLICE;
-    const size_t lds = (size_t)LOGITS_SLICE * (g.num_biases > 0 ? 12 : 4);
     // (a launch may have 2^32 threads at most: pieces of rows)
-    const int64_t most = (1 << 23) / g.slices < 1 ? 1 : (1 << 23) / g.slices;
+    const int64_t most = (1 << 22) / g.slices < 1 ? 1 : (1 << 22) / g.slices;
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
         const int64_t n = rows - r0 < most ? rows - r0 : most;
         LogitsArgs a = g;
@@ -174,10 +198,11 @@ static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
         if (a.token_start) a.token_start += r0;
         if (a.out_start) a.out_start += r0;
         if (a.bias_start) a.bias_start += r0;
-        hipLaunchKernelGGL(logits_adjust_kernel, dim3((unsigned)(n * g.slices)), dim3(LOGITS_THREADS), lds, stream, a);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(n * g.slices)), dim3(LOGITS_THREADS), lds, stream, a);
         IBERT_LAUNCH_CHECK("logits_adjust_kernel");
     }
-    g_last_kernel = "logits_adjust_kernel";
+    static const KernelName name("logits_adjust_kernel<%d>", LOGITS_SLICE);
+    g_last_kernel = name.text;
     return IBERT_OK;
 }
 
@@ -205,5 +230,8 @@ extern "C" int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_
     g.ldx = d.ldx; g.ldy = d.ldy;
     g.vocab = d.vocab; g.num_tokens = d.num_tokens; g.num_biases = d.num_biases; g.num_masks = d.num_masks; g.ld_mask = d.ld_mask;
     g.vec = ibert::aligned(x, 16) && ibert::aligned(y, 16) && d.ldx % 4 == 0 && d.ldy % 4 == 0;
-    return ibert::launch_logits(g, d.rows, static_cast<hipStream_t>(stream));
+    // Slices of 4096, or of 2048 where the longer ones would not be two workgroups to a unit.  us, 2048 / 4096 (8192): 1 x 50265 4.3 / 5.0 (6.6), 64 x 128000 with 262 thousand
+    // tokens and 10 thousand biases 26.6 / 22.9 (25.9), without any 18.7 / 16.0 (16.1).
+    if ((int64_t)d.rows * ((d.vocab + 4095) / 4096) < 512) return ibert::launch_logits<2048>(g, d.rows, static_cast<hipStream_t>(stream));
+    return ibert::launch_logits<4096>(g, d.rows, static_cast<hipStream_t>(stream));
 }
