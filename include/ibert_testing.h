@@ -66,11 +66,11 @@ void ibert_paged_attention_override(int32_t form);
  * negative: what is faster for the rows (the default).  The result never depends on it.  Process-wide, not thread-safe. */
 void ibert_rotary_override(int32_t heads);
 
-/* Which kernels the gated block and the products with 4-bit weights run: `tiles` = 1 or 2 tiles of 16 channels to a wavefront (the gated block takes pairs of them) and
- * 2^`groups` groups of channels to a workgroup (0 to 3); tiles = 9, 10 or 12: the kernel whose wavefronts have rings of their own, with one, two or four tiles (four: of products alone, at most 32 rows) and
- * 8 x `groups` (1, 2, 4, 8) rows to a workgroup, where it can run; tiles = 0: the persistent kernel of the INT8 gated block where it can run, its tiles 256 tokens high, or 128 with groups = 1.  Negative: what is faster (the default).  The result
- * never depends on it.  Process-wide, not thread-safe. */
-void ibert_rows_override(int32_t tiles, int32_t groups);
+/* Which kernels the gated block and the products with 4-bit weights run.  tiles = 1, 2 or 4: the kernels of few rows with so many tiles of 16 channels to a workgroup (pairs of the gated
+ * block; four: of products alone, at most 32 rows), and 8 x `rows` (1, 2, 4, 8) rows, requested straight into LDS where that can be; rows = 0: through registers, as for rows that
+ * are not aligned.  tiles = 0: the persistent kernel of the INT8 gated block where it can run, its tiles 256 tokens high, or 128 with rows = 1.  Negative tiles and rows: what is
+ * faster (the default).  The result never depends on it.  Process-wide, not thread-safe. */
+void ibert_rows_override(int32_t tiles, int32_t rows);
 
 /* Steps 1 to 4 of a layer as one kernel: 0 never; a tile (1000 wavefronts + 100 MFMA rows of one + 10 sequences + stages, one of those ibert_qkv_attention_plan names)
  * wherever its rows hold a sequence and the parameters allow it; negative where it is the faster way (the default).  Process-wide, not thread-safe. */

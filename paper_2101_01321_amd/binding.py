@@ -554,8 +554,8 @@ def ibert_paged_attention_i(desc: PagedAttentionDesc, cache: KvCache, q, ld_q: i
                                        nbytes, _stream(stream)), "ibert_paged_attention_i")
 
 
-def ibert_rows_override(tiles: int, groups: int):
-    lib().ibert_rows_override(tiles, groups)
+def ibert_rows_override(tiles: int, rows: int):
+    lib().ibert_rows_override(tiles, rows)
 
 
 def ibert_gemm_i8_gated(desc: GatedDesc, A, W, bias, mult, shift, out, stream=None):

@@ -10,21 +10,7 @@ template <> int launch_rows<true, 64>(RowsArgs g, const RowsPlan& plan, bool zer
 template <> int launch_rows<true, 128>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream);
 IBERT_ROWS_UNIT(false, 128)
 
-static int g_rows_tiles = -1, g_rows_groups = -1;
-
-static RowsPlan plan_rows(int32_t M, int32_t N)
-{
-    RowsPlan p{};
-    p.mt = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
-    p.nt = g_rows_tiles == 2 ? 2 : 1;
-    p.cg = 0;
-    if (g_rows_groups >= 0) p.cg = g_rows_groups > 3 ? 3 : g_rows_groups;
-    else {
-        const int64_t down = (M + 16 * p.mt - 1) / (16 * p.mt);
-        while (p.cg < 3 && down * ((N + (32 * p.nt << p.cg) - 1) / (32 * p.nt << p.cg)) >= 512) ++p.cg;
-    }
-    return p;
-}
+static int g_rows_tiles = -1, g_rows_rows = -1;
 
 // Tiles of rows_ring_kernel: 8 br rows that hold M, up to 32 (of INT8 weights 64), by nt tiles of 16 channels (pairs of a gated block).  Wider tiles read A less
 // often, and there must be enough of them.  us, tiles x blocks of rows, at N x K:
@@ -67,23 +53,26 @@ static int plan_gated(int32_t M, int32_t F, int32_t K)
     return M <= 32 || (ring <= low && ring <= tall) ? 0 : (low <= tall ? 1 : 2);
 }
 
-static int launch_few_rows(const RowsArgs& g, bool w4, int32_t group, bool zeros, bool gated, hipStream_t stream)
+static int launch_few_rows(RowsArgs& g, bool w4, int32_t group, bool zeros, bool gated, hipStream_t stream)
 {
-    RowsArgs r = g;
-    r.a_vec = g.a_vec && g.K % 16 == 0;
+    g.chunks = (g.K + 127) / 128;
+    g.per = (g.chunks + 7) / 8;
     RowsPlan p{};
     plan_ring(p, g.M, g.N, g.K, w4, gated);
-    if (g_rows_tiles >= 8) {
-        p.nt = g_rows_tiles == 12 && !gated ? 4 : (g_rows_tiles == 9 ? 1 : 2);
-        if (g_rows_groups >= 1) p.br = g_rows_groups;
+    if (g_rows_tiles > 0) {
+        p.nt = g_rows_tiles == 4 && (gated || !w4) ? 2 : g_rows_tiles;
+        if (g_rows_rows > 0) p.br = g_rows_rows;
     }
-    int per;
     size_t lds;
-    auto fits = [&] { return ring_stages(r, w4, p.br, (gated ? 2 : 1) * p.nt, gated, group, zeros, &per, &lds) > 0; };
-    while (p.nt > 1 && !fits()) p.nt >>= 1;                        // (rows that are held whole leave less room)
+    auto fits = [&] { return ring_stages(g, w4, p.br, (gated ? 2 : 1) * p.nt, gated, group, zeros, &lds) > 0; };
+    const int32_t rows = p.br, tiles = p.nt;
+    while (p.nt > 1 && !fits()) p.nt >>= 1;
     while (p.br > 1 && !fits()) p.br >>= 1;
-    p.ring = (g_rows_tiles < 0 || g_rows_tiles >= 8) && fits();
-    if (!p.ring) p = plan_rows(g.M, g.N);
+    p.ring = g_rows_rows != 0 && fits();
+    if (!p.ring) {
+        p.br = rows;
+        p.nt = tiles;
+    }
     if (!w4) return launch_rows<false, 128>(g, p, false, true, stream);
     if (group == 32) return launch_rows<true, 32>(g, p, zeros, gated, stream);
     if (group == 64) return launch_rows<true, 64>(g, p, zeros, gated, stream);
@@ -140,16 +129,16 @@ static RowsArgs rows_args(const int8_t* A, int64_t lda, int32_t M, int32_t N, in
     g.A = A; g.lda = lda; g.M = M; g.N = N; g.K = K;
     g.bias = bias; g.mult = mult; g.shift = shift;
     g.C = C; g.ldc = ldc;
-    g.a_vec = aligned(A, 16) && lda % 16 == 0;
+    g.a_vec = aligned(A, 16) && lda % 16 == 0 && K % 16 == 0;
     return g;
 }
 
 }  // namespace ibert
 
-extern "C" void ibert_rows_override(int32_t tiles, int32_t groups)
+extern "C" void ibert_rows_override(int32_t tiles, int32_t rows)
 {
     ibert::g_rows_tiles = tiles;
-    ibert::g_rows_groups = groups;
+    ibert::g_rows_rows = rows;
 }
 
 extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A, const int8_t* W, const int32_t* bias,
@@ -163,7 +152,7 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     if (!W) return IBERT_ERR_NULL;
     const ibert_gated_desc& d = *desc;
     if (ibert::overlap(C, ibert::span(d.M, d.ldc, d.F, 1), W, ibert::span(2 * (int64_t)d.F, d.ldw, d.K, 1))) return IBERT_ERR_SHAPE;
-    const int persistent = ibert::g_rows_tiles == 0 ? (ibert::g_rows_groups == 1 ? 1 : 2) : (ibert::g_rows_tiles < 0 ? ibert::plan_gated(d.M, d.F, d.K) : 0);
+    const int persistent = ibert::g_rows_tiles == 0 ? (ibert::g_rows_rows == 1 ? 1 : 2) : (ibert::g_rows_tiles < 0 ? ibert::plan_gated(d.M, d.F, d.K) : 0);
     if (persistent && ibert::gated_stream_ok(d, A, W))
         return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, persistent == 2, static_cast<hipStream_t>(stream));
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);

@@ -1,16 +1,16 @@
 // Products of few activation rows with weight matrices that are read once: 4-bit weights with group scales, and the INT8 weights of
 // a gated block; plain (bias, requantization, residual) or ending in the gated product.
 //
-//   * A wavefront owns 16 NT channels and every KS-th chunk of 128 of K; its weights come straight from memory into registers, a few
-//     chunks ahead, and are used once.  4-bit weights stand in memory as the matrix unit wants them: 1 KB a tile of 16 channels and
-//     chunk, 16 bytes a lane, whose low and high halves are the operands of two MFMAs.  A nibble shifted to the top of its byte is
-//     16 times its signed value, so that two operations on a dword unpack four weights, and the sums of a group (|sum| < 2^18) are
-//     shifted back.
-//   * The rows of A are staged in LDS in operand order, a slab of chunks at a time, bytes past K as zeros: what weights hold there
-//     does not matter.
-//   * sum_g s_g (sum_k a w - z_g sum_k a): the sum of a group's activations comes from an MFMA with ones, which leaves it in the lanes
-//     that need it.  Group terms are added by 24-bit multiply-adds in 32 bits, which hold 4096 values of K
-//     (4096 * 128 * 15 * 255 < 2^31), then in 64 bits in LDS, where the wavefronts of a workgroup meet: integer sums, any order.
+//   * The eight wavefronts of a workgroup share K in contiguous runs of chunks of 128, each for 8 BR rows and NT tiles of 16 channels, and work on their own until their
+//     sums meet in LDS: integer sums, any order.
+//   * 4-bit weights stand in memory as the matrix unit wants them: 1 KB a tile and chunk, 16 bytes a lane, whose low and high halves are the operands of two MFMAs.  A nibble
+//     shifted to the top of its byte is 16 times its signed value, so that two operations on a dword unpack four weights, and the sums of a group (|sum| < 2^18) are shifted
+//     back.
+//   * sum_g s_g (sum_k a w - z_g sum_k a): the sum of a group's activations comes from an MFMA with ones, which leaves it in the lanes that need it.  Group terms are added
+//     by 24-bit multiply-adds in 32 bits, which hold 4096 values of K (4096 * 128 * 15 * 255 < 2^31), then in 64.
+//   * Activations past K are zeros: what weights hold there does not matter.
+//   * Two kernels.  rows_ring_kernel: rows that are 16-byte aligned, K a multiple of 16; everything goes from memory straight into LDS, several chunks ahead.
+//     rows_any_kernel: everything else, through registers, one chunk ahead.
 #pragma once
 #include <type_traits>
 
@@ -39,35 +39,33 @@ struct RowsArgs {
     int64_t ldc;
     int32_t out_dtype, out_clamp;
     GateConst gate;
-    int32_t chunks, slab;          // chunks of 128 in K; of a slab (a multiple of KS * RING)
-    int32_t cg;                    // log2 of the groups of channels of a workgroup: 2^cg groups by KS = 8 >> cg shares of K
-    int32_t mp;                    // log2 of the rows held in LDS
-    int32_t a_vec, w_vec;          // 16-byte loads of A, of INT8 weights
+    int32_t chunks, per;           // chunks of 128 in K; of a wavefront's run
+    int32_t stages;                // of a wavefront's ring
+    int32_t a_vec, w_vec;          // rows of A, of INT8 weights are 16-byte aligned and K is a multiple of 16
     int32_t across, down;          // workgroups over the channels and over the rows
 };
 
 constexpr int ROWS_THREADS = 512;
-// chunks of weights that a wavefront has under way
-constexpr int rows_ring(int mt) { return mt == 4 ? 2 : 4; }
 
-// 16 bytes of a buffer, zeros past its end.
-__device__ __forceinline__ v4i buffer_16(const void* base, uint32_t bytes, uint32_t offset)
-{
-    typedef unsigned int v4u __attribute__((ext_vector_type(4)));
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
-    const v4u v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)offset, 0, 0);
-    return v4i{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
-}
-
-// 16 bytes of a row of n bytes at p from byte k on, zeros past its end; any alignment (memory is read unaligned here).
+// 16 bytes of a row of n bytes at p from byte k on, zeros past its end; any alignment (memory is read unaligned here).  The last bytes of a row are moved down from its last 16:
+// byte by byte they take as many trips to memory.
 __device__ __forceinline__ v4i bytes_16(const int8_t* p, int k, int n)
 {
-    union { v4i v; int8_t b[16]; } u;
+    union { v4i v; uint64_t h[2]; int8_t b[16]; } u;
     if (k + 16 <= n) {
         __builtin_memcpy(u.b, p + k, 16);
         return u.v;
     }
     u.v = v4i{0, 0, 0, 0};
+    if (k >= n) return u.v;
+    if (n >= 16) {
+        __builtin_memcpy(u.b, p + n - 16, 16);
+        const int s = 8 * (k + 16 - n);                            // 8 .. 120
+        if (s >= 64) u.h[0] = u.h[1] >> (s - 64);
+        else u.h[0] = u.h[0] >> s | u.h[1] << (64 - s);
+        u.h[1] = s >= 64 ? 0 : u.h[1] >> s;
+        return u.v;
+    }
     for (int i = 0; i < 16; ++i)
         if (k + i < n) u.b[i] = p[k + i];
     return u.v;
@@ -154,210 +152,38 @@ __device__ __forceinline__ void rows_finish(const RowsArgs& g, int m, int n, int
     }
 }
 
-// W4: 4-bit weights in groups of G (ZERO: with zero points), else INT8 rows.  GATED: NT / 2 tiles of gate channels, then as many of the up projection.
-template <bool W4, int MT, int NT, int G, bool ZERO, bool GATED>
-__global__ __launch_bounds__(ROWS_THREADS) void rows_kernel(RowsArgs g)
+// INT8 sums have 32 bits, and so has what the biases make of them.
+__device__ __forceinline__ void wrap_32(int64_t& s0, int64_t& s1, RowsChannel& c0, RowsChannel& c1)
 {
-    typedef std::conditional_t<W4, unsigned long long, unsigned int> sum_t;
-    constexpr int ROWS_RING = rows_ring(MT), NH = GATED ? NT / 2 : NT, GPC = W4 ? 128 / G : 1, WR = W4 ? 1 : 2;
-    static_assert(!GATED || NT % 2 == 0, "pairs of tiles");
-    extern __shared__ __align__(16) int8_t lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r = lane & 15, q = lane >> 4;
-    const int cgi = wave & ((1 << g.cg) - 1), kg = wave >> g.cg, ks = 8 >> g.cg;
-    // workgroups go round the XCDs: those of the same channels stand on the same one, whose L2 then holds their weights
-    const int j = blockIdx.x >> 3, jc = j / g.down, bx = jc * 8 + (blockIdx.x & 7);
-    if (bx >= g.across) return;
-    const int cols = 16 * NT << g.cg, m0 = (j - jc * g.down) * (16 * MT), rows = min(16 * MT, g.M - m0);
-    const int b0 = bx * (16 * NH << g.cg), n0 = b0 + cgi * (16 * NH);        // first output column of the workgroup, of the wavefront
-    const int abytes = (g.slab << 7) << g.mp;
-    sum_t* const sums = reinterpret_cast<sum_t*>(lds + abytes);                         // [16 MT][cols]
-
-    // the tiles that lie past the last channel read the last one again: nothing of them is stored
-    const uint8_t *wp[NT], *sp[NT], *zp[NT];
-    uint32_t wbytes[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int half = t / NH, c = n0 + 16 * (t - half * NH);
-        if (W4) {
-            const int tile = min(c, g.N - 1) >> 4;
-            wp[t] = static_cast<const uint8_t*>(g.w[half]) + (int64_t)tile * g.chunks * 1024;
-            wbytes[t] = (uint32_t)g.chunks * 1024u;
-            sp[t] = g.scales[half] + (int64_t)tile * g.chunks * (16 * GPC);
-            zp[t] = ZERO ? reinterpret_cast<const uint8_t*>(g.zeros[half]) + (int64_t)tile * g.chunks * (16 * GPC) : nullptr;
-        } else {
-            const int first = min(c, g.N - 1), left = min(16, g.N - first);
-            wp[t] = static_cast<const uint8_t*>(g.w[0]) + (int64_t)(half * g.N + first) * g.ldw;
-            wbytes[t] = (uint32_t)((left - 1) * g.ldw + g.K);
-            sp[t] = zp[t] = nullptr;
-        }
-    }
-    struct Piece {
-        v4i w[WR];
-        uint32_t s, z;
-    };
-    auto load = [&](int t, int c) {
-        Piece p;
-        if constexpr (W4) {
-            p.w[0] = buffer_16(wp[t], wbytes[t], (uint32_t)c * 1024u + (uint32_t)lane * 16u);      // (zeros from the last chunk on, without a request)
-            const int at = (min(c, g.chunks - 1) * 16 + r) * GPC;
-            if (GPC == 4) p.s = *reinterpret_cast<const uint32_t*>(sp[t] + at);
-            else if (GPC == 2) p.s = *reinterpret_cast<const uint16_t*>(sp[t] + at);
-            else p.s = sp[t][at];
-            if constexpr (ZERO) {
-                if (GPC == 4) p.z = *reinterpret_cast<const uint32_t*>(zp[t] + at);
-                else if (GPC == 2) p.z = *reinterpret_cast<const uint16_t*>(zp[t] + at);
-                else p.z = zp[t][at];
-            }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = 64 * h + 16 * q;
-                if (g.w_vec) p.w[h] = buffer_16(wp[t], wbytes[t], (uint32_t)(r * (int)g.ldw + k + c * 128));
-                else {
-                    const int half = t / NH, n = min(n0 + 16 * (t - half * NH) + r, g.N - 1);
-                    p.w[h] = bytes_16(static_cast<const int8_t*>(g.w[0]) + (int64_t)(half * g.N + n) * g.ldw, c * 128 + k, g.K);
-                }
-            }
-        }
-        return p;
-    };
-
-    Piece ring[ROWS_RING][NT];
-#pragma unroll
-    for (int i = 0; i < ROWS_RING; ++i)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) ring[i][t] = load(t, kg + i * ks);
-    for (int i = tid; i < 16 * MT * cols; i += ROWS_THREADS) sums[i] = 0;
-
-    v4i acc[MT][NT];
-#pragma unroll
-    for (int j = 0; j < MT; ++j)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[j][t] = v4i{0, 0, 0, 0};
-    auto flush = [&]() {
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    atomicAdd(&sums[(16 * j + 4 * q + e) * cols + cgi * 16 * NT + 16 * t + r], (sum_t)(int64_t)acc[j][t][e]);
-                acc[j][t] = v4i{0, 0, 0, 0};
-            }
-    };
-
-    int since = 0;                                                 // chunks in the 32-bit sums
-    const int mask = (1 << g.mp) - 1, qstep = 16 << g.mp;
-    for (int s0 = 0; s0 < g.chunks; s0 += g.slab) {
-        const int s1 = min(g.chunks, s0 + g.slab);
-        if (s0) __syncthreads();                                   // the slab before has been read
-        // ---- stage A: 16 bytes of a row at a time
-        for (int u = tid; u < ((s1 - s0) << 3) << g.mp; u += ROWS_THREADS) {
-            const int v = u & 7, row = (u >> 3) & mask, c = u >> (3 + g.mp), k = (s0 + c) * 128 + 16 * v;
-            if (row >= rows) continue;
-            const int8_t* p = g.A + (int64_t)(m0 + row) * g.lda;
-            const v4i x = g.a_vec && k + 16 <= g.K ? *reinterpret_cast<const v4i*>(p + k) : bytes_16(p, k, g.K);
-            int8_t* const at = lds + (c * 8 + (v >> 2) * 4) * qstep + row * 16;
-            if constexpr (W4) {
-                int8_t* const d = at + 2 * (v & 1) * qstep + ((v >> 1) & 1) * 8;
-                *reinterpret_cast<v2i*>(d) = v2i{x[0], x[1]};
-                *reinterpret_cast<v2i*>(d + qstep) = v2i{x[2], x[3]};
-            } else {
-                *reinterpret_cast<v4i*>(at + (v & 3) * qstep) = x;
-            }
-        }
-        __syncthreads();
-        for (int c0 = s0 + kg; c0 < s1; c0 += ks * ROWS_RING) {
-#pragma unroll
-            for (int i = 0; i < ROWS_RING; ++i) {
-                const int c = c0 + i * ks;
-                if (c < s1) {
-                    v4i xa[2][MT];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int j = 0; j < MT; ++j)
-                            xa[h][j] = *reinterpret_cast<const v4i*>(lds + ((c - s0) * 8 + h * 4 + q) * qstep + ((16 * j + r) & mask) * 16);
-                    if constexpr (!W4) {
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                                for (int j = 0; j < MT; ++j)
-                                    acc[j][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[h][j], ring[i][t].w[h], acc[j][t], 0, 0, 0);
-                    } else {
-                        v4i w[NT];
-                        uint32_t sc[NT], zc[NT];
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            w[t] = ring[i][t].w[0];
-                            sc[t] = ring[i][t].s;
-                            if constexpr (ZERO) zc[t] = ring[i][t].z;
-                        }
-                        chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) ring[i][t] = load(t, c + ROWS_RING * ks);
-            }
-            since += ROWS_RING;
-            if (W4 && since + ROWS_RING > 32) {
-                flush();
-                since = 0;
-            }
-        }
-    }
-    flush();
-    __syncthreads();
-
-    // ---- epilogue: an output a thread and round
-    for (int i = tid; i < rows * (16 * NH << g.cg); i += ROWS_THREADS) {
-        const int m = i / (16 * NH << g.cg), nn = i - m * (16 * NH << g.cg), n = b0 + nn;
-        if (n >= g.N) continue;
-        const sum_t* const row = sums + m * cols;
-        auto sum = [&](const sum_t& v) { return W4 ? (int64_t)v : (int64_t)(int32_t)v; };
-        const int wv = nn / (16 * NH), in = nn - wv * (16 * NH);
-        RowsChannel c0 = rows_channel(g, n), c1 = rows_channel(g, GATED ? g.N + n : n);
-        int64_t s0 = sum(row[GATED ? wv * 16 * NT + in : nn]), s1 = sum(row[GATED ? wv * 16 * NT + 16 * NH + in : nn]);
-        if constexpr (!W4) {                                       // (INT8 sums have 32 bits, and so has what the bias makes of them)
-            s0 = (int32_t)((uint32_t)s0 + (uint32_t)c0.b);
-            s1 = (int32_t)((uint32_t)s1 + (uint32_t)c1.b);
-            c0.b = c1.b = 0;
-        }
-        rows_finish<GATED>(g, m0 + m, n, s0, s1, c0, c1, !GATED && g.R ? g.R[(int64_t)(m0 + m) * g.ldr + n] : 0);
-    }
+    s0 = (int32_t)((uint32_t)s0 + (uint32_t)c0.b);
+    s1 = (int32_t)((uint32_t)s1 + (uint32_t)c1.b);
+    c0.b = c1.b = 0;
 }
 
-// The same where nothing in the loop waits for another wavefront.
-//   * The eight wavefronts of a workgroup share K in contiguous runs of chunks.  Each has a ring of stages of its own in LDS -- 1 KB blocks of eight rows of A by
-//     128 bytes, and of a tile's chunk of weights -- into which it requests straight from memory as many chunks ahead as LDS holds; scales (and zero points) of its
-//     whole run come first.  Rows of A that are not aligned (or K, to 16) are copied there whole before the loop, through registers, behind the first requests
-//     of weights.  The sums (a run is at most 4096 values: 32 bits) meet in LDS at the end.
+//   * Each wavefront has a ring of stages of its own in LDS -- 1 KB blocks of eight rows of A by 128 bytes, and of a tile's chunk of weights -- into which it requests
+//     straight from memory as many chunks ahead as LDS holds; scales (and zero points) of its whole run come first.  The sums (a run is at most 4096 values: 32 bits) meet in LDS at the end.
 //   * A's 16-byte units are swizzled by the row (see swz in gemm_kernel.h); a lane's operand is two reads of eight bytes, 32 apart.
-// BR: blocks of eight rows (1, 2, 4 or 8); NT, G, ZERO, GATED: see rows_kernel.
+// W4: 4-bit weights in groups of G (ZERO: with zero points), else INT8 rows.  BR: blocks of eight rows (1, 2, 4 or 8).  GATED: NT / 2 tiles of gate channels, then as many of the
+// up projection.
 template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
 __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
 {
     // (blocks of a tile's chunk of weights: 1, or 2 of eight INT8 rows; requests of a chunk)
-    constexpr int WB = W4 ? 1 : 2, NLW = WB * NT;
+    constexpr int WB = W4 ? 1 : 2, NL = BR + WB * NT, STAGE = NL * 1024;
     constexpr int MT = (BR + 1) / 2, NH = GATED ? NT / 2 : NT, GPC = W4 ? 128 / G : 0;
     constexpr int TM = 8 * BR, PITCH = 16 * NT + 4;                // rows of the tile; dwords of a row of sums
     constexpr int EP = (TM * 16 * NH + ROWS_THREADS - 1) / ROWS_THREADS;
     constexpr int SUMS = TM * PITCH * 4;                           // bytes of a wavefront's sums, where its stages were
-    static_assert(3 * (BR + NLW) < 64, "outstanding requests");
+    static_assert(3 * NL < 64, "outstanding requests");
     extern __shared__ __align__(16) int8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
     const int jb = blockIdx.x >> 3, jc = jb / g.down, bx = jc * 8 + (blockIdx.x & 7);
     if (bx >= g.across) return;
     const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
-    const int per = g.slab, c0 = wave * per, run = min(per, g.chunks - c0);           // this wavefront's chunks [c0, c0 + run)
-    const bool direct = g.a_vec;                                   // A through the ring
-    const int STAGE = ((direct ? BR : 0) + NLW) * 1024, held = direct ? 0 : per * BR * 1024;
-    const int stages = g.mp, scb = (per * 16 * GPC + 255) & ~255;                       // bytes of a tile's scales
-    const int own = (ZERO ? 2 : 1) * NT * scb + max(held + stages * STAGE, SUMS);
+    const int per = g.per, c0 = wave * per, run = min(per, g.chunks - c0);           // this wavefront's chunks [c0, c0 + run)
+    const int stages = g.stages, scb = (per * 16 * GPC + 255) & ~255;                       // bytes of a tile's scales
+    const int own = (ZERO ? 2 : 1) * NT * scb + max(stages * STAGE, SUMS);
     int8_t* const home = lds + wave * own;
     const uint32_t home0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds + (uint32_t)(wave * own);
     const uint32_t ring0 = home0 + (uint32_t)((ZERO ? 2 : 1) * NT * scb);
@@ -424,49 +250,29 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
                 for (int b = 0; b < 2; ++b) vw[2 * t + b] = (uint32_t)(min(8 * b + lr8, left - 1) * (int)g.ldw + (b ? unit1 : unit0) * 16);
             }
         }
-        const int ahead = direct ? BR * 1024 : 0;                  // where a stage's weights begin
         auto request = [&](int chunk, int st) {
             const int c = __builtin_amdgcn_readfirstlane(chunk);   // (the same in every lane: the compiler loses sight of it)
-            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)ring0 + held + st * STAGE);
-            if (direct) {
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)ring0 + st * STAGE);
 #pragma unroll
-                for (int b = 0; b < BR; ++b)
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+            for (int b = 0; b < BR; ++b)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                              :: "s"(to + (uint32_t)(b * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? va[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(da)
                              : "memory", "m0");
-            }
             if constexpr (W4) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
                     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                                 :: "s"(to + (uint32_t)(ahead + t * 1024)), "v"((uint32_t)lane * 16u), "s"(wp[t] + (int64_t)c * 1024) : "memory", "m0");
+                                 :: "s"(to + (uint32_t)((BR + t) * 1024)), "v"((uint32_t)lane * 16u), "s"(wp[t] + (int64_t)c * 1024) : "memory", "m0");
             } else {
 #pragma unroll
                 for (int b = 0; b < 2 * NT; ++b)
                     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                                 :: "s"(to + (uint32_t)(ahead + b * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? vw[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(dw[b / 2])
+                                 :: "s"(to + (uint32_t)((BR + b) * 1024)), "v"(c * 128 < (b & 1 ? left1 : left0) ? vw[b] + (uint32_t)(c * 128) : 0xfffffff0u), "s"(dw[b / 2])
                                  : "memory", "m0");
             }
         };
         for (int i = 0; i < stages; ++i)
             if (i < run) request(c0 + i, i);
-        if (!direct) {
-            constexpr int U = BR >= 4 ? 1 : 4 / BR;                // chunks whose loads are under way together
-            for (int i0 = 0; i0 < run; i0 += U) {
-                v4i x[U][BR];
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-#pragma unroll
-                    for (int b = 0; b < BR; ++b)
-                        if (i0 + i < run)
-                            x[i][b] = bytes_16(g.A + (int64_t)(m0 + min(8 * b + lr8, rows - 1)) * g.lda, (c0 + i0 + i) * 128 + (b & 1 ? unit1 : unit0) * 16, g.K);
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-#pragma unroll
-                    for (int b = 0; b < BR; ++b)
-                        if (i0 + i < run) *reinterpret_cast<v4i*>(ring + ((i0 + i) * BR + b) * 1024 + lane * 16) = x[i][b];
-            }
-        }
         ends();
 
         v4i acc[MT][NT];
@@ -481,17 +287,12 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
         int st = 0;
         for (int i = 0; i < run; ++i) {
             const int younger = min(run - 1 - i, stages - 1);
-            if (younger == 0 || !direct) {
-                if (younger == 0) __builtin_amdgcn_s_waitcnt(vm(0));
-                else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(NLW));
-                else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * NLW));
-                else __builtin_amdgcn_s_waitcnt(vm(3 * NLW));
-            } else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(BR + NLW));
-            else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * (BR + NLW)));
-            else __builtin_amdgcn_s_waitcnt(vm(3 * (BR + NLW)));
+            if (younger == 0) __builtin_amdgcn_s_waitcnt(vm(0));
+            else if (younger == 1) __builtin_amdgcn_s_waitcnt(vm(NL));
+            else if (younger == 2) __builtin_amdgcn_s_waitcnt(vm(2 * NL));
+            else __builtin_amdgcn_s_waitcnt(vm(3 * NL));
             asm volatile("" ::: "memory");
-            const int8_t* const wbase = ring + held + st * STAGE + ahead;
-            const int8_t* const base = direct ? ring + st * STAGE : ring + i * BR * 1024;
+            const int8_t* const base = ring + st * STAGE;
             v4i xa[2][MT];
             if constexpr (!W4) {
                 v4i w[2][NT];
@@ -500,7 +301,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
 #pragma unroll
                     for (int j = 0; j < MT; ++j) xa[h][j] = *reinterpret_cast<const v4i*>(base + j * 2048 + (a8 ^ (h * 64)));
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) w[h][t] = *reinterpret_cast<const v4i*>(wbase + 2 * t * 1024 + (w8 ^ (h * 64)));
+                    for (int t = 0; t < NT; ++t) w[h][t] = *reinterpret_cast<const v4i*>(base + (BR + 2 * t) * 1024 + (w8 ^ (h * 64)));
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -524,7 +325,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    w[t] = *reinterpret_cast<const v4i*>(wbase + t * 1024 + lane * 16);
+                    w[t] = *reinterpret_cast<const v4i*>(base + (BR + t) * 1024 + lane * 16);
                     auto scale = [&](const int8_t* p) {
                         p += (i * 16 + r) * GPC;
                         return GPC == 4 ? *reinterpret_cast<const uint32_t*>(p) : (GPC == 2 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint8_t*>(p));
@@ -566,11 +367,163 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
                 s0 += *reinterpret_cast<const int32_t*>(at + w * own);
                 if constexpr (GATED) s1 += *reinterpret_cast<const int32_t*>(at + w * own + 64 * NH);
             }
-        if constexpr (!W4) {                                       // (INT8 sums have 32 bits, and so has what the bias makes of them)
-            s0 = (int32_t)((uint32_t)s0 + (uint32_t)ch[p][0].b);
-            s1 = (int32_t)((uint32_t)s1 + (uint32_t)ch[p][GATED ? 1 : 0].b);
-            ch[p][0].b = ch[p][GATED ? 1 : 0].b = 0;
+        if constexpr (!W4) wrap_32(s0, s1, ch[p][0], ch[p][GATED ? 1 : 0]);
+        rows_finish<GATED>(g, m0 + m, n, s0, s1, ch[p][0], ch[p][GATED ? 1 : 0], res[p]);
+    }
+}
+
+// Rows of any alignment, any K.  A wavefront's next chunk is on its way into registers while it multiplies this one, whose rows pass through LDS (their units swizzled as in
+// rows_ring_kernel; 4-bit weights need not).  Sums of 4-bit weights go to 64 bits in LDS every 32 chunks.
+template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
+__global__ __launch_bounds__(ROWS_THREADS) void rows_any_kernel(RowsArgs g)
+{
+    typedef std::conditional_t<W4, int64_t, int32_t> sum_t;
+    constexpr int MT = (BR + 1) / 2, NH = GATED ? NT / 2 : NT, GPC = W4 ? 128 / G : 1, WB = W4 ? 1 : 2, TM = 8 * BR, PITCH = 16 * NT + 4;
+    constexpr int EP = (TM * 16 * NH + ROWS_THREADS - 1) / ROWS_THREADS;
+    constexpr int STAGE = (BR + (W4 ? 0 : 2 * NT)) * 1024, SUMS = TM * PITCH * (int)sizeof(sum_t);
+    // (sums of INT8 weights go, at the end, where the stage was)
+    constexpr int SUMS_AT = W4 ? STAGE : 0, OWN = W4 ? STAGE + SUMS : (STAGE > SUMS ? STAGE : SUMS);
+    extern __shared__ __align__(16) int8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const int jb = blockIdx.x >> 3, jc = jb / g.down, bx = jc * 8 + (blockIdx.x & 7);
+    if (bx >= g.across) return;
+    const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
+    const int per = g.per, c0 = wave * per, run = min(per, g.chunks - c0);
+    int8_t* const stage = lds + wave * OWN;
+    sum_t* const sums = reinterpret_cast<sum_t*>(stage + SUMS_AT);
+    // what the epilogue needs of its outputs' channels, behind the first loads: an output a thread and round
+    RowsChannel ch[EP][GATED ? 2 : 1];
+    int32_t res[EP];
+    auto ends = [&]() {
+#pragma unroll
+        for (int p = 0; p < EP; ++p) {
+            const int i = p * ROWS_THREADS + tid, m = i / (16 * NH), n = min(n0 + i - m * (16 * NH), g.N - 1);
+            res[p] = 0;
+            if (m < rows) {
+                ch[p][0] = rows_channel(g, n);
+                if constexpr (GATED) ch[p][1] = rows_channel(g, g.N + n);
+                if (!GATED && g.R) res[p] = g.R[(int64_t)(m0 + m) * g.ldr + n];
+            }
         }
+    };
+    if (run <= 0) ends();
+    else {
+        const int lr8 = lane >> 3, lp = lane & 7;
+        auto tile_of = [&](int t) { return min(n0 + 16 * (t % NH), g.N - 1) >> 4; };
+        struct Chunk {
+            v4i a[BR], w[WB * NT];
+            uint32_t s[NT], z[NT];
+        };
+        auto load = [&](int c, Chunk& x) {
+#pragma unroll
+            for (int b = 0; b < BR; ++b) x.a[b] = bytes_16(g.A + (int64_t)(m0 + min(8 * b + lr8, rows - 1)) * g.lda, c * 128 + 16 * lp, g.K);
+            if constexpr (W4) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int64_t at = (int64_t)tile_of(t) * g.chunks + c;
+                    x.w[t] = *reinterpret_cast<const v4i*>(static_cast<const uint8_t*>(g.w[t / NH]) + at * 1024 + lane * 16);
+                    auto scale = [&](const void* base) {
+                        const uint8_t* p = static_cast<const uint8_t*>(base) + (at * 16 + r) * GPC;
+                        return GPC == 4 ? *reinterpret_cast<const uint32_t*>(p) : (GPC == 2 ? *reinterpret_cast<const uint16_t*>(p) : *p);
+                    };
+                    x.s[t] = scale(g.scales[t / NH]);
+                    if constexpr (ZERO) x.z[t] = scale(g.zeros[t / NH]);
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < 2 * NT; ++b) {
+                    const int n = min(n0 + 16 * (b / 2 % NH) + 8 * (b & 1) + lr8, g.N - 1);
+                    x.w[b] = bytes_16(static_cast<const int8_t*>(g.w[0]) + ((int64_t)(b / 2 / NH) * g.N + n) * g.ldw, c * 128 + 16 * lp, g.K);
+                }
+            }
+        };
+        v4i acc[MT][NT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[j][t] = v4i{0, 0, 0, 0};
+        // (its own lanes read and write them: no other wavefront does before the barrier)
+        auto keep = [&](bool first) {
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (BR > 1 || q < 2) {
+                            sum_t& s = sums[(16 * j + 4 * q + e) * PITCH + 16 * t + r];
+                            s = (first ? 0 : s) + acc[j][t][e];
+                        }
+                    acc[j][t] = v4i{0, 0, 0, 0};
+                }
+        };
+        // where the lane's 16 bytes of a block go, and where its operands are
+        const int to0 = lr8 * 128 + ((lp ^ (lr8 >> 1)) << 4), ra = BR == 1 ? r & 7 : r;
+        const int a0 = ra * 128 + (((q >> 1) ^ ((ra >> 1) & 7)) << 4) + (q & 1) * 8;
+        const int a8 = ra * 128 + ((q ^ ((ra >> 1) & 7)) << 4), w8 = r * 128 + ((q ^ ((r >> 1) & 7)) << 4);
+        Chunk x;
+        load(c0, x);
+        ends();
+        for (int i = 0; i < run; ++i) {
+#pragma unroll
+            for (int b = 0; b < BR; ++b) *reinterpret_cast<v4i*>(stage + b * 1024 + (b & 1 ? to0 ^ 64 : to0)) = x.a[b];
+            v4i w[NT];
+            uint32_t sc[NT], zc[NT];
+            if constexpr (W4) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    w[t] = x.w[t];
+                    sc[t] = x.s[t];
+                    if constexpr (ZERO) zc[t] = x.z[t];
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < 2 * NT; ++b) *reinterpret_cast<v4i*>(stage + (BR + b) * 1024 + (b & 1 ? to0 ^ 64 : to0)) = x.w[b];
+            }
+            if (i + 1 < run) load(c0 + i + 1, x);
+            v4i xa[2][MT];
+            if constexpr (W4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) {
+                        const v2i lo = *reinterpret_cast<const v2i*>(stage + j * 2048 + (a0 ^ (h * 64))), hi = *reinterpret_cast<const v2i*>(stage + j * 2048 + (a0 ^ (h * 64 + 32)));
+                        xa[h][j] = v4i{lo[0], lo[1], hi[0], hi[1]};
+                    }
+                chunk_products<MT, NT, G, ZERO>(acc, xa, w, sc, zc);
+                if ((i & 31) == 31) keep(i == 31);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v4i wb[NT];
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) xa[h][j] = *reinterpret_cast<const v4i*>(stage + j * 2048 + (a8 ^ (h * 64)));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) wb[t] = *reinterpret_cast<const v4i*>(stage + (BR + 2 * t) * 1024 + (w8 ^ (h * 64)));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < MT; ++j) acc[j][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xa[h][j], wb[t], acc[j][t], 0, 0, 0);
+                }
+            }
+        }
+        keep(!W4 || run < 32);
+    }
+    __syncthreads();
+
+    const int runs = (g.chunks + per - 1) / per;
+#pragma unroll
+    for (int p = 0; p < EP; ++p) {
+        const int i = p * ROWS_THREADS + tid, m = i / (16 * NH), nn = i - m * (16 * NH), n = n0 + nn;
+        if (m >= rows || n >= g.N) continue;
+        int64_t s0 = 0, s1 = 0;
+        for (int w = 0; w < runs; ++w) {
+            const sum_t* const at = reinterpret_cast<const sum_t*>(lds + w * OWN + SUMS_AT) + m * PITCH + nn;
+            s0 += at[0];
+            if constexpr (GATED) s1 += at[16 * NH];
+        }
+        if constexpr (!W4) wrap_32(s0, s1, ch[p][0], ch[p][GATED ? 1 : 0]);
         rows_finish<GATED>(g, m0 + m, n, s0, s1, ch[p][0], ch[p][GATED ? 1 : 0], res[p]);
     }
 }

@@ -4,9 +4,9 @@
 
 namespace ibert {
 
-// ring: rows_ring_kernel, whose workgroups take 8 br rows (br: 1, 2, 4, 8) and nt tiles of channels.  Else rows of a workgroup / 16 (1, 2, 4); tiles of 16 channels to a wavefront, of each matrix of a gated block (1, 2); log2 of its groups of channels
+// ring: rows_ring_kernel, else rows_any_kernel.  A workgroup takes 8 br rows and nt tiles of 16 channels (of a gated block nt pairs).
 struct RowsPlan {
-    int32_t mt, nt, cg, ring, br;
+    int32_t br, nt, ring;
 };
 
 template <bool W4, int G>
@@ -37,51 +37,19 @@ int rows_pieces(F kern, RowsArgs g, int tm, int tn, size_t lds, hipStream_t stre
     return IBERT_OK;
 }
 
-template <bool W4, int MT, int NT, int G, bool ZERO, bool GATED>
-int launch_rows_as(RowsArgs g, const RowsPlan& plan, hipStream_t stream)
-{
-    auto kern = rows_kernel<W4, MT, NT, G, ZERO, GATED>;
-    static bool attr_done = false;
-    if (!attr_done) {
-        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, ROWS_LDS));
-        attr_done = true;
-    }
-    constexpr int NH = GATED ? NT / 2 : NT;
-    const int32_t rows = g.M < 16 * MT ? g.M : 16 * MT;
-    g.mp = 0;
-    while ((1 << g.mp) < rows) ++g.mp;
-    g.cg = plan.cg;
-    g.chunks = (g.K + 127) / 128;
-    // a slab: all of K where 64 KB (or what the sums leave) hold it, else whole rounds of the wavefronts' rings; fewer groups of channels where not one round fits
-    auto sums = [&]() { return (int64_t)16 * MT * (16 * NT << g.cg) * (W4 ? 8 : 4); };
-    auto round = [&]() { return (8 >> g.cg) * rows_ring(MT); };
-    while (g.cg > 0 && sums() + ((int64_t)round() << 7 << g.mp) > ROWS_LDS) --g.cg;
-    const int64_t left = ROWS_LDS - sums(), room = left < 65536 ? left : 65536;
-    const int32_t most = (int32_t)(room >> 7 >> g.mp) / round() * round();
-    g.slab = (g.chunks + round() - 1) / round() * round();
-    if (g.slab > most) g.slab = most < round() ? round() : most;
-    const size_t lds = ((size_t)g.slab << 7 << g.mp) + (size_t)sums();
-    if (lds > (size_t)ROWS_LDS) return IBERT_ERR_NOT_IMPLEMENTED;
-    return rows_pieces(kern, g, 16 * MT, 16 * NH << g.cg, lds, stream, [] {
-        static const KernelName name("rows_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", MT, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
-        return name.text;
-    });
-}
-
 // Can rows_ring_kernel serve these operands, and with how many stages (0: it cannot)?  As many as there is use for, at most four, of what LDS holds beside two
 // more workgroups where there are that many for a unit: us, [1,4096] x 12288 pairs of 4 bits, 768 workgroups, with one stage 13.3, two (three workgroups) 12.3, three
 // (two workgroups) 13.2, four (one) 19.8.
-inline int ring_stages(const RowsArgs& g, bool w4, int br, int tiles, bool gated, int group, bool zeros, int* per, size_t* lds)
+inline int ring_stages(const RowsArgs& g, bool w4, int br, int tiles, bool gated, int group, bool zeros, size_t* lds)
 {
-    const int chunks = (g.K + 127) / 128, tn = 16 * (gated ? tiles / 2 : tiles);
-    *per = (chunks + 7) / 8;
-    if (g.lda > (1 << 24) || (w4 ? *per > 32 : !g.w_vec)) return 0;
-    const size_t sc = w4 ? (size_t)((*per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1) : 0, sums = (size_t)32 * br * (16 * tiles + 4);
-    const size_t held = g.a_vec ? 0 : (size_t)*per * br * 1024, stage = (size_t)((g.a_vec ? br : 0) + tiles * (w4 ? 1 : 2)) * 1024;
-    auto bytes = [&](int n) { return 8 * (sc + (held + n * stage > sums ? held + n * stage : sums)); };
+    const int tn = 16 * (gated ? tiles / 2 : tiles);
+    if (!g.a_vec || g.lda > (1 << 24) || (w4 ? g.per > 32 : !g.w_vec)) return 0;
+    const size_t sc = w4 ? (size_t)((g.per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1) : 0, sums = (size_t)32 * br * (16 * tiles + 4);
+    const size_t stage = (size_t)(br + tiles * (w4 ? 1 : 2)) * 1024;
+    auto bytes = [&](int n) { return 8 * (sc + (n * stage > sums ? n * stage : sums)); };
     const int64_t blocks = (((int64_t)g.N + tn - 1) / tn) * ((g.M + 8 * br - 1) / (8 * br));
     const size_t side = blocks <= 256 ? 1 : (blocks <= 512 ? 2 : 3);
-    int n = *per < 4 ? *per : 4;
+    int n = g.per < 4 ? g.per : 4;
     while (n > 1 && bytes(n) > ROWS_LDS / side) --n;
     *lds = bytes(n);
     return *lds <= (size_t)ROWS_LDS ? n : 0;
@@ -98,10 +66,8 @@ int launch_ring_as(RowsArgs g, hipStream_t stream)
     }
     constexpr int NH = GATED ? NT / 2 : NT, TM = 8 * BR;
     size_t lds;
-    g.a_vec = g.a_vec && g.K % 16 == 0;
-    g.mp = ring_stages(g, W4, BR, NT, GATED, G, ZERO, &g.slab, &lds);
-    if (g.mp == 0) return IBERT_ERR_NOT_IMPLEMENTED;
-    g.chunks = (g.K + 127) / 128;
+    g.stages = ring_stages(g, W4, BR, NT, GATED, G, ZERO, &lds);
+    if (g.stages == 0) return IBERT_ERR_NOT_IMPLEMENTED;
     return rows_pieces(kern, g, TM, 16 * NH, lds, stream, [] {
         static const KernelName name("rows_ring_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", BR, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
         return name.text;
@@ -129,19 +95,32 @@ int launch_ring(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
     return launch_ring_as<W4, 8, 2 * PER, G, ZERO, GATED>(g, stream);
 }
 
-template <bool W4, int G, int MT>
-int launch_rows_of(const RowsArgs& g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream)
+template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
+int launch_any_as(RowsArgs g, hipStream_t stream)
 {
-    if (gated) {
-        if constexpr (!W4) return plan.nt == 2 ? launch_rows_as<W4, MT, 4, G, false, true>(g, plan, stream) : launch_rows_as<W4, MT, 2, G, false, true>(g, plan, stream);
-        else if (plan.nt == 2) return zeros ? launch_rows_as<W4, MT, 4, G, true, true>(g, plan, stream) : launch_rows_as<W4, MT, 4, G, false, true>(g, plan, stream);
-        else return zeros ? launch_rows_as<W4, MT, 2, G, true, true>(g, plan, stream) : launch_rows_as<W4, MT, 2, G, false, true>(g, plan, stream);
+    auto kern = rows_any_kernel<W4, BR, NT, G, ZERO, GATED>;
+    static bool attr_done = false;
+    if (!attr_done) {
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, ROWS_LDS));
+        attr_done = true;
     }
-    if constexpr (W4) {
-        if (plan.nt == 2) return zeros ? launch_rows_as<W4, MT, 2, G, true, false>(g, plan, stream) : launch_rows_as<W4, MT, 2, G, false, false>(g, plan, stream);
-        return zeros ? launch_rows_as<W4, MT, 1, G, true, false>(g, plan, stream) : launch_rows_as<W4, MT, 1, G, false, false>(g, plan, stream);
-    }
-    return IBERT_ERR_NOT_IMPLEMENTED;
+    constexpr int STAGE = (BR + (W4 ? 0 : 2 * NT)) * 1024, SUMS = 8 * BR * (16 * NT + 4) * (W4 ? 8 : 4);
+    constexpr int OWN = W4 ? STAGE + SUMS : (STAGE > SUMS ? STAGE : SUMS);
+    static_assert(8 * OWN <= ROWS_LDS, "LDS of a workgroup");
+    return rows_pieces(kern, g, 8 * BR, 16 * (GATED ? NT / 2 : NT), 8 * OWN, stream, [] {
+        static const KernelName name("rows_any_kernel<%s, %d, %d, %d, %s, %s>", W4 ? "true" : "false", BR, NT, G, ZERO ? "true" : "false", GATED ? "true" : "false");
+        return name.text;
+    });
+}
+
+// (one or four blocks of rows; of INT8 weights eight too, by two pairs)
+template <bool W4, int G, bool ZERO, bool GATED>
+int launch_any(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
+{
+    if constexpr (!W4) if (plan.br >= 8) return launch_any_as<W4, 8, 4, G, ZERO, GATED>(g, stream);
+    if (plan.br >= 2) return launch_any_as<W4, 4, 2, G, ZERO, GATED>(g, stream);
+    if constexpr (W4 && !GATED) if (plan.nt == 1) return launch_any_as<W4, 1, 1, G, ZERO, GATED>(g, stream);
+    return launch_any_as<W4, 1, 2, G, ZERO, GATED>(g, stream);
 }
 
 #define IBERT_ROWS_UNIT(W4_, G_)                                                                                          \
@@ -149,12 +128,13 @@ int launch_rows_of(const RowsArgs& g, const RowsPlan& plan, bool zeros, bool gat
     int launch_rows<W4_, G_>(RowsArgs g, const RowsPlan& plan, bool zeros, bool gated, hipStream_t stream)                \
     {                                                                                                                     \
         if constexpr (W4_) {                                                                                              \
-            if (plan.ring && gated) return zeros ? launch_ring<W4_, G_, true, true>(g, plan, stream) : launch_ring<W4_, G_, false, true>(g, plan, stream);      \
-            if (plan.ring) return zeros ? launch_ring<W4_, G_, true, false>(g, plan, stream) : launch_ring<W4_, G_, false, false>(g, plan, stream);             \
-        } else if (plan.ring) return launch_ring<W4_, G_, false, true>(g, plan, stream);                                  \
-        if (plan.mt == 1) return launch_rows_of<W4_, G_, 1>(g, plan, zeros, gated, stream);                               \
-        if (plan.mt == 2) return launch_rows_of<W4_, G_, 2>(g, plan, zeros, gated, stream);                               \
-        return launch_rows_of<W4_, G_, 4>(g, plan, zeros, gated, stream);                                                 \
+            if (gated) {                                                                                                  \
+                if (plan.ring) return zeros ? launch_ring<W4_, G_, true, true>(g, plan, stream) : launch_ring<W4_, G_, false, true>(g, plan, stream);     \
+                return zeros ? launch_any<W4_, G_, true, true>(g, plan, stream) : launch_any<W4_, G_, false, true>(g, plan, stream);                      \
+            }                                                                                                             \
+            if (plan.ring) return zeros ? launch_ring<W4_, G_, true, false>(g, plan, stream) : launch_ring<W4_, G_, false, false>(g, plan, stream);       \
+            return zeros ? launch_any<W4_, G_, true, false>(g, plan, stream) : launch_any<W4_, G_, false, false>(g, plan, stream);                        \
+        } else return plan.ring ? launch_ring<W4_, G_, false, true>(g, plan, stream) : launch_any<W4_, G_, false, true>(g, plan, stream);                 \
     }
 
 }  // namespace ibert
