@@ -21,7 +21,7 @@ struct GatedStreamArgs {
     const int32_t* mult;
     const int32_t* shift;
     int8_t* C;
-    int32_t M, F, nk;
+    int32_t M, F, K, nk;           // nk: steps of 128 bytes in K
     int32_t lda, ldw, ldc;
     int32_t tiles_m, bn;           // as in StreamArgs
     uint32_t bn_magic;
@@ -48,7 +48,8 @@ struct GatedLayout {
 
 enum { GS_GELU = 0, GS_SILU = 1, GS_GELU_TABLE = 2 };
 
-template <int ACT, int BM>
+// TAIL: K is no multiple of 128 (of 16 it is).
+template <int ACT, int BM, bool TAIL>
 __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArgs g)
 {
     using GL = GatedLayout<BM>;
@@ -106,22 +107,28 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
             int m0, n0;
             tile_at(l, m0, n0);
             const int rows = g.M - m0 < BM ? g.M - m0 : BM, cols = g.F - n0 < GS_BF ? g.F - n0 : GS_BF;
-            buffer(da, g.A + (int64_t)m0 * g.lda, (uint32_t)rows * (uint32_t)g.lda);
-            buffer(dg, g.W + (int64_t)n0 * g.ldw, (uint32_t)cols * (uint32_t)g.ldw);
-            buffer(du, g.W + ((int64_t)g.F + n0) * g.ldw, (uint32_t)cols * (uint32_t)g.ldw);
+            buffer(da, g.A + (int64_t)m0 * g.lda, (uint32_t)(rows - 1) * (uint32_t)g.lda + (uint32_t)g.K);
+            buffer(dg, g.W + (int64_t)n0 * g.ldw, (uint32_t)(cols - 1) * (uint32_t)g.ldw + (uint32_t)g.K);
+            buffer(du, g.W + ((int64_t)g.F + n0) * g.ldw, (uint32_t)(cols - 1) * (uint32_t)g.ldw + (uint32_t)g.K);
             kinc = 128;
         } else {
             da[2] = dg[2] = du[2] = 0;
             kinc = 0;
         }
     };
+    // In the last step of a TAIL the lanes whose bytes lie past K ask for A's outside its buffer: zeros, whatever they meet of W.
+    uint32_t past = 0;
+    auto mark_tail = [&]() {
+        if constexpr (TAIL) past = koff + chunk >= (uint32_t)g.K ? 1u << 30 : 0u;
+    };
+    mark_tail();
     auto request_one = [&](int h, int q) {
         const bool is_a = q < QA;
         const int k = is_a ? q : q - QA;
         const int row = is_a ? h * (WM / 2) + k * SA : h * 32 + k * SW;
         const uint32_t place = rstage + (uint32_t)((is_a ? pa : BM + pw) * 128);
         asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
-                     :: "s"(place), "i"(row * 128), "v"(is_a ? va[h][is_a ? k : 0] : vw[is_a ? 0 : k]), "s"(is_a ? da : (h == 0 ? dg : du)), "s"(koff)
+                     :: "s"(place), "i"(row * 128), "v"(is_a ? (TAIL ? va[h][is_a ? k : 0] + past : va[h][is_a ? k : 0]) : vw[is_a ? 0 : k]), "s"(is_a ? da : (h == 0 ? dg : du)), "s"(koff)
                      : "memory", "m0", "scc");
     };
     auto request_advance = [&]() {
@@ -132,6 +139,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
             rlt += g.per_xcd;
             request_tile(rlt);
         }
+        mark_tail();
     };
     // Constants of a tile: [bias, mult, shift][gate, up][128], by DMA, 64 dwords a request; zeros past the last channel.
     int par_n0 = -1, par_buf = 1;
@@ -418,6 +426,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
             koff = 0;
             rstage = lds0 + (uint32_t)stage;
             request_tile(rlt);
+            mark_tail();
             request_two_steps();
             __builtin_amdgcn_s_waitcnt(vm(0));
             asm volatile("s_barrier" ::: "memory");
@@ -431,11 +440,11 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 
 bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W)
 {
-    return d.K % 128 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
+    return d.K % 16 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
            (int64_t)((d.M + 127) / 128) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
 }
 
-template <int ACT, int BM>
+template <int ACT, int BM, bool TAIL>
 static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipStream_t stream)
 {
     s.tiles_m = (s.M + BM - 1) / BM;
@@ -448,7 +457,7 @@ static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipS
     s.bn_magic = udiv_magic(s.bn);
     const int64_t run = ((int64_t)s.tiles_m * s.bn + (1 << s.gs) - 1) >> s.gs;
     s.per_xcd = (int32_t)(run < 32 ? run : 32);
-    auto kern = gated_stream_kernel<ACT, BM>;
+    auto kern = gated_stream_kernel<ACT, BM, TAIL>;
     static bool attr_done = false;
     if (!attr_done) {
         IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
@@ -456,7 +465,7 @@ static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipS
     }
     hipLaunchKernelGGL(kern, dim3(8u * (unsigned)s.per_xcd), dim3(64 * GS_NW), GatedLayout<BM>::LDS, stream, s);
     IBERT_LAUNCH_CHECK("gated_stream_kernel");
-    static const KernelName name("gated_stream_kernel<%d, %d>", ACT, BM);
+    static const KernelName name("gated_stream_kernel<%d, %d, %s>", ACT, BM, TAIL ? "true" : "false");
     g_last_kernel = name.text;
     return IBERT_OK;
 }
@@ -466,7 +475,7 @@ int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t
 {
     GatedStreamArgs s{};
     s.A = A; s.W = W; s.bias = bias; s.mult = mult; s.shift = shift; s.C = C;
-    s.M = d.M; s.F = d.F; s.nk = d.K / 128;
+    s.M = d.M; s.F = d.F; s.K = d.K; s.nk = (d.K + 127) / 128;
     s.lda = (int32_t)d.lda; s.ldw = (int32_t)d.ldw; s.ldc = (int32_t)d.ldc;
     const ibert_gate_params& p = d.gate;
     s.gate = gate_const(p);
@@ -474,10 +483,14 @@ int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t
     s.fast = (int64_t)d.K * 16129 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
     s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
     const int64_t w = 2 * (int64_t)d.F * d.K;
-    if (!gelu) return tall ? launch_gated_stream_as<GS_SILU, 256>(s, w, stream) : launch_gated_stream_as<GS_SILU, 128>(s, w, stream);
-    if (gelu_fast && -2 * (int64_t)p.gelu.q_b < GS_ERF)
-        return tall ? launch_gated_stream_as<GS_GELU_TABLE, 256>(s, w, stream) : launch_gated_stream_as<GS_GELU_TABLE, 128>(s, w, stream);
-    return tall ? launch_gated_stream_as<GS_GELU, 256>(s, w, stream) : launch_gated_stream_as<GS_GELU, 128>(s, w, stream);
+    auto launch = [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (d.K % 128) return tall ? launch_gated_stream_as<ACT, 256, true>(s, w, stream) : launch_gated_stream_as<ACT, 128, true>(s, w, stream);
+        return tall ? launch_gated_stream_as<ACT, 256, false>(s, w, stream) : launch_gated_stream_as<ACT, 128, false>(s, w, stream);
+    };
+    if (!gelu) return launch(std::integral_constant<int, GS_SILU>{});
+    if (gelu_fast && -2 * (int64_t)p.gelu.q_b < GS_ERF) return launch(std::integral_constant<int, GS_GELU_TABLE>{});
+    return launch(std::integral_constant<int, GS_GELU>{});
 }
 
 }  // namespace ibert

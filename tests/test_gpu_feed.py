@@ -115,7 +115,7 @@ def ran(kernel):
 
 
 @pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
-@pytest.mark.parametrize("M,F,K", [(256, 128, 128), (257, 129, 256), (300, 400, 384), (1000, 127, 1024), (511, 1, 256), (5150, 2050, 128), (4100, 4096, 384), (9000, 1300, 256)])
+@pytest.mark.parametrize("M,F,K", [(256, 128, 128), (257, 129, 256), (300, 400, 384), (1000, 127, 1024), (511, 1, 256), (5150, 2050, 128), (4100, 4096, 384), (9000, 1300, 256), (300, 130, 16), (300, 130, 112), (700, 257, 144), (5000, 1500, 272), (2000, 400, 1040)])
 def test_persistent_gated(persistent, M, F, K, act):
     # ragged tokens and channels; up to two tiles and more to a workgroup, columns shared by XCDs or not
     run(U.Gated(M + F + K + act, M, F, K, act), "persistent gated %d x %d x %d" % (M, F, K))
