@@ -79,13 +79,15 @@ static int launch_few_rows(RowsArgs& g, bool w4, int32_t group, bool zeros, bool
     return launch_rows<true, 128>(g, p, zeros, gated, stream);
 }
 
-static bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes)
+// (128 bits: whatever leading dimensions and rows are given, no sum here passes them)
+typedef unsigned __int128 extent;
+static bool overlap(const void* a, extent abytes, const void* b, extent bbytes)
 {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return a && b && x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
+    const extent x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + bbytes && y < x + abytes;
 }
-// bytes from the first to the last element of `rows` rows of n elements
-static int64_t span(int64_t rows, int64_t ld, int64_t n, int64_t elem) { return ((rows - 1) * ld + n) * elem; }
+// bytes from the first to the last element of `rows` >= 1 rows of n elements
+static extent span(int64_t rows, int64_t ld, int64_t n, int64_t elem) { return ((extent)(rows - 1) * (extent)ld + (extent)n) * (extent)elem; }
 
 static int check_gate(const ibert_gate_params& p)
 {
@@ -176,7 +178,7 @@ extern "C" int ibert_gemm_w4_gated(const ibert_gated_desc* desc, const int8_t* A
     if (rc) return rc;
     if (gate->group != up->group || (gate->zeros != nullptr) != (up->zeros != nullptr)) return IBERT_ERR_PARAM_RANGE;
     const ibert_gated_desc& d = *desc;
-    const int64_t wbytes = (int64_t)ibert_w4_bytes(d.F, d.K), cbytes = ibert::span(d.M, d.ldc, d.F, 1);
+    const ibert::extent wbytes = ibert_w4_bytes(d.F, d.K), cbytes = ibert::span(d.M, d.ldc, d.F, 1);
     if (ibert::overlap(C, cbytes, gate->w, wbytes) || ibert::overlap(C, cbytes, up->w, wbytes)) return IBERT_ERR_SHAPE;
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
     g.w[0] = gate->w; g.w[1] = up->w;
@@ -200,8 +202,9 @@ extern "C" int ibert_gemm_w4_requant(const ibert_w4_desc* desc, const int8_t* A,
     if (!A || !mult || !shift || !C) return IBERT_ERR_NULL;
     const int rc = ibert::check_w4(weights);
     if (rc) return rc;
-    const int64_t elem = d.out_dtype == IBERT_I8 ? 1 : (d.out_dtype == IBERT_I16 ? 2 : 4), cbytes = ibert::span(d.M, d.ldc, d.N, elem);
-    if (ibert::overlap(C, cbytes, A, ibert::span(d.M, d.lda, d.K, 1)) || ibert::overlap(C, cbytes, weights->w, (int64_t)ibert_w4_bytes(d.N, d.K)) ||
+    const int64_t elem = d.out_dtype == IBERT_I8 ? 1 : (d.out_dtype == IBERT_I16 ? 2 : 4);
+    const ibert::extent cbytes = ibert::span(d.M, d.ldc, d.N, elem);
+    if (ibert::overlap(C, cbytes, A, ibert::span(d.M, d.lda, d.K, 1)) || ibert::overlap(C, cbytes, weights->w, ibert_w4_bytes(d.N, d.K)) ||
         (residual && ibert::overlap(C, cbytes, residual, ibert::span(d.M, d.ldr, d.N, 1)))) return IBERT_ERR_SHAPE;
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.N, d.K, bias, mult, shift, C, d.ldc);
     g.w[0] = weights->w;

@@ -219,8 +219,9 @@ extern "C" int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_
     if (d.rows == 0 || d.vocab == 0) return IBERT_OK;
     if (!x || !y || !params || (d.num_tokens > 0 && (!tokens || !token_start || !out_start)) ||
         (d.num_biases > 0 && (!bias_ids || !bias_values || !bias_start)) || (d.num_masks > 0 && !masks)) return IBERT_ERR_NULL;
-    const uintptr_t px = reinterpret_cast<uintptr_t>(x), py = reinterpret_cast<uintptr_t>(y);
-    const uint64_t sx = 4 * ((uint64_t)(d.rows - 1) * (uint64_t)d.ldx + d.vocab), sy = 4 * ((uint64_t)(d.rows - 1) * (uint64_t)d.ldy + d.vocab);
+    typedef unsigned __int128 extent;                              // (whatever leading dimensions are given)
+    const extent px = reinterpret_cast<uintptr_t>(x), py = reinterpret_cast<uintptr_t>(y);
+    const extent sx = 4 * ((extent)(d.rows - 1) * (extent)d.ldx + d.vocab), sy = 4 * ((extent)(d.rows - 1) * (extent)d.ldy + d.vocab);
     if (!(px == py && d.ldx == d.ldy) && px < py + sy && py < px + sx) return IBERT_ERR_SHAPE;
     ibert::LogitsArgs g{};
     g.x = x; g.y = y; g.params = params;

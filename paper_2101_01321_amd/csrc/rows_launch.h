@@ -18,7 +18,8 @@ constexpr int ROWS_LDS = 163840;
 template <typename F, typename Name>
 int rows_pieces(F kern, RowsArgs g, int tm, int tn, size_t lds, hipStream_t stream, Name name)
 {
-    const int64_t M = g.M, across = ((int64_t)g.N + tn - 1) / tn, down = (M + tm - 1) / tm, most = (1 << 22) / across < 1 ? 1 : (1 << 22) / across;
+    const int64_t M = g.M, across = ((int64_t)g.N + tn - 1) / tn, across8 = (across + 7) / 8 * 8, down = (M + tm - 1) / tm;
+    const int64_t most = (1 << 22) / across8;                       // (N is at most 2^24, across8 2^20)
     const int8_t *A = g.A, *R = g.R;
     char* C = static_cast<char*>(g.C);
     const int64_t elem = g.out_dtype == IBERT_I8 ? 1 : (g.out_dtype == IBERT_I16 ? 2 : 4);
@@ -30,7 +31,7 @@ int rows_pieces(F kern, RowsArgs g, int tm, int tn, size_t lds, hipStream_t stre
         g.M = (int32_t)(M - m0 < n * tm ? M - m0 : n * tm);
         g.down = (int32_t)n;
         g.across = (int32_t)across;
-        hipLaunchKernelGGL(kern, dim3((unsigned)((across + 7) / 8 * 8 * n)), dim3(ROWS_THREADS), lds, stream, g);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(across8 * n)), dim3(ROWS_THREADS), lds, stream, g);
         IBERT_LAUNCH_CHECK("rows_kernel");
     }
     g_last_kernel = name();

@@ -248,6 +248,14 @@ def test_logits_refuse():
     assert logits(logits_desc(), y=C.c_void_p(P.value + 4 * (3 * 104 + 99))) == -2
 
 
+def test_leading_dimensions_beyond_any_memory_do_not_wrap():
+    # rows 2^62 apart: their extent passes 64 bits; what stands between two rows of the one is not taken for free of the other
+    d = w4_desc(lda=1 << 62, M=5)
+    assert w4(d, c=C.c_void_p(P.value + 64)) == -2
+    assert i8_gated(gated_desc(ldw=1 << 62), c=C.c_void_p(Q.value + 64)) == -2 and i8_gated(gated_desc(lda=1 << 62), c=C.c_void_p(P.value + 64)) == -2
+    assert logits(logits_desc(ldx=1 << 62), y=C.c_void_p(P.value + 400)) == -2
+
+
 def test_structs_have_the_header_s_sizes():
     # ctypes and the C compiler agree on natural alignment; the arrays a program makes itself have 28 bytes a row
     assert C.sizeof(B.LogitsRow) == 28 and C.sizeof(B.GateParams) == 4 + 24 + 8 and C.sizeof(B.W4Weights) == 32 and C.sizeof(B.W4Desc) == 56

@@ -366,6 +366,35 @@ def test_logits_streams_and_graphs(gpu):
             x.check("replayed")
 
 
+def test_more_rows_than_a_launch_holds(gpu):
+    # 2^19 blocks of 32 rows of one channel tile, 2^22 rows of one slice: a second launch takes what is left
+    torch, G, B = libs()
+    M = (1 << 19) * 32 + 5
+    G.say("w4, %d rows" % M)
+    a = torch.randint(-128, 128, (M,), device=G.DEV, dtype=torch.int8)
+    w, s, _ = B.ibert_w4_pack(np.array([[-3]], np.int8), np.array([[5]], np.uint8), None, 32)
+    w, s, one = G.to_dev(w), G.to_dev(s), torch.ones(1, dtype=torch.int32, device=G.DEV)
+    out = torch.zeros(M + 9, dtype=torch.int16, device=G.DEV)
+    B.ibert_gemm_w4_requant(B.W4Desc(M, 1, 1, B.I16, 1, 1, 0, 32767, B.Dyadic(1, 0)), a, B.W4Weights(w.data_ptr(), s.data_ptr(), None, 32), None, one, one * 0, None, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:M], a.to(torch.int16) * -15) and not out[M:].any()
+    rows = (1 << 22) + 3
+    G.say("logits, %d rows" % rows)
+    x = torch.randint(-9, 9, (rows,), device=G.DEV, dtype=torch.int32)
+    x[-1] = U.LOW
+    params = torch.tensor([1, 0, 1, 0, 5, 7, -1], dtype=torch.int32, device=G.DEV).repeat(rows, 1)
+    made = torch.zeros(rows + 1, dtype=torch.int32, device=G.DEV)
+    made[rows - 1:] = torch.tensor([0, 2], device=G.DEV)      # the last but one row's two tokens are its own
+    y = torch.full((rows + 9,), 77, dtype=torch.int32, device=G.DEV)
+    start = made.clone()
+    start[rows - 1], start[rows] = 2, 2                       # row rows - 2 has tokens [0, 2)
+    B.ibert_logits_adjust_i(B.LogitsDesc(rows, 1, 1, 1, 2, 0, 0, 0), x, params, torch.zeros(2, dtype=torch.int32, device=G.DEV), start, made, None, None, None, None, y)
+    torch.cuda.synchronize()
+    want = x.clone()
+    want[rows - 2] -= 5 + 2 * 7
+    assert torch.equal(y[:rows], want) and bool((y[rows:] == 77).all())
+
+
 # ------------------------------------------------------------------------------------------- the run of them
 @pytest.mark.parametrize("M,group", [(1, 32), (5, 128), (70, 64)])
 def test_a_decoder_s_feed_forward_and_head(gpu, M, group):
