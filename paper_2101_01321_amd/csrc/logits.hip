@@ -3,7 +3,7 @@
 // A workgroup takes a slice of one row's vocabulary.  It counts the row's tokens that fall into the slice, and adds up the biases there, in
 // LDS (integer atomics: any order gives the same), then passes over the logits once.  The history is read once per slice, from L2.
 // What bounds it: the logits' way through HBM (64 x 128000, 65.5 MB: 16.0 us without a history, 4.1 TB/s with the launch), and behind it the trips to memory of a workgroup
-// whose row has a history (where its tokens are, the tokens): 22.9 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
+// whose row has a history (where its tokens are, the tokens): 22.7 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
 // slice (workgroups that go through several slices) or dealt to wavefronts of their own, the loads cost so many registers that fewer workgroups fit: 35.7 and 42.4 us.
 #include "common.h"
 
@@ -25,6 +25,7 @@ struct LogitsArgs {
     int64_t ldx, ldy;
     int32_t vocab, num_tokens, num_biases, num_masks, ld_mask;
     int32_t slices;                // of a row
+    uint32_t slices_magic;         // see udiv_fix
     int32_t vec;                   // rows allow 16-byte loads and stores
 };
 
@@ -50,7 +51,7 @@ template <int LOGITS_SLICE>
 __global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(LogitsArgs g)
 {
     extern __shared__ __align__(16) int32_t room[];
-    const int tid = threadIdx.x, row = blockIdx.x / g.slices, t0 = (blockIdx.x - row * g.slices) * LOGITS_SLICE;
+    const int tid = threadIdx.x, row = udiv_fix(blockIdx.x, g.slices, g.slices_magic), t0 = (blockIdx.x - row * g.slices) * LOGITS_SLICE;
     const int n = min(LOGITS_SLICE, g.vocab - t0);
     uint32_t* const count = reinterpret_cast<uint32_t*>(room);
     int32_t* const bias = room + LOGITS_SLICE;                      // where there are biases at all
@@ -118,7 +119,8 @@ __global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(Logits
     __syncthreads();
     for (int i = first;; i += ROUND) {
 #pragma unroll
-        for (int k = 0; k < LV; ++k)
+        for (int k = 0; k < LV; ++k) {
+            if (i + 4 * k * LOGITS_THREADS >= te) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t t = (uint32_t)a[k][e] - (uint32_t)t0;
@@ -127,6 +129,7 @@ __global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(Logits
                     else atomicOr(&count[t], SEEN);
                 }
             }
+        }
         if (i + ROUND >= te) break;
 #pragma unroll
         for (int k = 0; k < LV; ++k) a[k] = load4(i + ROUND + 4 * k * LOGITS_THREADS);
@@ -187,6 +190,7 @@ static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
         }
     }
     g.slices = (g.vocab + LOGITS_SLICE - 1) / LOGITS_SLICE;
+    g.slices_magic = udiv_magic(g.slices);
     // (a launch may have 2^32 threads at most: pieces of rows)
     const int64_t most = (1 << 22) / g.slices < 1 ? 1 : (1 << 22) / g.slices;
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
@@ -231,8 +235,8 @@ extern "C" int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_
     g.ldx = d.ldx; g.ldy = d.ldy;
     g.vocab = d.vocab; g.num_tokens = d.num_tokens; g.num_biases = d.num_biases; g.num_masks = d.num_masks; g.ld_mask = d.ld_mask;
     g.vec = ibert::aligned(x, 16) && ibert::aligned(y, 16) && d.ldx % 4 == 0 && d.ldy % 4 == 0;
-    // Slices of 4096, or of 2048 where the longer ones would not be two workgroups to a unit.  us, 2048 / 4096 (8192): 1 x 50265 4.3 / 5.0 (6.6), 64 x 128000 with 262 thousand
-    // tokens and 10 thousand biases 26.6 / 22.9 (25.9), without any 18.7 / 16.0 (16.1).
+    // Slices of 4096, or of 2048 where the longer ones would not be two workgroups to a unit.  us, 2048 / 4096 (8192): 1 x 50265 4.0 / 5.0 (6.6), 64 x 128000 with 262 thousand
+    // tokens and 10 thousand biases 26.6 / 22.7 (25.9), without any 18.7 / 16.0 (16.1).
     if ((int64_t)d.rows * ((d.vocab + 4095) / 4096) < 512) return ibert::launch_logits<2048>(g, d.rows, static_cast<hipStream_t>(stream));
     return ibert::launch_logits<4096>(g, d.rows, static_cast<hipStream_t>(stream));
 }

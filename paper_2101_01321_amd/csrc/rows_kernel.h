@@ -43,6 +43,7 @@ struct RowsArgs {
     int32_t stages;                // of a wavefront's ring
     int32_t a_vec, w_vec;          // rows of A, of INT8 weights are 16-byte aligned and K is a multiple of 16
     int32_t across, down;          // workgroups over the channels and over the rows
+    uint32_t down_magic;           // see udiv_fix
 };
 
 constexpr int ROWS_THREADS = 512;
@@ -69,6 +70,23 @@ __device__ __forceinline__ v4i bytes_16(const int8_t* p, int k, int n)
     for (int i = 0; i < 16; ++i)
         if (k + i < n) u.b[i] = p[k + i];
     return u.v;
+}
+
+// Every argument in registers from here on, after one trip to memory: fetched where each is first used, behind branches, they are five.
+template <bool W4, bool ZERO, bool GATED>
+__device__ __forceinline__ void rows_arguments(const RowsArgs& g)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" :: "s"(g.A), "s"(g.lda), "s"(g.M), "s"(g.N), "s"(g.K), "s"(g.w[0]), "s"(g.bias), "s"(g.mult), "s"(g.shift), "s"(g.C), "s"(g.ldc), "s"(g.chunks),
+                 "s"(g.per), "s"(g.across), "s"(g.down), "s"(g.down_magic));
+    if constexpr (W4) asm volatile("" :: "s"(g.scales[0]), "s"(g.stages));
+    else asm volatile("" :: "s"(g.ldw), "s"(g.stages));
+    if constexpr (W4 && GATED) asm volatile("" :: "s"(g.w[1]), "s"(g.scales[1]));
+    if constexpr (ZERO) asm volatile("" :: "s"(g.zeros[0]), "s"(g.zeros[1]));
+    if constexpr (GATED) asm volatile("" :: "s"(g.gate.silu), "s"(g.gate.m), "s"(g.gate.s), "s"(g.gate.gelu.q_b), "s"(g.gate.gelu.q_c), "s"(g.gate.gelu.q_1), "s"(g.gate.gelu.q_max),
+                                   "s"(g.gate.gelu.m), "s"(g.gate.gelu.s));
+    else asm volatile("" :: "s"(g.R), "s"(g.ldr), "s"(g.res_m), "s"(g.res_s), "s"(g.out_dtype), "s"(g.out_clamp));
+#endif
 }
 
 // acc += the products of a chunk: activations xa (two halves of the chunk), packed weights w of NT tiles, their scales and zero points.
@@ -128,7 +146,9 @@ struct RowsChannel {
 };
 __device__ __forceinline__ RowsChannel rows_channel(const RowsArgs& g, int ch)
 {
-    return RowsChannel{g.bias ? g.bias[ch] : 0, g.mult[ch], g.shift[ch]};
+    const uint32_t at = 4u * (uint32_t)ch;                         // (below 2^27: 32-bit offsets from the arrays' first entries)
+    auto entry = [&](const int32_t* p) { return *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(p) + at); };
+    return RowsChannel{g.bias ? entry(g.bias) : 0, entry(g.mult), entry(g.shift)};
 }
 
 // Output (m, n) from its sums (of a gated block: gate and up projection), its channels' constants and its residual.
@@ -178,7 +198,8 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
     extern __shared__ __align__(16) int8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
-    const int jb = blockIdx.x >> 3, jc = jb / g.down, bx = jc * 8 + (blockIdx.x & 7);
+    rows_arguments<W4, ZERO, GATED>(g);
+    const int jb = blockIdx.x >> 3, jc = udiv_fix(jb, g.down, g.down_magic), bx = jc * 8 + (blockIdx.x & 7);
     if (bx >= g.across) return;
     const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
     const int per = g.per, c0 = wave * per, run = min(per, g.chunks - c0);           // this wavefront's chunks [c0, c0 + run)
@@ -386,7 +407,8 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_any_kernel(RowsArgs g)
     extern __shared__ __align__(16) int8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
-    const int jb = blockIdx.x >> 3, jc = jb / g.down, bx = jc * 8 + (blockIdx.x & 7);
+    rows_arguments<W4, ZERO, GATED>(g);
+    const int jb = blockIdx.x >> 3, jc = udiv_fix(jb, g.down, g.down_magic), bx = jc * 8 + (blockIdx.x & 7);
     if (bx >= g.across) return;
     const int m0 = (jb - jc * g.down) * TM, rows = min(TM, g.M - m0), n0 = bx * (16 * NH);
     const int per = g.per, c0 = wave * per, run = min(per, g.chunks - c0);

@@ -30,6 +30,7 @@ int rows_pieces(F kern, RowsArgs g, int tm, int tn, size_t lds, hipStream_t stre
         g.C = C + m0 * g.ldc * elem;
         g.M = (int32_t)(M - m0 < n * tm ? M - m0 : n * tm);
         g.down = (int32_t)n;
+        g.down_magic = udiv_magic(g.down);
         g.across = (int32_t)across;
         hipLaunchKernelGGL(kern, dim3((unsigned)(across8 * n)), dim3(ROWS_THREADS), lds, stream, g);
         IBERT_LAUNCH_CHECK("rows_kernel");
