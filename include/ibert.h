@@ -15,7 +15,8 @@
  *     of Alg. 1).  The device sources contain no floating-point type or operation (the integer square root of
  *     Alg. 4 included); the only place the compiler may use its reciprocal unit is its own expansion of integer
  *     divisions (by a sum or a root: 2^31 / sum in Softmax, 2^24 / sigma in LayerNorm, 2^30 / sigma and 2^48 / W in the
- *     decoder calls; by an argument: workgroups to rows), each of which returns the exact integer quotient.
+ *     decoder calls, the sigmoid of the gated block; by an argument: workgroups to rows; by a length: INT32's end by a row's biases), each of which returns
+ *     the exact integer quotient.
  *   - Out-of-range data never faults: it is clamped as documented (the functions are total on int32
  *     inputs); out-of-range *constants* are refused with IBERT_ERR_PARAM_RANGE.
  *   - floor(.) is the mathematical floor; ">>" on signed values is an arithmetic shift.

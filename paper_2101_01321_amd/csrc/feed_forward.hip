@@ -44,12 +44,11 @@ static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, boo
 // 2741 x 1024 x 4096 - / 34.4 / 36.7, 8192 x 4096 x 12288 - / 780 / 639.
 static int plan_gated(int32_t M, int32_t F, int32_t K)
 {
-    const double k = K / 1024.0;
-    auto rounds = [&](int rows, int channels) {
+    auto ns = [&](int64_t fixed, int64_t per_k, int rows, int channels) {
         const int64_t tiles = (((int64_t)M + rows - 1) / rows) * (((int64_t)F + channels - 1) / channels);
-        return (double)((tiles + 255) / 256);
+        return (tiles + 255) / 256 * (fixed + per_k * K / 1024);
     };
-    const double ring = 4.0 + rounds(64, 32) * (4.5 + 2.0 * k), low = rounds(128, 128) * (5.5 + 6.3 * k), tall = rounds(256, 128) * (9.3 + 8.4 * k);
+    const int64_t ring = 4000 + ns(4500, 2000, 64, 32), low = ns(5500, 6300, 128, 128), tall = ns(9300, 8400, 256, 128);
     return M <= 32 || (ring <= low && ring <= tall) ? 0 : (low <= tall ? 1 : 2);
 }
 
