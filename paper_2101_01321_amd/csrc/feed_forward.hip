@@ -21,7 +21,7 @@ static int g_rows_tiles = -1, g_rows_rows = -1;
 //   INT8     64: 8192 x 2048 1x4 14.4 / 2x8 13.0;  128: 11008 x 4096 48.2 / 42.1, 2730 x 1024 7.9 / 8.3;  256: 2730 x 1024 12.1 / 14.6
 static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, bool gated)
 {
-    auto blocks = [&](int nt, int br) { return ((int64_t)N + 16 * nt - 1) / (16 * nt) * ((M + 8 * br - 1) / (8 * br)); };
+    auto blocks = [&](int nt, int br) { return ((int64_t)N + 16 * nt - 1) / (16 * nt) * (((int64_t)M + 8 * br - 1) / (8 * br)); };
     p.br = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
     p.nt = 1;
     if (!w4) {

@@ -441,13 +441,13 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W)
 {
     return d.K % 16 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
-           (int64_t)((d.M + 127) / 128) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
+           (((int64_t)d.M + 127) / 128) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
 }
 
 template <int ACT, int BM, bool TAIL>
 static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipStream_t stream)
 {
-    s.tiles_m = (s.M + BM - 1) / BM;
+    s.tiles_m = (int32_t)(((int64_t)s.M + BM - 1) / BM);
     const int tiles_n = (s.F + GS_BF - 1) / GS_BF;
     // as stream_shares and stream_deal
     s.xs = 0;

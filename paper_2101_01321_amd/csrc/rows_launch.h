@@ -49,7 +49,7 @@ inline int ring_stages(const RowsArgs& g, bool w4, int br, int tiles, bool gated
     const size_t sc = w4 ? (size_t)((g.per * 16 * (128 / group) + 255) & ~255) * tiles * (zeros ? 2 : 1) : 0, sums = (size_t)32 * br * (16 * tiles + 4);
     const size_t stage = (size_t)(br + tiles * (w4 ? 1 : 2)) * 1024;
     auto bytes = [&](int n) { return 8 * (sc + (n * stage > sums ? n * stage : sums)); };
-    const int64_t blocks = (((int64_t)g.N + tn - 1) / tn) * ((g.M + 8 * br - 1) / (8 * br));
+    const int64_t blocks = (((int64_t)g.N + tn - 1) / tn) * (((int64_t)g.M + 8 * br - 1) / (8 * br));
     const size_t side = blocks <= 256 ? 1 : (blocks <= 512 ? 2 : 3);
     int n = g.per < 4 ? g.per : 4;
     while (n > 1 && bytes(n) > ROWS_LDS / side) --n;

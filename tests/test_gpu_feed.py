@@ -199,6 +199,12 @@ def test_w4_ignores_what_stands_past_the_weights(gpu):
     d.check("w4 with filled padding")
 
 
+@pytest.mark.parametrize("group", [None, 128])
+def test_gated_without_biases(form, group):
+    for M, F, K in ((3, 50, 256), (40, 33, 100)):
+        run(U.Gated(M, M, F, K, M % 2, group, bias=False), "gated without biases, group %s" % group)
+
+
 def test_constants_at_their_ends(gpu):
     # shifts of 0 and 62, multipliers of both signs and of INT32's ends, biases that push a sum to an end
     for group in (None, 64):
@@ -378,6 +384,25 @@ def test_more_rows_than_a_launch_holds(gpu):
     B.ibert_gemm_w4_requant(B.W4Desc(M, 1, 1, B.I16, 1, 1, 0, 32767, B.Dyadic(1, 0)), a, B.W4Weights(w.data_ptr(), s.data_ptr(), None, 32), None, one, one * 0, None, out)
     torch.cuda.synchronize()
     assert torch.equal(out[:M], a.to(torch.int16) * -15) and not out[M:].any()
+    M = 2 ** 31 - 1
+    G.say("w4 and a gated block, %d rows" % M)
+    a = torch.randint(-8, 9, (M,), device=G.DEV, dtype=torch.int8)
+    out = torch.zeros(M, dtype=torch.int8, device=G.DEV)
+    B.ibert_gemm_w4_requant(B.W4Desc(M, 1, 1, B.I8, 1, 1, 0, 127, B.Dyadic(1, 0)), a, B.W4Weights(w.data_ptr(), s.data_ptr(), None, 32), None, one, one * 0, None, out)
+    torch.cuda.synchronize()
+    for x, y in zip(a.split(1 << 28), out.split(1 << 28)):
+        assert torch.equal(y, (x.to(torch.int16) * -15).clamp(-127, 127).to(torch.int8))
+    p = B.ibert_gate_params_from_scales(B.GATE_SILU, 0, 1 / 32767, 1.0)
+    p.out_dy = B.Dyadic(1, 20)
+    m, sh = torch.tensor([1 << 12, 1 << 10], dtype=torch.int32, device=G.DEV), torch.zeros(2, dtype=torch.int32, device=G.DEV)
+    B.ibert_gemm_i8_gated(B.GatedDesc(M, 1, 1, 1, 1, 1, p), a, torch.ones(2, dtype=torch.int8, device=G.DEV), None, m, sh, out)
+    torch.cuda.synchronize()
+    v = np.arange(-8, 9)
+    want = torch.from_numpy(U.gate(v[:, None] * 1, v[:, None] * 1, m.cpu().numpy(), sh.cpu().numpy(), p)[:, 0]).to(G.DEV)
+    assert want.unique().numel() == 7        # (of gates of -2.8 and less this output scale leaves nothing)
+    for x, y in zip(a.split(1 << 27), out.split(1 << 27)):
+        assert torch.equal(y, want[x.to(torch.int32) + 8])
+    del a, out
     rows = (1 << 22) + 3
     G.say("logits, %d rows" % rows)
     x = torch.randint(-9, 9, (rows,), device=G.DEV, dtype=torch.int32)
