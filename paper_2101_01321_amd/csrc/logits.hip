@@ -26,6 +26,7 @@ struct LogitsArgs {
     int32_t vocab, num_tokens, num_biases, num_masks, ld_mask;
     int32_t slices;                // of a row
     uint32_t slices_magic;         // see udiv_fix
+    int32_t rows, by_xcd;          // of this launch; slices of a row all on one XCD
     int32_t vec;                   // rows allow 16-byte loads and stores
 };
 
@@ -51,7 +52,10 @@ template <int LOGITS_SLICE>
 __global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(LogitsArgs g)
 {
     extern __shared__ __align__(16) int32_t room[];
-    const int tid = threadIdx.x, row = udiv_fix(blockIdx.x, g.slices, g.slices_magic), t0 = (blockIdx.x - row * g.slices) * LOGITS_SLICE;
+    // workgroups go round the XCDs: with many rows each XCD takes every eighth, whose tokens then come into one L2 and not into eight
+    const int tid = threadIdx.x, id = g.by_xcd ? (int)(blockIdx.x >> 3) : (int)blockIdx.x, part = udiv_fix(id, g.slices, g.slices_magic);
+    const int row = g.by_xcd ? 8 * part + (int)(blockIdx.x & 7) : part, t0 = (id - part * g.slices) * LOGITS_SLICE;
+    if (row >= g.rows) return;
     const int n = min(LOGITS_SLICE, g.vocab - t0);
     uint32_t* const count = reinterpret_cast<uint32_t*>(room);
     int32_t* const bias = room + LOGITS_SLICE;                      // where there are biases at all
@@ -192,7 +196,7 @@ static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
     g.slices = (g.vocab + LOGITS_SLICE - 1) / LOGITS_SLICE;
     g.slices_magic = udiv_magic(g.slices);
     // (a launch may have 2^32 threads at most: pieces of rows)
-    const int64_t most = (1 << 22) / g.slices < 1 ? 1 : (1 << 22) / g.slices;
+    const int64_t most = (1 << 22) / g.slices / 8 * 8;               // (at most 2^15 slices)
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
         const int64_t n = rows - r0 < most ? rows - r0 : most;
         LogitsArgs a = g;
@@ -202,7 +206,9 @@ static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
         if (a.token_start) a.token_start += r0;
         if (a.out_start) a.out_start += r0;
         if (a.bias_start) a.bias_start += r0;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(n * g.slices)), dim3(LOGITS_THREADS), lds, stream, a);
+        a.rows = (int32_t)n;
+        a.by_xcd = n % 8 == 0 || n >= 128;
+        hipLaunchKernelGGL(kern, dim3((unsigned)((a.by_xcd ? (n + 7) / 8 * 8 : n) * g.slices)), dim3(LOGITS_THREADS), lds, stream, a);
         IBERT_LAUNCH_CHECK("logits_adjust_kernel");
     }
     static const KernelName name("logits_adjust_kernel<%d>", LOGITS_SLICE);
