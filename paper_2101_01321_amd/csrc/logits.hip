@@ -34,18 +34,33 @@ struct LogitsArgs {
 constexpr int LOGITS_THREADS = 512;
 constexpr uint32_t SEEN = 0x80000000u, BIASED = 0x40000000u;     // in the prompt; has biases; the low bits count what has been produced
 
-__device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t bias, const ibert_logits_row& p, int32_t us, int32_t ds)
+// Into INT32: the low half where the high one is its sign.
+__device__ __forceinline__ int32_t saturated(int64_t v)
+{
+    const int32_t lo = (int32_t)v, hi = (int32_t)(v >> 32);
+    return hi == lo >> 31 ? lo : (hi >> 31) ^ INT32_MAX;
+}
+
+// What a row does to a logit, its halves of rounding made once.
+struct Penalty {
+    int32_t up_m, up_s, down_m, down_s, presence, frequency;
+    int64_t up_rnd, down_rnd;
+};
+__device__ __forceinline__ Penalty penalty_of(const ibert_logits_row& p)
+{
+    const int32_t us = clamp_i32(p.up.s, 0, 62), ds = clamp_i32(p.down.s, 0, 62);
+    return Penalty{p.up.m, us, p.down.m, ds, p.presence, p.frequency, ((int64_t)1 << us) >> 1, ((int64_t)1 << ds) >> 1};
+}
+
+// count != 0
+__device__ __forceinline__ int32_t adjusted(int32_t x, uint32_t count, int64_t bias, const Penalty& p)
 {
     if (x == INT32_MIN) return x;
-    int64_t v = x;
-    if (count & ~BIASED) {
-        v = dyadic64(x, x > 0 ? p.up.m : p.down.m, x > 0 ? us : ds);
-        v = v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v);
-        const int64_t n = count & ~(SEEN | BIASED);
-        v -= (n ? (int64_t)p.presence : 0) + p.frequency * n;
-    }
-    v += bias;
-    return (int32_t)(v <= INT32_MIN ? INT32_MIN + 1 : (v > INT32_MAX ? INT32_MAX : v));
+    const bool up = x > 0;
+    const int64_t m = (int64_t)x * (up ? p.up_m : p.down_m) + (up ? p.up_rnd : p.down_rnd);
+    const int32_t r = count & ~BIASED ? saturated(m >> (up ? p.up_s : p.down_s)) : x, n = (int32_t)(count & ~(SEEN | BIASED));
+    const int32_t y = saturated((int64_t)r - (n ? p.presence : 0) - (int64_t)p.frequency * n + bias);
+    return y == INT32_MIN ? INT32_MIN + 1 : y;
 }
 
 template <int LOGITS_SLICE>
@@ -159,10 +174,10 @@ __global__ __launch_bounds__(LOGITS_THREADS, 8) void logits_adjust_kernel(Logits
             if (g.bias_ids[k] == t0 + i) sum += g.bias_values[k];
         return sum;
     };
-    const int32_t us = clamp_i32(p.up.s, 0, 62), ds = clamp_i32(p.down.s, 0, 62);
+    const Penalty pen = penalty_of(p);
     auto plain = [&](int i, int32_t v) {
         const uint32_t c = count[i];
-        return c ? adjusted(v, c, c & BIASED ? bias_of(i) : 0, p, us, ds) : v;
+        return c ? adjusted(v, c, c & BIASED ? bias_of(i) : 0, pen) : v;
     };
     auto one = [&](int i, int32_t v, uint32_t word) {
         return mask && !((word >> ((t0 + i) & 31)) & 1u) ? INT32_MIN : plain(i, v);
