@@ -15,6 +15,15 @@ struct GateConst {
 constexpr int32_t SIG_TOP = 124 * 124 + 8180;      // i-exp at 0 with the constants of Eq. 13 at S = ln2/64
 constexpr int SIG_STEPS = 1024;                    // from 16 octaves on the sigmoid is one
 
+// DY(x; m, s) without a case for s = 0, and a 64-bit value inside INT32 (the low half where the high one is its sign) or inside +-lim of it.
+__device__ __forceinline__ int64_t dy64(int32_t x, int32_t m, int32_t s) { return ((int64_t)x * m + (((int64_t)1 << s) >> 1)) >> s; }
+__device__ __forceinline__ int32_t into_32(int64_t v)
+{
+    const int32_t lo = (int32_t)v, hi = (int32_t)(v >> 32);
+    return hi == lo >> 31 ? lo : (hi >> 31) ^ INT32_MAX;
+}
+__device__ __forceinline__ int32_t into(int64_t v, int32_t lim) { return med3_i32(into_32(v), -lim, lim); }
+
 // Sigmoid of a distance d in [0, 1024] steps of ln2/64, 15 bits: TOP / (TOP + e) rounded to nearest.  The numerator stays below 2^30.
 __host__ __device__ __forceinline__ uint32_t sigmoid15(uint32_t d)
 {
@@ -45,16 +54,16 @@ __device__ __forceinline__ int32_t gelu16(int32_t q, const GeluConst& a)
     const uint32_t poly = (uint32_t)v * (uint32_t)v + (uint32_t)a.q_c;
     const uint32_t erf = q < 0 ? 0u - poly : (q == 0 ? 0u : poly);
     const int32_t t = (int32_t)((uint32_t)q * (erf + (uint32_t)a.q_1));
-    return clamp_i64_to_i32(dyadic64(t, a.m, a.s), 32767);
+    return into(dy64(t, a.m, a.s), 32767);
 }
 
 // The INT8 result of one pair of sums.
 __device__ __forceinline__ int32_t gate_one(int32_t acc_g, int32_t acc_u, int32_t mg, int32_t sg, int32_t mu, int32_t su, const GateConst& c)
 {
-    const int32_t g = clamp_i64_to_i32(dyadic64(acc_g, mg, sg), c.silu ? 65535 : c.gelu.q_max);
-    const int32_t u = clamp_i64_to_i32(dyadic64(acc_u, mu, su), 32767);
+    const int32_t g = into(dy64(acc_g, mg, sg), c.silu ? 65535 : c.gelu.q_max);
+    const int32_t u = into(dy64(acc_u, mu, su), 32767);
     const int32_t a = c.silu ? silu_of(g, sigmoid15(silu_step(g))) : gelu16(g, c.gelu);
-    return clamp_i64_to_i32(dyadic64(a * u, c.m, c.s), 127);      // (65535 * 32767 < 2^31)
+    return into(dy64(a * u, c.m, c.s), 127);      // (65535 * 32767 < 2^31)
 }
 
 inline GateConst gate_const(const ibert_gate_params& p)

@@ -155,17 +155,13 @@ __device__ __forceinline__ RowsChannel rows_channel(const RowsArgs& g, int ch)
 template <bool GATED>
 __device__ __forceinline__ void rows_finish(const RowsArgs& g, int m, int n, int64_t s0, int64_t s1, const RowsChannel& c0, const RowsChannel& c1, int32_t res)
 {
-    auto value = [&](int64_t v, int32_t b) {
-        v += b;
-        return (int32_t)(v < INT32_MIN ? INT32_MIN : (v > INT32_MAX ? INT32_MAX : v));
-    };
     const int64_t off = (int64_t)m * g.ldc + n;
     if constexpr (GATED) {
-        static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(value(s0, c0.b), value(s1, c1.b), c0.m, c0.s, c1.m, c1.s, g.gate);
+        static_cast<int8_t*>(g.C)[off] = (int8_t)gate_one(into_32(s0 + c0.b), into_32(s1 + c1.b), c0.m, c0.s, c1.m, c1.s, g.gate);
     } else {
-        int64_t v = dyadic64(value(s0, c0.b), c0.m, c0.s);
-        if (g.R) v += dyadic64(res, g.res_m, g.res_s);
-        const int32_t y = clamp_i64_to_i32(v, g.out_clamp);
+        int64_t v = dy64(into_32(s0 + c0.b), c0.m, c0.s);
+        if (g.R) v += dy64(res, g.res_m, g.res_s);
+        const int32_t y = into(v, g.out_clamp);
         if (g.out_dtype == IBERT_I8) static_cast<int8_t*>(g.C)[off] = (int8_t)y;
         else if (g.out_dtype == IBERT_I16) static_cast<int16_t*>(g.C)[off] = (int16_t)y;
         else static_cast<int32_t*>(g.C)[off] = y;
@@ -381,13 +377,22 @@ __global__ __launch_bounds__(ROWS_THREADS) void rows_ring_kernel(RowsArgs g)
         const int i = p * ROWS_THREADS + tid, m = i / (16 * NH), nn = i - m * (16 * NH), n = n0 + nn;
         if (m >= rows || n >= g.N) continue;
         const int8_t* const at = lds + (ZERO ? 2 : 1) * NT * scb + (m * PITCH + nn) * 4;
+        // (of INT8 weights, and of up to 4096 values of K, all of a sum has 32 bits)
         int64_t s0 = 0, s1 = 0;
+        auto add = [&](auto zero) {
+            auto t0 = zero, t1 = zero;
 #pragma unroll
-        for (int w = 0; w < 8; ++w)
-            if (w < runs) {
-                s0 += *reinterpret_cast<const int32_t*>(at + w * own);
-                if constexpr (GATED) s1 += *reinterpret_cast<const int32_t*>(at + w * own + 64 * NH);
-            }
+            for (int w = 0; w < 8; ++w)
+                if (w < runs) {
+                    t0 += *reinterpret_cast<const int32_t*>(at + w * own);
+                    if constexpr (GATED) t1 += *reinterpret_cast<const int32_t*>(at + w * own + 64 * NH);
+                }
+            s0 = W4 ? (int64_t)t0 : (int64_t)(int32_t)t0;
+            s1 = W4 ? (int64_t)t1 : (int64_t)(int32_t)t1;
+        };
+        if (!W4) add(0u);
+        else if (g.K <= 4096) add(0);
+        else add((int64_t)0);
         if constexpr (!W4) wrap_32(s0, s1, ch[p][0], ch[p][GATED ? 1 : 0]);
         rows_finish<GATED>(g, m0 + m, n, s0, s1, ch[p][0], ch[p][GATED ? 1 : 0], res[p]);
     }
