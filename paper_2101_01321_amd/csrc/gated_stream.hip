@@ -8,6 +8,10 @@
 //   * Rows of W are dealt to the LDS rows such that lane r of 16 has channels 2 r and 2 r + 1 of its wavefront's 32.
 //   * F and M may be ragged: operands, constants and output are buffers that end with the last row or channel.
 //   * SiLU's sigmoids, and GELU's erf where it has room, are tables in LDS, built once by every workgroup with the function they stand for.
+//
+// What bounds it: where K is long the matrix units at the clock that power leaves (8192 x 4096 -> 2 x 12288 635 us, 2.6 POP/s, MFMA busy 0.72); where it is short the
+// epilogue, 20 ALU instructions a value that no MFMA runs beside (2741 x 1024 -> 2 x 4096 31 us eager: a low tile takes 4.7 us in its loop and 3.5 in its epilogue), and the
+// last round of tiles, three quarters full there.  Two heights of tile: 128 tokens fill more units, 256 read W half as often (see plan_gated for both sides).
 #include "gate_math.h"
 #include "gemm_stream.h"
 #include "gated_stream.h"
@@ -26,7 +30,7 @@ struct GatedStreamArgs {
     int32_t tiles_m, bn;           // as in StreamArgs
     uint32_t bn_magic;
     int32_t xs, gs, per_xcd;
-    int32_t fast;                  // K * 127^2 < 2^30, the product's shift in [33, 62], and gelu_fast_ok where it is GELU
+    int32_t fast;                  // K * 128^2 < 2^30, the product's shift in [33, 62], and gelu_fast_ok where it is GELU
     int32_t c_vec;                 // rows of C allow 16-byte stores
     GateConst gate;
 };
@@ -480,7 +484,7 @@ int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t
     const ibert_gate_params& p = d.gate;
     s.gate = gate_const(p);
     const bool gelu = !s.gate.silu, gelu_fast = gelu && gelu_fast_ok(p.gelu);
-    s.fast = (int64_t)d.K * 16129 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
+    s.fast = (int64_t)d.K * 16384 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
     s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
     const int64_t w = 2 * (int64_t)d.F * d.K;
     auto launch = [&](auto act) {

@@ -3,7 +3,7 @@
 // A workgroup takes a slice of one row's vocabulary.  It counts the row's tokens that fall into the slice, and adds up the biases there, in
 // LDS (integer atomics: any order gives the same), then passes over the logits once.  The history is read once per slice, from L2.
 // What bounds it: the logits' way through HBM (64 x 128000, 65.5 MB: 16.0 us without a history, 4.1 TB/s with the launch), and behind it the trips to memory of a workgroup
-// whose row has a history (where its tokens are, the tokens): 22.7 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
+// whose row has a history (where its tokens are, the tokens): 22.3 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
 // slice (workgroups that go through several slices) or dealt to wavefronts of their own, the loads cost so many registers that fewer workgroups fit: 35.7 and 42.4 us.
 #include "common.h"
 
@@ -201,13 +201,6 @@ static int launch_logits(LogitsArgs g, int64_t rows, hipStream_t stream)
 {
     auto kern = logits_adjust_kernel<LOGITS_SLICE>;
     const size_t lds = (size_t)LOGITS_SLICE * (g.num_biases > 0 ? 8 : 4);
-    if (lds > 60000) {
-        static bool attr_done = false;
-        if (!attr_done) {
-            IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 8 * LOGITS_SLICE));
-            attr_done = true;
-        }
-    }
     g.slices = (g.vocab + LOGITS_SLICE - 1) / LOGITS_SLICE;
     g.slices_magic = udiv_magic(g.slices);
     // (a launch may have 2^32 threads at most: pieces of rows)

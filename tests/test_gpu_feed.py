@@ -157,6 +157,26 @@ def test_persistent_gated_any_constants(persistent, act):
         ran("gated_stream_kernel<0")
 
 
+@pytest.mark.parametrize("form", [(0, 0), (0, 1), (-1, -1)], ids=["tall", "low", "rows"])
+@pytest.mark.parametrize("K", [65520, 66560])
+def test_gated_sums_at_the_end_of_32_bits(gpu, form, K):
+    # codes of -128 throughout and a bias next to 2^30: sums of 2^31 - 2^18 and, past the end of INT32, beyond it, where they wrap in every kernel
+    from paper_2101_01321_amd import binding as B
+    M = 3 if form[0] < 0 else 33
+    c = U.Gated(5, M, 20, K, 0)
+    c.a[:], c.w[:] = -128, -128
+    c.ch.b[:] = 2 ** 30 - 1
+    c.ch.m[:], c.ch.s[:] = 2 ** 30, 47
+    c.acc = (U.product(c.a, c.w) + c.ch.bias() + 2 ** 31) % 2 ** 32 - 2 ** 31
+    assert bool((c.acc < 0).all()) == (K > 65536)
+    B.ibert_rows_override(*form)
+    try:
+        run(c, "gated, K %d, %d rows" % (K, M))
+        ran("rows_ring_kernel" if form[0] < 0 else "gated_stream_kernel")
+    finally:
+        B.ibert_rows_override(-1, -1)
+
+
 @pytest.mark.parametrize("off", [0, 1, 4, 13])
 @pytest.mark.parametrize("ld", [(0, 0, 0), (16, 32, 16), (3, 5, 7), (12, 4, 1)])
 def test_rows_at_any_address(gpu, ld, off):
