@@ -38,18 +38,21 @@ static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, boo
     } else if (blocks(1, p.br) > 1536) p.nt = 2;
 }
 
-// The kernel of an INT8 gated block: 0 rows_ring_kernel, 1 and 2 the persistent one with tiles of 128 and 256 tokens; by what rounds of its workgroups over the chip's 256 units
-// are expected to take, us, from K / 1024 = k: a round of 64 x 32 rings 4.5 + 2 k behind the first 4, of 128 x 128 tiles 5.5 + 6.3 k, of 256 x 128 tiles 9.3 + 8.4 k.
-// Measured, us, rings / low / tall: 128 x 1024 x 4096 8.7 / 12.0 / 17.7, 256 x 1024 x 4096 14.9 / 12.3 / 17.8, 128 x 2048 x 8192 20.2 / 19 / 28, 1024 x 4096 x 4096 - / 36.2 / 45.7,
-// 2741 x 1024 x 4096 - / 34.4 / 36.7, 8192 x 4096 x 12288 - / 780 / 639.
+// The kernel of an INT8 gated block: 0 rows_ring_kernel, else the persistent one's tile; by what rounds of its workgroups over the chip's 256 units are expected to take, us, from
+// K / 1024 = k: a round of 64 x 32 rings 4 + 2.8 k behind the first 1.2, of 128 x 128 tiles 5.5 + 6.3 k, of 256 x 128 tiles 9.3 + 8.4 k, of 128 x 64 tiles 5.0 + 5.6 k where there
+// is one to a unit and 5.5 + 7 k where there are two.
+// Measured, us, rings / narrow / low / tall: 128 x 768 x 2048 4.8 / 8.8 / 10.9 / 15.7, 128 x 1024 x 4096 8.1 / 9.6 / 12.0 / 17.7, 64 x 4096 x 11008 31.3 / 27.2 / 34.5 / 43.0,
+// 256 x 1024 x 4096 14.9 / 9.3 / 11.9 / 17.8, 128 x 2048 x 8192 20.2 / 15.8 / 20.0 / 26.5, 1000 x 768 x 2048 - / 9.6 / 11.5 / 16.1, 512 x 1024 x 4096 - / 11.2 / 13.1 / 18.2,
+// 1024 x 4096 x 4096 - / 39.5 / 36.4 / 45.8, 2741 x 1024 x 4096 - / 33.8 / 34.0 / 36.3, 2048 x 4096 x 11008 - / 207 / 220 / 166, 8192 x 4096 x 12288 - / 882 / 787 / 652.
 static int plan_gated(int32_t M, int32_t F, int32_t K)
 {
-    auto ns = [&](int64_t fixed, int64_t per_k, int rows, int channels) {
-        const int64_t tiles = (((int64_t)M + rows - 1) / rows) * (((int64_t)F + channels - 1) / channels);
-        return (tiles + 255) / 256 * (fixed + per_k * K / 1024);
-    };
-    const int64_t ring = 4000 + ns(4500, 2000, 64, 32), low = ns(5500, 6300, 128, 128), tall = ns(9300, 8400, 256, 128);
-    return M <= 32 || (ring <= low && ring <= tall) ? 0 : (low <= tall ? 1 : 2);
+    auto tiles = [&](int rows, int channels) { return (((int64_t)M + rows - 1) / rows) * (((int64_t)F + channels - 1) / channels); };
+    auto ns = [&](int64_t fixed, int64_t per_k, int64_t n) { return (n + 255) / 256 * (fixed + per_k * K / 1024); };
+    const int64_t ring = 1200 + ns(4000, 2800, tiles(64, 32)), low = ns(5500, 6300, tiles(128, 128)), tall = ns(9300, 8400, tiles(256, 128));
+    const int64_t n = tiles(128, 64), odd = n % 512 > 0 && n % 512 <= 256, narrow = (odd ? ns(5000, 5600, 1) : 0) + ns(5500, 7000, ((n + 511) / 512 - odd) * 256);
+    if (M <= 32 || (ring <= narrow && ring <= low && ring <= tall)) return 0;
+    if (narrow < low && narrow < tall) return GATED_NARROW;
+    return low <= tall ? GATED_LOW : GATED_TALL;
 }
 
 static int launch_few_rows(RowsArgs& g, bool w4, int32_t group, bool zeros, bool gated, hipStream_t stream)
@@ -153,9 +156,11 @@ extern "C" int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A
     if (!W) return IBERT_ERR_NULL;
     const ibert_gated_desc& d = *desc;
     if (ibert::overlap(C, ibert::span(d.M, d.ldc, d.F, 1), W, ibert::span(2 * (int64_t)d.F, d.ldw, d.K, 1))) return IBERT_ERR_SHAPE;
-    const int persistent = ibert::g_rows_tiles == 0 ? (ibert::g_rows_rows == 1 ? 1 : 2) : (ibert::g_rows_tiles < 0 ? ibert::plan_gated(d.M, d.F, d.K) : 0);
-    if (persistent && ibert::gated_stream_ok(d, A, W))
-        return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, persistent == 2, static_cast<hipStream_t>(stream));
+    int tile = 0;
+    if (ibert::g_rows_tiles < 0) tile = ibert::plan_gated(d.M, d.F, d.K);
+    else if (ibert::g_rows_tiles == 0) tile = ibert::g_rows_rows == 1 ? ibert::GATED_LOW : (ibert::g_rows_rows == 3 ? ibert::GATED_NARROW : ibert::GATED_TALL);
+    if (tile > 0 && ibert::gated_stream_ok(d, A, W))
+        return ibert::launch_gated_stream(d, A, W, bias, mult, shift, C, tile, static_cast<hipStream_t>(stream));
     ibert::RowsArgs g = ibert::rows_args(A, d.lda, d.M, d.F, d.K, bias, mult, shift, C, d.ldc);
     g.w[0] = W;
     g.ldw = d.ldw;

@@ -1,6 +1,6 @@
 // The gated block for many tokens: the persistent workgroups of gemm_stream.h (streamed K steps of 128 bytes, two LDS stages, a step in
 // four phases by quadrants of the wavefront's tile), whose tile is 256 or 128 tokens by 128 channels of the gate and the same 128 of the up
-// projection.
+// projection, or 128 tokens by 64 of each, by four wavefronts.
 //
 //   * The first two MFMA blocks of a wavefront's four are rows of W_gate and the last two the same rows of W_up, so that the two halves of
 //     a step ("W first", "W second") bring one matrix each, and a lane ends up with gate and up sums of the same two neighbouring channels
@@ -10,8 +10,10 @@
 //   * SiLU's sigmoids, and GELU's erf where it has room, are tables in LDS, built once by every workgroup with the function they stand for.
 //
 // What bounds it: where K is long the matrix units at the clock that power leaves (8192 x 4096 -> 2 x 12288 635 us, 2.6 POP/s, MFMA busy 0.72); where it is short the
-// epilogue, 20 ALU instructions a value that no MFMA runs beside (2741 x 1024 -> 2 x 4096 31 us eager: a low tile takes 4.7 us in its loop and 3.5 in its epilogue), and the
-// last round of tiles, three quarters full there.  Two heights of tile: 128 tokens fill more units, 256 read W half as often (see plan_gated for both sides).
+// epilogue, 20 ALU instructions a value that no MFMA runs beside (2741 x 1024 -> 2 x 4096 31 us eager: a tile of 128 x 128 takes 4.7 us in its loop and 3.5 in its
+// epilogue), and the last round of tiles, three quarters full there.  Three tiles: 256 tokens read W half as often; 128 fill more units; 128 x 64, two workgroups to a unit,
+// fill them where 128 x 128 tiles do not (256 x 1024 -> 2 x 4096 11.9 / 9.3 us; see plan_gated).  Where both of a unit's workgroups have work they gain nothing of each
+// other's epilogues, with wave priorities that would put them out of phase neither (2741 tokens: 33.8 us with any).
 #include "gate_math.h"
 #include "gemm_stream.h"
 #include "gated_stream.h"
@@ -35,29 +37,28 @@ struct GatedStreamArgs {
     GateConst gate;
 };
 
-constexpr int GS_BF = 128, GS_NW = 8;                    // channels of a tile; wavefronts
 constexpr int GS_PITCH = 48, GS_TURN_WAVE = 32 * GS_PITCH;
-constexpr int GS_ERF = 3400;                             // entries that GELU's table may have
-
-// BM: tokens of a tile.
-template <int BM>
+// BM: tokens of a tile; BF: its channels (of each matrix).
+template <int BM, int BF>
 struct GatedLayout {
-    static constexpr int STAGE = (BM + 2 * GS_BF) * 128;
-    static constexpr int PAR = 2 * STAGE;                // two buffers of 3 x 256 constants
-    static constexpr int TURN = PAR + 2 * 3 * 256 * 4;   // rows on their way out: 32 rows of 32 bytes a wavefront
-    static constexpr int TABLE = TURN + GS_NW * GS_TURN_WAVE;
-    static constexpr int LDS = TABLE + 4 * GS_ERF;
-    static_assert(LDS <= 163840 && 2 * (2 * SIG_STEPS + 1) <= 4 * GS_ERF, "LDS of a workgroup");
+    static constexpr int NW = BF / 16, UNIT = 128 / BF;  // wavefronts; workgroups that a compute unit holds
+    static constexpr int STAGE = (BM + 2 * BF) * 128;
+    static constexpr int PAR = 2 * STAGE;                // two buffers of 3 x 2 BF constants
+    static constexpr int TURN = PAR + 2 * 3 * 2 * BF * 4;   // rows on their way out: 32 rows of 32 bytes a wavefront
+    static constexpr int TABLE = TURN + NW * GS_TURN_WAVE;
+    static constexpr int ERF = BF == 128 ? 3400 : 1792;     // entries that GELU's table may have
+    static constexpr int LDS = TABLE + 4 * ERF;
+    static_assert(LDS <= 163840 / UNIT && 2 * (2 * SIG_STEPS + 1) <= 4 * ERF, "LDS of a unit's workgroups");
 };
 
 enum { GS_GELU = 0, GS_SILU = 1, GS_GELU_TABLE = 2 };
 
 // TAIL: K is no multiple of 128 (of 16 it is).
-template <int ACT, int BM, bool TAIL>
-__global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArgs g)
+template <int ACT, int BM, int BF, bool TAIL>
+__global__ __launch_bounds__(4 * BF, 2) void gated_stream_kernel(GatedStreamArgs g)
 {
-    using GL = GatedLayout<BM>;
-    constexpr int GS_STAGE = GL::STAGE, GS_PAR = GL::PAR, BN = 256, NW = GS_NW, NT = 64 * NW, WR = 2, WC = 4;
+    using GL = GatedLayout<BM, BF>;
+    constexpr int GS_STAGE = GL::STAGE, GS_PAR = GL::PAR, BN = 2 * BF, NW = GL::NW, NT = 64 * NW, WR = 2, WC = NW / 2;
     constexpr int WM = BM / WR, WN = BN / WC, FM = WM / 16, FN = 4, FMH = FM / 2, FN0 = 2, FN1 = 2;
     constexpr int QA = FMH * 2 * WR / NW, QW = FN0 * 2 * WC / NW, NQ = QA + QW;       // requests of a wavefront: A half, W half, a group
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
     auto tile_at = [&](int l, int& m0, int& n0) {
         const int t = t0 + l, tm = udiv_fix(t, g.bn, g.bn_magic);
         m0 = tm * BM;
-        n0 = (first_col + t - tm * g.bn) * GS_BF;
+        n0 = (first_col + t - tm * g.bn) * BF;
     };
 
     // ---- requests (see gemm_stream.h) -----------------------------------------------------------
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
         if (l < count) {
             int m0, n0;
             tile_at(l, m0, n0);
-            const int rows = g.M - m0 < BM ? g.M - m0 : BM, cols = g.F - n0 < GS_BF ? g.F - n0 : GS_BF;
+            const int rows = g.M - m0 < BM ? g.M - m0 : BM, cols = g.F - n0 < BF ? g.F - n0 : BF;
             buffer(da, g.A + (int64_t)m0 * g.lda, (uint32_t)(rows - 1) * (uint32_t)g.lda + (uint32_t)g.K);
             buffer(dg, g.W + (int64_t)n0 * g.ldw, (uint32_t)(cols - 1) * (uint32_t)g.ldw + (uint32_t)g.K);
             buffer(du, g.W + ((int64_t)g.F + n0) * g.ldw, (uint32_t)(cols - 1) * (uint32_t)g.ldw + (uint32_t)g.K);
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
         }
         mark_tail();
     };
-    // Constants of a tile: [bias, mult, shift][gate, up][128], by DMA, 64 dwords a request; zeros past the last channel.
+    // Constants of a tile: [bias, mult, shift][gate, up][BF], by DMA, 64 dwords a request; zeros past the last channel.
     int par_n0 = -1, par_buf = 1;
     auto request_constants = [&](int n0) {
         if (n0 == par_n0) return;
@@ -157,13 +158,13 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
             const int32_t* src = a == 0 ? g.bias : (a == 1 ? g.mult : g.shift);
             if (src) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if ((a * 4 + c) % NW == wave) {
+                for (int c = 0; c < BN / 64; ++c)
+                    if ((a * (BN / 64) + c) % NW == wave) {
                         v4i d;
-                        buffer(d, src + (int64_t)(c >> 1) * g.F, (uint32_t)g.F * 4u);
+                        buffer(d, src + (int64_t)(c * 64 / BF) * g.F, (uint32_t)g.F * 4u);
                         d[3] = 0x00020000;
                         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                                     :: "s"(base + (uint32_t)((a * BN + c * 64) * 4)), "v"((uint32_t)(n0 + (c & 1) * 64 + lane) * 4u), "s"(d) : "memory", "m0");
+                                     :: "s"(base + (uint32_t)((a * BN + c * 64) * 4)), "v"((uint32_t)(n0 + c * 64 % BF + lane) * 4u), "s"(d) : "memory", "m0");
                     }
             } else {
                 int32_t* p = reinterpret_cast<int32_t*>(lds + GS_PAR + par_buf * 3 * BN * 4) + a * BN;
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
         kernel_args ga = nullptr;
 #endif
         const int last = ga->M - 1 - m0, rows = last < BM ? last : BM - 1;
-        const int cols = ga->F - n0 < GS_BF ? ga->F - n0 : GS_BF;
+        const int cols = ga->F - n0 < BF ? ga->F - n0 : BF;
         const int64_t out0 = (int64_t)m0 * ga->ldc + n0;
         // Fast form: every shift of the tile's channels in [33, 62], every |bias| below 2^30, and `fast`.
         bool fast;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 #pragma unroll
             for (int c = 0; c < BN; c += 64) {
                 const int32_t ps = par[2 * BN + c + el], pb = par[c + el];
-                if ((c & 64) + el < cols) ok = ok && ps >= 33 && ps <= 62 && (pb ^ (pb << 1)) >= 0;
+                if (c % BF + el < cols) ok = ok && ps >= 33 && ps <= 62 && (pb ^ (pb << 1)) >= 0;
             }
             fast = __builtin_amdgcn_ballot_w64(!ok) == 0 && ga->fast;
         }
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
             int32_t mm[FN], sh[FN];
 #pragma unroll
             for (int i = 0; i < FN; ++i) {
-                const int c = (i >> 1) * 128 + wf0 + 2 * r16 + (i & 1);
+                const int c = (i >> 1) * BF + wf0 + 2 * r16 + (i & 1);
                 const int32_t b = par[c], s = par[2 * BN + c];
                 mm[i] = par[BN + c];
                 c0[i] = (int64_t)b * mm[i] + ((int64_t)1 << ((s - 1) & 63));
@@ -411,18 +412,18 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 #pragma unroll
                         for (int i = 0; i < FN; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) st[(wave % WR * 16 + 4 * u + e) * SP + (i >> 1) * 128 + wf0 + 2 * r16 + (i & 1)] = acc[i][k][e];
+                            for (int e = 0; e < 4; ++e) st[(wave % WR * 16 + 4 * u + e) * SP + (i >> 1) * BF + wf0 + 2 * r16 + (i & 1)] = acc[i][k][e];
                     }
                 __syncthreads();
 #pragma unroll 1
-                for (int q = wave * 64 + el; q < 16 * WR * GS_BF; q += NT) {
-                    const int r = q / GS_BF, c = q - r * GS_BF, row = (r >> 4) * WM + 16 * j + (r & 15);
+                for (int q = wave * 64 + el; q < 16 * WR * BF; q += NT) {
+                    const int r = q / BF, c = q - r * BF, row = (r >> 4) * WM + 16 * j + (r & 15);
                     if (row > last || c >= cols) continue;
                     const GateConst gc{ga->gate.silu, GeluConst{ga->gate.gelu.q_b, ga->gate.gelu.q_c, ga->gate.gelu.q_1, ga->gate.gelu.q_max, ga->gate.gelu.m, ga->gate.gelu.s},
                                        ga->gate.m, ga->gate.s};
                     ga->C[out0 + (int64_t)row * ga->ldc + c] =
-                        (int8_t)gate_one((int32_t)((uint32_t)st[r * SP + c] + (uint32_t)par[c]), (int32_t)((uint32_t)st[r * SP + 128 + c] + (uint32_t)par[128 + c]),
-                                         par[BN + c], par[2 * BN + c] & 63, par[BN + 128 + c], par[2 * BN + 128 + c] & 63, gc);
+                        (int8_t)gate_one((int32_t)((uint32_t)st[r * SP + c] + (uint32_t)par[c]), (int32_t)((uint32_t)st[r * SP + BF + c] + (uint32_t)par[BF + c]),
+                                         par[BN + c], par[2 * BN + c] & 63, par[BN + BF + c], par[2 * BN + BF + c] & 63, gc);
                 }
                 __syncthreads();
             }
@@ -445,14 +446,15 @@ __global__ __launch_bounds__(64 * GS_NW) void gated_stream_kernel(GatedStreamArg
 bool gated_stream_ok(const ibert_gated_desc& d, const int8_t* A, const int8_t* W)
 {
     return d.K % 16 == 0 && aligned(A, 16) && aligned(W, 16) && d.lda % 16 == 0 && d.ldw % 16 == 0 && d.lda < (1 << 20) && d.ldw < (1 << 20) && d.ldc < (1 << 20) &&
-           (((int64_t)d.M + 127) / 128) * ((d.F + GS_BF - 1) / GS_BF) < (1 << 26);
+           (((int64_t)d.M + 127) / 128) * ((d.F + 63) / 64) < (1 << 26);
 }
 
-template <int ACT, int BM, bool TAIL>
+template <int ACT, int BM, int BF, bool TAIL>
 static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipStream_t stream)
 {
     s.tiles_m = (int32_t)(((int64_t)s.M + BM - 1) / BM);
-    const int tiles_n = (s.F + GS_BF - 1) / GS_BF;
+    using GL = GatedLayout<BM, BF>;
+    const int tiles_n = (s.F + BF - 1) / BF;
     // as stream_shares and stream_deal
     s.xs = 0;
     while (s.xs < 2 && tiles_n % (2 << s.xs) == 0 && (weight_bytes >> s.xs) > (2 << 20) && s.tiles_m >= (8 >> s.xs)) ++s.xs;
@@ -460,21 +462,22 @@ static int launch_gated_stream_as(GatedStreamArgs& s, int64_t weight_bytes, hipS
     s.bn = tiles_n >> s.xs;
     s.bn_magic = udiv_magic(s.bn);
     const int64_t run = ((int64_t)s.tiles_m * s.bn + (1 << s.gs) - 1) >> s.gs;
-    s.per_xcd = (int32_t)(run < 32 ? run : 32);
-    auto kern = gated_stream_kernel<ACT, BM, TAIL>;
+    const int most = 32 * GL::UNIT;                       // workgroups that an XCD holds
+    s.per_xcd = (int32_t)(run < most ? run : most);
+    auto kern = gated_stream_kernel<ACT, BM, BF, TAIL>;
     static bool attr_done = false;
     if (!attr_done) {
-        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 163840));
+        IBERT_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, GL::LDS));
         attr_done = true;
     }
-    hipLaunchKernelGGL(kern, dim3(8u * (unsigned)s.per_xcd), dim3(64 * GS_NW), GatedLayout<BM>::LDS, stream, s);
+    hipLaunchKernelGGL(kern, dim3(8u * (unsigned)s.per_xcd), dim3(64 * GL::NW), GL::LDS, stream, s);
     IBERT_LAUNCH_CHECK("gated_stream_kernel");
-    static const KernelName name("gated_stream_kernel<%d, %d, %s>", ACT, BM, TAIL ? "true" : "false");
+    static const KernelName name("gated_stream_kernel<%d, %d, %d, %s>", ACT, BM, BF, TAIL ? "true" : "false");
     g_last_kernel = name.text;
     return IBERT_OK;
 }
 
-int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, int tall,
+int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t* W, const int32_t* bias, const int32_t* mult, const int32_t* shift, int8_t* C, int tile,
                         hipStream_t stream)
 {
     GatedStreamArgs s{};
@@ -487,14 +490,19 @@ int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t
     s.fast = (int64_t)d.K * 16384 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
     s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
     const int64_t w = 2 * (int64_t)d.F * d.K;
-    auto launch = [&](auto act) {
-        constexpr int ACT = decltype(act)::value;
-        if (d.K % 128) return tall ? launch_gated_stream_as<ACT, 256, true>(s, w, stream) : launch_gated_stream_as<ACT, 128, true>(s, w, stream);
-        return tall ? launch_gated_stream_as<ACT, 256, false>(s, w, stream) : launch_gated_stream_as<ACT, 128, false>(s, w, stream);
+    auto launch = [&](auto act, auto bm, auto bf) {
+        constexpr int ACT = decltype(act)::value, BM = decltype(bm)::value, BF = decltype(bf)::value;
+        return d.K % 128 ? launch_gated_stream_as<ACT, BM, BF, true>(s, w, stream) : launch_gated_stream_as<ACT, BM, BF, false>(s, w, stream);
     };
-    if (!gelu) return launch(std::integral_constant<int, GS_SILU>{});
-    if (gelu_fast && -2 * (int64_t)p.gelu.q_b < GS_ERF) return launch(std::integral_constant<int, GS_GELU_TABLE>{});
-    return launch(std::integral_constant<int, GS_GELU>{});
+    auto with = [&](auto bm, auto bf) {
+        if (!gelu) return launch(std::integral_constant<int, GS_SILU>{}, bm, bf);
+        if (gelu_fast && -2 * (int64_t)p.gelu.q_b < GatedLayout<decltype(bm)::value, decltype(bf)::value>::ERF) return launch(std::integral_constant<int, GS_GELU_TABLE>{}, bm, bf);
+        return launch(std::integral_constant<int, GS_GELU>{}, bm, bf);
+    };
+    using std::integral_constant;
+    if (tile == GATED_TALL) return with(integral_constant<int, 256>{}, integral_constant<int, 128>{});
+    if (tile == GATED_LOW) return with(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+    return with(integral_constant<int, 128>{}, integral_constant<int, 64>{});
 }
 
 }  // namespace ibert

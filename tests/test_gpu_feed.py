@@ -101,7 +101,7 @@ def test_w4(form, M, N, K, group, zeros):
     run(U.Rows4(M + N + K, M, N, K, group, zeros, out, residual=bool((N + zeros) % 2), bias=M % 3 != 0), "w4 %d x %d x %d, groups of %d, %s" % (M, N, K, group, out))
 
 
-@pytest.fixture(params=[0, 1], ids=["tall", "low"])
+@pytest.fixture(params=[0, 1, 3], ids=["tall", "low", "narrow"])
 def persistent(request, gpu):
     from paper_2101_01321_amd import binding as B
     B.ibert_rows_override(0, request.param)
@@ -157,7 +157,7 @@ def test_persistent_gated_any_constants(persistent, act):
         ran("gated_stream_kernel<0")
 
 
-@pytest.mark.parametrize("form", [(0, 0), (0, 1), (-1, -1)], ids=["tall", "low", "rows"])
+@pytest.mark.parametrize("form", [(0, 0), (0, 1), (0, 3), (-1, -1)], ids=["tall", "low", "narrow", "rows"])
 @pytest.mark.parametrize("K", [65520, 66560])
 def test_gated_sums_at_the_end_of_32_bits(gpu, form, K):
     # codes of -128 throughout and a bias next to 2^30: sums of 2^31 - 2^18 and, past the end of INT32, beyond it, where they wrap in every kernel
