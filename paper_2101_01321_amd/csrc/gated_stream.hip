@@ -32,7 +32,7 @@ struct GatedStreamArgs {
     int32_t tiles_m, bn;           // as in StreamArgs
     uint32_t bn_magic;
     int32_t xs, gs, per_xcd;
-    int32_t fast;                  // K * 128^2 < 2^30, the product's shift in [33, 62], and gelu_fast_ok where it is GELU
+    int32_t fast;                  // K * 128^2 < 2^30, the product's shift in [32, 62], and gelu_fast_ok where it is GELU
     int32_t c_vec;                 // rows of C allow 16-byte stores
     GateConst gate;
 };
@@ -301,14 +301,14 @@ __global__ __launch_bounds__(4 * BF, 2) void gated_stream_kernel(GatedStreamArgs
         const int last = ga->M - 1 - m0, rows = last < BM ? last : BM - 1;
         const int cols = ga->F - n0 < BF ? ga->F - n0 : BF;
         const int64_t out0 = (int64_t)m0 * ga->ldc + n0;
-        // Fast form: every shift of the tile's channels in [33, 62], every |bias| below 2^30, and `fast`.
+        // Fast form: every shift of the tile's channels in [32, 62] (a multiplier below 1/2), every |bias| below 2^30, and `fast`.
         bool fast;
         {
             bool ok = true;
 #pragma unroll
             for (int c = 0; c < BN; c += 64) {
                 const int32_t ps = par[2 * BN + c + el], pb = par[c + el];
-                if (c % BF + el < cols) ok = ok && ps >= 33 && ps <= 62 && (pb ^ (pb << 1)) >= 0;
+                if (c % BF + el < cols) ok = ok && ps >= 32 && ps <= 62 && (pb ^ (pb << 1)) >= 0;
             }
             fast = __builtin_amdgcn_ballot_w64(!ok) == 0 && ga->fast;
         }
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(4 * BF, 2) void gated_stream_kernel(GatedStreamArgs
                 sh[i] = (s - 32) & 31;
             }
             const GeluConst gl{ga->gate.gelu.q_b, ga->gate.gelu.q_c, ga->gate.gelu.q_1, ga->gate.gelu.q_max, ga->gate.gelu.m, ga->gate.gelu.s};
-            // (x m + 2^(s-1)) >> s of a 32-bit x, s in [33, 62]: the high half of one 64-bit multiply-add, shifted
+            // (x m + 2^(s-1)) >> s of a 32-bit x, s in [32, 62]: the high half of one 64-bit multiply-add, shifted; below 2^30 + 1 in size
             const int64_t gl_rnd = (int64_t)1 << ((gl.s - 1) & 63), ornd = (int64_t)1 << ((ga->gate.s - 1) & 63);
             const int32_t gl_sh = (gl.s - 32) & 31, om = ga->gate.m, osh = (ga->gate.s - 32) & 31;
             const uint32_t table = lds0 + (uint32_t)GL::TABLE;
@@ -487,7 +487,7 @@ int launch_gated_stream(const ibert_gated_desc& d, const int8_t* A, const int8_t
     const ibert_gate_params& p = d.gate;
     s.gate = gate_const(p);
     const bool gelu = !s.gate.silu, gelu_fast = gelu && gelu_fast_ok(p.gelu);
-    s.fast = (int64_t)d.K * 16384 < (1 << 30) && p.out_dy.s >= 33 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
+    s.fast = (int64_t)d.K * 16384 < (1 << 30) && p.out_dy.s >= 32 && p.out_dy.s <= 62 && (!gelu || gelu_fast);
     s.c_vec = aligned(C, 16) && d.ldc % 16 == 0;
     const int64_t w = 2 * (int64_t)d.F * d.K;
     auto launch = [&](auto act, auto bm, auto bf) {

@@ -157,6 +157,25 @@ def test_persistent_gated_any_constants(persistent, act):
         ran("gated_stream_kernel<0")
 
 
+@pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
+def test_persistent_gated_shifts_from_31_on(persistent, act):
+    # one side of the fast epilogue's first shift and the other, multipliers at their ends, in the channels and behind the product
+    for K, shift in ((128, 32), (256, 32), (144, 33), (128, 31)):
+        c = U.Gated(K + act, 300, 140, K, act)
+        c.ch.s[:] = shift
+        c.ch.m[:] = c.ch.m // 8
+        c.ch.m[[3, 150]], c.ch.m[[5, 153]] = 2 ** 31 - 1, U.LOW
+        c.ch.b[[3, 5, 150]] = 2 ** 30 - 2 ** 23
+        c.ch.b[[4, 153]] = 2 ** 23 - 2 ** 30
+        acc = U.product(c.a, c.w) + c.ch.bias()
+        assert abs(acc).max() < 2 ** 31
+        c.acc = acc
+        run(c, "persistent gated, K %d, shift %d" % (K, shift))
+        c.params.out_dy.m, c.params.out_dy.s = (2 ** 31 - 1 if act else U.LOW), shift
+        run(c, "persistent gated, K %d, shift %d behind the product" % (K, shift))
+    ran("gated_stream_kernel")
+
+
 @pytest.mark.parametrize("form", [(0, 0), (0, 1), (0, 3), (-1, -1)], ids=["tall", "low", "narrow", "rows"])
 @pytest.mark.parametrize("K", [65520, 66560])
 def test_gated_sums_at_the_end_of_32_bits(gpu, form, K):
