@@ -670,7 +670,9 @@ int ibert_w4_pack(const int8_t* w, const uint8_t* scales, const int8_t* zeros, i
 int ibert_w4_from_float(const double* x, int32_t N, int32_t K, int32_t group, int8_t* w, uint8_t* scales, double* S_w);
 
 /* Host: the gated block's constants from real scales: with IBERT_GATE_SILU S_gate is not used (it is IBERT_SILU_SCALE), with IBERT_GATE_GELU gelu is that of
- * ibert_gelu_params_from_scale(S_gate, S_gate / 4);  out_dy = dyadic(S_a * S_up / S_out), S_a the scale of a. */
+ * ibert_gelu_params_from_scale(S_gate, S_gate / 4);  out_dy = dyadic(S_a * S_up / S_out), S_a the scale of a.
+ * Errors: IBERT_ERR_PARAM_RANGE: an activation that there is none of, scales not above 0, a multiplier of 2^31 or more, and with IBERT_GATE_GELU scales at which q_max < -q_b
+ * (S_gate below about 1/395).  A larger gate than q_max S_gate = about 1.55e8 S_gate^3 is taken as that one: 155 at 1/100, 19 at 1/200, 5.7 at 1/300, 2.5 at 1/395. */
 int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up, double S_out, ibert_gate_params* out);
 
 /* ------------------------------------------------------------------------------------------------

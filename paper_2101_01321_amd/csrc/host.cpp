@@ -365,6 +365,9 @@ int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up
         S_a = S_gate / 4.0;
         const int rc = ibert_gelu_params_from_scale(S_gate, S_a, &out->gelu);
         if (rc) return rc;
+        // Gates are cut off at q_max, which INT32 leaves for |t|: 1.55e8 S_gate^3 as a real number.  Below -q_b (2.50) GELU is still curved there, and nothing says
+        // x for what lies beyond: 0.05 is all that is left at 1/1500.
+        if (out->gelu.q_max < -out->gelu.q_b) return IBERT_ERR_PARAM_RANGE;
     }
     return ibert_dyadic_from_double(S_a * S_up / S_out, &out->out_dy);
 }

@@ -124,6 +124,20 @@ def test_gate_params_refuse():
     assert B.lib().ibert_gate_params_from_scales(0, 0.0, 1.0, 1.0, None) == -1
 
 
+def test_gelu_gates_reach_where_gelu_is_straight():
+    # what a gate can be at most, q_max S_gate, against -q_b S_gate = 2.50, from where on the integer erf is one: a finer scale cuts off gates at which GELU is still curved
+    for n in (10, 50, 100, 200, 300, 350, 390, 394, 395):
+        p = B.ibert_gate_params_from_scales(B.GATE_GELU, 1 / n, 1 / 2000, 1 / 16).gelu
+        assert p.q_max >= -p.q_b and abs(p.q_max / n / (1.55e8 / n ** 3) - 1) < 0.02, n
+    for n in (397, 398, 400, 450, 1500, 10000):
+        whole = B.ibert_gelu_params_from_scale(1 / n, 1 / (4 * n))
+        assert whole.q_max < -whole.q_b, n
+        with pytest.raises(B.IbertError) as e:
+            B.ibert_gate_params_from_scales(B.GATE_GELU, 1 / n, 1 / 2000, 1 / 16)
+        assert e.value.code == -3
+        B.ibert_gate_params_from_scales(B.GATE_SILU, 1 / n, 1 / 2000, 1 / 16)      # (not used with SiLU)
+
+
 def test_logits_row_from_reals():
     p = B.ibert_logits_row_from_reals(0.01, 1.25, 0.5, -0.1, 3)
     assert p.up.tuple() == U.dyadic(0.8) and p.down.tuple() == U.dyadic(1.25) and (p.presence, p.frequency, p.mask) == (50, -10, 3)
