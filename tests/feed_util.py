@@ -228,3 +228,29 @@ class Logits:
     def desc(self):
         return B.LogitsDesc(self.rows, self.vocab, self.vocab + self.ld[0], self.vocab + self.ld[1], self.tokens.size, self.ids.size, self.num_masks,
                             self.masks.shape[1] if self.num_masks else 0)
+
+
+def logits_by_rows(c, y0=None):
+    """Logits.expected, a row at a time in 64 bits: for rows that take too long token by token."""
+    out = (c.y0 if y0 is None else y0).copy()
+    inside = lambda t: (t >= 0) & (t < c.vocab)      # noqa: E731
+    for r in range(c.rows):
+        um, us, dm, ds, presence, frequency, mask = (int(v) for v in c.params[r])
+        ts, te = (min(max(int(v), 0), c.tokens.size) for v in c.start[r:r + 2])
+        te = max(te, ts)
+        made = min(max(int(c.made[r]), ts), te)
+        b0 = min(max(int(c.bstart[r]), 0), c.ids.size)
+        b1 = max(b0, min(max(int(c.bstart[r + 1]), 0), c.ids.size))
+        x, history, new, ids = c.x[r, :c.vocab].astype(np.int64), c.tokens[ts:te], c.tokens[made:te], c.ids[b0:b1]
+        seen, bias = np.zeros(c.vocab, bool), np.zeros(c.vocab, np.int64)
+        seen[history[inside(history)]] = True
+        n = np.bincount(new[inside(new)], minlength=c.vocab)
+        np.add.at(bias, ids[inside(ids)], c.values[b0:b1][inside(ids)].astype(np.int64))
+        pen = np.clip(dy(x, np.where(x > 0, um, dm), np.clip(np.where(x > 0, us, ds), 0, 62)), LOW, HIGH)
+        v = np.clip(np.where(seen, pen, x) - presence * (n > 0) - frequency * n + bias, LOW + 1, HIGH)
+        v[x == LOW] = LOW
+        if mask >= 0 and c.num_masks:
+            bits = np.unpackbits(np.ascontiguousarray(c.masks[min(mask, c.num_masks - 1)]).view(np.uint8), bitorder="little")[:c.vocab]
+            v[bits == 0] = LOW
+        out[r, :c.vocab] = v
+    return out

@@ -274,3 +274,13 @@ def test_structs_have_the_header_s_sizes():
     # ctypes and the C compiler agree on natural alignment; the arrays a program makes itself have 28 bytes a row
     assert C.sizeof(B.LogitsRow) == 28 and C.sizeof(B.GateParams) == 4 + 24 + 8 and C.sizeof(B.W4Weights) == 32 and C.sizeof(B.W4Desc) == 56
     assert C.sizeof(B.GatedDesc) == 16 + 24 + 40 and C.sizeof(B.LogitsDesc) == 40
+
+
+def test_logits_by_rows_are_those_token_by_token():
+    for seed, (lens, vocab, blens, masks, ld) in enumerate([([3], 1, [1], 1, (0, 0, 0)), ([0, 500, 77], 333, [9, 0, 300], 3, (3, 5, 2)), ([50, 60, 70, 80], 400, [20, 30, 10, 5], 0, (0, 0, 0))]):
+        c = U.Logits(seed, lens, vocab, blens, masks, ld)
+        assert np.array_equal(U.logits_by_rows(c), c.expected())
+        if len(lens) == 4:
+            c.start[:], c.made[:], c.bstart[:] = (-7, 10 ** 9, 100, U.LOW, U.HIGH), (U.LOW, 10 ** 8, 120, 100), (30, 20, -1, 10 ** 9, 40)
+            c.params[0, 1], c.params[1, 3], c.params[2, 1], c.params[3, 1] = 63, -1, U.HIGH, U.LOW
+            assert np.array_equal(U.logits_by_rows(c, c.y0), c.expected(c.y0))
