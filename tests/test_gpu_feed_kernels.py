@@ -75,3 +75,126 @@ def test_logits_a_long_list_of_biases_is_gone_through_a_fixed_number_of_times(gp
             best = min(best, a.elapsed_time(b))
         times.append(best)
     assert times[1] < 8 * times[0], times             # (three walks for one, and beside them the same work)
+
+
+@pytest.mark.parametrize("rows,vocab,kernel", SLICED + [(70, 33000, 4096)])
+def test_logits_slices(gpu, rows, vocab, kernel):
+    # histories, biases whose sums have 32 bits, masks; rows dealt to the XCDs (a multiple of eight, 128 and more) or not
+    rng = np.random.default_rng(rows)
+    lens, blens = rng.integers(0, 400, rows), rng.integers(0, 300, rows)
+    lens[0], lens[-1], blens[-1] = 9000, 0, 0
+    c = U.Logits(vocab + 1, lens, vocab, blens, 4)
+    c.values[:] = rng.integers(-700, 700, c.values.size)
+    for off, in_place in ((0, False), (2, False), (0, True)):
+        check_logits(c, kernel, "%d x %d" % (rows, vocab), off, in_place)
+    c = U.Logits(vocab + 2, lens, vocab, None, 0, (5, 3, 0))
+    check_logits(c, kernel, "%d x %d, strides, histories alone" % (rows, vocab))
+
+
+@pytest.mark.parametrize("rows,vocab,kernel", [(12, 5000, 2048), (72, 30000, 4096)])
+def test_logits_biases_on_both_sides_of_the_32_bit_line(gpu, rows, vocab, kernel):
+    # lists of n equal values for one token: (2^31 - 1) / n still has sums of 32 bits, one more in size has not
+    lens = [(1, 7, 1000)[r // 4 % 3] for r in range(rows)]
+    c = U.Logits(3, [20] * rows, vocab, lens, 0)
+    for r, n in enumerate(lens):
+        small = (2 ** 31 - 1) // n
+        c.values[c.bstart[r]:c.bstart[r + 1]] = (small, min(small + 1, U.HIGH), -small, -small - 1)[r % 4]
+        t = int(np.random.default_rng(r).integers(0, vocab))
+        c.ids[c.bstart[r]:c.bstart[r + 1]] = t
+        c.x[r, t] = (-5, 5, 5, -5)[r % 4]
+    check_logits(c, kernel, "biases at the line")
+
+
+# ------------------------------------------------------------------------------------------- few rows
+SHAPES = [(1, 1, 1), (1, 17, 15), (2, 33, 129), (5, 100, 304), (8, 64, 2048), (17, 130, 512), (33, 96, 1000), (64, 48, 640), (65, 341, 768), (130, 70, 128)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, False), (32, True), (64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("form", [(2, 1), (2, 4)], ids=["8_rows", "32_rows"])
+def test_w4_two_tiles_of_channels(gpu, form, group, zeros):
+    from paper_2101_01321_amd import binding as B
+    B.ibert_rows_override(*form)
+    try:
+        for M, N, K in SHAPES:
+            run(U.Rows4(M + N, M, N, K, group, zeros, ("i8", "i16", "i32")[(M + N) % 3], residual=bool(N % 2), bias=M % 3 != 0), "w4 %d x %d x %d, groups of %d" % (M, N, K, group))
+            if K % 16 == 0:
+                ran("rows_ring_kernel<true, %d, 2," % form[1])
+            if form == (2, 4):
+                run(U.Gated(M + N, M, N, K, M % 2, group, zeros), "w4 gated %d x %d x %d, groups of %d" % (M, N, K, group))
+                if K % 16 == 0:
+                    ran("rows_ring_kernel<true, 4, 4,")
+    finally:
+        B.ibert_rows_override(-1, -1)
+
+
+# what serving calls, small in K: heads of many channels, batches
+PICKED = [("w4", 1, 24600, 144, "<true, 1, 2,"), ("w4", 8, 30011, 128, "<true, 1, 2,"), ("w4", 13, 24600, 256, "<true, 2, 2,"), ("w4", 40, 4099, 272, "<true, 4, 2,"),
+          ("w4", 130, 6600, 2048, "<true, 4, 4,"), ("w4", 64, 8200, 8192, "<true, 4, 4,"), ("gated", 130, 3300, 144, "<true, 4, 4,"), ("gated", 64, 8200, 256, "<true, 4, 4,")]
+
+
+@pytest.mark.parametrize("kind,M,N,K,kernel", PICKED)
+def test_w4_kernels_that_the_rule_picks(gpu, kind, M, N, K, kernel):
+    for group, zeros in ((128, False), (32, True)):
+        if kind == "w4":
+            run(U.Rows4(M, M, N, K, group, zeros, "i32" if M < 16 else "i16", residual=M >= 16), "w4 %d x %d x %d by the rule" % (M, N, K))
+        else:
+            run(U.Gated(M, M, N, K, M % 3 // 2, group, zeros), "w4 gated %d x %d x %d by the rule" % (M, N, K))
+        ran("rows_ring_kernel" + kernel)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_w4_sums_of_the_longest_runs_in_32_bits(gpu, group, zeros):
+    # 32 chunks of K to a wavefront, every product at its largest: 4096 * 128 * 15 * 255 < 2^31; one chunk more is the other kernel's
+    for K, kernel in ((32768, "rows_ring_kernel"), (32784, "rows_any_kernel")):
+        for M in (1, 20):
+            c = U.Rows4(K, M, 20, K, group, zeros, "i32", extreme=True)
+            c.ch.m[:], c.ch.s[:] = 1 << 30, 36            # (nothing is cut off here but by INT32 itself)
+            c.a[-1] = 1
+            c.acc = np.clip(U.product(c.a, c.w4.whole()) + c.ch.bias(), U.LOW, U.HIGH)
+            run(c, "w4 extreme, groups of %d, K %d" % (group, K))
+            ran(kernel)
+            c = U.Rows4(K + 1, M, 20, K, group, zeros, "i32", extreme=True)
+            # signs in turn from run to run of 4096: every run's sum is at an end of its 32 bits, what they come to is small
+            c.a[:, :K] = np.where(np.arange(K) // 4096 % 2 == 0, -128, 127)
+            c.a[:, K - 4096:] = 3
+            c.ch.m[:], c.ch.s[:] = 1 << 30, 31
+            acc = U.product(c.a, c.w4.whole()) + c.ch.bias()
+            c.acc = np.clip(acc, U.LOW, U.HIGH)
+            run(c, "w4 runs of both signs, groups of %d, K %d" % (group, K))
+            ran(kernel)
+
+
+# ------------------------------------------------------------------------------------------- many tokens
+@pytest.fixture(params=[0, 1, 3], ids=["tall", "low", "narrow"])
+def persistent(request, gpu):
+    from paper_2101_01321_amd import binding as B
+    B.ibert_rows_override(0, request.param)
+    yield request.param
+    B.ibert_rows_override(-1, -1)
+
+
+@pytest.mark.parametrize("act", [0, 1], ids=["silu", "gelu"])
+def test_persistent_gated_columns_dealt_to_four_groups_of_xcds(persistent, act):
+    # columns of tiles a multiple of four, more than 4 MB of weights, eight rows of tiles and more
+    run(U.Gated(act, 2100, 2048, 1040, act), "persistent gated, 4.3 MB of weights")
+    ran("gated_stream_kernel")
+
+
+def test_persistent_gated_gelu_beyond_where_erf_is_one(persistent):
+    # gates on both sides of -q_b, where erf is cut off; its table has no room in the narrow tile, whose kernel computes it
+    from paper_2101_01321_amd import binding as B
+    for name in ("by hand", "from a scale"):
+        c = U.Gated(21, 700, 300, 256, B.GATE_GELU)
+        if name == "by hand":
+            c.params.gelu = B.GeluParams(-1000, -500000, -400000, (2 ** 31 - 1) // 900000, B.Dyadic(-(1 << 30), 46))
+        else:
+            c.params = B.ibert_gate_params_from_scales(B.GATE_GELU, 1 / 390, 1 / 2000, 1 / 16)
+        q_b, q_max = c.params.gelu.q_b, c.params.gelu.q_max
+        assert -1700 < q_b <= -896 and q_max > -q_b
+        c.ch.m[:300], c.ch.s[:300] = c.ch.m[:300], c.ch.s[:300] - 2        # gates four times as large
+        run(c, "persistent gated, gates beyond -q_b, constants " + name)
+        g = U.dy(c.acc[:, :300], c.ch.m[:300], c.ch.s[:300])
+        assert (np.abs(g) > -q_b).mean() > 0.05 and (np.abs(g) < -q_b).mean() > 0.05 and (np.abs(g) > q_max).any()
+        assert np.unique(c.expected()).size > 100
+        ran("gated_stream_kernel<%d" % (0 if persistent == 3 else 2))
