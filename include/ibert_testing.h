@@ -67,8 +67,8 @@ void ibert_paged_attention_override(int32_t form);
 void ibert_rotary_override(int32_t heads);
 
 /* Which kernels the gated block and the products with 4-bit weights run.  tiles = 1, 2 or 4: the kernels of few rows with so many tiles of 16 channels to a workgroup (pairs of the gated
- * block; four: of products alone, at most 32 rows), and 8 x `rows` (1, 2, 4, 8) rows, requested straight into LDS where that can be; rows = 0: through registers, as for rows that
- * are not aligned.  tiles = 0: the persistent kernel of the INT8 gated block where it can run, its tiles 256 tokens high, or 128 with rows = 1, or 128 by
+ * block) and 8 x `rows` (1, 2, 4, 8) rows, or what is nearest of those that the rule can pick, requested straight into LDS where that can be; rows = 0: through registers, as for rows
+ * that are not aligned.  tiles = 0: the persistent kernel of the INT8 gated block where it can run, its tiles 256 tokens high, or 128 with rows = 1, or 128 by
  * 64 channels with rows = 3.  Negative tiles and rows: what is
  * faster (the default).  The result never depends on it.  Process-wide, not thread-safe. */
 void ibert_rows_override(int32_t tiles, int32_t rows);

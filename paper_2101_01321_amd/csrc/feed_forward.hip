@@ -19,6 +19,8 @@ static int g_rows_tiles = -1, g_rows_rows = -1;
 //            128: 4096 x 4096 2x4 10.3 / 4x4 11.4, 4096 x 12288 22.8 / 19.8;  256: 4096 x 4096 17.5 / 15.4, 50000 x 1024 79 / 83
 //   pairs    64: 11008 x 4096 1x4 24.9 / 2x4 22.5, 4096 x 1024 6.1 / 6.6;  128: 4096 x 1024 9.3 / 8.5, 2730 x 1024 7.2 / 8.3
 //   INT8     64: 8192 x 2048 1x4 14.4 / 2x8 13.0;  128: 11008 x 4096 48.2 / 42.1, 2730 x 1024 7.9 / 8.3;  256: 2730 x 1024 12.1 / 14.6
+//   not there, by the rule / otherwise: 4 bits 2x8 64: 4096 x 12288 15.5 / 22.7, 256: 31.0 / 39.2, pairs 256: 11008 x 4096 56.5 / 67.9; 4 bits 4x1 8: 50000 x 1024 9.2 / 9.8,
+//            4x2 16: 11.0 / 13.0; pairs 2x1 8: 11008 x 4096 11.7 / 13.5, 2x2 16: 13.1 / 14.7, INT8 pairs 2x2 16: 19.7 / 21.7, 2x4 32: 22.7 / 26.1, 1x8 64: 2730 x 1024 5.3 / 5.6
 static void plan_ring(RowsPlan& p, int32_t M, int32_t N, int32_t K, bool w4, bool gated)
 {
     auto blocks = [&](int nt, int br) { return ((int64_t)N + 16 * nt - 1) / (16 * nt) * (((int64_t)M + 8 * br - 1) / (8 * br)); };
@@ -62,8 +64,11 @@ static int launch_few_rows(RowsArgs& g, bool w4, int32_t group, bool zeros, bool
     RowsPlan p{};
     plan_ring(p, g.M, g.N, g.K, w4, gated);
     if (g_rows_tiles > 0) {
-        p.nt = g_rows_tiles == 4 && (gated || !w4) ? 2 : g_rows_tiles;
-        if (g_rows_rows > 0) p.br = g_rows_rows;
+        // (of the tiles that there are: see launch_ring)
+        if (g_rows_rows > 0) p.br = w4 && g_rows_rows > 4 ? 4 : g_rows_rows;
+        if (!w4) p.nt = p.br == 8 ? 2 : 1;
+        else if (gated) p.nt = g_rows_tiles > 1 && p.br == 4 ? 2 : 1;
+        else p.nt = g_rows_tiles == 4 && p.br < 4 ? 2 : g_rows_tiles;
     }
     size_t lds;
     auto fits = [&] { return ring_stages(g, w4, p.br, (gated ? 2 : 1) * p.nt, gated, group, zeros, &lds) > 0; };

@@ -76,6 +76,8 @@ int launch_ring_as(RowsArgs g, hipStream_t stream)
     });
 }
 
+// The tiles that plan_ring picks, and those that it makes smaller where LDS is short: one tile (pair) of channels by up to four blocks of rows; beside them eight blocks by two
+// pairs of INT8 weights, four blocks by two pairs of 4-bit ones, and up to four blocks by two tiles, or four by four, of a product alone.
 template <bool W4, int G, bool ZERO, bool GATED>
 int launch_ring(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
 {
@@ -83,18 +85,15 @@ int launch_ring(const RowsArgs& g, const RowsPlan& plan, hipStream_t stream)
     if (plan.nt == 1) {
         if (plan.br == 1) return launch_ring_as<W4, 1, PER, G, ZERO, GATED>(g, stream);
         if (plan.br == 2) return launch_ring_as<W4, 2, PER, G, ZERO, GATED>(g, stream);
-        if (plan.br == 4) return launch_ring_as<W4, 4, PER, G, ZERO, GATED>(g, stream);
-        return launch_ring_as<W4, 8, PER, G, ZERO, GATED>(g, stream);
+        return launch_ring_as<W4, 4, PER, G, ZERO, GATED>(g, stream);
     }
-    if constexpr (W4 && !GATED) if (plan.nt == 4) {
-        if (plan.br == 1) return launch_ring_as<W4, 1, 4, G, ZERO, GATED>(g, stream);
-        if (plan.br == 2) return launch_ring_as<W4, 2, 4, G, ZERO, GATED>(g, stream);
-        return launch_ring_as<W4, 4, 4, G, ZERO, GATED>(g, stream);       // (8 rows' blocks: see launch_few_rows)
+    if constexpr (GATED) return launch_ring_as<W4, W4 ? 4 : 8, 4, G, ZERO, GATED>(g, stream);
+    else {
+        if (plan.nt == 4) return launch_ring_as<W4, 4, 4, G, ZERO, GATED>(g, stream);
+        if (plan.br == 1) return launch_ring_as<W4, 1, 2, G, ZERO, GATED>(g, stream);
+        if (plan.br == 2) return launch_ring_as<W4, 2, 2, G, ZERO, GATED>(g, stream);
+        return launch_ring_as<W4, 4, 2, G, ZERO, GATED>(g, stream);
     }
-    if (plan.br == 1) return launch_ring_as<W4, 1, 2 * PER, G, ZERO, GATED>(g, stream);
-    if (plan.br == 2) return launch_ring_as<W4, 2, 2 * PER, G, ZERO, GATED>(g, stream);
-    if (plan.br == 4) return launch_ring_as<W4, 4, 2 * PER, G, ZERO, GATED>(g, stream);
-    return launch_ring_as<W4, 8, 2 * PER, G, ZERO, GATED>(g, stream);
 }
 
 template <bool W4, int BR, int NT, int G, bool ZERO, bool GATED>
