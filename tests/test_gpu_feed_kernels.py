@@ -198,3 +198,103 @@ def test_persistent_gated_gelu_beyond_where_erf_is_one(persistent):
         assert (np.abs(g) > -q_b).mean() > 0.05 and (np.abs(g) < -q_b).mean() > 0.05 and (np.abs(g) > q_max).any()
         assert np.unique(c.expected()).size > 100
         ran("gated_stream_kernel<%d" % (0 if persistent == 3 else 2))
+
+
+# ------------------------------------------------------------------------------------------- the ends of what the calls take
+def strided(values, ld, fill=0):
+    """A [rows, n] int8 array as rows ld bytes apart on the GPU: the whole buffer and the view of its rows."""
+    torch, G, B = libs()
+    rows, n = values.shape
+    whole = torch.full((rows * ld,), fill, dtype=torch.int8, device=G.DEV)
+    view = whole.view(rows, ld)[:, :n]
+    view.copy_(torch.from_numpy(np.ascontiguousarray(values)).to(G.DEV))
+    return whole, view
+
+
+@pytest.mark.parametrize("M,F,K,lda,ldw,ldc,kernel", [
+    (40, 70, 144, 1 << 24, 1 << 26, 1 << 27, "rows_ring_kernel"), (300, 70, 150, (1 << 24) + 1, (1 << 26) + 16, (1 << 24) + 3, "rows_any_kernel"),
+    (4500, 2200, 144, (1 << 20) - 16, (1 << 20) - 16, (1 << 20) - 16, "gated_stream_kernel")])
+def test_i8_gated_offsets_beyond_32_bits(gpu, M, F, K, lda, ldw, ldc, kernel):
+    torch, G, B = libs()
+    c = U.Gated(M, M, F, K, M % 2)
+    G.say("i8 gated %d x %d x %d, leading dimensions %d, %d, %d" % (M, F, K, lda, ldw, ldc))
+    a, w = strided(c.a, lda)[0], strided(c.w, ldw)[0]
+    out, rows = strided(c.c0, ldc, 77)
+    desc = c.desc()
+    desc.lda, desc.ldw, desc.ldc = lda, ldw, ldc
+    B.ibert_gemm_i8_gated(desc, a, w, G.to_dev(c.ch.b), G.to_dev(c.ch.m), G.to_dev(c.ch.s), out)
+    torch.cuda.synchronize()
+    ran(kernel)
+    same(rows, c.expected(), "offsets beyond 32 bits")
+    rows.fill_(77)
+    assert all(bool((x == 77).all()) for x in out.split(1 << 30)), "wrote between the rows"
+
+
+@pytest.mark.parametrize("K,lda,kernel", [(144, 1 << 24, "rows_ring_kernel"), (150, (1 << 24) + 3, "rows_any_kernel")])
+def test_w4_offsets_beyond_32_bits(gpu, K, lda, kernel):
+    torch, G, B = libs()
+    M, N, ldc = 300, 40, (1 << 24) + 5
+    c = U.Rows4(K, M, N, K, 64, True, "i8", residual=True)
+    G.say("w4 %d x %d x %d, leading dimensions %d, %d" % (M, N, K, lda, ldc))
+    a, r = strided(c.a, lda)[0], strided(c.r, ldc)[0]
+    out, rows = strided(c.c0, ldc, 77)
+    t = [G.to_dev(x) for x in c.w4.pack()]
+    desc = c.desc()
+    desc.lda, desc.ldc, desc.ldr = lda, ldc, ldc
+    B.ibert_gemm_w4_requant(desc, a, B.W4Weights(t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), 64), G.to_dev(c.ch.b), G.to_dev(c.ch.m), G.to_dev(c.ch.s), r, out)
+    torch.cuda.synchronize()
+    ran(kernel)
+    same(rows, c.expected(), "offsets beyond 32 bits")
+    rows.fill_(77)
+    assert all(bool((x == 77).all()) for x in out.split(1 << 30)), "wrote between the rows"
+
+
+@pytest.mark.parametrize("out", ["i16", "i32"])
+def test_w4_results_at_odd_addresses(gpu, out):
+    torch, G, B = libs()
+    from test_gpu_feed import OnDevice
+    for M, N, K in ((3, 37, 144), (20, 70, 150)):
+        c = U.Rows4(M, M, N, K, 32, False, out, ld=(0, 3, 0))
+        d = OnDevice(c)
+        size = c.c0.nbytes
+        for off in (1, 2, 3):
+            G.say("w4, %s at %d bytes" % (out, off))
+            room = torch.full((size + 16,), 77, dtype=torch.uint8, device=G.DEV)
+            room[off:off + size] = torch.from_numpy(c.c0.reshape(-1).view(np.uint8)).to(G.DEV)
+            d.out = room[off:]
+            d.call()
+            torch.cuda.synchronize()
+            got = room.cpu().numpy()
+            assert np.array_equal(got[off:off + size].view(c.dtype), c.expected().reshape(-1)) and (got[:off] == 77).all() and (got[off + size:] == 77).all()
+
+
+def test_logits_of_the_largest_vocabulary(gpu):
+    torch, G, B = libs()
+    rows, vocab = 1, 1 << 26
+    c = U.Logits(5, [3000], vocab, [400])
+    G.say("logits, %d x %d" % (rows, vocab))
+    c.tokens[:5], c.ids[:5] = (vocab - 1, 0, vocab - 1, vocab, 4096), (vocab - 1, vocab - 1, 0, vocab, 4095)
+    check_logits(c, 4096, "the largest vocabulary")
+
+
+def test_logits_rows_of_two_slices_that_no_launch_holds(gpu):
+    # 2^21 rows of two slices; 34 GB in place, so that rows pass 2^32 elements too
+    torch, G, B = libs()
+    rows, vocab = (1 << 21) + 9, 4097
+    G.say("logits, %d rows of %d" % (rows, vocab))
+    x = torch.zeros(rows * vocab, dtype=torch.int32, device=G.DEV)
+    x[-1], x[0] = U.LOW, -3
+    params = torch.tensor([1, 0, 1, 0, 5, 7, -1], dtype=torch.int32, device=G.DEV).repeat(rows, 1)
+    first = torch.zeros(rows + 1, dtype=torch.int32, device=G.DEV)
+    tokens = torch.tensor([4096, 0, 0, 4096, 2, 4096, 17], dtype=torch.int32, device=G.DEV)
+    # row 0: [4096, 0, 0]; the last of the first launch: [4096, 2]; the last: [4096, 17]
+    first[1:], first[1 << 21:], first[rows:] = 3, 5, 7
+    B.ibert_logits_adjust_i(B.LogitsDesc(rows, vocab, vocab, vocab, 7, 0, 0, 0), x, params, tokens, first, first, None, None, None, None, x)
+    torch.cuda.synchronize()
+    ran("logits_adjust_kernel<4096>")
+    r = (1 << 21) - 1
+    want = {0: -3 - 5 - 14, 4096: -12, r * vocab + 2: -12, r * vocab + 4096: -12, (rows - 1) * vocab + 17: -12, rows * vocab - 1: U.LOW}
+    for at, v in want.items():
+        assert int(x[at]) == v, at
+        x[at] = 0
+    assert not any(bool(y.any()) for y in x.split(1 << 30))
