@@ -596,7 +596,8 @@ int ibert_paged_attention_from_scales(double S_q, double S_k, double S_v, double
  * ibert_gemm_i8_gated: W: device int8 [2F, K] (the gate's rows, then the up projection's), bias (may be NULL), mult, shift: device int32
  * [2F], shifts in [0, 62].  A: device int8 [M, lda]; C: device int8 [M, ldc], must not overlap A or W.  desc: host.  Single tokens and prompts
  * alike; no alignment is required; 16-byte aligned A and W (pointers and leading dimensions) with K a multiple of 16 are the fast path.
- * Errors: IBERT_ERR_SHAPE (M or F < 0, K outside [1, 2^17], F > 2^24, a leading dimension below its row), IBERT_ERR_PARAM_RANGE (activation,
+ * Errors: IBERT_ERR_SHAPE (M or F < 0, K outside [1, 2^17], F > 2^24, a leading dimension below its row, C over A or W, each taken from its first to its
+ * last element with what stands between rows), IBERT_ERR_PARAM_RANGE (activation,
  * gelu's preconditions with IBERT_GATE_GELU, out_dy's shift), IBERT_ERR_NULL.  M = 0 or F = 0: nothing to do.
  * |bias| + K * 16129 < 2^31 is the caller's responsibility, as for ibert_gemm_i8_requant.
  * ---------------------------------------------------------------------------------------------- */
@@ -632,8 +633,9 @@ int ibert_gemm_i8_gated(const ibert_gated_desc* desc, const int8_t* A, const int
  *   scales (uint8), zeros (int8; their low four bits count): [n/16][k/128][n%16][k%128/group]
  * What stands past N and K is never looked at.  w, scales, zeros, bias, mult, shift, A, residual, C: device; the structs: host.
  * w: 16-byte aligned; scales and zeros: 4-byte aligned (IBERT_ERR_ALIGN).  bias, residual, zeros may be NULL.  A, C, residual: any alignment.
- * Errors: IBERT_ERR_SHAPE (M or N < 0, K outside [1, 2^17], N > 2^24, a leading dimension below its row), IBERT_ERR_PARAM_RANGE (group, out_dtype,
- * out_clamp as for ibert_gemm_i8_requant, a dyadic's shift, gate), IBERT_ERR_NULL.  M = 0 or N = 0: nothing to do.  C must not overlap the inputs.
+ * Errors: IBERT_ERR_SHAPE (M or N < 0, K outside [1, 2^17], N > 2^24, a leading dimension below its row, C over A, w or residual as for the gated block),
+ * IBERT_ERR_PARAM_RANGE (group, out_dtype, out_clamp as for ibert_gemm_i8_requant, a dyadic's shift, gate, two matrices of different groups or one of them with
+ * zero points), IBERT_ERR_NULL.  M = 0 or N = 0: nothing to do.  C must not overlap any input; that it keeps clear of scales, zeros, bias, mult and shift is the caller's part.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
     const uint8_t* w;
@@ -689,7 +691,8 @@ int ibert_gate_params_from_scales(int32_t activation, double S_gate, double S_up
  * [num_tokens]; token_start: device int32 [rows + 1]; out_start: device int32 [rows]; both NULL where num_tokens = 0.  bias_ids, bias_values: device int32
  * [num_biases], bias_start: device int32 [rows + 1]; a token may be named more than once.  masks: device uint32 [num_masks, ld_mask], bit t % 32 of word t / 32.
  * Starts are clamped into [0, num_tokens] ([0, num_biases]) and into order; token numbers outside [0, vocab) are ignored; shifts outside [0, 62] are clamped into it.
- * Errors: IBERT_ERR_SHAPE (negative sizes, num_tokens or num_biases >= 2^30, vocab > 2^26, ldx or ldy < vocab, ld_mask < ceil(vocab / 32), x and y overlap), IBERT_ERR_NULL.
+ * Errors: IBERT_ERR_SHAPE (negative sizes, num_tokens or num_biases >= 2^30, vocab > 2^26, ldx or ldy < vocab, ld_mask < ceil(vocab / 32), x and y overlap, each
+ * taken from its first to its last element), IBERT_ERR_NULL.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
     ibert_dyadic up, down;

@@ -1,5 +1,5 @@
 // The persistent kernel of the INT8 gated block (gated_stream.hip): does it serve these operands, and its launch (validated arguments, M and F >= 1;
-// tall: tiles of 256 tokens, else 128).
+// tile: one of GATED_*).
 #pragma once
 #include "common.h"
 

@@ -9,8 +9,8 @@
 //   * F and M may be ragged: operands, constants and output are buffers that end with the last row or channel.
 //   * SiLU's sigmoids, and GELU's erf where it has room, are tables in LDS, built once by every workgroup with the function they stand for.
 //
-// What bounds it: where K is long the matrix units at the clock that power leaves (8192 x 4096 -> 2 x 12288 635 us, 2.6 POP/s, MFMA busy 0.72); where it is short the
-// epilogue, 20 ALU instructions a value that no MFMA runs beside (2741 x 1024 -> 2 x 4096 31 us eager: a tile of 128 x 128 takes 4.7 us in its loop and 3.5 in its
+// What bounds it: where K is long the matrix units at the clock that power leaves (8192 x 4096 -> 2 x 12288 636 to 671 us by the card, 2.6 to 2.5 POP/s, MFMA busy 0.72); where it is short the
+// epilogue, 20 ALU instructions a value that no MFMA runs beside (2741 x 1024 -> 2 x 4096 31 to 34 us: a tile of 128 x 128 takes 4.7 us in its loop and 3.5 in its
 // epilogue), and the last round of tiles, three quarters full there.  Three tiles: 256 tokens read W half as often; 128 fill more units; 128 x 64, two workgroups to a unit,
 // fill them where 128 x 128 tiles do not (256 x 1024 -> 2 x 4096 11.9 / 9.3 us; see plan_gated).  Where both of a unit's workgroups have work they gain nothing of each
 // other's epilogues, with wave priorities that would put them out of phase neither (2741 tokens: 33.8 us with any).

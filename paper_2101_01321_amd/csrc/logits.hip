@@ -2,9 +2,11 @@
 //
 // A workgroup takes a slice of one row's vocabulary.  It counts the row's tokens that fall into the slice, and adds up the biases there, in
 // LDS (integer atomics: any order gives the same), then passes over the logits once.  The history is read once per slice, from L2.
-// What bounds it: the logits' way through HBM (64 x 128000, 65.5 MB: 16.0 us without a history, 4.1 TB/s with the launch), and behind it the trips to memory of a workgroup
-// whose row has a history (where its tokens are, the tokens): 22.3 us with 262 thousand tokens, four workgroups a unit to hide them.  Kept in registers for the next
-// slice (workgroups that go through several slices) or dealt to wavefronts of their own, the loads cost so many registers that fewer workgroups fit: 35.7 and 42.4 us.
+// What bounds it (64 x 128000, 65.5 MB, us, inputs from memory): the logits' way through HBM, 14.8 without a history (4.4 TB/s with the launch).  A short history (up to 500 tokens a
+// row) adds trips to memory, for where its tokens are and for the tokens, 17.6; a long one (up to 8191) instructions, 2.5 times those without: counting, and 64-bit penalties that a
+// wavefront goes through where one of its lanes has a token seen, 21.4 (ALU slots 0.63, waits 0.20, four workgroups a unit).  22.1 with biases and masks; 18.4 with three sets of inputs in
+// turn, which the memory-side cache holds in part.  Kept in registers for the next slice (workgroups that go through several slices) or dealt to wavefronts of their own, the loads
+// cost so many registers that fewer workgroups fit: 35.7 and 42.4 us.
 #include "common.h"
 
 namespace ibert {
@@ -258,7 +260,7 @@ extern "C" int ibert_logits_adjust_i(const ibert_logits_desc* desc, const int32_
     g.ldx = d.ldx; g.ldy = d.ldy;
     g.vocab = d.vocab; g.num_tokens = d.num_tokens; g.num_biases = d.num_biases; g.num_masks = d.num_masks; g.ld_mask = d.ld_mask;
     g.vec = ibert::aligned(x, 16) && ibert::aligned(y, 16) && d.ldx % 4 == 0 && d.ldy % 4 == 0;
-    // Slices of 4096, or of 2048 where the longer ones would not be two workgroups to a unit.  us, 2048 / 4096 (8192): 1 x 50265 4.0 / 5.0 (6.6), 64 x 128000 with 262 thousand
+    // Slices of 4096, or of 2048 where the longer ones would not be two workgroups to a unit.  us with inputs from memory, 2048 / 4096 (8192): 1 x 50265 4.0 / 5.0 (6.6), 64 x 128000 with 262 thousand
     // tokens and 10 thousand biases 26.6 / 22.7 (25.9), without any 18.7 / 16.0 (16.1).
     if ((int64_t)d.rows * ((d.vocab + 4095) / 4096) < 512) return ibert::launch_logits<2048>(g, d.rows, static_cast<hipStream_t>(stream));
     return ibert::launch_logits<4096>(g, d.rows, static_cast<hipStream_t>(stream));

@@ -12,9 +12,10 @@
 //   * Two kernels.  rows_ring_kernel: rows that are 16-byte aligned, K a multiple of 16; everything goes from memory straight into LDS, several chunks ahead.
 //     rows_any_kernel: everything else, through registers, one chunk ahead.
 //
-// What bounds them: for one row HBM (4096 -> 2 x 12288 in 4 bits, 51 MB: 10.3 us, 5.0 TB/s, weights changing from call to call), which takes several stages a wavefront and several
-// workgroups a unit under way; for some ten rows instructions (16 x 1024 -> 50265 8.9 us, a wavefront has one chunk of K and its beginning and end beside it); for 64 the bytes
-// that a unit has under way and what a block of rows reads again (64 x 4096 -> 12288 11.7 us).  Rows unaligned: latency (33 rows, 5.5 us with the launch).
+// What bounds them (us with weights from memory / with three sets of them in turn, which the memory-side cache holds in part): for one row HBM (1 x 4096 -> 2 x 12288 in 4 bits,
+// 51 MB: 11.8 / 10.3, 4.35 TB/s from memory), which takes several stages a wavefront and several workgroups a unit under way; for some ten rows instructions (16 x 1024 -> 50265
+// 10.8 / 8.9, a wavefront has one chunk of K and its beginning and end beside it); for 64 the bytes that a unit has under way and what a block of rows reads again (64 x 12288 -> 4096
+// 15.4 / 11.9).  rows_any_kernel: latency for few rows (5 x 2730 -> 1024 4.2), then one workgroup to a unit and one chunk ahead (2730 -> 4096: 33 rows 7.8, 256 25.7).
 #pragma once
 #include <type_traits>
 
